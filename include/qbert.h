@@ -41,7 +41,8 @@ typedef enum {
     QB_ERR_SHAPE = 3,      /* non-positive dim, K % QB_K_ALIGN != 0, K > QB_MAX_K, N % G != 0  */
     QB_ERR_CLIP = 4,       /* activation range not a positive finite number                  */
     QB_ERR_WORKSPACE = 5,  /* workspace NULL or misaligned although the call needs one       */
-    QB_ERR_HIP = 6         /* the HIP runtime refused a launch (its error state is cleared) */
+    QB_ERR_HIP = 6,        /* the HIP runtime refused a launch (its error state is cleared) */
+    QB_ERR_VALUE = 7       /* attention, loss, dropout: a type, stride, alignment, scale or probability out of range */
 } qb_status;
 
 /* Host, pure.  Static string for a status. */
@@ -424,6 +425,98 @@ qb_status qb_embedding_quantize_bits(const float *E, int64_t V, int64_t d, int b
 qb_status qb_embedding_gather_bits(const uint8_t *codes, const float *h, int64_t V, int64_t d, int bits,
                                    int groups, const int64_t *ids, int64_t n_ids, float *out,
                                    void *stream);
+
+/*
+ * Between and behind the linears: dropout, attention, the loss over the vocabulary.  16-bit values are bit patterns, `type`
+ * says of which kind.  Arithmetic is in binary32; products run on the 16-bit matrix cores with binary32 accumulation.
+ */
+enum { QB_TYPE_BF16 = 0, QB_TYPE_FP16 = 1, QB_TYPE_FP32 = 2 };
+
+/*
+ * Dropout with the mask recomputed instead of stored.  Value i of the flat tensor is dropped where draw i % 4 of
+ * Threefry-2x32-13 at the counter i / 4 (low word first), key *seed, is below t = round(p * 65536) (at most 65535):
+ * four 16-bit draws, the low and the high half of word 0, then of word 1.  Kept values are divided by the exact share that
+ * is kept, (65536 - t) / 65536.
+ *   qb_dropout_fwd   Y[i]  = X[i] / share or 0  (+ residual[i])
+ *   qb_dropout_bwd   dX[i] = dY[i] / share or 0   (the residual's gradient is dY itself)
+ *   n         number of values, >= 0 (0 does nothing)
+ *   seed      device, one int64 (a captured graph draws other bits when its owner changes it)
+ *   p         0 <= p < 1, else QB_ERR_VALUE; type: any of the three
+ * Y may be X or residual, dX may be dY.  Pointers need the alignment of their type only.
+ */
+qb_status qb_dropout_fwd(const void *X, const void *residual, int64_t n, int type, float p, const int64_t *seed,
+                         void *Y, void *stream);
+qb_status qb_dropout_bwd(const void *dY, int64_t n, int type, float p, const int64_t *seed, void *dX, void *stream);
+
+/*
+ * Softmax attention of packed sequences with grouped heads.  Sequence b holds rows cu_q[b] .. cu_q[b+1]-1 of Q and rows
+ * cu_k[b] .. of K and V: up to cu_k[b+1], or with k_len given the first k_len[b] of these (a cache with room to grow).
+ * With n_q queries and n_k keys, query i sees all keys, or if causal the keys j <= i + n_k - n_q (the last query
+ * sees them all).  Query head h reads key head h / (heads / kv_heads).
+ *   S = scale * q.k;  P = softmax of S over the keys that are seen;  lse = log sum exp S
+ *   O = sum_k P[k] M[k] V[k],  M[k] = 0 or 1 / share with dropout of the weights (p > 0), else 1
+ * A query that sees no key gets O = 0 and lse = -infinity, and no gradient.
+ * Dropout as qb_dropout_fwd: key k of its sequence takes draw k % 4 of the counter with words (row of Q, 2^31 + h * 2^22 + k / 4).
+ *
+ *   Q [total_q, heads, dim], K, V [total_k, kv_heads, dim]: `type` bf16 or fp16.  Strides in values between rows and
+ *   between heads, multiples of 8 (queries, keys and values may lie side by side as one projection writes them); the dim values of a
+ *   head are dense.  dim is 64 or 128.
+ *   cu_q, cu_k  device [n_seqs + 1] int32, ascending, within total_q and total_k (clamped on the device to stay inside);
+ *   k_len       device [n_seqs] int32 or NULL; forward only
+ *   max_q, max_k  host: no sequence has more queries, keys; max_q * heads / kv_heads < 2^30.  Results of sequences that
+ *   have more are undefined
+ *   scale positive and finite; 0 <= p < 1, and where p > 0: seed, heads <= 512, max_k <= 2^24
+ *   O, dO [total_q, heads, dim] dense; lse [total_q, heads] fp32.  Rows outside all sequences are not written.
+ *   What lies in K and V outside the sequences is not read; inside it must be finite.
+ *
+ * Workspace: qb_attention_fwd_workspace_nbytes / qb_attention_bwd_workspace_nbytes (0: NULL will do), 256-byte aligned, contents undefined before and
+ * after.  Refused before anything is enqueued: QB_ERR_NULL, _SHAPE (dims, sizes), _VALUE (strides, types, scale, p), _WORKSPACE.
+ *
+ * qb_attention_bwd: O and lse as the forward wrote them.  dQ, dK, dV have the type of Q, with strides of their own (g_*),
+ * and are overwritten.  The same call gives the same bits every time.
+ */
+typedef struct {
+    const void *Q, *K, *V;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+    int type, heads, kv_heads, dim;
+    int64_t total_q, total_k;
+    int n_seqs, causal;
+    const int32_t *cu_q, *cu_k, *k_len;
+    int64_t max_q, max_k;
+    float scale, p;
+    const int64_t *seed;
+} qb_attention;
+typedef struct {
+    void *dQ, *dK, *dV;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+} qb_attention_grads;
+size_t qb_attention_fwd_workspace_nbytes(const qb_attention *a);
+size_t qb_attention_bwd_workspace_nbytes(const qb_attention *a);
+qb_status qb_attention_fwd(const qb_attention *a, void *O, float *lse, void *workspace, void *stream);
+qb_status qb_attention_bwd(const qb_attention *a, const void *dO, const void *O, const float *lse,
+                           const qb_attention_grads *grads, void *workspace, void *stream);
+
+/*
+ * Softmax cross entropy behind the projection to the vocabulary; the logits are never kept.
+ *   z[t,v] = sum_j X[t,j] W[v,j] (+ bias[v]);  lse[t] = log sum_v exp z[t,v];  loss[t] = lse[t] - z[t, targets[t]]
+ * A target outside [0, V) is no word (masked language modelling, padding): the token has loss 0, lse 0 and no gradient, and
+ * no work is done for it.
+ *   X  [T,K], W [V,K] bfloat16 (bit patterns), bias [V] fp32 or NULL, targets [T] int64, all on the device
+ *   loss, lse  out  [T] fp32
+ * qb_vocab_loss_bwd, with d[t,v] = dloss[t] * (exp(z[t,v] - lse[t]) - [v = targets[t]]):
+ *   dX[t] = sum_v d[t,v] W[v],  dW[v] = sum_t d[t,v] X[t],  dbias[v] = sum_t d[t,v]
+ *   lse as the forward wrote it, dloss [T] fp32 (finite);  dX [T,K], dW [V,K] bfloat16, dbias [V] fp32 or NULL; overwritten
+ * d is held in bfloat16, relative to the largest |dloss| and so exact in the weight of a mean over tokens.
+ * Base pointers and the workspace (qb_vocab_loss_workspace_nbytes(T,V,K, 0 forward / 1 backward) bytes): 16- and 256-byte aligned.  The backward
+ * works through the vocabulary in pieces, d of one piece at a time.  The same call gives the same bits every time.
+ * QB_ERR_SHAPE: T or V below 1 or above 2^24, K no multiple of QB_K_ALIGN or above QB_MAX_K.
+ */
+size_t qb_vocab_loss_workspace_nbytes(int64_t T, int64_t V, int64_t K, int backward);
+qb_status qb_vocab_loss_fwd(const uint16_t *X, const uint16_t *W, const float *bias, const int64_t *targets,
+                            int64_t T, int64_t V, int64_t K, float *loss, float *lse, void *workspace, void *stream);
+qb_status qb_vocab_loss_bwd(const float *dloss, const uint16_t *X, const uint16_t *W, const float *bias,
+                            const int64_t *targets, const float *lse, int64_t T, int64_t V, int64_t K,
+                            uint16_t *dX, uint16_t *dW, float *dbias, void *workspace, void *stream);
 
 #ifdef __cplusplus
 }

@@ -32,7 +32,8 @@ EXPORTS = ("qb_status_string", "qb_packed_nbytes", "qb_bwd_workspace_nbytes", "q
            "qb_quantize_act_dyn", "qb_qlinear_fwd_dyn", "qb_quantize_groupwise_clip", "qb_quantize_act_dyn_tensor", "qb_qlinear_bwd_ste_masked",
            "qb_quantize_groupwise_asym", "qb_quantize_groupwise_asym_range", "qb_qlinear_fwd_asym", "qb_qlinear_fwd_asym_dyn", "qb_qlinear_bwd_ste_asym",
            "qb_power_iteration_scratch_floats", "qb_power_iteration", "qb_sensitivity_omega", "qb_rank_by_sensitivity",
-           "qb_probe_mfma_i8")
+           "qb_probe_mfma_i8", "qb_dropout_fwd", "qb_dropout_bwd", "qb_attention_fwd_workspace_nbytes", "qb_attention_bwd_workspace_nbytes",
+           "qb_attention_fwd", "qb_attention_bwd", "qb_vocab_loss_workspace_nbytes", "qb_vocab_loss_fwd", "qb_vocab_loss_bwd")
 
 
 # int hv(void *ctx, const float *v, float *out, void *stream)
@@ -55,6 +56,22 @@ class _FwdJob(ctypes.Structure):
                 ("h", ctypes.c_void_p), ("rs_w", ctypes.c_void_p), ("bits", ctypes.c_int), ("groups", ctypes.c_int),
                 ("T", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("bias", ctypes.c_void_p),
                 ("Y", ctypes.c_void_p)]
+
+
+class Attention(ctypes.Structure):
+    """qb_attention of the C ABI"""
+    _fields_ = [("Q", ctypes.c_void_p), ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("q_row", ctypes.c_int64), ("q_head", ctypes.c_int64),
+                ("k_row", ctypes.c_int64), ("k_head", ctypes.c_int64), ("v_row", ctypes.c_int64), ("v_head", ctypes.c_int64),
+                ("type", ctypes.c_int), ("heads", ctypes.c_int), ("kv_heads", ctypes.c_int), ("dim", ctypes.c_int), ("total_q", ctypes.c_int64),
+                ("total_k", ctypes.c_int64), ("n_seqs", ctypes.c_int), ("causal", ctypes.c_int), ("cu_q", ctypes.c_void_p), ("cu_k", ctypes.c_void_p),
+                ("k_len", ctypes.c_void_p), ("max_q", ctypes.c_int64), ("max_k", ctypes.c_int64), ("scale", ctypes.c_float), ("p", ctypes.c_float),
+                ("seed", ctypes.c_void_p)]
+
+
+class AttentionGrads(ctypes.Structure):
+    """qb_attention_grads of the C ABI"""
+    _fields_ = [("dQ", ctypes.c_void_p), ("dK", ctypes.c_void_p), ("dV", ctypes.c_void_p), ("q_row", ctypes.c_int64), ("q_head", ctypes.c_int64),
+                ("k_row", ctypes.c_int64), ("k_head", ctypes.c_int64), ("v_row", ctypes.c_int64), ("v_head", ctypes.c_int64)]
 
 
 class QBError(RuntimeError):
@@ -121,6 +138,24 @@ def load_library():
     lib.qb_rank_by_sensitivity.argtypes = [vp, ci, vp]
     lib.qb_qlinear_bwd_ste_masked.restype = ci
     lib.qb_qlinear_bwd_ste_masked.argtypes = [vp, vp, cf, vp, vp, ci, ci, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp]
+    lib.qb_dropout_fwd.restype = ci
+    lib.qb_dropout_fwd.argtypes = [vp, vp, i64, ci, cf, vp, vp, vp]
+    lib.qb_dropout_bwd.restype = ci
+    lib.qb_dropout_bwd.argtypes = [vp, i64, ci, cf, vp, vp, vp]
+    lib.qb_attention_fwd_workspace_nbytes.restype = ctypes.c_size_t
+    lib.qb_attention_fwd_workspace_nbytes.argtypes = [ctypes.POINTER(Attention)]
+    lib.qb_attention_bwd_workspace_nbytes.restype = ctypes.c_size_t
+    lib.qb_attention_bwd_workspace_nbytes.argtypes = [ctypes.POINTER(Attention)]
+    lib.qb_attention_fwd.restype = ci
+    lib.qb_attention_fwd.argtypes = [ctypes.POINTER(Attention), vp, vp, vp, vp]
+    lib.qb_attention_bwd.restype = ci
+    lib.qb_attention_bwd.argtypes = [ctypes.POINTER(Attention), vp, vp, vp, ctypes.POINTER(AttentionGrads), vp, vp]
+    lib.qb_vocab_loss_workspace_nbytes.restype = ctypes.c_size_t
+    lib.qb_vocab_loss_workspace_nbytes.argtypes = [i64, i64, i64, ci]
+    lib.qb_vocab_loss_fwd.restype = ci
+    lib.qb_vocab_loss_fwd.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, vp]
+    lib.qb_vocab_loss_bwd.restype = ci
+    lib.qb_vocab_loss_bwd.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, vp, vp]
     lib.qb_unpack_codes.restype = ci
     lib.qb_unpack_codes.argtypes = [vp, i64, i64, ci, vp, vp]
     lib.qb_embedding_quantize.restype = ci
@@ -387,3 +422,40 @@ def qb_qlinear_fwd_dyn(Xq, rs_x, hx_rows, packed, h, rs_w, bits, groups, N, bias
 def qb_quantize_groupwise_clip(W, bits, m_in, packed=None, h=None, rs_w=None):
     """Group ranges [-m_in[g], +m_in[g]] given by the caller (device fp32 [G]). Returns (packed, h, rs_w)."""
     return _native().quantize_groupwise_clip(W, bits, m_in, packed, h, rs_w)
+
+
+def qb_dropout_fwd(X, p, seed, residual=None, Y=None):
+    """X / share kept where kept, else 0 (+ residual).  X: contiguous fp32, bf16 or fp16; seed: int64 tensor of one on the GPU."""
+    return _native().dropout_fwd(X, p, seed, residual, Y)
+
+
+def qb_dropout_bwd(dY, p, seed, dX=None):
+    """dY / share kept where qb_dropout_fwd kept the value, else 0."""
+    return _native().dropout_bwd(dY, p, seed, dX)
+
+
+def qb_attention_fwd(Q, K, V, cu_q, cu_k, max_q, max_k, causal=False, scale=None, k_len=None, p=0.0, seed=None, O=None, lse=None,
+                     workspace=None):
+    """Attention of packed sequences: Q[total_q,heads,dim], K, V[total_k,kv_heads,dim] bf16 or fp16 with any strides that are multiples
+    of 8 between rows and heads; cu_q, cu_k int32 offsets of the sequences, k_len int32 lengths where a cache has room to grow.
+    max_q, max_k: at least the longest sequence's queries and keys.  scale: 1 / sqrt(dim) if None.  p, seed: dropout of the weights.
+    Returns (O[total_q,heads,dim], lse[total_q,heads] fp32)."""
+    return _native().attention_fwd(Q, K, V, cu_q, cu_k, max_q, max_k, causal, scale, k_len, p, seed, O, lse, workspace)
+
+
+def qb_attention_bwd(dO, Q, K, V, O, lse, cu_q, cu_k, max_q, max_k, causal=False, scale=None, p=0.0, seed=None, dQ=None, dK=None,
+                     dV=None, workspace=None):
+    """Gradients of qb_attention_fwd called with the same arguments, which gave O and lse.  dQ, dK, dV may be parts of one wider
+    tensor (the gradient of a projection that gives queries, keys and values).  Returns (dQ, dK, dV)."""
+    return _native().attention_bwd(Q, K, V, cu_q, cu_k, max_q, max_k, causal, scale, None, p, seed, dO, O, lse, dQ, dK, dV, workspace)
+
+
+def qb_vocab_loss_fwd(X, W, targets, bias=None, loss=None, lse=None, workspace=None):
+    """Cross entropy of softmax(X W^T + bias): X[T,K], W[V,K] bf16, targets[T] int64 (outside 0 .. V-1: no loss), bias[V] fp32.
+    Returns (loss[T], lse[T]) fp32."""
+    return _native().vocab_loss_fwd(X, W, targets, bias, loss, lse, workspace)
+
+
+def qb_vocab_loss_bwd(dloss, X, W, targets, lse, bias=None, dX=None, dW=None, dbias=None, workspace=None):
+    """Gradients for dloss[T] fp32: (dX[T,K] bf16, dW[V,K] bf16, dbias[V] fp32, or None where neither bias nor dbias is given)."""
+    return _native().vocab_loss_bwd(dloss, X, W, targets, lse, bias, dX, dW, dbias, workspace)

@@ -13,6 +13,7 @@ extern "C" const char *qb_status_string(qb_status s)
         case QB_ERR_CLIP: return "activation range must be a positive finite number";
         case QB_ERR_WORKSPACE: return "workspace missing or not 256-byte aligned";
         case QB_ERR_HIP: return "the HIP runtime refused a kernel launch";
+        case QB_ERR_VALUE: return "a type, stride, alignment, scale or probability out of range";
     }
     return "unknown status";
 }

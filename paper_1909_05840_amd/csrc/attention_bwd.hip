@@ -1,0 +1,395 @@
+// Attention of packed sequences, backward.
+//
+//   P = exp(S - lse);  dP = M (dO V^T);  delta = sum_k P dP;  dS = P (dP - delta)
+//   dQ = scale dS K;  dK = scale dS^T Q;  dV = (P M)^T dO
+//
+// Two launches, each of which forms S and dP again: one goes over the keys of a tile of rows (dQ, delta), the other over the rows
+// of a tile of keys (dK, dV; shared heads of keys sum over their queries there).  Seven products instead of the five
+// that one launch would need, but nothing is added to memory by several workgroups: no atomics, the same bits every time.
+// dS and P are rounded to the inputs' type for the last products only.
+#include "attention.hpp"
+
+namespace qb {
+namespace {
+
+constexpr int kKeys = 64, kRowsOfTile = 64;
+
+struct GradArgs {
+    const uint16_t *dO, *O;
+    const float *lse;
+    uint16_t *dQ, *dK, *dV;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+    float *stat;  // [2][total_q * heads]: lse / ln 2 (+infinity for a row that sees nothing: its P is zero), delta
+};
+
+template <typename T, int D>
+__device__ __forceinline__ void write_scaled(uint16_t *row, const v16f (&o)[D / 32], float f, int hf)
+{
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+            const v2u w = {T::pair(o[i][j] * f, o[i][j + 1] * f), T::pair(o[i][j + 2] * f, o[i][j + 3] * f)};
+            *reinterpret_cast<v2u *>(row + 32 * i + 2 * j + 4 * hf) = w;
+        }
+}
+template <int N>
+__device__ __forceinline__ void clear(v16f (&x)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[i][j] = 0.0f;
+}
+template <typename T>
+__device__ __forceinline__ v8s rounded(const v16f &x, int half)
+{
+    v4u w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = T::pair(x[8 * half + 2 * i], x[8 * half + 2 * i + 1]);
+    return __builtin_bit_cast(v8s, w);
+}
+
+// dQ and delta; 128 rows to a workgroup, 32 to a wavefront, a lane's results all of one row (as in the forward).
+//
+// delta = dO.O takes O as the forward rounded it.  Where few keys carry a row's weight that error is as large as the rounding
+// of dS (384 keys of random scores of deviation 2: together 1.5 times the error of exact arithmetic rounded once).  EXACT therefore
+// sums eps = sum_k P (dP - delta) on the way, which is what delta lacks, and B = sum_k P K beside A = sum_k dS K: dQ = scale (A - eps B),
+// and the second launch gets delta + eps.  With many keys |O| is small beside |V|, and the rounding with it.
+template <typename T, int D, bool DROP, bool EXACT>
+__global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_kernel(const AttnArgs a, const GradArgs g, bool by_xcd)
+{
+    typedef Rows<D> R;
+    constexpr int kTile = kKeys * R::kBytes;
+    __shared__ __align__(1024) uint8_t lds[2][2 * kTile];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place at = place(blockIdx.x, a.n_seqs * a.kv_heads, a.tiles, by_xcd);
+    if (at.pair >= a.n_seqs * a.kv_heads) return;
+    const int b = at.pair / a.kv_heads, kv = at.pair - b * a.kv_heads;
+    const Segment seg = segment(a, b);
+    const int rows = seg.nq * a.group, first = at.tile * 128;
+    if (first >= rows) return;
+    const int row = first + wave * 32 + l32;
+    const int token = min((unsigned)row / (unsigned)a.group, (unsigned)seg.nq - 1u);
+    const int head = kv * a.group + (row - (int)((unsigned)row / (unsigned)a.group) * a.group);
+    const int row_q = seg.q0 + token;
+    const int64_t at_row = (int64_t)row_q * a.heads + head;
+
+    v8s q[D / 16], dO[D / 16];
+    const uint16_t *const q_from = a.Q + (int64_t)row_q * a.q_row + (int64_t)head * a.q_head + 8 * hf;
+    const uint16_t *const do_from = g.dO + at_row * D + 8 * hf, *const o_from = g.O + at_row * D + 8 * hf;
+    float delta = 0.0f;
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) {
+        q[d] = *reinterpret_cast<const v8s *>(q_from + 16 * d);
+        dO[d] = *reinterpret_cast<const v8s *>(do_from + 16 * d);
+        const v4u x = __builtin_bit_cast(v4u, dO[d]), y = *reinterpret_cast<const v4u *>(o_from + 16 * d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) delta += T::lo(x[i]) * T::lo(y[i]) + T::hi(x[i]) * T::hi(y[i]);
+    }
+    delta = halves_sum(delta);
+    const float lse = g.lse[at_row];
+    const float lse2 = lse > -__builtin_inff() ? lse * 1.44269504088896341f : __builtin_inff();
+
+    const auto sees = [&](int t) { return a.causal ? min(seg.nk, max(0, seg.first_hidden(t))) : seg.nk; };
+    const auto token_of = [&](int r) { return min(r / a.group, seg.nq - 1); };
+    const int limit = sees(token);
+    const int wave_least = __builtin_amdgcn_readfirstlane(sees(token_of(first + wave * 32)));
+    const int wave_most = __builtin_amdgcn_readfirstlane(sees(token_of(first + wave * 32 + 31)));
+    const int most = __builtin_amdgcn_readfirstlane(sees(token_of(first + 127)));
+    const int tiles = (most + kKeys - 1) / kKeys;
+
+    const uint16_t *const K = a.K + (int64_t)seg.k0 * a.k_row + (int64_t)kv * a.k_head;
+    const uint16_t *const V = a.V + (int64_t)seg.k0 * a.v_row + (int64_t)kv * a.v_head;
+    const uint32_t lds0 = lds_address(lds);
+    const auto fetch = [&](int tile, int stage) {
+        const uint32_t to = lds0 + stage * 2 * kTile;
+        copy_rows<D, kKeys, 4>(to, wave, lane, [&](int r) { return K + (int64_t)min(tile * kKeys + r, seg.nk - 1) * a.k_row; });
+        copy_rows<D, kKeys, 4>(to + kTile, wave, lane, [&](int r) { return V + (int64_t)min(tile * kKeys + r, seg.nk - 1) * a.v_row; });
+    };
+    const Threefry bits(DROP ? (uint64_t)*a.seed : 0);
+    v16f A[D / 32], B[EXACT ? D / 32 : 1];
+    clear(A);
+    clear(B);
+    float eps = 0.0f;
+    if (tiles) fetch(0, 0);
+    for (int t = 0; t < tiles; ++t) {
+        wait_copies<0>();
+        barrier();
+        if (t + 1 < tiles) fetch(t + 1, (t + 1) & 1);
+        if (t * kKeys >= wave_most) continue;
+        const uint8_t *const tk = lds[t & 1], *const tv = tk + kTile;
+        const bool masked = (t + 1) * kKeys > wave_least;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            v16f s, dp;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) s = T::mma32(R::along(tk, 32 * kb, d, lane), q[d], s);
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) dp = T::mma32(R::along(tv, 32 * kb, d, lane), dO[d], dp);
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = t * kKeys + 32 * kb + 8 * (i >> 2) + 4 * hf + (i & 3) < limit ? s[i] : -__builtin_inff();
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c, -lse2));
+            if constexpr (DROP) {
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const v2u w = weight_draws(bits, row_q, head, t * kKeys + 32 * kb + 2 * i + 4 * hf);
+                    dp[i] = kept_low(w[0], a.threshold) ? dp[i] * a.inv_share : 0.0f;
+                    dp[i + 1] = kept_high(w[0], a.threshold) ? dp[i + 1] * a.inv_share : 0.0f;
+                    dp[i + 2] = kept_low(w[1], a.threshold) ? dp[i + 2] * a.inv_share : 0.0f;
+                    dp[i + 3] = kept_high(w[1], a.threshold) ? dp[i + 3] * a.inv_share : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                dp[i] = s[i] * (dp[i] - delta);
+                if constexpr (EXACT) eps += dp[i];
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const v8s ds = rounded<T>(dp, h);
+                v8s p;
+                if constexpr (EXACT) p = rounded<T>(s, h);
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const v8s k = R::across(tk, 32 * kb + 16 * h, 32 * i, lane);
+                    A[i] = T::mma32(k, ds, A[i]);
+                    if constexpr (EXACT) B[i] = T::mma32(k, p, B[i]);
+                }
+            }
+        }
+    }
+    if constexpr (EXACT) {
+        eps = halves_sum(eps);
+        delta += eps;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) A[i][j] -= eps * B[i][j];
+    }
+    if (row >= rows) return;
+    write_scaled<T, D>(g.dQ + (int64_t)row_q * g.q_row + (int64_t)head * g.q_head, A, a.scale, hf);
+    if (hf == 0) {
+        g.stat[at_row] = lse2;
+        g.stat[(int64_t)a.total_q * a.heads + at_row] = delta;
+    }
+}
+
+__device__ __forceinline__ void copy4(const void *from, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(lds) : "memory", "m0");
+}
+// word of lane B of every four, as a constant of the instruction
+template <int B>
+__device__ __forceinline__ uint32_t of_four(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, B * 0x55, 0xF, 0xF, true); }
+
+// dK and dV; 128 keys to a workgroup, 32 to a wavefront: a lane's results all of one key.  Scores are taken as S = Q K^T, so that a
+// lane holds sixteen rows of its key and P and dS are, as they lie, the operands of dV^T = dO^T P and dK^T = Q^T dS.
+template <typename T, int D, bool DROP>
+__global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a, const GradArgs g, bool by_xcd)
+{
+    typedef Rows<D> R;
+    constexpr int kTile = kRowsOfTile * R::kBytes, kStage = 2 * kTile + 2 * kRowsOfTile * 4;
+    __shared__ __align__(1024) uint8_t lds[2][kStage];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place at = place(blockIdx.x, a.n_seqs * a.kv_heads, a.tiles, by_xcd);
+    if (at.pair >= a.n_seqs * a.kv_heads) return;
+    const int b = at.pair / a.kv_heads, kv = at.pair - b * a.kv_heads;
+    const Segment seg = segment(a, b);
+    const int first = (a.tiles - 1 - at.tile) * 128;  // (the first keys are seen by the most rows)
+    if (first >= seg.nk) return;
+    const int rows = max(0, seg.nq) * a.group;
+    const int wave_first = first + wave * 32, key = wave_first + l32;
+    const int key_in = min(key, seg.nk - 1);
+
+    v8s k[D / 16], v[D / 16];
+    const uint16_t *const k_from = a.K + (int64_t)(seg.k0 + key_in) * a.k_row + (int64_t)kv * a.k_head + 8 * hf;
+    const uint16_t *const v_from = a.V + (int64_t)(seg.k0 + key_in) * a.v_row + (int64_t)kv * a.v_head + 8 * hf;
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) {
+        k[d] = *reinterpret_cast<const v8s *>(k_from + 16 * d);
+        v[d] = *reinterpret_cast<const v8s *>(v_from + 16 * d);
+    }
+    // the first row that sees a key: causal, key <= token + nk - nq
+    const auto first_row = [&](int key_) { return a.causal ? (int)min((int64_t)rows, (int64_t)max(0, key_ - (seg.nk - seg.nq)) * a.group) : 0; };
+    const int from_row = first_row(key);
+    const int wave_from = __builtin_amdgcn_readfirstlane(first_row(wave_first)), wave_all = __builtin_amdgcn_readfirstlane(first_row(wave_first + 31));
+    const int begin = __builtin_amdgcn_readfirstlane(first_row(first)) / kRowsOfTile, end = (rows + kRowsOfTile - 1) / kRowsOfTile;
+
+    const uint32_t lds0 = lds_address(lds);
+    const int64_t stats = (int64_t)a.total_q * a.heads;
+    const auto fetch = [&](int tile, int stage) {
+        const uint32_t to = lds0 + stage * kStage;
+        const auto split = [&](int r, int &token, int &head) {  // rows past the end repeat the last one; their P is set to zero
+            r = min(tile * kRowsOfTile + r, rows - 1);
+            token = a.group == 1 ? r : (int)((unsigned)r / (unsigned)a.group);
+            head = kv * a.group + r - token * a.group;
+        };
+        copy_rows<D, kRowsOfTile, 4>(to, wave, lane, [&](int r) {
+            int token, head;
+            split(r, token, head);
+            return a.Q + (int64_t)(seg.q0 + token) * a.q_row + (int64_t)head * a.q_head;
+        });
+        copy_rows<D, kRowsOfTile, 4>(to + kTile, wave, lane, [&](int r) {
+            int token, head;
+            split(r, token, head);
+            return g.dO + ((int64_t)(seg.q0 + token) * a.heads + head) * D;
+        });
+        if (wave < 2) {
+            int token, head;
+            split(lane, token, head);
+            copy4(g.stat + wave * stats + (int64_t)(seg.q0 + token) * a.heads + head, to + 2 * kTile + wave * kRowsOfTile * 4);
+        }
+    };
+    const Threefry bits(DROP ? (uint64_t)*a.seed : 0);
+    v16f dK[D / 32], dV[D / 32];
+    clear(dK);
+    clear(dV);
+    if (begin < end) fetch(begin, begin & 1);
+    for (int t = begin; t < end; ++t) {
+        wait_copies<0>();
+        barrier();
+        if (t + 1 < end) fetch(t + 1, (t + 1) & 1);
+        const uint8_t *const tq = lds[t & 1], *const td = tq + kTile;
+        const float *const stat = reinterpret_cast<const float *>(td + kTile);
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) {
+            const int row0 = t * kRowsOfTile + 32 * rb;
+            if (row0 + 32 <= wave_from || row0 >= rows) continue;  // none of these rows sees a key of the wavefront
+            const bool masked = row0 < wave_all || row0 + 32 > rows;
+            v16f s, dp;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) s = T::mma32(R::along(tq, 32 * rb, d, lane), k[d], s);
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) dp = T::mma32(R::along(td, 32 * rb, d, lane), v[d], dp);
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int r = row0 + 8 * (i >> 2) + 4 * hf + (i & 3);
+                    s[i] = r >= from_row && r < rows ? s[i] : -__builtin_inff();
+                }
+            }
+            v16f p;
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const v4f lse2 = *reinterpret_cast<const v4f *>(stat + 32 * rb + 2 * i + 4 * hf);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p[i + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + j], a.c, -lse2[j]));
+            }
+            v16f pm = p;
+            if constexpr (DROP) {
+                // Four neighbouring lanes need the four draws of the same counters: each of them forms the counters of every
+                // fourth row, and they take each other's words.
+                v2u w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = min(row0 + 8 * i + 4 * hf + (lane & 3), rows - 1);
+                    const int token = a.group == 1 ? r : (int)((unsigned)r / (unsigned)a.group);
+                    w[i] = weight_draws(bits, seg.q0 + token, kv * a.group + r - token * a.group, key);
+                }
+                const auto take = [&](int i, uint32_t w0, uint32_t w1) {
+                    const uint32_t word = (lane & 2) ? w1 : w0;
+                    const bool kept = ((lane & 1) ? word >> 16 : word & 0xFFFFu) >= a.threshold;
+                    pm[i] = kept ? p[i] : 0.0f;
+                    dp[i] = kept ? dp[i] * a.inv_share : 0.0f;
+                };
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    take(4 * i, of_four<0>(w[i][0]), of_four<0>(w[i][1]));
+                    take(4 * i + 1, of_four<1>(w[i][0]), of_four<1>(w[i][1]));
+                    take(4 * i + 2, of_four<2>(w[i][0]), of_four<2>(w[i][1]));
+                    take(4 * i + 3, of_four<3>(w[i][0]), of_four<3>(w[i][1]));
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const v4f delta = *reinterpret_cast<const v4f *>(stat + kRowsOfTile + 32 * rb + 2 * i + 4 * hf);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) dp[i + j] = p[i + j] * (dp[i + j] - delta[j]);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const v8s pr = rounded<T>(pm, h), ds = rounded<T>(dp, h);
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    dV[i] = T::mma32(R::across(td, 32 * rb + 16 * h, 32 * i, lane), pr, dV[i]);
+                    dK[i] = T::mma32(R::across(tq, 32 * rb + 16 * h, 32 * i, lane), ds, dK[i]);
+                }
+            }
+        }
+    }
+    if (key >= seg.nk) return;
+    write_scaled<T, D>(g.dK + (int64_t)(seg.k0 + key) * g.k_row + (int64_t)kv * g.k_head, dK, a.scale, hf);
+    write_scaled<T, D>(g.dV + (int64_t)(seg.k0 + key) * g.v_row + (int64_t)kv * g.v_head, dV, DROP ? a.inv_share : 1.0f, hf);
+}
+
+// Above this many keys delta is taken from the rounded O (see there).
+constexpr int64_t kExactKeys = 2048;
+
+template <typename T, int D>
+qb_status backward(AttnArgs a, const GradArgs &g, int64_t max_q, int64_t max_k, bool drop, hipStream_t stream)
+{
+    const int64_t pairs = (int64_t)a.n_seqs * a.kv_heads;
+    const bool by_xcd = deal_by_xcd(pairs);
+    if (max_q > 0) {
+        a.tiles = (int)((max_q * a.group + 127) / 128);
+        const int64_t grid = dealt_workgroups(pairs, a.tiles);
+        if (grid > INT32_MAX / 256) return QB_ERR_SHAPE;
+        const bool exact = max_k <= kExactKeys;
+        if (drop && exact) attention_dq_kernel<T, D, true, true><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
+        else if (drop) attention_dq_kernel<T, D, true, false><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
+        else if (exact) attention_dq_kernel<T, D, false, true><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
+        else attention_dq_kernel<T, D, false, false><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
+    }
+    if (max_k > 0) {
+        a.tiles = (int)((max_k + 127) / 128);
+        const int64_t grid = dealt_workgroups(pairs, a.tiles);
+        if (drop) attention_dkv_kernel<T, D, true><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
+        else attention_dkv_kernel<T, D, false><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
+    }
+    return launch_status();
+}
+
+}  // namespace
+}  // namespace qb
+
+using namespace qb;
+
+extern "C" size_t qb_attention_bwd_workspace_nbytes(const qb_attention *p)
+{
+    AttnArgs a;
+    if (attention_args(p, a) != QB_OK) return 0;
+    return ((size_t)p->total_q * p->heads * 8 + 255) / 256 * 256;
+}
+
+extern "C" qb_status qb_attention_bwd(const qb_attention *p, const void *dO, const void *O, const float *lse,
+                                      const qb_attention_grads *grads, void *workspace, void *stream)
+{
+    AttnArgs a;
+    const qb_status s = attention_args(p, a);
+    if (s != QB_OK) return s;
+    if (!grads) return QB_ERR_NULL;
+    if (p->k_len || (grads->q_row | grads->q_head | grads->k_row | grads->k_head | grads->v_row | grads->v_head) % 8 != 0) return QB_ERR_VALUE;
+    if (p->n_seqs == 0 || (p->total_q == 0 && p->total_k == 0)) return QB_OK;
+    if (p->total_q > 0 && (!dO || !O || !lse || !grads->dQ)) return QB_ERR_NULL;
+    if (p->total_k > 0 && (!grads->dK || !grads->dV)) return QB_ERR_NULL;
+    if (!aligned16(dO) || !aligned16(O) || !aligned16(grads->dQ) || !aligned16(grads->dK) || !aligned16(grads->dV)) return QB_ERR_VALUE;
+    if (p->total_q > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255))) return QB_ERR_WORKSPACE;
+    const int64_t pairs = (int64_t)p->n_seqs * p->kv_heads;
+    if (dealt_workgroups(pairs, (p->max_q * a.group + 127) / 128) > INT32_MAX / 256 || dealt_workgroups(pairs, (p->max_k + 127) / 128) > INT32_MAX / 256) return QB_ERR_SHAPE;
+    const GradArgs g = {static_cast<const uint16_t *>(dO), static_cast<const uint16_t *>(O), lse, static_cast<uint16_t *>(grads->dQ), static_cast<uint16_t *>(grads->dK),
+                        static_cast<uint16_t *>(grads->dV), grads->q_row, grads->q_head, grads->k_row, grads->k_head, grads->v_row, grads->v_head, static_cast<float *>(workspace)};
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool drop = p->p > 0.0f;
+    if (p->type == QB_TYPE_BF16) return p->dim == 64 ? backward<Bf16, 64>(a, g, p->max_q, p->max_k, drop, st) : backward<Bf16, 128>(a, g, p->max_q, p->max_k, drop, st);
+    return p->dim == 64 ? backward<Fp16, 64>(a, g, p->max_q, p->max_k, drop, st) : backward<Fp16, 128>(a, g, p->max_q, p->max_k, drop, st);
+}

@@ -12,6 +12,7 @@
 #include <torch/csrc/utils/object_ptr.h>
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPStream.h>
+#include <cmath>
 #include <cstdarg>
 #include <vector>
 #include "../../include/qbert.h"
@@ -61,6 +62,7 @@ const char *type_name(at::ScalarType t)
     switch (t) {
         case at::kFloat: return "torch.float32";
         case at::kBFloat16: return "torch.bfloat16";
+        case at::kHalf: return "torch.float16";
         case at::kChar: return "torch.int8";
         case at::kByte: return "torch.uint8";
         case at::kInt: return "torch.int32";
@@ -668,6 +670,192 @@ QB_CALL(embedding_gather_bits, 6)  // codes, h, bits, groups, ids, out
     }, bits, codes, a[4], a[5]);
 }
 
+// ---- dropout, attention, the vocabulary's loss
+
+int type_code(const Tensor &t, const char *name, bool fp32)
+{
+    const at::ScalarType s = t.scalar_type();
+    if (s == at::kBFloat16) return QB_TYPE_BF16;
+    if (s == at::kHalf) return QB_TYPE_FP16;
+    if (s != at::kFloat || !fp32) raise(PyExc_TypeError, "%s must be a bfloat16 or float16%s tensor", name, fp32 ? " or float32" : "");
+    return QB_TYPE_FP32;
+}
+
+const int64_t *seed_of(PyObject *o)  // None or one number on the GPU
+{
+    if (o == Py_None) return nullptr;
+    const Tensor &t = typed(o, at::kLong, "seed");
+    if (t.numel() != 1) raise(PyExc_ValueError, "seed must hold one number");
+    return ptr<int64_t>(t);
+}
+
+// an output that was passed in: the type and sizes of what would be made
+void same_as(const Tensor &t, at::IntArrayRef size, at::ScalarType type, const char *name)
+{
+    if (!t.is_cuda() || t.scalar_type() != type || !t.is_contiguous()) raise(PyExc_TypeError, "%s must be a contiguous %s tensor on the GPU", name, type_name(type));
+    if (t.sizes() != size) raise(PyExc_ValueError, "%s has other sizes than the result", name);
+}
+Tensor result(PyObject *o, at::IntArrayRef size, at::ScalarType type, const at::Device &dev, const char *name)
+{
+    if (o == Py_None) return fresh(size, type, dev);
+    same_as(tensor(o, name), size, type, name);
+    return tensor(o, name);
+}
+
+Tensor workspace_of(PyObject *o, size_t bytes, const at::Device &dev)  // undefined where none is needed
+{
+    if (o != Py_None) {
+        const Tensor &t = tensor(o, "workspace");
+        if (!t.is_cuda() || !t.is_contiguous()) raise(PyExc_TypeError, "workspace must be a contiguous tensor on the GPU");
+        if (t.nbytes() < bytes) raise(PyExc_ValueError, "workspace is too small");
+        return t;
+    }
+    return bytes ? fresh({static_cast<int64_t>(bytes)}, at::kByte, dev) : Tensor();
+}
+void *where(const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+
+PyObject *wrapped(const Tensor &t)
+{
+    PyObject *v = THPVariable_Wrap(t);
+    if (!v) throw_python_error();
+    return v;
+}
+
+QB_CALL(dropout_fwd, 5)  // X, p, seed, residual, Y
+{
+    const Tensor &X = tensor(a[0], "X");
+    const int type = type_code(X, "X", true);
+    const Tensor &x = typed(a[0], X.scalar_type(), "X");
+    const float p = real(a[1]);
+    if (a[3] != Py_None) same_as(tensor(a[3], "residual"), x.sizes(), x.scalar_type(), "residual");
+    const Tensor Y = result(a[4], x.sizes(), x.scalar_type(), x.device(), "Y");
+    call(qb_dropout_fwd, x.data_ptr(), ptr<void>(a[3], "residual"), x.numel(), type, p, seed_of(a[2]), Y.data_ptr(), stream());
+    return wrapped(Y);
+}
+
+QB_CALL(dropout_bwd, 4)  // dY, p, seed, dX
+{
+    const Tensor &D = tensor(a[0], "dY");
+    const int type = type_code(D, "dY", true);
+    const Tensor &d = typed(a[0], D.scalar_type(), "dY");
+    const float p = real(a[1]);
+    const Tensor dX = result(a[3], d.sizes(), d.scalar_type(), d.device(), "dX");
+    call(qb_dropout_bwd, d.data_ptr(), d.numel(), type, p, seed_of(a[2]), dX.data_ptr(), stream());
+    return wrapped(dX);
+}
+
+// [rows, heads, dim] whose last dimension is dense
+const Tensor &heads_of(PyObject *o, at::ScalarType t, const char *name)
+{
+    const Tensor &x = tensor(o, name);
+    if (!x.is_cuda() || x.scalar_type() != t) raise(PyExc_TypeError, "%s must be a %s tensor on the GPU", name, type_name(t));
+    if (x.dim() != 3 || (x.size(2) > 1 && x.stride(2) != 1)) raise(PyExc_ValueError, "%s must be [rows, heads, dim] with a dense last dimension", name);
+    return x;
+}
+
+struct Attention : qb_attention {
+    const Tensor &q, &k, &v;
+    // q, k, v, cu_q, cu_k, max_q, max_k, causal, scale, k_len, p, seed
+    explicit Attention(Args a) : qb_attention(), q(tensor(a[0], "Q")), k(tensor(a[1], "K")), v(tensor(a[2], "V"))
+    {
+        type = type_code(q, "Q", false);
+        heads_of(a[0], q.scalar_type(), "Q");
+        heads_of(a[1], q.scalar_type(), "K");
+        heads_of(a[2], q.scalar_type(), "V");
+        if (k.sizes() != v.sizes() || k.size(2) != q.size(2)) raise(PyExc_ValueError, "K and V must have the same sizes, and the head size of Q");
+        const Tensor &cq = typed(a[3], at::kInt, "cu_q"), &ck = typed(a[4], at::kInt, "cu_k");
+        if (cq.dim() != 1 || ck.dim() != 1 || cq.size(0) < 1 || cq.size(0) != ck.size(0)) raise(PyExc_ValueError, "cu_q and cu_k must hold one more offset than there are sequences");
+        Q = q.data_ptr(); K = k.data_ptr(); V = v.data_ptr();
+        q_row = q.stride(0); q_head = q.stride(1);
+        k_row = k.stride(0); k_head = k.stride(1);
+        v_row = v.stride(0); v_head = v.stride(1);
+        heads = static_cast<int>(q.size(1)); kv_heads = static_cast<int>(k.size(1)); dim = static_cast<int>(q.size(2));
+        total_q = q.size(0); total_k = k.size(0);
+        n_seqs = static_cast<int>(cq.size(0) - 1);
+        cu_q = ptr<int32_t>(cq); cu_k = ptr<int32_t>(ck);
+        max_q = integer(a[5]); max_k = integer(a[6]);
+        causal = PyObject_IsTrue(a[7]);
+        if (causal < 0) throw_python_error();
+        scale = a[8] == Py_None ? 1.0f / std::sqrt(static_cast<float>(dim)) : real(a[8]);
+        if (a[9] != Py_None) {
+            const Tensor &n = typed(a[9], at::kInt, "k_len");
+            if (n.dim() != 1 || n.size(0) != n_seqs) raise(PyExc_ValueError, "k_len must hold one length per sequence");
+            k_len = ptr<int32_t>(n);
+        }
+        p = real(a[10]);
+        seed = seed_of(a[11]);
+    }
+};
+
+QB_CALL(attention_fwd, 15)  // the twelve of Attention, O, lse, workspace
+{
+    const Attention t(a);
+    const at::Device dev = t.q.device();
+    const Tensor O = result(a[12], t.q.sizes(), t.q.scalar_type(), dev, "O"), lse = result(a[13], {t.total_q, t.heads}, at::kFloat, dev, "lse");
+    const Tensor ws = workspace_of(a[14], qb_attention_fwd_workspace_nbytes(&t), dev);
+    call(qb_attention_fwd, &t, O.data_ptr(), ptr<float>(lse), where(ws), stream());
+    return tuple({O, lse});
+}
+
+QB_CALL(attention_bwd, 19)  // the twelve of Attention, dO, O, lse, dQ, dK, dV, workspace
+{
+    const Attention t(a);
+    const at::Device dev = t.q.device();
+    const at::ScalarType type = t.q.scalar_type();
+    same_as(tensor(a[12], "dO"), t.q.sizes(), type, "dO");
+    same_as(tensor(a[13], "O"), t.q.sizes(), type, "O");
+    same_as(tensor(a[14], "lse"), {t.total_q, t.heads}, at::kFloat, "lse");
+    const auto grad = [&](PyObject *o, const Tensor &of, const char *name) {  // may be a part of a wider tensor
+        if (o == Py_None) return fresh(of.sizes(), type, dev);
+        if (heads_of(o, type, name).sizes() != of.sizes()) raise(PyExc_ValueError, "%s has other sizes than its tensor", name);
+        return Tensor(tensor(o, name));
+    };
+    const Tensor dQ = grad(a[15], t.q, "dQ"), dK = grad(a[16], t.k, "dK"), dV = grad(a[17], t.v, "dV");
+    const qb_attention_grads g = {dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), dQ.stride(0), dQ.stride(1), dK.stride(0), dK.stride(1), dV.stride(0), dV.stride(1)};
+    const Tensor ws = workspace_of(a[18], qb_attention_bwd_workspace_nbytes(&t), dev);
+    call(qb_attention_bwd, &t, tensor(a[12], "dO").data_ptr(), tensor(a[13], "O").data_ptr(), ptr<float>(tensor(a[14], "lse")), &g, where(ws), stream());
+    return tuple({dQ, dK, dV});
+}
+
+struct VocabLoss {
+    const Tensor &X, &W, &targets;
+    int64_t T, V, K;
+    const float *bias = nullptr;
+    VocabLoss(PyObject *x, PyObject *w, PyObject *t, PyObject *b)
+        : X(matrix(x, at::kBFloat16, "X")), W(matrix(w, at::kBFloat16, "W")), targets(typed(t, at::kLong, "targets")), T(X.size(0)), V(W.size(0)), K(X.size(1))
+    {
+        if (W.size(1) != K) raise(PyExc_ValueError, "W must be [V, K] with the K of X");
+        if (targets.dim() != 1 || targets.size(0) != T) raise(PyExc_ValueError, "targets must hold one number per row of X");
+        if (b == Py_None) return;
+        same_as(tensor(b, "bias"), {V}, at::kFloat, "bias");
+        bias = ptr<float>(tensor(b, "bias"));
+    }
+};
+
+QB_CALL(vocab_loss_fwd, 7)  // X, W, targets, bias, loss, lse, workspace
+{
+    const VocabLoss l(a[0], a[1], a[2], a[3]);
+    const at::Device dev = l.X.device();
+    const Tensor loss = result(a[4], {l.T}, at::kFloat, dev, "loss"), lse = result(a[5], {l.T}, at::kFloat, dev, "lse");
+    const Tensor ws = workspace_of(a[6], qb_vocab_loss_workspace_nbytes(l.T, l.V, l.K, 0), dev);
+    call(qb_vocab_loss_fwd, bits16(l.X), bits16(l.W), l.bias, ptr<int64_t>(l.targets), l.T, l.V, l.K, ptr<float>(loss), ptr<float>(lse), where(ws), stream());
+    return tuple({loss, lse});
+}
+
+QB_CALL(vocab_loss_bwd, 10)  // dloss, X, W, targets, lse, bias, dX, dW, dbias, workspace
+{
+    const VocabLoss l(a[1], a[2], a[3], a[5]);
+    const at::Device dev = l.X.device();
+    same_as(tensor(a[0], "dloss"), {l.T}, at::kFloat, "dloss");
+    same_as(tensor(a[4], "lse"), {l.T}, at::kFloat, "lse");
+    const Tensor dX = result(a[6], l.X.sizes(), at::kBFloat16, dev, "dX"), dW = result(a[7], l.W.sizes(), at::kBFloat16, dev, "dW");
+    const Tensor db = l.bias || a[8] != Py_None ? result(a[8], {l.V}, at::kFloat, dev, "dbias") : Tensor();
+    const Tensor ws = workspace_of(a[9], qb_vocab_loss_workspace_nbytes(l.T, l.V, l.K, 1), dev);
+    call(qb_vocab_loss_bwd, ptr<float>(tensor(a[0], "dloss")), bits16(l.X), bits16(l.W), l.bias, ptr<int64_t>(l.targets), ptr<float>(tensor(a[4], "lse")), l.T, l.V, l.K,
+         bits16(dX), bits16(dW), static_cast<float *>(where(db)), where(ws), stream());
+    return tuple({dX, dW, db});
+}
+
 PyObject *set_error(PyObject *, PyObject *cls)
 {
     Py_INCREF(cls);
@@ -683,7 +871,8 @@ PyMethodDef g_methods[] = {
     QB_ENTRY(qlinear_fwd), QB_ENTRY(qlinear_fwd_dyn), QB_ENTRY(qlinear_fwd_asym), QB_ENTRY(qlinear_fwd_asym_dyn),
     QB_ENTRY(qlinear_fwd_q8), QB_ENTRY(qlinear_bwd_ste), QB_ENTRY(qlinear_bwd_ste_static), QB_ENTRY(qlinear_bwd_ste_masked),
     QB_ENTRY(qlinear_bwd_ste_asym), QB_ENTRY(embedding_quantize), QB_ENTRY(embedding_quantize_bits), QB_ENTRY(embedding_gather),
-    QB_ENTRY(embedding_gather_bits),
+    QB_ENTRY(embedding_gather_bits), QB_ENTRY(dropout_fwd), QB_ENTRY(dropout_bwd), QB_ENTRY(attention_fwd), QB_ENTRY(attention_bwd),
+    QB_ENTRY(vocab_loss_fwd), QB_ENTRY(vocab_loss_bwd),
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

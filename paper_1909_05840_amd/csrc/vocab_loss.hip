@@ -1,0 +1,568 @@
+// Softmax cross entropy behind the projection to the vocabulary, and its gradients.
+//
+//   z[t,v] = X[t].W[v] + bias[v];  lse[t] = log sum_v exp z;  loss[t] = lse[t] - z[t, target]
+//   d[t,v] = dloss[t] (exp(z - lse[t]) - [v = target]);  dX = d W;  dW = d^T X;  dbias = sum_t d
+//
+// Only tokens that have a target take part: a first launch numbers them, the products fetch their rows of X through that list.
+// The logits are formed tile by tile and never written: the forward keeps a maximum and a sum per token and tile, the
+// backward forms them again, piece by piece of the vocabulary, and writes d of one piece in bfloat16, from which dX and dW take their share.
+// d is held relative to the largest |dloss|, which multiplies the binary32 sums: the weight 1 / n of a mean over n tokens is
+// then 1, where rounding d itself would put one error of up to 2^-8 on every token alike.
+#include "qb_tiles.hpp"
+#include <algorithm>
+
+namespace qb {
+namespace {
+
+constexpr int64_t kMost = 1 << 24;              // tokens, words
+constexpr int64_t kPieceBytes = 512ll << 20;    // d of a piece
+constexpr float kLow = -1.0e30f;               // the maximum of no words (finite, also in powers of two)
+constexpr int kRowPad = 256;                    // the list of tokens is padded to this
+constexpr int kSlices = 32;                     // most slices that a tile of dX is cut into
+
+struct Counted {
+    int n;        // tokens that have a target
+    float scale;  // the largest |dloss| among them
+    int pad[62];
+};
+
+struct LossArgs {
+    const uint16_t *X, *W;
+    const float *bias, *dloss;
+    const int64_t *targets;
+    int T, V, K;
+    Counted *counted;
+    int *list;       // [Tp] token of every counted row; padded with the last one
+    int *place;      // [T] the other way round; -1 where a token has no target
+    // forward
+    float *loss, *lse;
+    v2f *part;       // [vocabulary tiles][Tp] maximum, sum
+    float *hit;      // [Tp] the target's logit
+    // backward
+    int v0, piece;   // this piece's first word and width (a multiple of kRowPad)
+    uint16_t *d;     // [Tp][piece]
+    float *db;       // [token tiles][piece], or null
+    float *dXs;      // tiles of dX: [tile][slice], binary32
+    uint16_t *dX, *dW;
+    float *dbias;
+    int Tp;
+};
+
+__device__ __forceinline__ bool is_word(int64_t t, int V) { return t >= 0 && t < V; }
+
+// Numbers the tokens that have a target, in order.  A workgroup does 1024 tokens; it counts those before them itself.
+template <bool BACKWARD>
+__global__ __launch_bounds__(1024) void loss_rows_kernel(const LossArgs a)
+{
+    __shared__ int sums[16];
+    __shared__ float tops[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, first = blockIdx.x * 1024, t = first + tid;
+    const bool last = blockIdx.x == gridDim.x - 1;
+    int before = 0;
+    float top = 0.0f;
+    for (int i = tid; i < first; i += 1024) {
+        const bool word = is_word(a.targets[i], a.V);
+        before += word;
+        if (BACKWARD && last && word) top = fmaxf(top, fabsf(a.dloss[i]));
+    }
+    const bool mine = t < a.T && is_word(a.targets[t], a.V);
+    if (BACKWARD && last && mine) top = fmaxf(top, fabsf(a.dloss[t]));
+    const uint64_t who = __builtin_amdgcn_ballot_w64(mine);
+    before = wave_sum(before);
+    if constexpr (BACKWARD) top = wave_max(top);
+    if (lane == 0) {
+        sums[wave] = before;
+        tops[wave] = top;
+    }
+    __syncthreads();
+    int start = 0;
+    for (int i = 0; i < 16; ++i) start += sums[i];
+    __syncthreads();
+    if (lane == 0) sums[wave] = __builtin_popcountll(who);
+    __syncthreads();
+    int all = 0;
+    for (int i = 0; i < 16; ++i) {
+        if (i == wave) before = start + all;
+        all += sums[i];
+    }
+    all += start;
+    const int at = before + __builtin_popcountll(who & ((1ull << lane) - 1));
+    if (t < a.T) {
+        if (mine) a.list[at] = t;
+        if constexpr (BACKWARD) {
+            a.place[t] = mine ? at : -1;
+        } else if (!mine) {
+            a.loss[t] = 0.0f;
+            a.lse[t] = 0.0f;
+        }
+    }
+    if (!last) return;
+    if (tid == 0) {
+        a.counted->n = all;
+        float s = 0.0f;
+        for (int i = 0; i < 16; ++i) s = fmaxf(s, tops[i]);
+        a.counted->scale = s;
+    }
+    const int end = min(a.Tp, (all + kRowPad - 1) / kRowPad * kRowPad);
+    if (all + tid < end) a.list[all + tid] = 0;
+}
+
+// ---- products ------------------------------------------------------------------------------------------------------
+// Tiles of BM x BN results by WM x WN wavefronts, TM x TN blocks of 32 x 32 each; the contraction goes in steps of 64 through two
+// stages in LDS, one under way while the other is multiplied.  An operand lies in LDS as it does in memory: rows of results with the
+// contraction along them, or rows along the contraction (in blocks of 64 results), read turned.
+template <int WM_, int WN_, int TM_, int TN_>
+struct Shape {
+    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, kWaves = WM * WN;
+    static constexpr int BM = 32 * WM * TM, BN = 32 * WN * TN;
+    static constexpr int kStage = (BM + BN) * 128;
+    // row number i that a lane copies
+    static __device__ __forceinline__ int row(int i, int wave, int lane) { return (i * kWaves + wave) * 8 + (lane >> 3); }
+};
+
+// eight steps of the contraction in their own order: rows row0 + 8 * (lane / 32) ..
+__device__ __forceinline__ v8s across_in_order(const uint8_t *tile, int row0, int col0, int lane)
+{
+    typedef Rows<64> R;
+    typedef __attribute__((address_space(3))) v4s *turned;
+    const int row = row0 + 8 * (lane >> 5) + ((lane >> 2) & 3), col = col0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    const uint8_t *first = tile + R::at(row, col >> 3) + 2 * (col & 7), *second = tile + R::at(row + 4, col >> 3) + 2 * (col & 7);
+    const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((turned)first), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((turned)second);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+template <bool ACROSS>
+__device__ __forceinline__ v8s operand(const uint8_t *tile, int result, int sub, int lane)
+{
+    if constexpr (ACROSS) return across_in_order(tile + (result >> 6) * 8192, 16 * sub, result & 63, lane);
+    else return Rows<64>::along(tile, result, sub, lane);
+}
+
+// acc += A B^T over steps [s0, s1); row_a(i, r, s) is the address of LDS row r of step s: of result r (along), or for r = 64 * block + k of
+// step k, result block `block` (across); i numbers the rows that the lane copies.  after(s) is called behind a step's copies.
+template <typename S, bool A_ACROSS, bool B_ACROSS, typename FA, typename FB, typename FN>
+__device__ __forceinline__ void multiply(v16f (&acc)[S::TM][S::TN], uint8_t *lds, int s0, int s1, int wave, int lane, const FA &row_a, const FB &row_b, const FN &after)
+{
+    const int wm = wave / S::WN, wn = wave - wm * S::WN;
+    const uint32_t lds0 = lds_address(lds);
+    const auto fetch = [&](int s, int stage) {
+        const uint32_t to = lds0 + stage * S::kStage;
+        typedef Rows<64> R;
+        constexpr int NA = S::BM / 8, NB = S::BN / 8;
+        static_assert(NA % S::kWaves == 0 && NB % S::kWaves == 0, "every wavefront copies the same number of times");
+#pragma unroll
+        for (int i = 0; i < NA / S::kWaves; ++i) {
+            const int first = (i * S::kWaves + wave) * 8, r = first + R::copy_row(lane);
+            copy16(row_a(i, r, s) + 8 * R::copy_chunk(r, lane), to + first * 128);
+        }
+#pragma unroll
+        for (int i = 0; i < NB / S::kWaves; ++i) {
+            const int first = (i * S::kWaves + wave) * 8, r = first + R::copy_row(lane);
+            copy16(row_b(i, r, s) + 8 * R::copy_chunk(r, lane), to + S::BM * 128 + first * 128);
+        }
+        after(s);
+    };
+    fetch(s0, s0 & 1);
+    for (int s = s0; s < s1; ++s) {
+        wait_copies<0>();
+        barrier();
+        if (s + 1 < s1) fetch(s + 1, (s + 1) & 1);
+        const uint8_t *const ta = lds + (s & 1) * S::kStage, *const tb = ta + S::BM * 128;
+#pragma unroll
+        for (int sub = 0; sub < 4; ++sub) {
+            v8s x[S::TM], y[S::TN];
+#pragma unroll
+            for (int i = 0; i < S::TM; ++i) x[i] = operand<A_ACROSS>(ta, (wm * S::TM + i) * 32, sub, lane);
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j) y[j] = operand<B_ACROSS>(tb, (wn * S::TN + j) * 32, sub, lane);
+#pragma unroll
+            for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::TN; ++j) acc[i][j] = Bf16::mma32(x[i], y[j], acc[i][j]);
+        }
+    }
+    barrier();  // the stages are free again
+}
+template <int M, int N>
+__device__ __forceinline__ void clear(v16f (&x)[M][N])
+{
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) x[i][j][k] = 0.0f;
+}
+// Workgroups are dealt to the XCDs in turn: numbers that follow each other on one XCD get neighbouring tiles.
+__device__ __forceinline__ int first_tile() { return (gridDim.x & 7) ? (int)blockIdx.x : (int)((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3)); }
+
+// Logits, a tile of words by tokens at a time: a lane's results belong to one token.
+template <typename S, bool BACKWARD>
+__global__ __launch_bounds__(64 * S::kWaves, 1) void loss_logits_kernel(const LossArgs a)
+{
+    __shared__ __align__(1024) uint8_t lds[2 * S::kStage];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave - wm * S::WN;
+    const int n = a.counted->n, K = a.K;
+    const float scale = BACKWARD ? a.counted->scale : 0.0f, inv = scale > 0.0f ? 1.0f / scale : 0.0f;
+    const int words = BACKWARD ? a.piece / S::BM : (a.V + S::BM - 1) / S::BM, tiles = words * ((n + S::BN - 1) / S::BN);
+    for (int tile = first_tile(); tile < tiles; tile += gridDim.x) {
+        const int tt = tile / words, tv = tile - tt * words, t0 = tt * S::BN, v0 = (BACKWARD ? a.v0 : 0) + tv * S::BM;
+        v16f z[S::TM][S::TN];
+        clear(z);
+        const uint16_t *x[S::BN / 8 / S::kWaves];
+#pragma unroll
+        for (int i = 0; i < S::BN / 8 / S::kWaves; ++i) x[i] = a.X + (int64_t)a.list[t0 + S::row(i, wave, lane)] * K;
+        multiply<S, false, false>(z, lds, 0, K / 64, wave, lane,
+            [&](int, int r, int s) { return a.W + (int64_t)min(v0 + r, a.V - 1) * K + s * 64; },
+            [&](int i, int, int s) { return x[i] + s * 64; }, [](int) {});
+        // + bias; words past the end have no weight
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const int v = v0 + (wm * S::TM + i) * 32 + 8 * (k >> 2) + 4 * hf + (k & 3);
+                const float add = v >= a.V ? -__builtin_inff() : a.bias ? a.bias[v] : 0.0f;
+#pragma unroll
+                for (int j = 0; j < S::TN; ++j) z[i][j][k] = v >= a.V ? add : z[i][j][k] + add;
+            }
+        constexpr float kLog2e = 1.44269504088896341f;
+        if constexpr (!BACKWARD) {
+            v2f *const both = reinterpret_cast<v2f *>(lds);  // [WM][BN] maximum, sum of a wavefront's words
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j) {
+                const int row = t0 + (wn * S::TN + j) * 32 + l32;
+                float m = z[0][j][0];
+#pragma unroll
+                for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) m = fmaxf(m, z[i][j][k]);
+                m = fmaxf(halves_max(m), kLow);
+                const float m2 = m * kLog2e;
+                float l = 0.0f, hit = 0.0f;
+                const int target = row < n ? (int)a.targets[a.list[row]] - v0 - wm * S::TM * 32 - 4 * hf : -1;
+                bool have = false;
+#pragma unroll
+                for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        if (target == i * 32 + 8 * (k >> 2) + (k & 3)) {
+                            hit = z[i][j][k];
+                            have = true;
+                        }
+                        l += __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][j][k], kLog2e, -m2));
+                    }
+                l = halves_sum(l);
+                if (have) a.hit[row] = hit;
+                if (hf == 0) both[wm * S::BN + (wn * S::TN + j) * 32 + l32] = v2f{m, l};
+            }
+            barrier();
+            for (int r = threadIdx.x; r < S::BN; r += 64 * S::kWaves) {
+                v2f x = both[r];
+#pragma unroll
+                for (int i = 1; i < S::WM; ++i) {
+                    const v2f y = both[i * S::BN + r];
+                    const float m = fmaxf(x[0], y[0]);
+                    x = v2f{m, x[1] * __builtin_amdgcn_exp2f((x[0] - m) * kLog2e) + y[1] * __builtin_amdgcn_exp2f((y[0] - m) * kLog2e)};
+                }
+                a.part[(int64_t)tv * a.Tp + t0 + r] = x;
+            }
+            barrier();
+        } else {
+            float *const sums = reinterpret_cast<float *>(lds);  // [WN][BM] of d over a wavefront's tokens
+            v16f over[S::TM];
+#pragma unroll
+            for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) over[i][k] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j) {
+                const int row = t0 + (wn * S::TN + j) * 32 + l32, token = a.list[row];
+                const bool in = row < n;
+                const float lse2 = a.lse[token] * kLog2e, w = in ? a.dloss[token] * inv : 0.0f;
+                const int target = (int)a.targets[token] - v0 - wm * S::TM * 32 - 4 * hf;
+                uint16_t *const to = a.d + (int64_t)row * a.piece + tv * S::BM + wm * S::TM * 32 + 4 * hf;
+#pragma unroll
+                for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                    for (int k = 0; k < 16; k += 4) {
+                        float d[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][j][k + e], kLog2e, -lse2));
+                            d[e] = in ? (target == i * 32 + 2 * k + e ? p - 1.0f : p) * w : 0.0f;
+                            over[i][k + e] += d[e];
+                        }
+                        *reinterpret_cast<v2u *>(to + i * 32 + 2 * k) = v2u{Bf16::pair(d[0], d[1]), Bf16::pair(d[2], d[3])};
+                    }
+            }
+            if (a.db) {  // (uniform)
+#pragma unroll
+                for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        float x = over[i][k];
+#pragma unroll
+                        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor(x, o);
+                        if (l32 == 0) sums[wn * S::BM + (wm * S::TM + i) * 32 + 8 * (k >> 2) + 4 * hf + (k & 3)] = x;
+                    }
+                barrier();
+                for (int v = threadIdx.x; v < S::BM; v += 64 * S::kWaves) {
+                    float x = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < S::WN; ++i) x += sums[i * S::BM + v];
+                    a.db[(int64_t)tt * a.piece + tv * S::BM + v] = x;
+                }
+                barrier();
+            }
+        }
+    }
+}
+
+// loss and lse of 64 tokens from the maxima and sums of the vocabulary's tiles
+__global__ __launch_bounds__(256) void loss_join_kernel(const LossArgs a, int words)
+{
+    __shared__ v2f both[4][64];
+    const int n = a.counted->n, r = threadIdx.x & 63, q = threadIdx.x >> 6, row = blockIdx.x * 64 + r;
+    if (blockIdx.x * 64 >= n) return;
+    float m = kLow, l = 0.0f;
+    const auto add = [&](float m1, float l1) {
+        const float top = fmaxf(m, m1);
+        l = l * __expf(m - top) + l1 * __expf(m1 - top);
+        m = top;
+    };
+    for (int i = q; i < words; i += 4) {
+        const v2f x = a.part[(int64_t)i * a.Tp + row];  // (rows past n are computed too)
+        add(x[0], x[1]);
+    }
+    both[q][r] = v2f{m, l};
+    __syncthreads();
+    if (q != 0 || row >= n) return;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) add(both[i][r][0], both[i][r][1]);
+    const float lse = m + logf(l);
+    const int token = a.list[row];
+    a.lse[token] = lse;
+    a.loss[token] = lse - a.hit[row];
+}
+
+// A tile of dX is cut into slices of the contraction, the same number whoever asks.
+__device__ __host__ inline int dx_slices(int tiles, int steps)
+{
+    int s = 512 / (tiles > 0 ? tiles : 1);
+    s = s < steps / 8 ? s : steps / 8;
+    return s < 1 ? 1 : s < kSlices ? s : kSlices;
+}
+
+// The piece's share of both gradients: results lie transposed in the products (hidden units by tokens or words), so that a lane
+// holds neighbours of a row of dX or dW.
+template <typename S>
+__global__ __launch_bounds__(64 * S::kWaves, 1) void loss_grads_kernel(const LossArgs a)
+{
+    __shared__ __align__(1024) uint8_t lds[2 * S::kStage];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave - wm * S::WN;
+    const int n = a.counted->n, K = a.K;
+    const float scale = a.counted->scale;
+    const int kt = (K + S::BM - 1) / S::BM;
+    const int words = min(a.piece, (a.V - a.v0 + 63) / 64 * 64);                 // of this piece, in whole steps
+    const int x_tiles = kt * ((n + S::BN - 1) / S::BN), slices = dx_slices(x_tiles, a.piece / 64), x_steps = words / 64;
+    const int w_tiles = kt * ((words + S::BN - 1) / S::BN), w_steps = (n + 63) / 64;
+    for (int id = first_tile(); id < x_tiles * slices + w_tiles; id += gridDim.x) {
+        v16f acc[S::TM][S::TN];
+        clear(acc);
+        if (id < x_tiles * slices) {
+            const int tile = id / slices, slice = id - tile * slices, tt = tile / kt, k0 = (tile - tt * kt) * S::BM, t0 = tt * S::BN;
+            const int s0 = x_steps * slice / slices, s1 = x_steps * (slice + 1) / slices;
+            if (s0 < s1)
+                multiply<S, true, false>(acc, lds, s0, s1, wave, lane,
+                    [&](int, int r, int s) { return a.W + (int64_t)min(a.v0 + s * 64 + (r & 63), a.V - 1) * K + min(k0 + (r & ~63), K - 64); },
+                    [&](int, int r, int s) { return a.d + (int64_t)(t0 + r) * a.piece + s * 64; }, [](int) {});
+            float *const to = a.dXs + (int64_t)id * S::BM * S::BN;
+#pragma unroll
+            for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+                    for (int k = 0; k < 16; k += 4) {
+                        v4f *const p = reinterpret_cast<v4f *>(to + ((wn * S::TN + j) * 32 + l32) * S::BM + (wm * S::TM + i) * 32 + 2 * k + 4 * hf);
+                        v4f x = {acc[i][j][k], acc[i][j][k + 1], acc[i][j][k + 2], acc[i][j][k + 3]};
+                        if (a.v0 > 0) x += *p;
+                        *p = x;
+                    }
+        } else {
+            const int tile = id - x_tiles * slices, tv = tile / kt, k0 = (tile - tv * kt) * S::BM, v0 = tv * S::BN;
+            if (w_steps > 0) {
+                int token[S::BM / 8 / S::kWaves];  // of the next step, fetched a step ahead
+                const auto look_up = [&](int s) {
+                    if (s + 1 >= w_steps) return;
+#pragma unroll
+                    for (int i = 0; i < S::BM / 8 / S::kWaves; ++i) token[i] = a.list[(s + 1) * 64 + (S::row(i, wave, lane) & 63)];
+                };
+                look_up(-1);
+                multiply<S, true, true>(acc, lds, 0, w_steps, wave, lane,
+                    [&](int i, int r, int) { return a.X + (int64_t)token[i] * K + min(k0 + (r & ~63), K - 64); },
+                    [&](int, int r, int s) { return a.d + (int64_t)(s * 64 + (r & 63)) * a.piece + v0 + (r & ~63); }, look_up);
+            }
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j) {
+                const int v = a.v0 + v0 + (wn * S::TN + j) * 32 + l32;
+                if (v >= a.V) continue;
+#pragma unroll
+                for (int i = 0; i < S::TM; ++i) {
+                    const int k1 = k0 + (wm * S::TM + i) * 32;
+                    if (k1 >= K) continue;
+#pragma unroll
+                    for (int k = 0; k < 16; k += 4)
+                        *reinterpret_cast<v2u *>(a.dW + (int64_t)v * K + k1 + 2 * k + 4 * hf) =
+                            v2u{Bf16::pair(acc[i][j][k] * scale, acc[i][j][k + 1] * scale), Bf16::pair(acc[i][j][k + 2] * scale, acc[i][j][k + 3] * scale)};
+                }
+            }
+        }
+    }
+}
+
+// dX from its slices, a zero row for a token without a target
+template <typename S>
+__global__ __launch_bounds__(256) void loss_dx_kernel(const LossArgs a)
+{
+    const int n = a.counted->n, K = a.K, quads = K / 4;
+    const float scale = a.counted->scale;
+    const int kt = (K + S::BM - 1) / S::BM, slices = dx_slices(kt * ((n + S::BN - 1) / S::BN), a.piece / 64);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)a.T * quads; i += (int64_t)gridDim.x * 256) {
+        const int t = (int)(i / quads), k = (int)(i - (int64_t)t * quads) * 4, row = a.place[t];
+        v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (row >= 0) {
+            const int tile = (row / S::BN) * kt + k / S::BM;
+            const float *p = a.dXs + (int64_t)tile * slices * S::BM * S::BN + (row % S::BN) * S::BM + k % S::BM;
+            for (int s = 0; s < slices; ++s) x += *reinterpret_cast<const v4f *>(p + (int64_t)s * S::BM * S::BN);
+        }
+        *reinterpret_cast<v2u *>(a.dX + (int64_t)t * K + k) = v2u{Bf16::pair(x[0] * scale, x[1] * scale), Bf16::pair(x[2] * scale, x[3] * scale)};
+    }
+}
+
+// the piece's share of dbias
+template <typename S>
+__global__ __launch_bounds__(256) void loss_dbias_kernel(const LossArgs a)
+{
+    const int v = blockIdx.x * 256 + threadIdx.x;
+    if (v >= a.piece || a.v0 + v >= a.V) return;
+    const int tiles = (a.counted->n + S::BN - 1) / S::BN;
+    float x = 0.0f;
+    for (int i = 0; i < tiles; ++i) x += a.db[(int64_t)i * a.piece + v];
+    a.dbias[a.v0 + v] = x * a.counted->scale;
+}
+
+typedef Shape<2, 4, 4, 2> Large;  // 256 x 256
+typedef Shape<4, 1, 1, 2> Small;  // 128 x 64
+inline bool few(int64_t T) { return T <= 1024; }
+
+inline size_t up(size_t v) { return (v + 255) / 256 * 256; }
+
+// where everything lies in the workspace; returns its size
+size_t lay_out(LossArgs &a, uint8_t *base, bool backward)
+{
+    size_t at = 0;
+    const auto take = [&](size_t bytes) {
+        uint8_t *p = base + at;
+        at += up(bytes);
+        return p;
+    };
+    const int bm = few(a.T) ? Small::BM : Large::BM, bn = few(a.T) ? Small::BN : Large::BN;
+    a.Tp = (int)((a.T + kRowPad - 1) / kRowPad * kRowPad);
+    a.counted = reinterpret_cast<Counted *>(take(sizeof(Counted)));
+    a.list = reinterpret_cast<int *>(take((size_t)a.Tp * 4));
+    if (!backward) {
+        a.part = reinterpret_cast<v2f *>(take((size_t)((a.V + bm - 1) / bm) * a.Tp * 8));
+        a.hit = reinterpret_cast<float *>(take((size_t)a.Tp * 4));
+        return at;
+    }
+    a.place = reinterpret_cast<int *>(take((size_t)a.T * 4));
+    const int64_t widest = ((int64_t)a.V + kRowPad - 1) / kRowPad * kRowPad;
+    a.piece = (int)std::min(widest, std::max<int64_t>(kRowPad, kPieceBytes / (2ll * a.Tp) / kRowPad * kRowPad));
+    const int64_t pieces = (widest + a.piece - 1) / a.piece;
+    a.piece = (int)((widest / kRowPad + pieces - 1) / pieces * kRowPad);  // pieces of about one size
+    a.d = reinterpret_cast<uint16_t *>(take((size_t)a.Tp * a.piece * 2));
+    a.db = reinterpret_cast<float *>(take((size_t)(a.Tp / bn) * a.piece * 4));
+    const int64_t x_tiles = (int64_t)(a.Tp / bn) * ((a.K + bm - 1) / bm);
+    a.dXs = reinterpret_cast<float *>(take((size_t)std::max(x_tiles, std::min<int64_t>(512, x_tiles * kSlices)) * bm * bn * 4));
+    return at;
+}
+
+bool shape_ok(int64_t T, int64_t V, int64_t K) { return T >= 1 && T <= kMost && V >= 1 && V <= kMost && k_ok(K); }
+
+template <typename S>
+qb_status forward(const LossArgs &a, hipStream_t st)
+{
+    const int words = (a.V + S::BM - 1) / S::BM;
+    const int64_t tiles = (int64_t)words * (a.Tp / S::BN);
+    const int grid = (int)std::min<int64_t>(tiles, S::kWaves == 8 ? 256 : 1024);
+    loss_rows_kernel<false><<<(a.T + 1023) / 1024, 1024, 0, st>>>(a);
+    loss_logits_kernel<S, false><<<grid, 64 * S::kWaves, 0, st>>>(a);
+    loss_join_kernel<<<(a.T + 63) / 64, 256, 0, st>>>(a, words);
+    return launch_status();
+}
+
+template <typename S>
+qb_status backward(LossArgs a, hipStream_t st)
+{
+    loss_rows_kernel<true><<<(a.T + 1023) / 1024, 1024, 0, st>>>(a);
+    const int most = S::kWaves == 8 ? 256 : 1024;
+    for (a.v0 = 0; a.v0 < a.V; a.v0 += a.piece) {
+        const int64_t tiles = (int64_t)(a.piece / S::BM) * (a.Tp / S::BN);
+        loss_logits_kernel<S, true><<<(int)std::min<int64_t>(tiles, most), 64 * S::kWaves, 0, st>>>(a);
+        if (a.dbias) loss_dbias_kernel<S><<<(a.piece + 255) / 256, 256, 0, st>>>(a);
+        loss_grads_kernel<S><<<most, 64 * S::kWaves, 0, st>>>(a);
+    }
+    loss_dx_kernel<S><<<(int)std::min<int64_t>(4096, ((int64_t)a.T * (a.K / 4) + 255) / 256), 256, 0, st>>>(a);
+    return launch_status();
+}
+
+}  // namespace
+}  // namespace qb
+
+using namespace qb;
+
+extern "C" size_t qb_vocab_loss_workspace_nbytes(int64_t T, int64_t V, int64_t K, int backward)
+{
+    if (!shape_ok(T, V, K)) return 0;
+    LossArgs a = {};
+    a.T = (int)T;
+    a.V = (int)V;
+    a.K = (int)K;
+    return lay_out(a, nullptr, backward != 0);
+}
+
+extern "C" qb_status qb_vocab_loss_fwd(const uint16_t *X, const uint16_t *W, const float *bias, const int64_t *targets,
+                                       int64_t T, int64_t V, int64_t K, float *loss, float *lse, void *workspace, void *stream)
+{
+    if (!shape_ok(T, V, K)) return QB_ERR_SHAPE;
+    if (!X || !W || !targets || !loss || !lse) return QB_ERR_NULL;
+    if (!aligned16(X) || !aligned16(W) || !aligned16(bias) || !aligned16(targets)) return QB_ERR_VALUE;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255)) return QB_ERR_WORKSPACE;
+    LossArgs a = {};
+    a.X = X; a.W = W; a.bias = bias; a.targets = targets;
+    a.T = (int)T; a.V = (int)V; a.K = (int)K;
+    a.loss = loss; a.lse = lse;
+    lay_out(a, static_cast<uint8_t *>(workspace), false);
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return few(T) ? forward<Small>(a, st) : forward<Large>(a, st);
+}
+
+extern "C" qb_status qb_vocab_loss_bwd(const float *dloss, const uint16_t *X, const uint16_t *W, const float *bias,
+                                       const int64_t *targets, const float *lse, int64_t T, int64_t V, int64_t K,
+                                       uint16_t *dX, uint16_t *dW, float *dbias, void *workspace, void *stream)
+{
+    if (!shape_ok(T, V, K)) return QB_ERR_SHAPE;
+    if (!dloss || !X || !W || !targets || !lse || !dX || !dW) return QB_ERR_NULL;
+    if (!aligned16(X) || !aligned16(W) || !aligned16(bias) || !aligned16(targets) || !aligned16(dX) || !aligned16(dW)) return QB_ERR_VALUE;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255)) return QB_ERR_WORKSPACE;
+    LossArgs a = {};
+    a.X = X; a.W = W; a.bias = bias; a.targets = targets; a.dloss = dloss;
+    a.T = (int)T; a.V = (int)V; a.K = (int)K;
+    a.lse = const_cast<float *>(lse);
+    a.dX = dX; a.dW = dW; a.dbias = dbias;
+    lay_out(a, static_cast<uint8_t *>(workspace), true);
+    if (!dbias) a.db = nullptr;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return few(T) ? backward<Small>(a, st) : backward<Large>(a, st);
+}

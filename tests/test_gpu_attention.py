@@ -1,0 +1,339 @@
+"""Attention of packed sequences against the definition in 64 bits, forward and backward.
+
+Tolerances follow from the roundings.  u is the type's largest relative rounding error (2^-8 bfloat16, 2^-11 float16).  Results are
+rounded once (u of themselves); exponentials (for O, dV) and dS (for dQ, dK) are rounded once before their product: u of the
+same sum over absolute values.  Sums in 32 bits add 2^-18 of the sums of absolute values.  delta = dO.O takes the rounded O
+where a call allows more than 2048 keys: u of |dO|.|O|; below that only products of two roundings are left."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"bf16": (torch.bfloat16, 2.0 ** -8), "fp16": (torch.float16, 2.0 ** -11)}
+E32 = 2.0 ** -18
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def draws(row, word1, index, seed):
+    """16-bit draw number `index` of the counters (row, word1): Threefry-2x32, 13 rounds, in int64"""
+    m = 0xFFFFFFFF
+    k = [seed & m, (seed >> 32) & m]
+    k.append(k[0] ^ k[1] ^ 0x1BD11BDA)
+    a, b = torch.broadcast_tensors((row + k[0]) & m, (word1 + k[1]) & m)
+    for i in range(13):
+        a = (a + b) & m
+        t = (13, 15, 26, 6, 17, 29, 16, 24)[i % 8]
+        b = (((b << t) & m) | (b >> (32 - t))) ^ a
+        if i % 4 == 3:
+            j = i // 4 + 1
+            a, b = (a + k[j % 3]) & m, (b + k[(j + 1) % 3] + j) & m
+    return (torch.where(index >= 2, b, a) >> (16 * (index % 2))) & 0xFFFF
+
+
+def keep64(q0, nq, h, nk, p, seed):
+    if p == 0.0:
+        return 1.0
+    j = torch.arange(nk, device=DEV)
+    t = min(65535, round(p * 65536))
+    d = draws(torch.arange(q0, q0 + nq, device=DEV)[:, None], (1 << 31) + (h << 22) + j // 4, j % 4, seed)
+    return (d >= t).double() * (65536.0 / (65536 - t))
+
+
+def offsets(lens, gaps=None):
+    at = [0]
+    for i, n in enumerate(lens):
+        at.append(at[-1] + n + (gaps[i] if gaps else 0))
+    return at
+
+
+class Case:
+    def __init__(self, type, dim, heads, kv_heads, q_lens, k_lens=None, causal=False, p=0.0, fused=False, cap=None, std=1.4, seed=1, max_k=None):
+        self.dtype, self.u = TYPES[type]
+        self.dim, self.heads, self.kv, self.causal, self.p, self.group = dim, heads, kv_heads, causal, p, heads // kv_heads
+        self.q_lens, self.k_lens = q_lens, k_lens if k_lens is not None else q_lens
+        self.scale = 1.0 / math.sqrt(dim)
+        g = torch.Generator(device=DEV)
+        g.manual_seed(seed)
+        self.cq = offsets(q_lens)
+        gaps = None if cap is None else [cap - n for n in self.k_lens]
+        self.ck = offsets(self.k_lens, gaps)
+        tq, tk = self.cq[-1], self.ck[-1]
+        rnd = lambda *s, w=1.0: (torch.randn(*s, generator=g, device=DEV) * w).to(self.dtype)  # noqa: E731
+        if fused:
+            assert k_lens is None
+            x = rnd(tq, heads + 2 * kv_heads, dim, w=std)
+            self.Q, self.K, self.V = x[:, :heads], x[:, heads:heads + kv_heads], x[:, heads + kv_heads:]
+        else:
+            self.Q, self.K, self.V = rnd(tq, heads, dim, w=std), rnd(tk, kv_heads, dim, w=std), rnd(tk, kv_heads, dim)
+        self.k_len = None
+        if cap is not None:
+            self.k_len = torch.tensor(self.k_lens, dtype=torch.int32, device=DEV)
+            for b, n in enumerate(self.k_lens):  # what lies behind a sequence in its cache is not read
+                self.K[self.ck[b] + n:self.ck[b + 1]] = float("nan")
+                self.V[self.ck[b] + n:self.ck[b + 1]] = float("inf")
+        self.dO = rnd(tq, heads, dim)
+        self.cu_q, self.cu_k = (torch.tensor(c, dtype=torch.int32, device=DEV) for c in (self.cq, self.ck))
+        self.max_q, self.max_k = max(q_lens), max_k or max(self.k_lens)
+        self.seed = torch.randint(-(1 << 62), 1 << 62, (1,), generator=g, device=DEV, dtype=torch.int64) if p else None
+
+    def forward(self, qb, **k):
+        return qb.qb_attention_fwd(self.Q, self.K, self.V, self.cu_q, self.cu_k, self.max_q, self.max_k, causal=self.causal, k_len=self.k_len, p=self.p, seed=self.seed, **k)
+
+    def backward(self, qb, O, lse, **k):
+        return qb.qb_attention_bwd(self.dO, self.Q, self.K, self.V, O, lse, self.cu_q, self.cu_k, self.max_q, self.max_k, causal=self.causal, p=self.p, seed=self.seed, **k)
+
+    def exact(self, backward=False, Q=None, K=None, V=None):
+        """(values, tolerances) of O, lse(, dQ, dK, dV) in 64 bits"""
+        Q, K, V = (self.Q if Q is None else Q), (self.K if K is None else K), (self.V if V is None else V)
+        z = lambda x: torch.zeros(x.shape, dtype=torch.float64, device=DEV)  # noqa: E731
+        names = ("O", "lse", "dQ", "dK", "dV")
+        val = dict(zip(names, (z(Q), torch.full(Q.shape[:2], -math.inf, dtype=torch.float64, device=DEV), z(Q), z(K), z(V))))
+        tol = dict(zip(names, (z(Q), torch.zeros(Q.shape[:2], dtype=torch.float64, device=DEV), z(Q), z(K), z(V))))
+        seed = int(self.seed) if self.p else 0
+        for b, (nq, nk) in enumerate(zip(self.q_lens, self.k_lens)):
+            if nq == 0 or nk == 0:
+                continue
+            rq, rk = slice(self.cq[b], self.cq[b] + nq), slice(self.ck[b], self.ck[b] + nk)
+            hidden = torch.zeros(nq, nk, dtype=torch.bool, device=DEV)
+            if self.causal:
+                hidden = torch.arange(nk, device=DEV)[None, :] > torch.arange(nq, device=DEV)[:, None] + nk - nq
+            for h in range(self.heads):
+                q, k, v = Q[rq, h].double(), K[rk, h // self.group].double(), V[rk, h // self.group].double()
+                s = (q @ k.t() * self.scale).masked_fill(hidden, -math.inf)
+                lse = torch.logsumexp(s, 1)
+                P = torch.exp(s - torch.where(lse > -math.inf, lse, 0.0)[:, None])
+                M = keep64(self.cq[b], nq, h, nk, self.p, seed)
+                PM = P * M
+                val["lse"][rq, h] = lse
+                tol["lse"][rq, h] = 2e-6 + 2e-6 * torch.where(lse > -math.inf, lse.abs(), 0.0) + E32 / 4 * self.scale * (q.abs() @ k.abs().t()).amax(1)
+                val["O"][rq, h] = O = PM @ v
+                s_err = E32 / 4 * self.scale * (q.abs() @ k.abs().t())  # of a score, and relative of its exponential
+                tol["O"][rq, h] = self.u * O.abs() + (PM * (1.05 * self.u + 2 * s_err)) @ v.abs() + 1e-6
+                if not backward:
+                    continue
+                d = self.dO[rq, h].double()
+                dP = (d @ v.t()) * M
+                delta = (P * dP).sum(1, keepdim=True)
+                dS = P * (dP - delta)
+                d_abs = (d.abs() @ O.abs().t()).diagonal()[:, None] if nq <= 4096 else (d.abs() * O.abs()).sum(1, keepdim=True)
+                off = self.u * d_abs if self.max_k > 2048 else 8 * self.u ** 2 * d_abs
+                S_tol = 1.05 * self.u * dS.abs() + P * (E32 * ((d.abs() @ v.abs().t()) * M + d_abs) + off) + 2 * s_err * dS.abs()
+                val["dQ"][rq, h] = dS @ k * self.scale
+                tol["dQ"][rq, h] = S_tol @ k.abs() * self.scale
+                val["dK"][rk, h // self.group] += dS.t() @ q * self.scale
+                tol["dK"][rk, h // self.group] += S_tol.t() @ q.abs() * self.scale
+                val["dV"][rk, h // self.group] += PM.t() @ d
+                tol["dV"][rk, h // self.group] += (PM * (1.05 * self.u + 2 * s_err)).t() @ d.abs()
+        for n in ("dQ", "dK", "dV"):
+            tol[n] += self.u * val[n].abs() + 1e-6
+        return val, tol
+
+
+def check(name, got, val, tol):
+    got = got.double()
+    assert torch.equal(torch.isinf(got), torch.isinf(val)), name
+    fine = torch.isfinite(val)
+    assert torch.isfinite(got[fine]).all(), name
+    off, tol = (got - val).abs()[fine], tol[fine]
+    assert (off[tol == 0] == 0).all(), name  # sequences without keys: exactly nothing
+    worst = (off / tol.clamp(min=1e-300)).max().item() if fine.any() else 0.0
+    say("  %s: worst error %.3f of its bound" % (name, worst))
+    assert worst <= 1.0, (name, worst)
+
+
+FORWARD = {
+    "one token": dict(type="bf16", dim=64, heads=2, kv_heads=2, q_lens=[1]),
+    "lengths round a tile": dict(type="bf16", dim=64, heads=3, kv_heads=3, q_lens=[63, 64, 65, 127, 128, 129, 1, 31, 33], fused=True),
+    "the same, causal": dict(type="fp16", dim=64, heads=3, kv_heads=3, q_lens=[63, 64, 65, 127, 128, 129, 1, 31, 33], fused=True, causal=True),
+    "wide heads, groups of three": dict(type="bf16", dim=128, heads=6, kv_heads=2, q_lens=[200, 1, 77], causal=True),
+    "groups of seven, fp16": dict(type="fp16", dim=128, heads=7, kv_heads=1, q_lens=[130, 19], fused=True),
+    "empty sequences": dict(type="bf16", dim=64, heads=4, kv_heads=2, q_lens=[0, 5, 0, 70, 0], k_lens=[7, 0, 0, 66, 3]),
+    "more queries than keys, causal": dict(type="bf16", dim=64, heads=2, kv_heads=1, q_lens=[100, 3, 70], k_lens=[40, 1, 69], causal=True),
+    "more keys than queries, causal": dict(type="fp16", dim=128, heads=2, kv_heads=2, q_lens=[40, 1, 69], k_lens=[300, 200, 71], causal=True),
+    "large scores": dict(type="bf16", dim=64, heads=2, kv_heads=2, q_lens=[300], std=12.0),
+    "dropout": dict(type="bf16", dim=64, heads=4, kv_heads=4, q_lens=[130, 5, 64], p=0.1, fused=True),
+    "dropout, groups, causal, wide": dict(type="fp16", dim=128, heads=6, kv_heads=2, q_lens=[70, 131], p=0.5, causal=True),
+    "cache, single tokens": dict(type="bf16", dim=64, heads=4, kv_heads=4, q_lens=[1, 1, 1, 1, 1], k_lens=[1, 390, 64, 0, 129], cap=400, causal=True),
+    "cache, single tokens, groups, long": dict(type="bf16", dim=128, heads=8, kv_heads=2, q_lens=[1, 1, 1], k_lens=[5000, 1, 1027], cap=5003, causal=True),
+    "cache, five new tokens": dict(type="fp16", dim=64, heads=12, kv_heads=4, q_lens=[5, 5, 5], k_lens=[5, 700, 2049], cap=2050, causal=True),
+    "cache, three new tokens, not causal": dict(type="bf16", dim=128, heads=5, kv_heads=1, q_lens=[3, 3], k_lens=[900, 2], cap=1000),
+    "cache, groups of forty": dict(type="bf16", dim=64, heads=40, kv_heads=1, q_lens=[1, 2], k_lens=[3000, 77], cap=3000, causal=True),
+    "cache, one long conversation": dict(type="fp16", dim=64, heads=2, kv_heads=1, q_lens=[1], k_lens=[70001], cap=70100, causal=True),
+    "many short sequences": dict(type="bf16", dim=64, heads=2, kv_heads=2, q_lens=[(i * 7) % 23 for i in range(150)], causal=True),
+}
+TRAIN = {n: FORWARD[n] for n in ("one token", "lengths round a tile", "the same, causal", "wide heads, groups of three", "groups of seven, fp16", "empty sequences",
+                                 "more queries than keys, causal", "more keys than queries, causal", "dropout", "dropout, groups, causal, wide", "many short sequences")}
+TRAIN["more than 2048 keys, causal"] = dict(type="bf16", dim=64, heads=4, kv_heads=1, q_lens=[2100, 50], causal=True, fused=True)
+TRAIN["more than 2048 keys, wide"] = dict(type="fp16", dim=128, heads=2, kv_heads=1, q_lens=[70], k_lens=[2300], p=0.1)
+TRAIN["more keys allowed than there are"] = dict(type="bf16", dim=128, heads=4, kv_heads=4, q_lens=[65, 200], max_k=4000, p=0.1)
+
+
+@pytest.mark.parametrize("name", FORWARD)
+def test_forward(qb, name):
+    say("attention forward:", name)
+    c = Case(**FORWARD[name])
+    O = torch.full(c.Q.shape, float("nan"), dtype=c.dtype, device=DEV)
+    lse = torch.full(c.Q.shape[:2], float("nan"), device=DEV)
+    got = c.forward(qb, O=O, lse=lse)
+    assert got[0] is O or got[0].data_ptr() == O.data_ptr()
+    val, tol = c.exact()
+    check("O", O, val["O"], tol["O"])
+    check("lse", lse, val["lse"], tol["lse"])
+    again = c.forward(qb)
+    assert torch.equal(again[0], O) and torch.equal(again[1], lse)
+
+
+@pytest.mark.parametrize("name", TRAIN)
+def test_backward(qb, name):
+    say("attention backward:", name)
+    c = Case(**TRAIN[name])
+    O, lse = c.forward(qb)
+    grads = [torch.full(x.shape, float("nan"), dtype=c.dtype, device=DEV) for x in (c.Q, c.K, c.V)]
+    c.backward(qb, O, lse, dQ=grads[0], dK=grads[1], dV=grads[2])
+    val, tol = c.exact(backward=True)
+    for n, x in zip(("dQ", "dK", "dV"), grads):
+        check(n, x, val[n], tol[n])
+    for x, y in zip(grads, c.backward(qb, O, lse)):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("name", ["lengths round a tile", "wide heads, groups of three", "dropout, groups, causal, wide"])
+def test_gradients_against_differences(qb, name):
+    """the change of sum(dO * O), in 64 bits, along random directions"""
+    say("attention differences:", name)
+    c = Case(**TRAIN[name])
+    O, lse = c.forward(qb)
+    grads = dict(zip("QKV", c.backward(qb, O, lse)))
+    val, tol = c.exact(backward=True)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(9)
+    for n in "QKV":
+        x = getattr(c, n).double()
+        r = torch.randn(x.shape, generator=g, device=DEV, dtype=torch.float64)
+        loss = lambda e: (c.exact(**{n: x + e * r})[0]["O"] * c.dO.double()).sum().item()  # noqa: E731
+        e = 1e-4
+        slope = (loss(e) - loss(-e)) / (2 * e)
+        bound = (tol["d" + n] * r.abs()).sum().item() + 1e-6 * abs(slope)
+        assert abs((grads[n].double() * r).sum().item() - slope) <= bound, n
+
+
+def test_gradients_into_one_tensor(qb):
+    """dQ, dK and dV side by side, as the backward of one projection takes them; rows outside the sequences stay as they are"""
+    c = Case("bf16", 64, 4, 2, [70, 33], fused=True)
+    O, lse = c.forward(qb)
+    want = c.backward(qb, O, lse)
+    all_ = torch.full((c.Q.shape[0], 8, 64), 7.0, dtype=c.dtype, device=DEV)
+    c.backward(qb, O, lse, dQ=all_[:, :4], dK=all_[:, 4:6], dV=all_[:, 6:])
+    assert torch.equal(all_, torch.cat(want, 1))
+    c.cu_q = c.cu_k = torch.tensor([0, 70, 90], dtype=torch.int32, device=DEV)
+    out = torch.full_like(O, 5.0)
+    c.forward(qb, O=out)
+    assert (out[90:] == 5.0).all() and not (out[:90] == 5.0).all(1).all(1).any()
+    all_.fill_(7.0)
+    c.backward(qb, O, lse, dQ=all_[:, :4], dK=all_[:, 4:6], dV=all_[:, 6:])
+    assert (all_[90:] == 7.0).all()
+
+
+def test_offsets_that_leave_the_tensors_are_cut(qb):
+    c = Case("bf16", 64, 2, 2, [40, 30])
+    want = c.forward(qb)[0]
+    c.cu_q = torch.tensor([0, 40, 5000], dtype=torch.int32, device=DEV)
+    c.cu_k = torch.tensor([0, 40, 5000], dtype=torch.int32, device=DEV)
+    assert torch.equal(c.forward(qb)[0], want)
+
+
+def test_rows_far_apart(qb):
+    """keys whose offsets pass 32 bits"""
+    n, stride = 70, 1 << 25
+    big = torch.empty(n * stride, dtype=torch.bfloat16, device=DEV)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    K, V = big.as_strided((n, 1, 64), (stride, 64, 1)), big.as_strided((n, 1, 64), (stride, 64, 1), 64)
+    K.copy_(torch.randn(n, 1, 64, generator=g, device=DEV))
+    V.copy_(torch.randn(n, 1, 64, generator=g, device=DEV))
+    for q in (1, 70):
+        Q = torch.randn(q, 1, 64, generator=g, device=DEV).bfloat16()
+        cu = [torch.tensor([0, x], dtype=torch.int32, device=DEV) for x in (q, n)]
+        got = qb.qb_attention_fwd(Q, K, V, *cu, q, n, causal=True)
+        assert all(torch.equal(x, y) for x, y in zip(got, qb.qb_attention_fwd(Q, K.contiguous(), V.contiguous(), *cu, q, n, causal=True)))
+
+
+def test_on_another_stream_and_in_a_graph(qb):
+    c = Case("bf16", 64, 4, 2, [130, 70], causal=True, p=0.1)
+    want = c.forward(qb)
+    grads = c.backward(qb, *want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = c.forward(qb)
+        got_grads = c.backward(qb, *got)
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(want + grads, got + got_grads))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = c.forward(qb)
+        held_grads = c.backward(qb, *held)
+    first = int(c.seed)
+    for i in range(4):  # other dropout bits with every new seed
+        c.seed.fill_(first + i % 2)
+        graph.replay()
+        torch.cuda.synchronize()
+        now = c.forward(qb)
+        assert all(torch.equal(x, y) for x, y in zip(held + held_grads, now + c.backward(qb, *now)))
+    assert not torch.equal(held[0], want[0])
+
+
+def test_refusals(qb):
+    c = Case("bf16", 64, 4, 2, [40, 30])
+    O, lse = c.forward(qb)
+
+    def status(**changes):
+        with pytest.raises(qb.QBError) as e:
+            for k, v in changes.items():
+                setattr(c, k, v)
+            c.forward(qb)
+        return e.value.status
+    keep = dict(Q=c.Q, K=c.K, V=c.V, p=0.0, seed=None, max_q=40)
+    for changes, want in ((dict(Q=c.Q[:, :, :32], K=c.K[:, :, :32], V=c.V[:, :, :32]), 3), (dict(Q=c.Q[:, :3]), 3), (dict(p=1.0), 7), (dict(p=-0.1), 7),
+                          (dict(p=float("nan")), 7), (dict(p=0.1), 1), (dict(max_q=-1), 3)):
+        assert status(**changes) == want, changes
+        for k, v in keep.items():
+            setattr(c, k, v)
+    odd = torch.zeros(70 * 4 * 66, dtype=torch.bfloat16, device=DEV)
+    assert status(Q=odd.as_strided((70, 4, 64), (4 * 66, 66, 1))) == 7
+    assert status(Q=odd[1:].as_strided((70, 4, 64), (256, 64, 1))) == 7
+    c.Q = keep["Q"]
+    for scale in (0.0, -1.0, float("inf"), float("nan")):
+        with pytest.raises(qb.QBError):
+            c.forward(qb, scale=scale)
+    for bad in (dict(Q=c.Q.float()), dict(K=c.K.half()), dict(cu_q=c.cu_q.long()), dict(k_len=c.cu_q.long()), dict(Q=c.Q.cpu())):
+        held = {k: getattr(c, k) for k in bad}
+        for k, v in bad.items():
+            setattr(c, k, v)
+        with pytest.raises(TypeError):
+            c.forward(qb)
+        for k, v in held.items():
+            setattr(c, k, v)
+    for bad in (dict(V=c.V[:-1]), dict(cu_q=c.cu_q[:-1]), dict(Q=c.Q[0]), dict(k_len=c.cu_q)):
+        held = {k: getattr(c, k) for k in bad}
+        for k, v in bad.items():
+            setattr(c, k, v)
+        with pytest.raises(ValueError):
+            c.forward(qb)
+        for k, v in held.items():
+            setattr(c, k, v)
+    with pytest.raises(ValueError):
+        c.forward(qb, O=O[:-1])
+    with pytest.raises(TypeError):
+        c.forward(qb, lse=lse.double())
+    with pytest.raises(ValueError):
+        c.backward(qb, O, lse, workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
+    with pytest.raises(ValueError):
+        c.backward(qb, O, lse, dK=c.V[:-1])
+    with pytest.raises(TypeError):
+        c.backward(qb, O.half(), lse)
