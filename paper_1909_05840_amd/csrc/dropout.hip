@@ -10,6 +10,8 @@
 namespace qb {
 namespace {
 
+constexpr int kAtOnce = 4;  // chunks of sixteen bytes that a thread has under way
+
 struct DropArgs {
     const void *X, *residual;
     void *Y;
@@ -19,44 +21,124 @@ struct DropArgs {
     float scale;
 };
 
-// one value of a type as a float, and back (rounded to nearest even)
-template <int TYPE>
-__device__ __forceinline__ float value(const void *p, int64_t i)
+// sixteen bytes at any address (the load unit takes them with the same instruction, aligned or not)
+__device__ __forceinline__ v4u load16(const void *p, int64_t byte)
 {
-    if constexpr (TYPE == QB_TYPE_FP32) return static_cast<const float *>(p)[i];
-    const uint32_t w = static_cast<const uint16_t *>(p)[i];
-    return TYPE == QB_TYPE_BF16 ? Bf16::lo(w) : Fp16::lo(w);
+    struct __attribute__((packed)) Loose { v4u v; };
+    return reinterpret_cast<const Loose *>(static_cast<const uint8_t *>(p) + byte)->v;
+}
+__device__ __forceinline__ void store16(void *p, int64_t byte, v4u v)
+{
+    struct __attribute__((packed)) Loose { v4u v; };
+    reinterpret_cast<Loose *>(static_cast<uint8_t *>(p) + byte)->v = v;
+}
+
+// Sixteen bytes are a chunk: four values and one counter in 32 bits, eight values and two counters in 16.
+template <int TYPE>
+struct Chunk {
+    static constexpr int kSize = TYPE == QB_TYPE_FP32 ? 4 : 2, kValues = 16 / kSize, kCounters = kValues / 4;
+    typedef std::conditional_t<TYPE == QB_TYPE_BF16, Bf16, Fp16> T;
+    float v[kValues];
+    __device__ __forceinline__ explicit Chunk(v4u w)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (TYPE == QB_TYPE_FP32) {
+                v[i] = __uint_as_float(w[i]);
+            } else {
+                v[2 * i] = T::lo(w[i]);
+                v[2 * i + 1] = T::hi(w[i]);
+            }
+        }
+    }
+    __device__ __forceinline__ v4u words() const
+    {
+        v4u w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (TYPE == QB_TYPE_FP32) w[i] = __float_as_uint(v[i]);
+            else w[i] = T::pair(v[2 * i], v[2 * i + 1]);
+        }
+        return w;
+    }
+    __device__ __forceinline__ void drop(const Threefry &bits, int64_t chunk, uint32_t threshold, float scale)
+    {
+#pragma unroll
+        for (int c = 0; c < kCounters; ++c) {
+            const uint64_t counter = (uint64_t)chunk * kCounters + c;
+            const v2u d = bits.draws((uint32_t)counter, (uint32_t)(counter >> 32));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool keep = j & 1 ? kept_high(d[j >> 1], threshold) : kept_low(d[j >> 1], threshold);
+                v[4 * c + j] = keep ? v[4 * c + j] * scale : 0.0f;
+            }
+        }
+    }
+    __device__ __forceinline__ void add(const Chunk &x)
+    {
+#pragma unroll
+        for (int i = 0; i < kValues; ++i) v[i] += x.v[i];
+    }
+};
+// the last values of a tensor, fewer than a chunk
+template <int TYPE>
+__device__ v4u load_some(const void *p, int64_t byte, int values)
+{
+    v4u w = {0, 0, 0, 0};
+    for (int i = 0; i < values; ++i) {
+        if constexpr (TYPE == QB_TYPE_FP32) w[i] = reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(p) + byte)[i];
+        else w[i >> 1] |= (uint32_t)reinterpret_cast<const uint16_t *>(static_cast<const uint8_t *>(p) + byte)[i] << (16 * (i & 1));
+    }
+    return w;
 }
 template <int TYPE>
-__device__ __forceinline__ void put(void *p, int64_t i, float v)
+__device__ void store_some(void *p, int64_t byte, v4u w, int values)
 {
-    if constexpr (TYPE == QB_TYPE_FP32) static_cast<float *>(p)[i] = v;
-    else static_cast<uint16_t *>(p)[i] = (uint16_t)(TYPE == QB_TYPE_BF16 ? Bf16::pair(v, v) : Fp16::pair(v, v));
+    for (int i = 0; i < values; ++i) {
+        if constexpr (TYPE == QB_TYPE_FP32) reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(p) + byte)[i] = w[i];
+        else reinterpret_cast<uint16_t *>(static_cast<uint8_t *>(p) + byte)[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+    }
 }
 
 template <int TYPE, bool RESIDUAL>
 __global__ __launch_bounds__(256) void dropout_kernel(const DropArgs a)
 {
+    typedef Chunk<TYPE> C;
     const Threefry bits((uint64_t)*a.seed);
-    const int64_t step = (int64_t)gridDim.x * 256;
-    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; 4 * c < a.n; c += step) {
-        const v2u d = bits.draws((uint32_t)c, (uint32_t)((uint64_t)c >> 32));
+    const int64_t whole = a.n / C::kValues, step = (int64_t)gridDim.x * (256 * kAtOnce);
+    for (int64_t first = (int64_t)blockIdx.x * (256 * kAtOnce) + threadIdx.x; first < whole; first += step) {
+        // all loads of a round before the bits of its first chunk
+        v4u x[kAtOnce], r[kAtOnce];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (4 * c + j >= a.n) break;
-            const bool keep = j & 1 ? kept_high(d[j >> 1], a.threshold) : kept_low(d[j >> 1], a.threshold);
-            float v = keep ? value<TYPE>(a.X, 4 * c + j) * a.scale : 0.0f;
-            if constexpr (RESIDUAL) v += value<TYPE>(a.residual, 4 * c + j);
-            put<TYPE>(a.Y, 4 * c + j, v);
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int64_t c = min(first + u * 256, whole - 1);
+            x[u] = load16(a.X, 16 * c);
+            if constexpr (RESIDUAL) r[u] = load16(a.residual, 16 * c);
         }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int64_t c = first + u * 256;
+            if (c >= whole) break;
+            C v(x[u]);
+            v.drop(bits, c, a.threshold, a.scale);
+            if constexpr (RESIDUAL) v.add(C(r[u]));
+            store16(a.Y, 16 * c, v.words());
+        }
+    }
+    const int rest = (int)(a.n - whole * C::kValues);
+    if (rest > 0 && blockIdx.x == gridDim.x - 1 && threadIdx.x == 255) {
+        C v(load_some<TYPE>(a.X, 16 * whole, rest));
+        v.drop(bits, whole, a.threshold, a.scale);
+        if constexpr (RESIDUAL) v.add(C(load_some<TYPE>(a.residual, 16 * whole, rest)));
+        store_some<TYPE>(a.Y, 16 * whole, v.words(), rest);
     }
 }
 
 template <bool RESIDUAL>
 qb_status launch(const DropArgs &a, int type, hipStream_t stream)
 {
-    const int64_t need = (a.n + 1023) / 1024;
-    const int blocks = (int)(need < 8192 ? need : 8192);
+    const int64_t chunks = a.n / (type == QB_TYPE_FP32 ? 4 : 8), need = (chunks + 256 * kAtOnce - 1) / (256 * kAtOnce);
+    const int blocks = (int)(need < 1 ? 1 : need < 8192 ? need : 8192);
     if (type == QB_TYPE_BF16) dropout_kernel<QB_TYPE_BF16, RESIDUAL><<<blocks, 256, 0, stream>>>(a);
     else if (type == QB_TYPE_FP16) dropout_kernel<QB_TYPE_FP16, RESIDUAL><<<blocks, 256, 0, stream>>>(a);
     else dropout_kernel<QB_TYPE_FP32, RESIDUAL><<<blocks, 256, 0, stream>>>(a);
