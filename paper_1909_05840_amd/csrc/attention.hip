@@ -8,6 +8,7 @@
 // transposing LDS reads in the same order.  Exponentials are rounded to the inputs' type for that product only: l sums
 // them unrounded.
 #include "attention.hpp"
+#include <algorithm>
 #include <cmath>
 
 namespace qb {
@@ -79,17 +80,17 @@ struct Softmax {
 
 constexpr int kKeys = 64;  // keys to a tile
 
-// One tile of keys: keys tile0 .. tile0 + 63 in LDS, of which the lane's row sees those below `limit` (masked: some row of the
+// KB blocks of 32 keys from tile0 on, in LDS, of which the lane's row sees those below `limit` (masked: some row of the
 // wavefront does not see all of them).
-template <typename T, int D, bool DROP>
+template <typename T, int D, bool DROP, int KB = 2>
 __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], const uint8_t *tk, const uint8_t *tv, int tile0, int limit,
                                        bool masked, float c, const Threefry &bits, uint32_t threshold, int row_q, int head, int lane)
 {
     typedef Rows<D> R;
     const int hf = lane >> 5;
-    v16f s[2];
+    v16f s[KB];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[kb][i] = 0.0f;
 #pragma unroll
@@ -97,13 +98,13 @@ __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], co
     }
     if (masked) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[kb][i] = tile0 + 32 * kb + 8 * (i >> 2) + 4 * hf + (i & 3) < limit ? s[kb][i] : -__builtin_inff();
     }
     float top = s[0][0];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, fmaxf(s[0][i], s[1][i]));
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, KB == 2 ? fmaxf(s[0][i], s[KB - 1][i]) : s[0][i]);
     top = halves_max(top);
     if (__builtin_amdgcn_ballot_w64((top - x.m) * c > kLazy)) {
         const float m = fmaxf(x.m, top), f = __builtin_amdgcn_exp2f((x.m - m) * c);
@@ -117,7 +118,7 @@ __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], co
     const float mc = x.m * c;
     float sum = 0.0f;
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             s[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], c, -mc));
@@ -126,7 +127,7 @@ __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], co
     x.l += sum;
     if constexpr (DROP) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
                 const v2u d = weight_draws(bits, row_q, head, tile0 + 32 * kb + 2 * i + 4 * hf);
@@ -137,7 +138,7 @@ __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], co
             }
     }
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             v4u w;
@@ -224,6 +225,184 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uin
     if (hf == 0) lse[at_row] = l > 0.0f ? x.m * a.scale + __logf(l) : -__builtin_inff();
 }
 
+// ---- few rows: the new tokens over a cache
+// Up to 32 rows of a key head are one wavefront's; its keys are what there is to share out.  They are cut into chunks, a workgroup
+// each, whose four wavefronts take the chunk's tiles in turn, each through two stages of its own in LDS and with no barrier: it
+// waits for its own copies only, the next stage's under way.  The wavefronts' sums are joined in LDS, the chunks' by a second launch.
+// Bound by the keys' and values' bytes; the products of up to 31 idle rows cost nothing beside them.
+template <typename T, int D, bool SPLIT>
+__global__ __launch_bounds__(256, 1) void attention_cache_kernel(const AttnArgs a, uint16_t *O, float *lse, int chunk, int chunks, float *part)
+{
+    typedef Rows<D> R;
+    constexpr int KB = D == 64 ? 2 : 1, kTileKeys = 32 * KB, kTile = kTileKeys * R::kBytes, kCopies = kTileKeys / R::kPerCopy;
+    constexpr int kJoin = 32 * (D + 4) * 4;  // a wavefront's O, m, l
+    __shared__ __align__(1024) uint8_t lds_all[4][4 * kTile > kJoin ? 4 * kTile : kJoin];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int pairs = a.n_seqs * a.kv_heads, pair = (int)(blockIdx.x % pairs), at_chunk = (int)(blockIdx.x / pairs) % chunks, tile_r = (int)(blockIdx.x / pairs) / chunks;
+    const int b = pair / a.kv_heads, kv = pair - b * a.kv_heads;
+    const Segment seg = segment(a, b);
+    const int rows = seg.nq * a.group, first = tile_r * 32;
+    if (first >= rows) return;
+    const int row = first + l32;
+    const int token = min((unsigned)row / (unsigned)a.group, (unsigned)seg.nq - 1u);
+    const int head = kv * a.group + (row - (int)((unsigned)row / (unsigned)a.group) * a.group);
+    const int row_q = seg.q0 + token;
+    const auto sees = [&](int t) { return a.causal ? min(seg.nk, max(0, seg.first_hidden(t))) : seg.nk; };
+    const int limit = sees(token);
+    const int least = __builtin_amdgcn_readfirstlane(sees(min(first / a.group, seg.nq - 1))), most = __builtin_amdgcn_readfirstlane(sees(min((first + 31) / a.group, seg.nq - 1)));
+    const int begin = SPLIT ? at_chunk * chunk : 0, end = SPLIT ? min(most, begin + chunk) : most;
+    if (SPLIT && at_chunk > 0 && begin >= end) return;  // (the joining launch knows which chunks there are)
+
+    const uint16_t *const K = a.K + (int64_t)seg.k0 * a.k_row + (int64_t)kv * a.k_head;
+    const uint16_t *const V = a.V + (int64_t)seg.k0 * a.v_row + (int64_t)kv * a.v_head;
+    uint8_t *const lds = lds_all[wave];
+    const uint32_t lds0 = lds_address(lds);
+    const auto fetch = [&](int key0, int stage) {
+        const uint32_t to = lds0 + stage * 2 * kTile;
+        copy_rows<D, kTileKeys, 1>(to, 0, lane, [&](int r) { return K + (int64_t)min(key0 + r, seg.nk - 1) * a.k_row; });
+        copy_rows<D, kTileKeys, 1>(to + kTile, 0, lane, [&](int r) { return V + (int64_t)min(key0 + r, seg.nk - 1) * a.v_row; });
+    };
+    Softmax<D> x;
+    x.clear();
+    const int step = 4 * kTileKeys, mine = begin + wave * kTileKeys;
+    if (mine < end) fetch(mine, 0);
+    v8s q[D / 16];
+    const uint16_t *const from = a.Q + (int64_t)row_q * a.q_row + (int64_t)head * a.q_head + 8 * hf;
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) q[d] = *reinterpret_cast<const v8s *>(from + 16 * d);
+    const Threefry bits(0);
+    int stage = 0;
+    for (int key0 = mine; key0 < end; key0 += step, stage ^= 1) {
+        if (key0 + step < end) {
+            fetch(key0 + step, stage ^ 1);
+            wait_copies<2 * kCopies>();
+        } else {
+            wait_copies<0>();
+        }
+        asm volatile("" ::: "memory");
+        attend<T, D, false, KB>(x, q, lds + stage * 2 * kTile, lds + stage * 2 * kTile + kTile, key0, limit, key0 + kTileKeys > least, a.c, bits, 0, row_q, head, lane);
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // this stage's reads have returned before the next copies into it
+        asm volatile("" ::: "memory");
+    }
+    x.l = halves_sum(x.l);
+    // joined in LDS: [row][D values, m, l]
+    float *const own = reinterpret_cast<float *>(lds);
+    constexpr int kPitch = D + 4;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) *reinterpret_cast<v4f *>(own + l32 * kPitch + 32 * i + 2 * j + 4 * hf) = v4f{x.o[i][j], x.o[i][j + 1], x.o[i][j + 2], x.o[i][j + 3]};
+    if (hf == 0) {
+        own[l32 * kPitch + D] = x.m;
+        own[l32 * kPitch + D + 1] = x.l;
+    }
+    barrier();
+    // a thread does eight neighbouring values of a row
+    constexpr int kThreads = D / 8;
+    const int here = min(32, rows - first);
+    for (int i = threadIdx.x; i < here * kThreads; i += 256) {
+        const int r = i / kThreads, d = (i - r * kThreads) * 8;
+        float m = kNothing, l = 0.0f;
+        const float *const all = reinterpret_cast<const float *>(lds_all[0]) + r * kPitch;
+        constexpr int kWaveFloats = (int)(sizeof(lds_all[0]) / 4);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) m = fmaxf(m, all[w * kWaveFloats + D]);
+        v4f o[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = __builtin_amdgcn_exp2f((all[w * kWaveFloats + D] - m) * a.c);
+            l += f * all[w * kWaveFloats + D + 1];
+            o[0] += f * *reinterpret_cast<const v4f *>(all + w * kWaveFloats + d);
+            o[1] += f * *reinterpret_cast<const v4f *>(all + w * kWaveFloats + d + 4);
+        }
+        const int t = (first + r) / a.group, h = kv * a.group + first + r - t * a.group;
+        if constexpr (SPLIT) {
+            float *const to = part + ((int64_t)((pair * (int64_t)a.tiles + tile_r) * chunks + at_chunk) * 32 + r) * kPitch;
+            *reinterpret_cast<v4f *>(to + d) = o[0];
+            *reinterpret_cast<v4f *>(to + d + 4) = o[1];
+            if (d == 0) {
+                to[D] = m;
+                to[D + 1] = l;
+            }
+        } else {
+            const float f = l > 0.0f ? 1.0f / l : 0.0f;
+            const int64_t at_row = (int64_t)(seg.q0 + t) * a.heads + h;
+            *reinterpret_cast<v4u *>(O + at_row * D + d) = v4u{T::pair(o[0][0] * f, o[0][1] * f), T::pair(o[0][2] * f, o[0][3] * f), T::pair(o[1][0] * f, o[1][1] * f), T::pair(o[1][2] * f, o[1][3] * f)};
+            if (d == 0) lse[at_row] = l > 0.0f ? m * a.scale + __logf(l) : -__builtin_inff();
+        }
+    }
+}
+
+// the chunks of every row joined: a wavefront to a row, D / 64 values a lane
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a, uint16_t *O, float *lse, int chunk, int chunks, const float *part, int max_rows)
+{
+    constexpr int kPitch = D + 4, N = D / 64;
+    const int lane = threadIdx.x & 63, id = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int pair = id / max_rows, r = id - pair * max_rows;
+    if (pair >= a.n_seqs * a.kv_heads) return;
+    const int b = pair / a.kv_heads, kv = pair - b * a.kv_heads;
+    const Segment seg = segment(a, b);
+    if (r >= seg.nq * a.group) return;
+    const int tile_r = r >> 5, t = r / a.group, h = kv * a.group + r - t * a.group;
+    const int last_token = min((tile_r * 32 + 31) / a.group, seg.nq - 1);  // the tile's chunks reach as far as its last row sees
+    const int most = a.causal ? min(seg.nk, max(0, seg.first_hidden(last_token))) : seg.nk;
+    const int n = min(chunks, max(1, (most + chunk - 1) / chunk));
+    const float *const from = part + ((int64_t)(pair * (int64_t)a.tiles + tile_r) * chunks * 32 + (r & 31)) * kPitch;
+    float m = kNothing, l = 0.0f, o[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = 0.0f;
+    for (int c = 0; c < n; ++c) {
+        const float *const p = from + (int64_t)c * 32 * kPitch;
+        const float m1 = p[D], top = fmaxf(m, m1), f = __builtin_amdgcn_exp2f((m - top) * a.c), g = __builtin_amdgcn_exp2f((m1 - top) * a.c);
+        m = top;
+        l = l * f + p[D + 1] * g;
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] = o[i] * f + p[N * lane + i] * g;
+    }
+    const float f = l > 0.0f ? 1.0f / l : 0.0f;
+    const int64_t at_row = (int64_t)(seg.q0 + t) * a.heads + h;
+    if constexpr (N == 2) *reinterpret_cast<uint32_t *>(O + at_row * D + 2 * lane) = T::pair(o[0] * f, o[N - 1] * f);
+    else O[at_row * D + lane] = (uint16_t)T::pair(o[0] * f, 0.0f);
+    if (lane == 0) lse[at_row] = l > 0.0f ? m * a.scale + __logf(l) : -__builtin_inff();
+}
+
+// Few rows (without dropout, which serving has none of): up to kFewRows of a key head.  The chunks: as many as fill the GPU with
+// about 2048 workgroups, half of which find no keys where lengths differ, of 512 keys or more.
+constexpr int64_t kFewRows = 64;
+struct Chunks {
+    int64_t size, count;
+};
+inline Chunks chunks_of(int64_t pairs, int64_t max_k)
+{
+    Chunks c;
+    c.count = std::max<int64_t>(1, std::min((max_k + 511) / 512, (2048 + pairs - 1) / pairs));
+    c.size = std::max<int64_t>(256, (((max_k + c.count - 1) / c.count) + 255) / 256 * 256);
+    c.count = std::max<int64_t>(1, (max_k + c.size - 1) / c.size);
+    return c;
+}
+inline bool few_rows(const AttnArgs &a, const qb_attention *p) { return p->max_q * a.group <= kFewRows && !(p->p > 0.0f); }
+
+template <typename T, int D>
+qb_status forward_few(AttnArgs a, int64_t max_q, int64_t max_k, void *O, float *lse, void *workspace, hipStream_t stream)
+{
+    const int64_t pairs = (int64_t)a.n_seqs * a.kv_heads, rows = max_q * a.group;
+    a.tiles = (int)((rows + 31) / 32);
+    const Chunks c = chunks_of(pairs, max_k);
+    const int64_t grid = pairs * a.tiles * c.count;
+    if (grid > INT32_MAX / 256 || pairs * rows > INT32_MAX / 256) return QB_ERR_SHAPE;
+    uint16_t *const out = static_cast<uint16_t *>(O);
+    float *const part = static_cast<float *>(workspace);
+    if (c.count == 1) {
+        attention_cache_kernel<T, D, false><<<(int)grid, 256, 0, stream>>>(a, out, lse, 0, 1, nullptr);
+    } else {
+        attention_cache_kernel<T, D, true><<<(int)grid, 256, 0, stream>>>(a, out, lse, (int)c.size, (int)c.count, part);
+        attention_join_kernel<T, D><<<(int)((pairs * rows + 3) / 4), 256, 0, stream>>>(a, out, lse, (int)c.size, (int)c.count, part, (int)rows);
+    }
+    return launch_status();
+}
+
 template <typename T, int D>
 qb_status forward(AttnArgs a, int64_t max_q, bool drop, void *O, float *lse, hipStream_t stream)
 {
@@ -245,9 +424,20 @@ using namespace qb;
 extern "C" size_t qb_attention_fwd_workspace_nbytes(const qb_attention *p)
 {
     AttnArgs a;
-    if (attention_args(p, a) != QB_OK) return 0;
-    return 0;
+    if (attention_args(p, a) != QB_OK || p->max_q == 0 || p->n_seqs == 0 || !few_rows(a, p)) return 0;
+    const int64_t pairs = (int64_t)a.n_seqs * a.kv_heads, tiles = (p->max_q * a.group + 31) / 32;
+    const Chunks c = chunks_of(pairs, p->max_k);
+    return c.count == 1 ? 0 : (size_t)(pairs * tiles * c.count) * 32 * (p->dim + 4) * 4;
 }
+
+namespace {
+template <typename T, int D>
+qb_status forward_any(const AttnArgs &a, const qb_attention *p, void *O, float *lse, void *workspace, hipStream_t stream)
+{
+    if (few_rows(a, p)) return forward_few<T, D>(a, p->max_q, p->max_k, O, lse, workspace, stream);
+    return forward<T, D>(a, p->max_q, p->p > 0.0f, O, lse, stream);
+}
+}  // namespace
 
 extern "C" qb_status qb_attention_fwd(const qb_attention *p, void *O, float *lse, void *workspace, void *stream)
 {
@@ -257,9 +447,8 @@ extern "C" qb_status qb_attention_fwd(const qb_attention *p, void *O, float *lse
     if (p->total_q == 0 || p->n_seqs == 0 || p->max_q == 0) return QB_OK;
     if (!O || !lse) return QB_ERR_NULL;
     if (!aligned16(O)) return QB_ERR_VALUE;
-    (void)workspace;
+    if (qb_attention_fwd_workspace_nbytes(p) > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255))) return QB_ERR_WORKSPACE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const bool drop = p->p > 0.0f;
-    if (p->type == QB_TYPE_BF16) return p->dim == 64 ? forward<Bf16, 64>(a, p->max_q, drop, O, lse, st) : forward<Bf16, 128>(a, p->max_q, drop, O, lse, st);
-    return p->dim == 64 ? forward<Fp16, 64>(a, p->max_q, drop, O, lse, st) : forward<Fp16, 128>(a, p->max_q, drop, O, lse, st);
+    if (p->type == QB_TYPE_BF16) return p->dim == 64 ? forward_any<Bf16, 64>(a, p, O, lse, workspace, st) : forward_any<Bf16, 128>(a, p, O, lse, workspace, st);
+    return p->dim == 64 ? forward_any<Fp16, 64>(a, p, O, lse, workspace, st) : forward_any<Fp16, 128>(a, p, O, lse, workspace, st);
 }
