@@ -8,6 +8,7 @@
 // that one launch would need, but nothing is added to memory by several workgroups: no atomics, the same bits every time.
 // dS and P are rounded to the inputs' type for the last products only.
 #include "attention.hpp"
+#include <algorithm>
 
 namespace qb {
 namespace {
@@ -20,6 +21,7 @@ struct GradArgs {
     uint16_t *dQ, *dK, *dV;
     int64_t q_row, q_head, k_row, k_head, v_row, v_head;
     float *stat;  // [2][total_q * heads]: lse / ln 2 (+infinity for a row that sees nothing: its P is zero), delta
+    float *part;  // [pairs][tiles of keys][splits][128][dK, dV] where rows are split
 };
 
 template <typename T, int D>
@@ -55,7 +57,9 @@ __device__ __forceinline__ v8s rounded(const v16f &x, int half)
 // delta = dO.O takes O as the forward rounded it.  Where few keys carry a row's weight that error is as large as the rounding
 // of dS (384 keys of random scores of deviation 2: together 1.5 times the error of exact arithmetic rounded once).  EXACT therefore
 // sums eps = sum_k P (dP - delta) on the way, which is what delta lacks, and B = sum_k P K beside A = sum_k dS K: dQ = scale (A - eps B),
-// and the second launch gets delta + eps.  With many keys |O| is small beside |V|, and the rounding with it.
+// and the second launch gets delta + eps.  With many keys |O| is small beside |V|, and the rounding with it: tiles of rows that see more than
+// kExactKeys are left to the other variant, which needs two thirds of the registers and six sevenths of the products.
+constexpr int kExactKeys = 2048;
 template <typename T, int D, bool DROP, bool EXACT>
 __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_kernel(const AttnArgs a, const GradArgs g, bool by_xcd)
 {
@@ -98,6 +102,7 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
     const int wave_least = __builtin_amdgcn_readfirstlane(sees(token_of(first + wave * 32)));
     const int wave_most = __builtin_amdgcn_readfirstlane(sees(token_of(first + wave * 32 + 31)));
     const int most = __builtin_amdgcn_readfirstlane(sees(token_of(first + 127)));
+    if (EXACT != (most <= kExactKeys)) return;
     const int tiles = (most + kKeys - 1) / kKeys;
 
     const uint16_t *const K = a.K + (int64_t)seg.k0 * a.k_row + (int64_t)kv * a.k_head;
@@ -189,21 +194,37 @@ __device__ __forceinline__ void copy4(const void *from, uint32_t lds)
 template <int B>
 __device__ __forceinline__ uint32_t of_four(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, B * 0x55, 0xF, 0xF, true); }
 
-// dK and dV; 128 keys to a workgroup, 32 to a wavefront: a lane's results all of one key.  Scores are taken as S = Q K^T, so that a
+// The rows that a tile of 128 keys is seen by, in tiles of 64, cut into `splits` parts of about the same number.
+struct RowTiles {
+    int begin, end;
+};
+__device__ __forceinline__ int first_row(const AttnArgs &a, const Segment &seg, int rows, int key)  // causal: key <= token + nk - nq
+{
+    return a.causal ? (int)min((int64_t)rows, (int64_t)max(0, key - (seg.nk - seg.nq)) * a.group) : 0;
+}
+__device__ __forceinline__ RowTiles row_tiles(const AttnArgs &a, const Segment &seg, int rows, int first_key, int part, int splits)
+{
+    const int all = (rows + kRowsOfTile - 1) / kRowsOfTile, each = (all + splits - 1) / splits;
+    return {max(first_row(a, seg, rows, first_key) / kRowsOfTile, part * each), min(all, (part + 1) * each)};
+}
+
+// dK and dV; 128 keys to a workgroup, 32 to a wavefront: a lane's results all of one key.  Where tiles of keys are few, a workgroup does
+// a part of the rows, and its binary32 sums go to the workspace for a third launch to join.  Scores are taken as S = Q K^T, so that a
 // lane holds sixteen rows of its key and P and dS are, as they lie, the operands of dV^T = dO^T P and dK^T = Q^T dS.
 template <typename T, int D, bool DROP>
-__global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a, const GradArgs g, bool by_xcd)
+__global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a, const GradArgs g, int splits, bool by_xcd)
 {
     typedef Rows<D> R;
     constexpr int kTile = kRowsOfTile * R::kBytes, kStage = 2 * kTile + 2 * kRowsOfTile * 4;
     __shared__ __align__(1024) uint8_t lds[2][kStage];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Place at = place(blockIdx.x, a.n_seqs * a.kv_heads, a.tiles, by_xcd);
+    const Place at = place(blockIdx.x, a.n_seqs * a.kv_heads, a.tiles * splits, by_xcd);
     if (at.pair >= a.n_seqs * a.kv_heads) return;
     const int b = at.pair / a.kv_heads, kv = at.pair - b * a.kv_heads;
     const Segment seg = segment(a, b);
-    const int first = (a.tiles - 1 - at.tile) * 128;  // (the first keys are seen by the most rows)
+    const int back = a.tiles * splits - 1 - at.tile, tile = back / splits, part = back - tile * splits;  // (the first keys are seen by the most rows)
+    const int first = tile * 128;
     if (first >= seg.nk) return;
     const int rows = max(0, seg.nq) * a.group;
     const int wave_first = first + wave * 32, key = wave_first + l32;
@@ -217,11 +238,11 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
         k[d] = *reinterpret_cast<const v8s *>(k_from + 16 * d);
         v[d] = *reinterpret_cast<const v8s *>(v_from + 16 * d);
     }
-    // the first row that sees a key: causal, key <= token + nk - nq
-    const auto first_row = [&](int key_) { return a.causal ? (int)min((int64_t)rows, (int64_t)max(0, key_ - (seg.nk - seg.nq)) * a.group) : 0; };
-    const int from_row = first_row(key);
-    const int wave_from = __builtin_amdgcn_readfirstlane(first_row(wave_first)), wave_all = __builtin_amdgcn_readfirstlane(first_row(wave_first + 31));
-    const int begin = __builtin_amdgcn_readfirstlane(first_row(first)) / kRowsOfTile, end = (rows + kRowsOfTile - 1) / kRowsOfTile;
+    const int from_row = first_row(a, seg, rows, key);
+    const int wave_from = __builtin_amdgcn_readfirstlane(first_row(a, seg, rows, wave_first)), wave_all = __builtin_amdgcn_readfirstlane(first_row(a, seg, rows, wave_first + 31));
+    const RowTiles todo = row_tiles(a, seg, rows, first, part, splits);
+    const int begin = __builtin_amdgcn_readfirstlane(todo.begin), end = __builtin_amdgcn_readfirstlane(todo.end);
+    if (splits > 1 && begin >= end) return;  // (the joining launch knows)
 
     const uint32_t lds0 = lds_address(lds);
     const int64_t stats = (int64_t)a.total_q * a.heads;
@@ -328,12 +349,54 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
         }
     }
     if (key >= seg.nk) return;
+    if (splits > 1) {
+        float *const to = g.part + ((int64_t)((at.pair * (int64_t)a.tiles + tile) * splits + part) * 128 + key - first) * (2 * D);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                *reinterpret_cast<v4f *>(to + 32 * i + 2 * j + 4 * hf) = v4f{dK[i][j], dK[i][j + 1], dK[i][j + 2], dK[i][j + 3]};
+                *reinterpret_cast<v4f *>(to + D + 32 * i + 2 * j + 4 * hf) = v4f{dV[i][j], dV[i][j + 1], dV[i][j + 2], dV[i][j + 3]};
+            }
+        return;
+    }
     write_scaled<T, D>(g.dK + (int64_t)(seg.k0 + key) * g.k_row + (int64_t)kv * g.k_head, dK, a.scale, hf);
     write_scaled<T, D>(g.dV + (int64_t)(seg.k0 + key) * g.v_row + (int64_t)kv * g.v_head, dV, DROP ? a.inv_share : 1.0f, hf);
 }
 
-// Above this many keys delta is taken from the rounded O (see there).
-constexpr int64_t kExactKeys = 2048;
+// dK and dV of 16 keys from their parts; a thread does eight neighbouring values
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attention_dkv_join_kernel(const AttnArgs a, const GradArgs g, int splits, float inv_share)
+{
+    constexpr int kEach = 2 * D / 8;  // threads to a key
+    const int pair = blockIdx.x / (a.tiles * (128 * kEach / 256)), in_pair = blockIdx.x - pair * (a.tiles * (128 * kEach / 256));
+    const int id = in_pair * 256 + threadIdx.x, key = id / kEach, d = (id - key * kEach) * 8;
+    const int b = pair / a.kv_heads, kv = pair - b * a.kv_heads;
+    const Segment seg = segment(a, b);
+    if (key >= seg.nk) return;
+    const int rows = max(0, seg.nq) * a.group, tile = key / 128;
+    const float *const from = g.part + ((int64_t)(pair * (int64_t)a.tiles + tile) * splits * 128 + key % 128) * (2 * D) + d;
+    v4f x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    for (int p = 0; p < splits; ++p) {
+        const RowTiles t = row_tiles(a, seg, rows, tile * 128, p, splits);
+        if (t.begin >= t.end) continue;
+        const v4f *const q = reinterpret_cast<const v4f *>(from + (int64_t)p * 128 * (2 * D));
+        x[0] += q[0];
+        x[1] += q[1];
+    }
+    const float f = d < D ? a.scale : inv_share;
+    uint16_t *const to = d < D ? g.dK + (int64_t)(seg.k0 + key) * g.k_row + (int64_t)kv * g.k_head + d : g.dV + (int64_t)(seg.k0 + key) * g.v_row + (int64_t)kv * g.v_head + d - D;
+    *reinterpret_cast<v4u *>(to) = v4u{T::pair(x[0][0] * f, x[0][1] * f), T::pair(x[0][2] * f, x[0][3] * f), T::pair(x[1][0] * f, x[1][1] * f), T::pair(x[1][2] * f, x[1][3] * f)};
+}
+
+// Into how many parts the rows of a tile of keys are cut: such that about kParts workgroups are at work, of eight tiles of rows or more
+constexpr int64_t kParts = 1024;
+inline int64_t row_splits(int64_t pairs, int64_t max_q, int64_t group, int64_t max_k)
+{
+    const int64_t tiles = pairs * ((max_k + 127) / 128);
+    return std::max<int64_t>(1, std::min({kParts / std::max<int64_t>(1, tiles), (max_q * group / kRowsOfTile) / 8, (int64_t)16}));
+}
+inline size_t stat_bytes(const qb_attention *p) { return ((size_t)p->total_q * p->heads * 8 + 255) / 256 * 256; }
 
 template <typename T, int D>
 qb_status backward(AttnArgs a, const GradArgs &g, int64_t max_q, int64_t max_k, bool drop, hipStream_t stream)
@@ -344,17 +407,20 @@ qb_status backward(AttnArgs a, const GradArgs &g, int64_t max_q, int64_t max_k, 
         a.tiles = (int)((max_q * a.group + 127) / 128);
         const int64_t grid = dealt_workgroups(pairs, a.tiles);
         if (grid > INT32_MAX / 256) return QB_ERR_SHAPE;
-        const bool exact = max_k <= kExactKeys;
-        if (drop && exact) attention_dq_kernel<T, D, true, true><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
-        else if (drop) attention_dq_kernel<T, D, true, false><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
-        else if (exact) attention_dq_kernel<T, D, false, true><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
-        else attention_dq_kernel<T, D, false, false><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
+        if (drop) attention_dq_kernel<T, D, true, true><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
+        else attention_dq_kernel<T, D, false, true><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
+        if (max_k > kExactKeys) {
+            if (drop) attention_dq_kernel<T, D, true, false><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
+            else attention_dq_kernel<T, D, false, false><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
+        }
     }
     if (max_k > 0) {
         a.tiles = (int)((max_k + 127) / 128);
-        const int64_t grid = dealt_workgroups(pairs, a.tiles);
-        if (drop) attention_dkv_kernel<T, D, true><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
-        else attention_dkv_kernel<T, D, false><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
+        const int splits = (int)row_splits(pairs, max_q, a.group, max_k);
+        const int64_t grid = dealt_workgroups(pairs, (int64_t)a.tiles * splits);
+        if (drop) attention_dkv_kernel<T, D, true><<<(int)grid, 256, 0, stream>>>(a, g, splits, by_xcd);
+        else attention_dkv_kernel<T, D, false><<<(int)grid, 256, 0, stream>>>(a, g, splits, by_xcd);
+        if (splits > 1) attention_dkv_join_kernel<T, D><<<(int)(pairs * a.tiles * (128 * 2 * D / 8 / 256)), 256, 0, stream>>>(a, g, splits, drop ? a.inv_share : 1.0f);
     }
     return launch_status();
 }
@@ -368,7 +434,8 @@ extern "C" size_t qb_attention_bwd_workspace_nbytes(const qb_attention *p)
 {
     AttnArgs a;
     if (attention_args(p, a) != QB_OK) return 0;
-    return ((size_t)p->total_q * p->heads * 8 + 255) / 256 * 256;
+    const int64_t pairs = (int64_t)a.n_seqs * a.kv_heads, splits = row_splits(pairs, p->max_q, a.group, p->max_k);
+    return stat_bytes(p) + (splits > 1 ? (size_t)(pairs * ((p->max_k + 127) / 128) * splits) * 128 * 2 * p->dim * 4 : 0);
 }
 
 extern "C" qb_status qb_attention_bwd(const qb_attention *p, const void *dO, const void *O, const float *lse,
@@ -385,9 +452,9 @@ extern "C" qb_status qb_attention_bwd(const qb_attention *p, const void *dO, con
     if (!aligned16(dO) || !aligned16(O) || !aligned16(grads->dQ) || !aligned16(grads->dK) || !aligned16(grads->dV)) return QB_ERR_VALUE;
     if (p->total_q > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255))) return QB_ERR_WORKSPACE;
     const int64_t pairs = (int64_t)p->n_seqs * p->kv_heads;
-    if (dealt_workgroups(pairs, (p->max_q * a.group + 127) / 128) > INT32_MAX / 256 || dealt_workgroups(pairs, (p->max_k + 127) / 128) > INT32_MAX / 256) return QB_ERR_SHAPE;
+    if (dealt_workgroups(pairs, (p->max_q * a.group + 127) / 128) > INT32_MAX / 256 || dealt_workgroups(pairs, (p->max_k + 127) / 128) > INT32_MAX / 4096) return QB_ERR_SHAPE;
     const GradArgs g = {static_cast<const uint16_t *>(dO), static_cast<const uint16_t *>(O), lse, static_cast<uint16_t *>(grads->dQ), static_cast<uint16_t *>(grads->dK),
-                        static_cast<uint16_t *>(grads->dV), grads->q_row, grads->q_head, grads->k_row, grads->k_head, grads->v_row, grads->v_head, static_cast<float *>(workspace)};
+                        static_cast<uint16_t *>(grads->dV), grads->q_row, grads->q_head, grads->k_row, grads->k_head, grads->v_row, grads->v_head, static_cast<float *>(workspace), reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + stat_bytes(p))};
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool drop = p->p > 0.0f;
     if (p->type == QB_TYPE_BF16) return p->dim == 64 ? backward<Bf16, 64>(a, g, p->max_q, p->max_k, drop, st) : backward<Bf16, 128>(a, g, p->max_q, p->max_k, drop, st);
