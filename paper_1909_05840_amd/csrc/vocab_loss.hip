@@ -41,7 +41,8 @@ struct LossArgs {
     // backward
     int v0, piece;   // this piece's first word and width (a multiple of kRowPad)
     uint16_t *d;     // [Tp][piece]
-    float *db;       // [token tiles][piece], or null
+    uint16_t *Xc;    // [Tp][K] the rows that have a target
+    float *db;       // [token tiles][V], or null
     float *dXs;      // tiles of dX: [tile][slice], binary32
     uint16_t *dX, *dW;
     float *dbias;
@@ -108,12 +109,12 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossArgs a)
 }
 
 // ---- products ------------------------------------------------------------------------------------------------------
-// Tiles of BM x BN results by WM x WN wavefronts, TM x TN blocks of 32 x 32 each; the contraction goes in steps of 64 through two
-// stages in LDS, one under way while the other is multiplied.  An operand lies in LDS as it does in memory: rows of results with the
+// Tiles of BM x BN results by WM x WN wavefronts, TM x TN blocks of 32 x 32 each; the contraction goes in steps of 64 through a ring of
+// stages in LDS, one multiplied while the others are under way.  An operand lies in LDS as it does in memory: rows of results with the
 // contraction along them, or rows along the contraction (in blocks of 64 results), read turned.
-template <int WM_, int WN_, int TM_, int TN_>
+template <int WM_, int WN_, int TM_, int TN_, int STAGES_>
 struct Shape {
-    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, kWaves = WM * WN;
+    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, kWaves = WM * WN, kStages = STAGES_;
     static constexpr int BM = 32 * WM * TM, BN = 32 * WN * TN;
     static constexpr int kStage = (BM + BN) * 128;
     // row number i that a lane copies
@@ -137,36 +138,39 @@ __device__ __forceinline__ v8s operand(const uint8_t *tile, int result, int sub,
     else return Rows<64>::along(tile, result, sub, lane);
 }
 
-// acc += A B^T over steps [s0, s1); row_a(i, r, s) is the address of LDS row r of step s: of result r (along), or for r = 64 * block + k of
-// step k, result block `block` (across); i numbers the rows that the lane copies.  after(s) is called behind a step's copies.
-template <typename S, bool A_ACROSS, bool B_ACROSS, typename FA, typename FB, typename FN>
-__device__ __forceinline__ void multiply(v16f (&acc)[S::TM][S::TN], uint8_t *lds, int s0, int s1, int wave, int lane, const FA &row_a, const FB &row_b, const FN &after)
+// acc += A B^T over steps [s0, s1); row_a(r, s) is the address of LDS row r of step s: of result r (along), or for r = 64 * block + k of
+// step k, result block `block` (across).  The addresses must not come from memory: a load between the copies waits for those before it.
+template <typename S, bool A_ACROSS, bool B_ACROSS, typename FA, typename FB>
+__device__ __forceinline__ void multiply(v16f (&acc)[S::TM][S::TN], uint8_t *lds, int s0, int s1, int wave, int lane, const FA &row_a, const FB &row_b)
 {
     const int wm = wave / S::WN, wn = wave - wm * S::WN;
     const uint32_t lds0 = lds_address(lds);
+    constexpr int NA = S::BM / 8 / S::kWaves, NB = S::BN / 8 / S::kWaves, kAhead = S::kStages - 1;
+    static_assert(NA * 8 * S::kWaves == S::BM && NB * 8 * S::kWaves == S::BN, "every wavefront copies the same number of times");
     const auto fetch = [&](int s, int stage) {
         const uint32_t to = lds0 + stage * S::kStage;
         typedef Rows<64> R;
-        constexpr int NA = S::BM / 8, NB = S::BN / 8;
-        static_assert(NA % S::kWaves == 0 && NB % S::kWaves == 0, "every wavefront copies the same number of times");
 #pragma unroll
-        for (int i = 0; i < NA / S::kWaves; ++i) {
+        for (int i = 0; i < NA; ++i) {
             const int first = (i * S::kWaves + wave) * 8, r = first + R::copy_row(lane);
             copy16(row_a(i, r, s) + 8 * R::copy_chunk(r, lane), to + first * 128);
         }
 #pragma unroll
-        for (int i = 0; i < NB / S::kWaves; ++i) {
+        for (int i = 0; i < NB; ++i) {
             const int first = (i * S::kWaves + wave) * 8, r = first + R::copy_row(lane);
             copy16(row_b(i, r, s) + 8 * R::copy_chunk(r, lane), to + S::BM * 128 + first * 128);
         }
-        after(s);
     };
-    fetch(s0, s0 & 1);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+        if (s0 + u < s1) fetch(s0 + u, u);
+    int stage = 0;
     for (int s = s0; s < s1; ++s) {
-        wait_copies<0>();
+        if (s + kAhead <= s1) wait_copies<(kAhead - 1) * (NA + NB)>();  // (younger steps' stay under way)
+        else wait_copies<0>();
         barrier();
-        if (s + 1 < s1) fetch(s + 1, (s + 1) & 1);
-        const uint8_t *const ta = lds + (s & 1) * S::kStage, *const tb = ta + S::BM * 128;
+        if (s + kAhead < s1) fetch(s + kAhead, stage == 0 ? kAhead : stage - 1);  // (into the stage that the last step was multiplied from)
+        const uint8_t *const ta = lds + stage * S::kStage, *const tb = ta + S::BM * 128;
 #pragma unroll
         for (int sub = 0; sub < 4; ++sub) {
             v8s x[S::TM], y[S::TN];
@@ -179,6 +183,7 @@ __device__ __forceinline__ void multiply(v16f (&acc)[S::TM][S::TN], uint8_t *lds
 #pragma unroll
                 for (int j = 0; j < S::TN; ++j) acc[i][j] = Bf16::mma32(x[i], y[j], acc[i][j]);
         }
+        stage = stage == kAhead ? 0 : stage + 1;
     }
     barrier();  // the stages are free again
 }
@@ -195,42 +200,59 @@ __device__ __forceinline__ void clear(v16f (&x)[M][N])
 // Workgroups are dealt to the XCDs in turn: numbers that follow each other on one XCD get neighbouring tiles.
 __device__ __forceinline__ int first_tile() { return (gridDim.x & 7) ? (int)blockIdx.x : (int)((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3)); }
 
-// Logits, a tile of words by tokens at a time: a lane's results belong to one token.
+// the sum over the 32 lanes of a half, in every lane
+__device__ __forceinline__ float half_sum(float x)
+{
+    const auto add = [&](auto ctrl) { x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(ctrl)::value, 0xF, 0xF, true)); };
+    add(std::integral_constant<int, 0xB1>());   // lane ^ 1
+    add(std::integral_constant<int, 0x4E>());   // lane ^ 2
+    add(std::integral_constant<int, 0x141>());  // the other four of eight
+    add(std::integral_constant<int, 0x140>());  // the other eight of sixteen
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+// Logits, a tile of words by tokens at a time: a lane's results belong to one token.  The sums start from the bias, and from
+// -infinity for words past the end, which so have no weight.
 template <typename S, bool BACKWARD>
 __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_logits_kernel(const LossArgs a)
 {
-    __shared__ __align__(1024) uint8_t lds[2 * S::kStage];
+    __shared__ __align__(1024) uint8_t lds[S::kStages * S::kStage];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave - wm * S::WN;
     const int n = a.counted->n, K = a.K;
     const float scale = BACKWARD ? a.counted->scale : 0.0f, inv = scale > 0.0f ? 1.0f / scale : 0.0f;
     const int words = BACKWARD ? a.piece / S::BM : (a.V + S::BM - 1) / S::BM, tiles = words * ((n + S::BN - 1) / S::BN);
+    if (BACKWARD && a.v0 == 0) {  // the rows that take part, side by side, for dW
+        const int64_t chunks = (int64_t)((n + S::BN - 1) / S::BN * S::BN) * (K / 8);
+        for (int64_t c = (int64_t)blockIdx.x * (64 * S::kWaves) + threadIdx.x; c < chunks; c += (int64_t)gridDim.x * (64 * S::kWaves)) {
+            const int row = (int)(c / (K / 8)), k = (int)(c - (int64_t)row * (K / 8)) * 8;
+            *reinterpret_cast<v4u *>(a.Xc + (int64_t)row * K + k) = *reinterpret_cast<const v4u *>(a.X + (int64_t)a.list[row] * K + k);
+        }
+    }
     for (int tile = first_tile(); tile < tiles; tile += gridDim.x) {
         const int tt = tile / words, tv = tile - tt * words, t0 = tt * S::BN, v0 = (BACKWARD ? a.v0 : 0) + tv * S::BM;
         v16f z[S::TM][S::TN];
-        clear(z);
-        const uint16_t *x[S::BN / 8 / S::kWaves];
-#pragma unroll
-        for (int i = 0; i < S::BN / 8 / S::kWaves; ++i) x[i] = a.X + (int64_t)a.list[t0 + S::row(i, wave, lane)] * K;
-        multiply<S, false, false>(z, lds, 0, K / 64, wave, lane,
-            [&](int, int r, int s) { return a.W + (int64_t)min(v0 + r, a.V - 1) * K + s * 64; },
-            [&](int i, int, int s) { return x[i] + s * 64; }, [](int) {});
-        // + bias; words past the end have no weight
 #pragma unroll
         for (int i = 0; i < S::TM; ++i)
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
                 const int v = v0 + (wm * S::TM + i) * 32 + 8 * (k >> 2) + 4 * hf + (k & 3);
-                const float add = v >= a.V ? -__builtin_inff() : a.bias ? a.bias[v] : 0.0f;
+                const float start = v >= a.V ? -__builtin_inff() : a.bias ? a.bias[v] : 0.0f;
 #pragma unroll
-                for (int j = 0; j < S::TN; ++j) z[i][j][k] = v >= a.V ? add : z[i][j][k] + add;
+                for (int j = 0; j < S::TN; ++j) z[i][j][k] = start;
             }
+        const uint16_t *x[S::BN / 8 / S::kWaves];
+#pragma unroll
+        for (int i = 0; i < S::BN / 8 / S::kWaves; ++i) x[i] = a.X + (int64_t)a.list[t0 + S::row(i, wave, lane)] * K;
+        multiply<S, false, false>(z, lds, 0, K / 64, wave, lane,
+            [&](int, int r, int s) { return a.W + (int64_t)min(v0 + r, a.V - 1) * K + s * 64; },
+            [&](int i, int, int s) { return x[i] + s * 64; });
         constexpr float kLog2e = 1.44269504088896341f;
         if constexpr (!BACKWARD) {
             v2f *const both = reinterpret_cast<v2f *>(lds);  // [WM][BN] maximum, sum of a wavefront's words
 #pragma unroll
             for (int j = 0; j < S::TN; ++j) {
-                const int row = t0 + (wn * S::TN + j) * 32 + l32;
                 float m = z[0][j][0];
 #pragma unroll
                 for (int i = 0; i < S::TM; ++i)
@@ -238,22 +260,28 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_logits_kernel(const Lo
                     for (int k = 0; k < 16; ++k) m = fmaxf(m, z[i][j][k]);
                 m = fmaxf(halves_max(m), kLow);
                 const float m2 = m * kLog2e;
-                float l = 0.0f, hit = 0.0f;
-                const int target = row < n ? (int)a.targets[a.list[row]] - v0 - wm * S::TM * 32 - 4 * hf : -1;
-                bool have = false;
+                float l = 0.0f;
 #pragma unroll
                 for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        if (target == i * 32 + 8 * (k >> 2) + (k & 3)) {
-                            hit = z[i][j][k];
-                            have = true;
-                        }
-                        l += __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][j][k], kLog2e, -m2));
-                    }
+                    for (int k = 0; k < 16; ++k) l += __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][j][k], kLog2e, -m2));
                 l = halves_sum(l);
-                if (have) a.hit[row] = hit;
                 if (hf == 0) both[wm * S::BN + (wn * S::TN + j) * 32 + l32] = v2f{m, l};
+                const int row = t0 + (wn * S::TN + j) * 32 + l32;
+                const int target = row < n ? (int)a.targets[a.list[row]] - v0 - wm * S::TM * 32 : -1;
+                if (__builtin_amdgcn_ballot_w64(target >= 0 && target < S::TM * 32)) {  // (one wavefront in four at 30522 words)
+                    bool have = false;
+                    float hit = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k)
+                            if (target - 4 * hf == i * 32 + 8 * (k >> 2) + (k & 3)) {
+                                hit = z[i][j][k];
+                                have = true;
+                            }
+                    if (have) a.hit[row] = hit;
+                }
             }
             barrier();
             for (int r = threadIdx.x; r < S::BN; r += 64 * S::kWaves) {
@@ -269,40 +297,38 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_logits_kernel(const Lo
             barrier();
         } else {
             float *const sums = reinterpret_cast<float *>(lds);  // [WN][BM] of d over a wavefront's tokens
-            v16f over[S::TM];
-#pragma unroll
-            for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-                for (int k = 0; k < 16; ++k) over[i][k] = 0.0f;
 #pragma unroll
             for (int j = 0; j < S::TN; ++j) {
                 const int row = t0 + (wn * S::TN + j) * 32 + l32, token = a.list[row];
-                const bool in = row < n;
-                const float lse2 = a.lse[token] * kLog2e, w = in ? a.dloss[token] * inv : 0.0f;
-                const int target = (int)a.targets[token] - v0 - wm * S::TM * 32 - 4 * hf;
+                const bool in = row < n;  // (a padding row has weight 0 and exponentials of 0)
+                const float lse2 = in ? a.lse[token] * kLog2e : __builtin_inff(), w = in ? a.dloss[token] * inv : 0.0f;
+                const int target = in ? (int)a.targets[token] - v0 - wm * S::TM * 32 : -1;
+#pragma unroll
+                for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) z[i][j][k] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][j][k], kLog2e, -lse2)) * w;
+                if (__builtin_amdgcn_ballot_w64(target >= 0 && target < S::TM * 32)) {
+#pragma unroll
+                    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) z[i][j][k] -= target - 4 * hf == i * 32 + 8 * (k >> 2) + (k & 3) ? w : 0.0f;
+                }
                 uint16_t *const to = a.d + (int64_t)row * a.piece + tv * S::BM + wm * S::TM * 32 + 4 * hf;
 #pragma unroll
                 for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-                    for (int k = 0; k < 16; k += 4) {
-                        float d[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][j][k + e], kLog2e, -lse2));
-                            d[e] = in ? (target == i * 32 + 2 * k + e ? p - 1.0f : p) * w : 0.0f;
-                            over[i][k + e] += d[e];
-                        }
-                        *reinterpret_cast<v2u *>(to + i * 32 + 2 * k) = v2u{Bf16::pair(d[0], d[1]), Bf16::pair(d[2], d[3])};
-                    }
+                    for (int k = 0; k < 16; k += 4)
+                        *reinterpret_cast<v2u *>(to + i * 32 + 2 * k) = v2u{Bf16::pair(z[i][j][k], z[i][j][k + 1]), Bf16::pair(z[i][j][k + 2], z[i][j][k + 3])};
             }
             if (a.db) {  // (uniform)
 #pragma unroll
                 for (int i = 0; i < S::TM; ++i)
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
-                        float x = over[i][k];
+                        float x = z[i][0][k];
 #pragma unroll
-                        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor(x, o);
+                        for (int j = 1; j < S::TN; ++j) x += z[i][j][k];
+                        x = half_sum(x);
                         if (l32 == 0) sums[wn * S::BM + (wm * S::TM + i) * 32 + 8 * (k >> 2) + 4 * hf + (k & 3)] = x;
                     }
                 barrier();
@@ -310,7 +336,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_logits_kernel(const Lo
                     float x = 0.0f;
 #pragma unroll
                     for (int i = 0; i < S::WN; ++i) x += sums[i * S::BM + v];
-                    a.db[(int64_t)tt * a.piece + tv * S::BM + v] = x;
+                    if (v0 + v < a.V) a.db[(int64_t)tt * a.V + v0 + v] = x;
                 }
                 barrier();
             }
@@ -318,27 +344,34 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_logits_kernel(const Lo
     }
 }
 
-// loss and lse of 64 tokens from the maxima and sums of the vocabulary's tiles
+// loss and lse of 16 tokens from the maxima and sums of the vocabulary's tiles, sixteen threads to a token
 __global__ __launch_bounds__(256) void loss_join_kernel(const LossArgs a, int words)
 {
-    __shared__ v2f both[4][64];
-    const int n = a.counted->n, r = threadIdx.x & 63, q = threadIdx.x >> 6, row = blockIdx.x * 64 + r;
-    if (blockIdx.x * 64 >= n) return;
+    __shared__ v2f both[16][16];
+    const int n = a.counted->n, r = threadIdx.x & 15, q = threadIdx.x >> 4, row = blockIdx.x * 16 + r;
+    if (blockIdx.x * 16 >= n) return;
     float m = kLow, l = 0.0f;
-    const auto add = [&](float m1, float l1) {
-        const float top = fmaxf(m, m1);
-        l = l * __expf(m - top) + l1 * __expf(m1 - top);
+    const auto add = [&](v2f x) {
+        const float top = fmaxf(m, x[0]);
+        l = l * __expf(m - top) + x[1] * __expf(x[0] - top);
         m = top;
     };
-    for (int i = q; i < words; i += 4) {
-        const v2f x = a.part[(int64_t)i * a.Tp + row];  // (rows past n are computed too)
-        add(x[0], x[1]);
+    constexpr int kAtOnce = 8;
+    for (int i = q; i < words; i += 16 * kAtOnce) {
+        v2f x[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            x[u] = a.part[(int64_t)min(i + 16 * u, words - 1) * a.Tp + row];  // (rows past n are computed too)
+            if (i + 16 * u >= words) x[u][1] = 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) add(x[u]);
     }
     both[q][r] = v2f{m, l};
     __syncthreads();
     if (q != 0 || row >= n) return;
 #pragma unroll
-    for (int i = 1; i < 4; ++i) add(both[i][r][0], both[i][r][1]);
+    for (int i = 1; i < 16; ++i) add(both[i][r]);
     const float lse = m + logf(l);
     const int token = a.list[row];
     a.lse[token] = lse;
@@ -358,7 +391,7 @@ __device__ __host__ inline int dx_slices(int tiles, int steps)
 template <typename S>
 __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_grads_kernel(const LossArgs a)
 {
-    __shared__ __align__(1024) uint8_t lds[2 * S::kStage];
+    __shared__ __align__(1024) uint8_t lds[S::kStages * S::kStage];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave - wm * S::WN;
     const int n = a.counted->n, K = a.K;
@@ -376,7 +409,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_grads_kernel(const Los
             if (s0 < s1)
                 multiply<S, true, false>(acc, lds, s0, s1, wave, lane,
                     [&](int, int r, int s) { return a.W + (int64_t)min(a.v0 + s * 64 + (r & 63), a.V - 1) * K + min(k0 + (r & ~63), K - 64); },
-                    [&](int, int r, int s) { return a.d + (int64_t)(t0 + r) * a.piece + s * 64; }, [](int) {});
+                    [&](int, int r, int s) { return a.d + (int64_t)(t0 + r) * a.piece + s * 64; });
             float *const to = a.dXs + (int64_t)id * S::BM * S::BN;
 #pragma unroll
             for (int i = 0; i < S::TM; ++i)
@@ -391,18 +424,10 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_grads_kernel(const Los
                     }
         } else {
             const int tile = id - x_tiles * slices, tv = tile / kt, k0 = (tile - tv * kt) * S::BM, v0 = tv * S::BN;
-            if (w_steps > 0) {
-                int token[S::BM / 8 / S::kWaves];  // of the next step, fetched a step ahead
-                const auto look_up = [&](int s) {
-                    if (s + 1 >= w_steps) return;
-#pragma unroll
-                    for (int i = 0; i < S::BM / 8 / S::kWaves; ++i) token[i] = a.list[(s + 1) * 64 + (S::row(i, wave, lane) & 63)];
-                };
-                look_up(-1);
+            if (w_steps > 0)
                 multiply<S, true, true>(acc, lds, 0, w_steps, wave, lane,
-                    [&](int i, int r, int) { return a.X + (int64_t)token[i] * K + min(k0 + (r & ~63), K - 64); },
-                    [&](int, int r, int s) { return a.d + (int64_t)(s * 64 + (r & 63)) * a.piece + v0 + (r & ~63); }, look_up);
-            }
+                    [&](int, int r, int s) { return a.Xc + (int64_t)(s * 64 + (r & 63)) * K + min(k0 + (r & ~63), K - 64); },
+                    [&](int, int r, int s) { return a.d + (int64_t)(s * 64 + (r & 63)) * a.piece + v0 + (r & ~63); });
 #pragma unroll
             for (int j = 0; j < S::TN; ++j) {
                 const int v = a.v0 + v0 + (wn * S::TN + j) * 32 + l32;
@@ -421,40 +446,40 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_grads_kernel(const Los
     }
 }
 
-// dX from its slices, a zero row for a token without a target
+// dX from its slices, a zero row for a token without a target; the last workgroups join dbias
 template <typename S>
-__global__ __launch_bounds__(256) void loss_dx_kernel(const LossArgs a)
+__global__ __launch_bounds__(256) void loss_ends_kernel(const LossArgs a, int x_groups)
 {
     const int n = a.counted->n, K = a.K, quads = K / 4;
     const float scale = a.counted->scale;
+    if ((int)blockIdx.x >= x_groups) {
+        const int v = ((int)blockIdx.x - x_groups) * 256 + threadIdx.x, tiles = (n + S::BN - 1) / S::BN;
+        if (v >= a.V) return;
+        float x = 0.0f;
+#pragma unroll 8
+        for (int i = 0; i < tiles; ++i) x += a.db[(int64_t)i * a.V + v];
+        a.dbias[v] = x * scale;
+        return;
+    }
     const int kt = (K + S::BM - 1) / S::BM, slices = dx_slices(kt * ((n + S::BN - 1) / S::BN), a.piece / 64);
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)a.T * quads; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)a.T * quads; i += (int64_t)x_groups * 256) {
         const int t = (int)(i / quads), k = (int)(i - (int64_t)t * quads) * 4, row = a.place[t];
         v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
         if (row >= 0) {
             const int tile = (row / S::BN) * kt + k / S::BM;
             const float *p = a.dXs + (int64_t)tile * slices * S::BM * S::BN + (row % S::BN) * S::BM + k % S::BM;
+#pragma unroll 8
             for (int s = 0; s < slices; ++s) x += *reinterpret_cast<const v4f *>(p + (int64_t)s * S::BM * S::BN);
         }
         *reinterpret_cast<v2u *>(a.dX + (int64_t)t * K + k) = v2u{Bf16::pair(x[0] * scale, x[1] * scale), Bf16::pair(x[2] * scale, x[3] * scale)};
     }
 }
 
-// the piece's share of dbias
-template <typename S>
-__global__ __launch_bounds__(256) void loss_dbias_kernel(const LossArgs a)
-{
-    const int v = blockIdx.x * 256 + threadIdx.x;
-    if (v >= a.piece || a.v0 + v >= a.V) return;
-    const int tiles = (a.counted->n + S::BN - 1) / S::BN;
-    float x = 0.0f;
-    for (int i = 0; i < tiles; ++i) x += a.db[(int64_t)i * a.piece + v];
-    a.dbias[a.v0 + v] = x * a.counted->scale;
-}
-
-typedef Shape<2, 4, 4, 2> Large;  // 256 x 256
-typedef Shape<4, 1, 1, 2> Small;  // 128 x 64
-inline bool few(int64_t T) { return T <= 1024; }
+// 256 x 256 fills a CU with one workgroup; with few tokens the weights' bytes are what counts, and 64 x 64 with four stages keeps
+// 48 KB of them under way on every CU, two workgroups to a CU
+typedef Shape<2, 4, 4, 2, 2> Large;
+typedef Shape<2, 2, 1, 1, 4> Small;
+inline bool few(int64_t T) { return T <= 512; }
 
 inline size_t up(size_t v) { return (v + 255) / 256 * 256; }
 
@@ -482,7 +507,8 @@ size_t lay_out(LossArgs &a, uint8_t *base, bool backward)
     const int64_t pieces = (widest + a.piece - 1) / a.piece;
     a.piece = (int)((widest / kRowPad + pieces - 1) / pieces * kRowPad);  // pieces of about one size
     a.d = reinterpret_cast<uint16_t *>(take((size_t)a.Tp * a.piece * 2));
-    a.db = reinterpret_cast<float *>(take((size_t)(a.Tp / bn) * a.piece * 4));
+    a.Xc = reinterpret_cast<uint16_t *>(take((size_t)a.Tp * a.K * 2));
+    a.db = reinterpret_cast<float *>(take((size_t)(a.Tp / bn) * a.V * 4));
     const int64_t x_tiles = (int64_t)(a.Tp / bn) * ((a.K + bm - 1) / bm);
     a.dXs = reinterpret_cast<float *>(take((size_t)std::max(x_tiles, std::min<int64_t>(512, x_tiles * kSlices)) * bm * bn * 4));
     return at;
@@ -491,14 +517,16 @@ size_t lay_out(LossArgs &a, uint8_t *base, bool backward)
 bool shape_ok(int64_t T, int64_t V, int64_t K) { return T >= 1 && T <= kMost && V >= 1 && V <= kMost && k_ok(K); }
 
 template <typename S>
+constexpr int kAtWork = S::kWaves == 8 ? 256 : 512;  // workgroups of a launch: as many as are resident
+
+template <typename S>
 qb_status forward(const LossArgs &a, hipStream_t st)
 {
     const int words = (a.V + S::BM - 1) / S::BM;
     const int64_t tiles = (int64_t)words * (a.Tp / S::BN);
-    const int grid = (int)std::min<int64_t>(tiles, S::kWaves == 8 ? 256 : 1024);
     loss_rows_kernel<false><<<(a.T + 1023) / 1024, 1024, 0, st>>>(a);
-    loss_logits_kernel<S, false><<<grid, 64 * S::kWaves, 0, st>>>(a);
-    loss_join_kernel<<<(a.T + 63) / 64, 256, 0, st>>>(a, words);
+    loss_logits_kernel<S, false><<<(int)std::min<int64_t>(tiles, kAtWork<S>), 64 * S::kWaves, 0, st>>>(a);
+    loss_join_kernel<<<(a.T + 15) / 16, 256, 0, st>>>(a, words);
     return launch_status();
 }
 
@@ -506,14 +534,13 @@ template <typename S>
 qb_status backward(LossArgs a, hipStream_t st)
 {
     loss_rows_kernel<true><<<(a.T + 1023) / 1024, 1024, 0, st>>>(a);
-    const int most = S::kWaves == 8 ? 256 : 1024;
     for (a.v0 = 0; a.v0 < a.V; a.v0 += a.piece) {
         const int64_t tiles = (int64_t)(a.piece / S::BM) * (a.Tp / S::BN);
-        loss_logits_kernel<S, true><<<(int)std::min<int64_t>(tiles, most), 64 * S::kWaves, 0, st>>>(a);
-        if (a.dbias) loss_dbias_kernel<S><<<(a.piece + 255) / 256, 256, 0, st>>>(a);
-        loss_grads_kernel<S><<<most, 64 * S::kWaves, 0, st>>>(a);
+        loss_logits_kernel<S, true><<<(int)std::min<int64_t>(tiles, kAtWork<S>), 64 * S::kWaves, 0, st>>>(a);
+        loss_grads_kernel<S><<<kAtWork<S>, 64 * S::kWaves, 0, st>>>(a);
     }
-    loss_dx_kernel<S><<<(int)std::min<int64_t>(4096, ((int64_t)a.T * (a.K / 4) + 255) / 256), 256, 0, st>>>(a);
+    const int x_groups = (int)std::min<int64_t>(4096, ((int64_t)a.T * (a.K / 4) + 255) / 256);
+    loss_ends_kernel<S><<<x_groups + (a.dbias ? (a.V + 255) / 256 : 0), 256, 0, st>>>(a, x_groups);
     return launch_status();
 }
 
