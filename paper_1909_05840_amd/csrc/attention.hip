@@ -102,9 +102,13 @@ __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], co
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[kb][i] = tile0 + 32 * kb + 8 * (i >> 2) + 4 * hf + (i & 3) < limit ? s[kb][i] : -__builtin_inff();
     }
-    float top = s[0][0];
+    float top = s[0][0], other = s[KB - 1][1];  // (two chains)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, KB == 2 ? fmaxf(s[0][i], s[KB - 1][i]) : s[0][i]);
+    for (int i = 0; i < 16; i += 2) {
+        top = max3(top, s[0][i], s[0][i + 1]);
+        if (KB == 2) other = max3(other, s[KB - 1][i], s[KB - 1][i + 1]);
+    }
+    top = fmaxf(top, other);
     top = halves_max(top);
     if (__builtin_amdgcn_ballot_w64((top - x.m) * c > kLazy)) {
         const float m = fmaxf(x.m, top), f = __builtin_amdgcn_exp2f((x.m - m) * c);
@@ -201,9 +205,16 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uin
     const uint16_t *const K = a.K + (int64_t)seg.k0 * a.k_row + (int64_t)kv * a.k_head;
     const uint16_t *const V = a.V + (int64_t)seg.k0 * a.v_row + (int64_t)kv * a.v_head;
     const uint32_t lds0 = lds_address(lds);
+    const bool near = near_rows(a.k_row) && near_rows(a.v_row);
+    const TileCopy<D, kKeys, 4> copy_k(wave, lane, [&](int r) { return (uint32_t)r * (uint32_t)a.k_row; }), copy_v(wave, lane, [&](int r) { return (uint32_t)r * (uint32_t)a.v_row; });
     const auto fetch = [&](int tile, int stage) {
-        // rows past the last key repeat it: its scores are masked, its values meet weights of zero
         const uint32_t to = lds0 + stage * 2 * kTile;
+        if (near && (tile + 1) * kKeys <= seg.nk) {
+            copy_k.copy(K + (int64_t)tile * kKeys * a.k_row, to, wave);
+            copy_v.copy(V + (int64_t)tile * kKeys * a.v_row, to + kTile, wave);
+            return;
+        }
+        // rows past the last key repeat it: its scores are masked, its values meet weights of zero
         copy_rows<D, kKeys, 4>(to, wave, lane, [&](int r) { return K + (int64_t)min(tile * kKeys + r, seg.nk - 1) * a.k_row; });
         copy_rows<D, kKeys, 4>(to + kTile, wave, lane, [&](int r) { return V + (int64_t)min(tile * kKeys + r, seg.nk - 1) * a.v_row; });
     };

@@ -78,6 +78,32 @@ __device__ __forceinline__ void copy_rows(uint32_t lds, int wave, int lane, cons
     }
 }
 
+// The same for whole tiles of rows whose distances from the tile's first row do not change from tile to tile: the lane's offsets are
+// formed once, and a copy takes no vector arithmetic.  (Formed anew they were a third of the forward's vector instructions, and with the
+// division by the group more than half of those of dK and dV.)
+template <int D, int ROWS, int WAVES>
+struct TileCopy {
+    typedef Rows<D> R;
+    static constexpr int N = ROWS / R::kPerCopy / WAVES;
+    uint32_t offset[N];
+    template <typename F>  // values from the tile's first row to row i
+    __device__ __forceinline__ TileCopy(int wave, int lane, const F &distance)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int r = (i * WAVES + wave) * R::kPerCopy + R::copy_row(lane);
+            offset[i] = (uint32_t)(distance(r) + 8 * R::copy_chunk(r, lane)) * 2;
+        }
+    }
+    __device__ __forceinline__ void copy(const uint16_t *base, uint32_t lds, int wave) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) copy16(base, offset[i], lds + (i * WAVES + wave) * (R::kPerCopy * R::kBytes));
+    }
+};
+// whether the rows of a tile lie less than 2^31 bytes apart
+__device__ __forceinline__ bool near_rows(int64_t stride) { return stride >= 0 && stride < (1 << 23); }
+
 // The draws of four neighbouring keys of a query (k a multiple of 4).
 __device__ __forceinline__ v2u weight_draws(const Threefry &bits, int row_q, int head, int k)
 {

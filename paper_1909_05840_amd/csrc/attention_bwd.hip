@@ -21,7 +21,7 @@ struct GradArgs {
     uint16_t *dQ, *dK, *dV;
     int64_t q_row, q_head, k_row, k_head, v_row, v_head;
     float *stat;  // [2][total_q * heads]: lse / ln 2 (+infinity for a row that sees nothing: its P is zero), delta
-    float *part;  // [pairs][tiles of keys][splits][128][dK, dV] where rows are split
+    float *part;  // [pairs][tiles of keys][splits][128][dK, dV] of tiles in parts
 };
 
 template <typename T, int D>
@@ -108,8 +108,15 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
     const uint16_t *const K = a.K + (int64_t)seg.k0 * a.k_row + (int64_t)kv * a.k_head;
     const uint16_t *const V = a.V + (int64_t)seg.k0 * a.v_row + (int64_t)kv * a.v_head;
     const uint32_t lds0 = lds_address(lds);
+    const bool near = near_rows(a.k_row) && near_rows(a.v_row);
+    const TileCopy<D, kKeys, 4> copy_k(wave, lane, [&](int r) { return (uint32_t)r * (uint32_t)a.k_row; }), copy_v(wave, lane, [&](int r) { return (uint32_t)r * (uint32_t)a.v_row; });
     const auto fetch = [&](int tile, int stage) {
         const uint32_t to = lds0 + stage * 2 * kTile;
+        if (near && (tile + 1) * kKeys <= seg.nk) {
+            copy_k.copy(K + (int64_t)tile * kKeys * a.k_row, to, wave);
+            copy_v.copy(V + (int64_t)tile * kKeys * a.v_row, to + kTile, wave);
+            return;
+        }
         copy_rows<D, kKeys, 4>(to, wave, lane, [&](int r) { return K + (int64_t)min(tile * kKeys + r, seg.nk - 1) * a.k_row; });
         copy_rows<D, kKeys, 4>(to + kTile, wave, lane, [&](int r) { return V + (int64_t)min(tile * kKeys + r, seg.nk - 1) * a.v_row; });
     };
@@ -190,29 +197,35 @@ __device__ __forceinline__ void copy4(const void *from, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(lds) : "memory", "m0");
 }
+__device__ __forceinline__ void copy4(const void *base, uint32_t offset, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory", "m0");
+}
 // word of lane B of every four, as a constant of the instruction
 template <int B>
 __device__ __forceinline__ uint32_t of_four(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, B * 0x55, 0xF, 0xF, true); }
 
-// The rows that a tile of 128 keys is seen by, in tiles of 64, cut into `splits` parts of about the same number.
+// The rows that a tile of 128 keys is seen by, in tiles of 64, are cut into parts of about the same number, at most `most` of them to a part
+// (with causal masks the first keys are seen by many more rows than the last).
 struct RowTiles {
-    int begin, end;
+    int begin, end, parts;
 };
 __device__ __forceinline__ int first_row(const AttnArgs &a, const Segment &seg, int rows, int key)  // causal: key <= token + nk - nq
 {
     return a.causal ? (int)min((int64_t)rows, (int64_t)max(0, key - (seg.nk - seg.nq)) * a.group) : 0;
 }
-__device__ __forceinline__ RowTiles row_tiles(const AttnArgs &a, const Segment &seg, int rows, int first_key, int part, int splits)
+__device__ __forceinline__ RowTiles row_tiles(const AttnArgs &a, const Segment &seg, int rows, int first_key, int part, int most)
 {
-    const int all = (rows + kRowsOfTile - 1) / kRowsOfTile, each = (all + splits - 1) / splits;
-    return {max(first_row(a, seg, rows, first_key) / kRowsOfTile, part * each), min(all, (part + 1) * each)};
+    const int begin = first_row(a, seg, rows, first_key) / kRowsOfTile, n = max(0, (rows + kRowsOfTile - 1) / kRowsOfTile - begin);
+    const int parts = max(1, (n + most - 1) / most);
+    return {begin + (int)((int64_t)n * part / parts), begin + (int)((int64_t)n * (part + 1) / parts), parts};
 }
 
 // dK and dV; 128 keys to a workgroup, 32 to a wavefront: a lane's results all of one key.  Where tiles of keys are few, a workgroup does
 // a part of the rows, and its binary32 sums go to the workspace for a third launch to join.  Scores are taken as S = Q K^T, so that a
 // lane holds sixteen rows of its key and P and dS are, as they lie, the operands of dV^T = dO^T P and dK^T = Q^T dS.
 template <typename T, int D, bool DROP>
-__global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a, const GradArgs g, int splits, bool by_xcd)
+__global__ __launch_bounds__(256, D == 64 && !DROP ? 3 : 2) void attention_dkv_kernel(const AttnArgs a, const GradArgs g, int splits, int most, bool by_xcd)
 {
     typedef Rows<D> R;
     constexpr int kTile = kRowsOfTile * R::kBytes, kStage = 2 * kTile + 2 * kRowsOfTile * 4;
@@ -223,7 +236,8 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
     if (at.pair >= a.n_seqs * a.kv_heads) return;
     const int b = at.pair / a.kv_heads, kv = at.pair - b * a.kv_heads;
     const Segment seg = segment(a, b);
-    const int back = a.tiles * splits - 1 - at.tile, tile = back / splits, part = back - tile * splits;  // (the first keys are seen by the most rows)
+    // `splits`: the most parts that a tile of keys has (the first keys are seen by the most rows: they come first)
+    const int back = a.tiles * splits - 1 - at.tile, tile = back / splits, part = back - tile * splits;
     const int first = tile * 128;
     if (first >= seg.nk) return;
     const int rows = max(0, seg.nq) * a.group;
@@ -240,14 +254,29 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
     }
     const int from_row = first_row(a, seg, rows, key);
     const int wave_from = __builtin_amdgcn_readfirstlane(first_row(a, seg, rows, wave_first)), wave_all = __builtin_amdgcn_readfirstlane(first_row(a, seg, rows, wave_first + 31));
-    const RowTiles todo = row_tiles(a, seg, rows, first, part, splits);
+    const RowTiles todo = row_tiles(a, seg, rows, first, part, most);
+    if (part >= todo.parts) return;
     const int begin = __builtin_amdgcn_readfirstlane(todo.begin), end = __builtin_amdgcn_readfirstlane(todo.end);
-    if (splits > 1 && begin >= end) return;  // (the joining launch knows)
 
     const uint32_t lds0 = lds_address(lds);
     const int64_t stats = (int64_t)a.total_q * a.heads;
+    // where the group divides a tile, a tile's rows lie at the same distances from its first token's whatever the tile
+    const int shift = __builtin_ctz(a.group);
+    const bool near = (a.group & (a.group - 1)) == 0 && a.group <= kRowsOfTile && near_rows(a.q_row) && near_rows(a.q_head) && (int64_t)a.heads * D < (1 << 23);
+    const auto token_in = [&](int r) { return (uint32_t)(r >> shift); };
+    const auto head_in = [&](int r) { return (uint32_t)(r & (a.group - 1)); };
+    const TileCopy<D, kRowsOfTile, 4> copy_q(wave, lane, [&](int r) { return token_in(r) * (uint32_t)a.q_row + head_in(r) * (uint32_t)a.q_head; }),
+        copy_d(wave, lane, [&](int r) { return (token_in(r) * (uint32_t)a.heads + head_in(r)) * D; });
+    const uint32_t stat_offset = (token_in(lane) * (uint32_t)a.heads + head_in(lane)) * 4;
     const auto fetch = [&](int tile, int stage) {
         const uint32_t to = lds0 + stage * kStage;
+        if (near && (tile + 1) * kRowsOfTile <= rows) {
+            const int64_t token = seg.q0 + (tile * kRowsOfTile >> shift), at_row = token * a.heads + kv * a.group;
+            copy_q.copy(a.Q + token * a.q_row + (int64_t)kv * a.group * a.q_head, to, wave);
+            copy_d.copy(g.dO + at_row * D, to + kTile, wave);
+            if (wave < 2) copy4(g.stat + wave * stats + at_row, stat_offset, to + 2 * kTile + wave * kRowsOfTile * 4);
+            return;
+        }
         const auto split = [&](int r, int &token, int &head) {  // rows past the end repeat the last one; their P is set to zero
             r = min(tile * kRowsOfTile + r, rows - 1);
             token = a.group == 1 ? r : (int)((unsigned)r / (unsigned)a.group);
@@ -349,7 +378,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
         }
     }
     if (key >= seg.nk) return;
-    if (splits > 1) {
+    if (todo.parts > 1) {
         float *const to = g.part + ((int64_t)((at.pair * (int64_t)a.tiles + tile) * splits + part) * 128 + key - first) * (2 * D);
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
@@ -366,7 +395,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
 
 // dK and dV of 16 keys from their parts; a thread does eight neighbouring values
 template <typename T, int D>
-__global__ __launch_bounds__(256) void attention_dkv_join_kernel(const AttnArgs a, const GradArgs g, int splits, float inv_share)
+__global__ __launch_bounds__(256) void attention_dkv_join_kernel(const AttnArgs a, const GradArgs g, int splits, int most, float inv_share)
 {
     constexpr int kEach = 2 * D / 8;  // threads to a key
     const int pair = blockIdx.x / (a.tiles * (128 * kEach / 256)), in_pair = blockIdx.x - pair * (a.tiles * (128 * kEach / 256));
@@ -377,9 +406,10 @@ __global__ __launch_bounds__(256) void attention_dkv_join_kernel(const AttnArgs 
     const int rows = max(0, seg.nq) * a.group, tile = key / 128;
     const float *const from = g.part + ((int64_t)(pair * (int64_t)a.tiles + tile) * splits * 128 + key % 128) * (2 * D) + d;
     v4f x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-    for (int p = 0; p < splits; ++p) {
-        const RowTiles t = row_tiles(a, seg, rows, tile * 128, p, splits);
-        if (t.begin >= t.end) continue;
+    const int parts = min(splits, row_tiles(a, seg, rows, tile * 128, 0, most).parts);
+    if (parts == 1) return;  // (written whole)
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
         const v4f *const q = reinterpret_cast<const v4f *>(from + (int64_t)p * 128 * (2 * D));
         x[0] += q[0];
         x[1] += q[1];
@@ -389,12 +419,17 @@ __global__ __launch_bounds__(256) void attention_dkv_join_kernel(const AttnArgs 
     *reinterpret_cast<v4u *>(to) = v4u{T::pair(x[0][0] * f, x[0][1] * f), T::pair(x[0][2] * f, x[0][3] * f), T::pair(x[1][0] * f, x[1][1] * f), T::pair(x[1][2] * f, x[1][3] * f)};
 }
 
-// Into how many parts the rows of a tile of keys are cut: such that about kParts workgroups are at work, of eight tiles of rows or more
-constexpr int64_t kParts = 1024;
-inline int64_t row_splits(int64_t pairs, int64_t max_q, int64_t group, int64_t max_k)
+// How many tiles of rows a part has at most: such that the longest sequences' parts come to about kParts workgroups (three fit a CU:
+// two rounds of them even out what differs), but eight or more; and the most parts of a tile of keys
+constexpr int64_t kParts = 1536;
+struct Parts {
+    int64_t most, splits;
+};
+inline Parts row_parts(int64_t pairs, int64_t max_q, int64_t group, int64_t max_k, bool causal)
 {
-    const int64_t tiles = pairs * ((max_k + 127) / 128);
-    return std::max<int64_t>(1, std::min({kParts / std::max<int64_t>(1, tiles), (max_q * group / kRowsOfTile) / 8, (int64_t)16}));
+    const int64_t tiles = pairs * ((max_k + 127) / 128), rows = (max_q * group + kRowsOfTile - 1) / kRowsOfTile;
+    const int64_t most = std::max<int64_t>(8, tiles * rows / (causal ? 2 : 1) / kParts);
+    return {most, std::max<int64_t>(1, (rows + most - 1) / most)};
 }
 inline size_t stat_bytes(const qb_attention *p) { return ((size_t)p->total_q * p->heads * 8 + 255) / 256 * 256; }
 
@@ -416,11 +451,12 @@ qb_status backward(AttnArgs a, const GradArgs &g, int64_t max_q, int64_t max_k, 
     }
     if (max_k > 0) {
         a.tiles = (int)((max_k + 127) / 128);
-        const int splits = (int)row_splits(pairs, max_q, a.group, max_k);
+        const Parts parts = row_parts(pairs, max_q, a.group, max_k, a.causal);
+        const int splits = (int)parts.splits, most = (int)parts.most;
         const int64_t grid = dealt_workgroups(pairs, (int64_t)a.tiles * splits);
-        if (drop) attention_dkv_kernel<T, D, true><<<(int)grid, 256, 0, stream>>>(a, g, splits, by_xcd);
-        else attention_dkv_kernel<T, D, false><<<(int)grid, 256, 0, stream>>>(a, g, splits, by_xcd);
-        if (splits > 1) attention_dkv_join_kernel<T, D><<<(int)(pairs * a.tiles * (128 * 2 * D / 8 / 256)), 256, 0, stream>>>(a, g, splits, drop ? a.inv_share : 1.0f);
+        if (drop) attention_dkv_kernel<T, D, true><<<(int)grid, 256, 0, stream>>>(a, g, splits, most, by_xcd);
+        else attention_dkv_kernel<T, D, false><<<(int)grid, 256, 0, stream>>>(a, g, splits, most, by_xcd);
+        if (splits > 1) attention_dkv_join_kernel<T, D><<<(int)(pairs * a.tiles * (128 * 2 * D / 8 / 256)), 256, 0, stream>>>(a, g, splits, most, drop ? a.inv_share : 1.0f);
     }
     return launch_status();
 }
@@ -434,7 +470,7 @@ extern "C" size_t qb_attention_bwd_workspace_nbytes(const qb_attention *p)
 {
     AttnArgs a;
     if (attention_args(p, a) != QB_OK) return 0;
-    const int64_t pairs = (int64_t)a.n_seqs * a.kv_heads, splits = row_splits(pairs, p->max_q, a.group, p->max_k);
+    const int64_t pairs = (int64_t)a.n_seqs * a.kv_heads, splits = row_parts(pairs, p->max_q, a.group, p->max_k, p->causal).splits;
     return stat_bytes(p) + (splits > 1 ? (size_t)(pairs * ((p->max_k + 127) / 128) * splits) * 128 * 2 * p->dim * 4 : 0);
 }
 
@@ -452,7 +488,7 @@ extern "C" qb_status qb_attention_bwd(const qb_attention *p, const void *dO, con
     if (!aligned16(dO) || !aligned16(O) || !aligned16(grads->dQ) || !aligned16(grads->dK) || !aligned16(grads->dV)) return QB_ERR_VALUE;
     if (p->total_q > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255))) return QB_ERR_WORKSPACE;
     const int64_t pairs = (int64_t)p->n_seqs * p->kv_heads;
-    if (dealt_workgroups(pairs, (p->max_q * a.group + 127) / 128) > INT32_MAX / 256 || dealt_workgroups(pairs, (p->max_k + 127) / 128) > INT32_MAX / 4096) return QB_ERR_SHAPE;
+    if (dealt_workgroups(pairs, (p->max_q * a.group + 127) / 128) > INT32_MAX / 256 || dealt_workgroups(pairs, (p->max_k + 127) / 128 * row_parts(pairs, p->max_q, a.group, p->max_k, p->causal).splits) > INT32_MAX / 256) return QB_ERR_SHAPE;
     const GradArgs g = {static_cast<const uint16_t *>(dO), static_cast<const uint16_t *>(O), lse, static_cast<uint16_t *>(grads->dQ), static_cast<uint16_t *>(grads->dK),
                         static_cast<uint16_t *>(grads->dV), grads->q_row, grads->q_head, grads->k_row, grads->k_head, grads->v_row, grads->v_head, static_cast<float *>(workspace), reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + stat_bytes(p))};
     const hipStream_t st = static_cast<hipStream_t>(stream);

@@ -59,6 +59,11 @@ __device__ __forceinline__ void copy16(const void *from, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory", "m0");
 }
+// the same with the address as a base that the wavefront shares and an offset in bytes
+__device__ __forceinline__ void copy16(const void *base, uint32_t offset, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory", "m0");
+}
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p; }
 
 // A tile of rows of D 16-bit values in LDS, rows dense.  The 16-byte chunks of a row are XORed with a key of the row such
@@ -95,6 +100,8 @@ struct Rows {
     }
 };
 
+// the largest of three in one instruction (fmaxf has the compiler quieten its operands first, an instruction each)
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 // the value of the other half of the wavefront joined with the lane's own
 __device__ __forceinline__ float halves_max(float v)
 {

@@ -257,7 +257,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_logits_kernel(const Lo
 #pragma unroll
                 for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) m = fmaxf(m, z[i][j][k]);
+                    for (int k = 0; k < 16; k += 2) m = max3(m, z[i][j][k], z[i][j][k + 1]);
                 m = fmaxf(halves_max(m), kLow);
                 const float m2 = m * kLog2e;
                 float l = 0.0f;
