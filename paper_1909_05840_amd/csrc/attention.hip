@@ -83,19 +83,36 @@ constexpr int kKeys = 64;  // keys to a tile
 // KB blocks of 32 keys from tile0 on, in LDS, of which the lane's row sees those below `limit` (masked: some row of the
 // wavefront does not see all of them).
 template <typename T, int D, bool DROP, int KB = 2>
-__device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], const uint8_t *tk, const uint8_t *tv, int tile0, int limit,
+__device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], const Operands<D> &op, uint32_t tk, uint32_t tv, int tile0, int limit,
                                        bool masked, float c, const Threefry &bits, uint32_t threshold, int row_q, int head, int lane)
 {
-    typedef Rows<D> R;
     const int hf = lane >> 5;
+    // All operands of a product are read before its first multiplication (left to itself the compiler reads each just in front of its
+    // use, and every multiplication waits for the LDS): the keys here, the values in front of the exponentials.
     v16f s[KB];
+    {
+        v8s k[KB][D / 16];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
+        for (int d = 0; d < D / 16; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[kb][i] = 0.0f;
+            for (int kb = 0; kb < KB; ++kb) k[kb][d] = op.along(tk, 32 * kb, d);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) s[kb] = T::mma32(R::along(tk, 32 * kb, d, lane), q[d], s[kb]);
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[kb][i] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) s[kb] = T::mma32(k[kb][d], q[d], s[kb]);
     }
+    v8s v[D == 64 ? KB : 1][2][D / 32];
+    const auto read_values = [&](int kb, v8s (&to)[2][D / 32]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) to[h][i] = op.across(tv, 32 * kb + 16 * h, i);
+    };
     if (masked) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
@@ -119,6 +136,9 @@ __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], co
 #pragma unroll
             for (int j = 0; j < 16; ++j) x.o[i][j] *= f;
     }
+    read_values(0, v[0]);
+    if constexpr (D == 64 && KB == 2) read_values(1, v[KB - 1]);
+    __builtin_amdgcn_sched_barrier(0);
     const float mc = x.m * c;
     float sum = 0.0f;
 #pragma unroll
@@ -142,7 +162,8 @@ __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], co
             }
     }
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+    for (int kb = 0; kb < KB; ++kb) {
+        if (D != 64 && kb > 0) read_values(kb, v[0]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             v4u w;
@@ -150,8 +171,9 @@ __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], co
             for (int i = 0; i < 4; ++i) w[i] = T::pair(s[kb][8 * h + 2 * i], s[kb][8 * h + 2 * i + 1]);
             const v8s p = __builtin_bit_cast(v8s, w);
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) x.o[i] = T::mma32(R::across(tv, 32 * kb + 16 * h, 32 * i, lane), p, x.o[i]);
+            for (int i = 0; i < D / 32; ++i) x.o[i] = T::mma32(v[D == 64 ? kb : 0][h][i], p, x.o[i]);
         }
+    }
 }
 
 // O^T / l to a row of O: the lane holds four neighbouring values of its row at a time
@@ -219,6 +241,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uin
         copy_rows<D, kKeys, 4>(to + kTile, wave, lane, [&](int r) { return V + (int64_t)min(tile * kKeys + r, seg.nk - 1) * a.v_row; });
     };
     const Threefry bits(DROP ? (uint64_t)*a.seed : 0);
+    const Operands<D> op(lane);
     Softmax<D> x;
     x.clear();
     if (tiles) fetch(0, 0);
@@ -227,7 +250,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uin
         barrier();
         if (t + 1 < tiles) fetch(t + 1, (t + 1) & 1);
         if (t * kKeys < wave_most)
-            attend<T, D, DROP>(x, q, lds[t & 1], lds[t & 1] + kTile, t * kKeys, limit, (t + 1) * kKeys > wave_least, a.c, bits, a.threshold, row_q, head, lane);
+            attend<T, D, DROP>(x, q, op, lds0 + (t & 1) * 2 * kTile, lds0 + (t & 1) * 2 * kTile + kTile, t * kKeys, limit, (t + 1) * kKeys > wave_least, a.c, bits, a.threshold, row_q, head, lane);
     }
     if (row >= rows) return;
     const float l = halves_sum(x.l);
@@ -274,6 +297,7 @@ __global__ __launch_bounds__(256, 1) void attention_cache_kernel(const AttnArgs 
         copy_rows<D, kTileKeys, 1>(to, 0, lane, [&](int r) { return K + (int64_t)min(key0 + r, seg.nk - 1) * a.k_row; });
         copy_rows<D, kTileKeys, 1>(to + kTile, 0, lane, [&](int r) { return V + (int64_t)min(key0 + r, seg.nk - 1) * a.v_row; });
     };
+    const Operands<D> op(lane);
     Softmax<D> x;
     x.clear();
     const int step = 4 * kTileKeys, mine = begin + wave * kTileKeys;
@@ -292,7 +316,7 @@ __global__ __launch_bounds__(256, 1) void attention_cache_kernel(const AttnArgs 
             wait_copies<0>();
         }
         asm volatile("" ::: "memory");
-        attend<T, D, false, KB>(x, q, lds + stage * 2 * kTile, lds + stage * 2 * kTile + kTile, key0, limit, key0 + kTileKeys > least, a.c, bits, 0, row_q, head, lane);
+        attend<T, D, false, KB>(x, q, op, lds0 + stage * 2 * kTile, lds0 + stage * 2 * kTile + kTile, key0, limit, key0 + kTileKeys > least, a.c, bits, 0, row_q, head, lane);
         __builtin_amdgcn_s_waitcnt(0xC07F);  // this stage's reads have returned before the next copies into it
         asm volatile("" ::: "memory");
     }

@@ -20,7 +20,7 @@ struct GradArgs {
     const float *lse;
     uint16_t *dQ, *dK, *dV;
     int64_t q_row, q_head, k_row, k_head, v_row, v_head;
-    float *stat;  // [2][total_q * heads]: lse / ln 2 (+infinity for a row that sees nothing: its P is zero), delta
+    float *stat;  // [2][total_q * heads + 1]: -lse / scale (-infinity for a row that sees nothing, and for the last entry: P is zero), -delta
     float *part;  // [pairs][tiles of keys][splits][128][dK, dV] of tiles in parts
 };
 
@@ -59,7 +59,7 @@ __device__ __forceinline__ v8s rounded(const v16f &x, int half)
 // sums eps = sum_k P (dP - delta) on the way, which is what delta lacks, and B = sum_k P K beside A = sum_k dS K: dQ = scale (A - eps B),
 // and the second launch gets delta + eps.  With many keys |O| is small beside |V|, and the rounding with it: tiles of rows that see more than
 // kExactKeys are left to the other variant, which needs two thirds of the registers and six sevenths of the products.
-constexpr int kExactKeys = 2048;
+constexpr int kExactKeys = 1024;
 template <typename T, int D, bool DROP, bool EXACT>
 __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_kernel(const AttnArgs a, const GradArgs g, bool by_xcd)
 {
@@ -68,6 +68,7 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
     __shared__ __align__(1024) uint8_t lds[2][2 * kTile];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (EXACT && blockIdx.x == 0 && threadIdx.x < 2) g.stat[threadIdx.x ? 2 * (int64_t)a.total_q * a.heads + 1 : (int64_t)a.total_q * a.heads] = threadIdx.x ? 0.0f : -__builtin_inff();
     const Place at = place(blockIdx.x, a.n_seqs * a.kv_heads, a.tiles, by_xcd);
     if (at.pair >= a.n_seqs * a.kv_heads) return;
     const int b = at.pair / a.kv_heads, kv = at.pair - b * a.kv_heads;
@@ -121,6 +122,7 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
         copy_rows<D, kKeys, 4>(to + kTile, wave, lane, [&](int r) { return V + (int64_t)min(tile * kKeys + r, seg.nk - 1) * a.v_row; });
     };
     const Threefry bits(DROP ? (uint64_t)*a.seed : 0);
+    const Operands<D> op(lane);
     v16f A[D / 32], B[EXACT ? D / 32 : 1];
     clear(A);
     clear(B);
@@ -131,17 +133,39 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
         barrier();
         if (t + 1 < tiles) fetch(t + 1, (t + 1) & 1);
         if (t * kKeys >= wave_most) continue;
-        const uint8_t *const tk = lds[t & 1], *const tv = tk + kTile;
+        const uint32_t tk = lds0 + (t & 1) * 2 * kTile, tv = tk + kTile;
         const bool masked = (t + 1) * kKeys > wave_least;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
+            // (all operands are read in front of their products, those turned for the last one in front of the exponentials)
             v16f s, dp;
+            {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.0f;
+                for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.0f;
 #pragma unroll
-            for (int d = 0; d < D / 16; ++d) s = T::mma32(R::along(tk, 32 * kb, d, lane), q[d], s);
+                for (int d0 = 0; d0 < D / 16; d0 += 4) {
+                    v8s k[4], v[4];
 #pragma unroll
-            for (int d = 0; d < D / 16; ++d) dp = T::mma32(R::along(tv, 32 * kb, d, lane), dO[d], dp);
+                    for (int d = 0; d < 4; ++d) k[d] = op.along(tk, 32 * kb, d0 + d);
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) v[d] = op.along(tv, 32 * kb, d0 + d);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        s = T::mma32(k[d], q[d0 + d], s);
+                        dp = T::mma32(v[d], dO[d0 + d], dp);
+                    }
+                }
+            }
+            v8s turned[2][D / 32];
+            const auto turn = [&](int h) {
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) turned[h][i] = op.across(tk, 32 * kb + 16 * h, i);
+            };
+            if constexpr (D == 64) {
+                turn(0);
+                turn(1);
+            }
             if (masked) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = t * kKeys + 32 * kb + 8 * (i >> 2) + 4 * hf + (i & 3) < limit ? s[i] : -__builtin_inff();
@@ -165,14 +189,14 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+                if constexpr (D != 64) turn(h);
                 const v8s ds = rounded<T>(dp, h);
                 v8s p;
                 if constexpr (EXACT) p = rounded<T>(s, h);
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) {
-                    const v8s k = R::across(tk, 32 * kb + 16 * h, 32 * i, lane);
-                    A[i] = T::mma32(k, ds, A[i]);
-                    if constexpr (EXACT) B[i] = T::mma32(k, p, B[i]);
+                    A[i] = T::mma32(turned[h][i], ds, A[i]);
+                    if constexpr (EXACT) B[i] = T::mma32(turned[h][i], p, B[i]);
                 }
             }
         }
@@ -188,8 +212,8 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
     if (row >= rows) return;
     write_scaled<T, D>(g.dQ + (int64_t)row_q * g.q_row + (int64_t)head * g.q_head, A, a.scale, hf);
     if (hf == 0) {
-        g.stat[at_row] = lse2;
-        g.stat[(int64_t)a.total_q * a.heads + at_row] = delta;
+        g.stat[at_row] = lse > -__builtin_inff() ? -lse / a.scale : -__builtin_inff();
+        g.stat[(int64_t)a.total_q * a.heads + 1 + at_row] = -delta;
     }
 }
 
@@ -197,39 +221,43 @@ __device__ __forceinline__ void copy4(const void *from, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(lds) : "memory", "m0");
 }
-__device__ __forceinline__ void copy4(const void *base, uint32_t offset, uint32_t lds)
-{
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory", "m0");
-}
 // word of lane B of every four, as a constant of the instruction
 template <int B>
 __device__ __forceinline__ uint32_t of_four(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, B * 0x55, 0xF, 0xF, true); }
 
-// The rows that a tile of 128 keys is seen by, in tiles of 64, are cut into parts of about the same number, at most `most` of them to a part
+// For dK and dV the rows of a key head are dealt to tiles of 64: `heads` of the group's heads of each of `tokens` tokens, so that a row's
+// place in its tile tells its token and head without a division.  Rows of a tile that are none (three heads: the last of 64) have
+// P = 0.  `chunks`: tiles to a group of more than 64.
+struct RowTiling {
+    int heads, tokens, chunks;
+};
+inline RowTiling row_tiling(int group)
+{
+    const int heads = group < kRowsOfTile ? group : kRowsOfTile;
+    return {heads, kRowsOfTile / heads, (group + heads - 1) / heads};
+}
+// The tiles that a tile of 128 keys is seen by are cut into parts of about the same number, at most `most` of them to a part
 // (with causal masks the first keys are seen by many more rows than the last).
 struct RowTiles {
     int begin, end, parts;
 };
-__device__ __forceinline__ int first_row(const AttnArgs &a, const Segment &seg, int rows, int key)  // causal: key <= token + nk - nq
+__device__ __forceinline__ RowTiles row_tiles(const AttnArgs &a, const RowTiling &r, const Segment &seg, int first_key, int part, int most)
 {
-    return a.causal ? (int)min((int64_t)rows, (int64_t)max(0, key - (seg.nk - seg.nq)) * a.group) : 0;
-}
-__device__ __forceinline__ RowTiles row_tiles(const AttnArgs &a, const Segment &seg, int rows, int first_key, int part, int most)
-{
-    const int begin = first_row(a, seg, rows, first_key) / kRowsOfTile, n = max(0, (rows + kRowsOfTile - 1) / kRowsOfTile - begin);
-    const int parts = max(1, (n + most - 1) / most);
-    return {begin + (int)((int64_t)n * part / parts), begin + (int)((int64_t)n * (part + 1) / parts), parts};
+    const int nq = max(0, seg.nq), token = a.causal ? min(nq, max(0, first_key - (seg.nk - seg.nq))) : 0;  // causal: key <= token + nk - nq
+    const int all = (nq + r.tokens - 1) / r.tokens, first = token < nq ? token / r.tokens : all;
+    const int n = (all - first) * r.chunks, parts = max(1, (n + most - 1) / most);
+    return {first * r.chunks + (int)((int64_t)n * part / parts), first * r.chunks + (int)((int64_t)n * (part + 1) / parts), parts};
 }
 
 // dK and dV; 128 keys to a workgroup, 32 to a wavefront: a lane's results all of one key.  Where tiles of keys are few, a workgroup does
 // a part of the rows, and its binary32 sums go to the workspace for a third launch to join.  Scores are taken as S = Q K^T, so that a
 // lane holds sixteen rows of its key and P and dS are, as they lie, the operands of dV^T = dO^T P and dK^T = Q^T dS.
 template <typename T, int D, bool DROP>
-__global__ __launch_bounds__(256, D == 64 && !DROP ? 3 : 2) void attention_dkv_kernel(const AttnArgs a, const GradArgs g, int splits, int most, bool by_xcd)
+__global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a, const GradArgs g, const RowTiling tiling, int splits, int most, bool by_xcd)
 {
     typedef Rows<D> R;
-    constexpr int kTile = kRowsOfTile * R::kBytes, kStage = 2 * kTile + 2 * kRowsOfTile * 4;
-    __shared__ __align__(1024) uint8_t lds[2][kStage];
+    constexpr int kTile = kRowsOfTile * R::kBytes, kStage = 2 * kTile + 2 * kRowsOfTile * 4, kStages = 3;
+    __shared__ __align__(1024) uint8_t lds[kStages][kStage];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place at = place(blockIdx.x, a.n_seqs * a.kv_heads, a.tiles * splits, by_xcd);
@@ -240,9 +268,10 @@ __global__ __launch_bounds__(256, D == 64 && !DROP ? 3 : 2) void attention_dkv_k
     const int back = a.tiles * splits - 1 - at.tile, tile = back / splits, part = back - tile * splits;
     const int first = tile * 128;
     if (first >= seg.nk) return;
-    const int rows = max(0, seg.nq) * a.group;
-    const int wave_first = first + wave * 32, key = wave_first + l32;
-    const int key_in = min(key, seg.nk - 1);
+    const RowTiles todo = row_tiles(a, tiling, seg, first, part, most);
+    if (part >= todo.parts) return;
+    const int begin = __builtin_amdgcn_readfirstlane(todo.begin), end = __builtin_amdgcn_readfirstlane(todo.end);
+    const int key = first + wave * 32 + l32, key_in = min(key, seg.nk - 1);
 
     v8s k[D / 16], v[D / 16];
     const uint16_t *const k_from = a.K + (int64_t)(seg.k0 + key_in) * a.k_row + (int64_t)kv * a.k_head + 8 * hf;
@@ -252,131 +281,199 @@ __global__ __launch_bounds__(256, D == 64 && !DROP ? 3 : 2) void attention_dkv_k
         k[d] = *reinterpret_cast<const v8s *>(k_from + 16 * d);
         v[d] = *reinterpret_cast<const v8s *>(v_from + 16 * d);
     }
-    const int from_row = first_row(a, seg, rows, key);
-    const int wave_from = __builtin_amdgcn_readfirstlane(first_row(a, seg, rows, wave_first)), wave_all = __builtin_amdgcn_readfirstlane(first_row(a, seg, rows, wave_first + 31));
-    const RowTiles todo = row_tiles(a, seg, rows, first, part, most);
-    if (part >= todo.parts) return;
-    const int begin = __builtin_amdgcn_readfirstlane(todo.begin), end = __builtin_amdgcn_readfirstlane(todo.end);
+    // causal: the key is seen from this token on; the wavefront's last key from wave_token on
+    const int from_token = a.causal ? key - (seg.nk - seg.nq) : INT32_MIN / 128;
+    const int wave_token = __builtin_amdgcn_readfirstlane(a.causal ? first + wave * 32 + 31 - (seg.nk - seg.nq) : INT32_MIN / 128);
 
     const uint32_t lds0 = lds_address(lds);
     const int64_t stats = (int64_t)a.total_q * a.heads;
-    // where the group divides a tile, a tile's rows lie at the same distances from its first token's whatever the tile
-    const int shift = __builtin_ctz(a.group);
-    const bool near = (a.group & (a.group - 1)) == 0 && a.group <= kRowsOfTile && near_rows(a.q_row) && near_rows(a.q_head) && (int64_t)a.heads * D < (1 << 23);
-    const auto token_in = [&](int r) { return (uint32_t)(r >> shift); };
-    const auto head_in = [&](int r) { return (uint32_t)(r & (a.group - 1)); };
-    const TileCopy<D, kRowsOfTile, 4> copy_q(wave, lane, [&](int r) { return token_in(r) * (uint32_t)a.q_row + head_in(r) * (uint32_t)a.q_head; }),
-        copy_d(wave, lane, [&](int r) { return (token_in(r) * (uint32_t)a.heads + head_in(r)) * D; });
-    const uint32_t stat_offset = (token_in(lane) * (uint32_t)a.heads + head_in(lane)) * 4;
-    const auto fetch = [&](int tile, int stage) {
+    const int head0 = kv * a.group, last_token = seg.nq - 1;
+    const bool near = near_rows(a.q_row) && near_rows(a.q_head) && (int64_t)a.heads * D < (1 << 23);
+    const auto token_in = [&](int r) { return r / tiling.heads; };
+    const auto head_in = [&](int r) { return r - r / tiling.heads * tiling.heads; };
+    const TileCopy<D, kRowsOfTile, 4> copy_q(wave, lane, [&](int r) { return (uint32_t)token_in(r) * (uint32_t)a.q_row + (uint32_t)head_in(r) * (uint32_t)a.q_head; }),
+        copy_d(wave, lane, [&](int r) { return (uint32_t)(token_in(r) * a.heads + head_in(r)) * D; });
+    const int stat_token = token_in(lane), stat_head = head_in(lane);  // of row `lane` of a tile
+    const auto place_of = [&](int tile, int &token, int &head) __attribute__((always_inline)) {       // first token and head of a tile
+        const int block = tiling.chunks == 1 ? tile : __builtin_amdgcn_readfirstlane(tile / tiling.chunks);
+        token = block * tiling.tokens;
+        head = (tile - block * tiling.chunks) * tiling.heads;
+    };
+    const auto fetch = [&](int tile, int stage) __attribute__((always_inline)) {
         const uint32_t to = lds0 + stage * kStage;
-        if (near && (tile + 1) * kRowsOfTile <= rows) {
-            const int64_t token = seg.q0 + (tile * kRowsOfTile >> shift), at_row = token * a.heads + kv * a.group;
-            copy_q.copy(a.Q + token * a.q_row + (int64_t)kv * a.group * a.q_head, to, wave);
+        int token, head;
+        place_of(tile, token, head);
+        if (near && token + kRowsOfTile / tiling.heads < seg.nq && head + tiling.heads <= a.group) {  // (a row that is none lies one token on)
+            const int64_t at = seg.q0 + token, at_row = at * a.heads + head0 + head;
+            copy_q.copy(a.Q + at * a.q_row + (int64_t)(head0 + head) * a.q_head, to, wave);
             copy_d.copy(g.dO + at_row * D, to + kTile, wave);
-            if (wave < 2) copy4(g.stat + wave * stats + at_row, stat_offset, to + 2 * kTile + wave * kRowsOfTile * 4);
-            return;
+        } else {
+            const auto row_of = [&](int r, int64_t &t, int64_t &h) {
+                t = seg.q0 + min(token + token_in(r), last_token);
+                h = head0 + min(head + head_in(r), a.group - 1);
+            };
+            copy_rows<D, kRowsOfTile, 4>(to, wave, lane, [&](int r) {
+                int64_t t, h;
+                row_of(r, t, h);
+                return a.Q + t * a.q_row + h * a.q_head;
+            });
+            copy_rows<D, kRowsOfTile, 4>(to + kTile, wave, lane, [&](int r) {
+                int64_t t, h;
+                row_of(r, t, h);
+                return g.dO + (t * a.heads + h) * D;
+            });
         }
-        const auto split = [&](int r, int &token, int &head) {  // rows past the end repeat the last one; their P is set to zero
-            r = min(tile * kRowsOfTile + r, rows - 1);
-            token = a.group == 1 ? r : (int)((unsigned)r / (unsigned)a.group);
-            head = kv * a.group + r - token * a.group;
-        };
-        copy_rows<D, kRowsOfTile, 4>(to, wave, lane, [&](int r) {
-            int token, head;
-            split(r, token, head);
-            return a.Q + (int64_t)(seg.q0 + token) * a.q_row + (int64_t)head * a.q_head;
-        });
-        copy_rows<D, kRowsOfTile, 4>(to + kTile, wave, lane, [&](int r) {
-            int token, head;
-            split(r, token, head);
-            return g.dO + ((int64_t)(seg.q0 + token) * a.heads + head) * D;
-        });
-        if (wave < 2) {
-            int token, head;
-            split(lane, token, head);
-            copy4(g.stat + wave * stats + (int64_t)(seg.q0 + token) * a.heads + head, to + 2 * kTile + wave * kRowsOfTile * 4);
+        if (wave < 2) {  // a row that is none takes the entry behind the last: P = 0
+            const bool row = stat_token < tiling.tokens && token + stat_token <= last_token && head + stat_head < a.group;
+            const int64_t at = row ? (int64_t)(seg.q0 + token + stat_token) * a.heads + head0 + head + stat_head : stats;
+            copy4(g.stat + wave * (stats + 1) + at, to + 2 * kTile + wave * kRowsOfTile * 4);
         }
     };
     const Threefry bits(DROP ? (uint64_t)*a.seed : 0);
     v16f dK[D / 32], dV[D / 32];
     clear(dK);
     clear(dV);
-    if (begin < end) fetch(begin, begin & 1);
-    for (int t = begin; t < end; ++t) {
-        wait_copies<0>();
+    const Operands<D> op(lane);
+    typedef const __attribute__((address_space(3))) v4f *lds_v4f;
+
+    // A block of 32 rows goes through three steps: its operands are read; scores and dP are formed; P, dS and their products.  The
+    // second step of a block runs next to the exponentials of the block before it, which do not depend on it: the matrix cores work
+    // on the one while the vector units work on the other.  (sched_barrier: the compiler keeps to the order written here.)
+    // The sums start from -lse / scale and -delta, as they lie in LDS: exp(S - lse) and dP - delta take a multiplication each.
+    const auto start = [&](uint32_t tq, int rb, v16f &p, v16f &ds) __attribute__((always_inline)) {
+        const uint32_t stat = tq + 2 * kTile + 4 * (32 * rb) + 16 * hf;
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const v4f x = *(lds_v4f)(stat + 8 * i);
+            v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
+            if constexpr (!DROP) y = *(lds_v4f)(stat + 4 * kRowsOfTile + 8 * i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                p[i + j] = x[j];
+                ds[i + j] = y[j];
+            }
+        }
+    };
+    constexpr int kBatch = 4;  // operands of a product that are read at a time
+    const auto read = [&](uint32_t tq, int rb, int d0, v8s (&x)[kBatch], v8s (&y)[kBatch]) {
+#pragma unroll
+        for (int d = 0; d < kBatch; ++d) x[d] = op.along(tq, 32 * rb, d0 + d);
+#pragma unroll
+        for (int d = 0; d < kBatch; ++d) y[d] = op.along(tq + kTile, 32 * rb, d0 + d);
+    };
+    const auto turn = [&](uint32_t tq, int rb, int h, v8s (&x)[D / 32], v8s (&y)[D / 32]) {
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            x[i] = op.across(tq + kTile, 32 * rb + 16 * h, i);
+            y[i] = op.across(tq, 32 * rb + 16 * h, i);
+        }
+    };
+    const auto hide = [&](int rb, int token, v16f &p) __attribute__((always_inline)) {
+        const int from = (from_token - token) * tiling.heads - 32 * rb - 4 * hf;  // (row r's token is at or behind x if r >= x * heads)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = 8 * (i >> 2) + (i & 3) >= from ? p[i] : -__builtin_inff();
+    };
+    // rows 8 * q + 4 * hf .. + 3 of a block: P and dS
+    v2u bits_of[4];
+    const auto draw = [&](int rb, int token, int head) __attribute__((always_inline)) {
+        // Four neighbouring lanes need the four draws of the same counters: each of them forms the counters of every fourth row,
+        // and they take each other's words.
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 32 * rb + 8 * i + 4 * hf + (lane & 3);
+            bits_of[i] = weight_draws(bits, seg.q0 + token + token_in(r), head0 + head + head_in(r), key);
+        }
+    };
+    const auto weights = [&](uint32_t tq, int rb, auto quarter, v16f &p, v16f &ds) __attribute__((always_inline)) {
+        constexpr int q4 = decltype(quarter)::value, i0 = 4 * q4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[i0 + j] = __builtin_amdgcn_exp2f(p[i0 + j] * a.c);
+        if constexpr (!DROP) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ds[i0 + j] *= p[i0 + j];
+        } else {
+            const v4f minus_delta = *(lds_v4f)(tq + 2 * kTile + 4 * (kRowsOfTile + 32 * rb + 8 * q4) + 16 * hf);
+            const auto take = [&](int j, uint32_t w0, uint32_t w1) {
+                const uint32_t word = (lane & 2) ? w1 : w0;
+                const bool in = ((lane & 1) ? word >> 16 : word & 0xFFFFu) >= a.threshold;
+                ds[i0 + j] = p[i0 + j] * ((in ? ds[i0 + j] * a.inv_share : 0.0f) + minus_delta[j]);
+                p[i0 + j] = in ? p[i0 + j] : 0.0f;
+            };
+            const v2u w = bits_of[q4];
+            take(0, of_four<0>(w[0]), of_four<0>(w[1]));
+            take(1, of_four<1>(w[0]), of_four<1>(w[1]));
+            take(2, of_four<2>(w[0]), of_four<2>(w[1]));
+            take(3, of_four<3>(w[0]), of_four<3>(w[1]));
+        }
+    };
+    // block (tq, rb), whose scores are in p, ds, next to the scores of block (tn, rn), into pn, dsn
+    const auto both = [&](uint32_t tq, int rb, v16f &p, v16f &ds, uint32_t tn, int rn, v16f &pn, v16f &dsn, int token, int head, auto masked) __attribute__((always_inline)) {
+        v8s x[kBatch], y[kBatch], tx[D / 32], ty[D / 32];
+        start(tn, rn, pn, dsn);
+        read(tn, rn, 0, x, y);
+        if constexpr (decltype(masked)::value) hide(rb, token, p);
+        if constexpr (DROP) draw(rb, token, head);
+        __builtin_amdgcn_sched_barrier(0);
+        each<D / 16>([&](auto number) {
+            constexpr int d = decltype(number)::value;
+            if constexpr (d > 0 && d % kBatch == 0) {
+                read(tn, rn, d, x, y);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            pn = T::mma32(x[d % kBatch], k[d], pn);
+            dsn = T::mma32(y[d % kBatch], v[d], dsn);
+            if constexpr (d % (D / 64) == 0) weights(tq, rb, std::integral_constant<int, d / (D / 64)>{}, p, ds);
+            if constexpr (d == D / 16 - 1) turn(tq, rb, 0, tx, ty);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const v8s pr = rounded<T>(p, h), dr = rounded<T>(ds, h);
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                dV[i] = T::mma32(tx[i], pr, dV[i]);
+                dK[i] = T::mma32(ty[i], dr, dK[i]);
+            }
+            if (h == 0) turn(tq, rb, 1, tx, ty);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (begin < end) fetch(begin, 0);
+    if (begin + 1 < end) fetch(begin + 1, 1);
+    v16f p[2], ds[2];
+    if (begin < end) {
+        if (begin + 1 < end) wait_copies<2 * decltype(copy_q)::N>();  // (the first tile's; the second's may be under way)
+        else wait_copies<0>();
         barrier();
-        if (t + 1 < end) fetch(t + 1, (t + 1) & 1);
-        const uint8_t *const tq = lds[t & 1], *const td = tq + kTile;
-        const float *const stat = reinterpret_cast<const float *>(td + kTile);
+        v8s x[kBatch], y[kBatch];
+        start(lds0, 0, p[0], ds[0]);
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb) {
-            const int row0 = t * kRowsOfTile + 32 * rb;
-            if (row0 + 32 <= wave_from || row0 >= rows) continue;  // none of these rows sees a key of the wavefront
-            const bool masked = row0 < wave_all || row0 + 32 > rows;
-            v16f s, dp;
+        for (int d0 = 0; d0 < D / 16; d0 += kBatch) {
+            read(lds0, 0, d0, x, y);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.0f;
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) s = T::mma32(R::along(tq, 32 * rb, d, lane), k[d], s);
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) dp = T::mma32(R::along(td, 32 * rb, d, lane), v[d], dp);
-            if (masked) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int r = row0 + 8 * (i >> 2) + 4 * hf + (i & 3);
-                    s[i] = r >= from_row && r < rows ? s[i] : -__builtin_inff();
-                }
-            }
-            v16f p;
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const v4f lse2 = *reinterpret_cast<const v4f *>(stat + 32 * rb + 2 * i + 4 * hf);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) p[i + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + j], a.c, -lse2[j]));
-            }
-            v16f pm = p;
-            if constexpr (DROP) {
-                // Four neighbouring lanes need the four draws of the same counters: each of them forms the counters of every
-                // fourth row, and they take each other's words.
-                v2u w[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = min(row0 + 8 * i + 4 * hf + (lane & 3), rows - 1);
-                    const int token = a.group == 1 ? r : (int)((unsigned)r / (unsigned)a.group);
-                    w[i] = weight_draws(bits, seg.q0 + token, kv * a.group + r - token * a.group, key);
-                }
-                const auto take = [&](int i, uint32_t w0, uint32_t w1) {
-                    const uint32_t word = (lane & 2) ? w1 : w0;
-                    const bool kept = ((lane & 1) ? word >> 16 : word & 0xFFFFu) >= a.threshold;
-                    pm[i] = kept ? p[i] : 0.0f;
-                    dp[i] = kept ? dp[i] * a.inv_share : 0.0f;
-                };
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    take(4 * i, of_four<0>(w[i][0]), of_four<0>(w[i][1]));
-                    take(4 * i + 1, of_four<1>(w[i][0]), of_four<1>(w[i][1]));
-                    take(4 * i + 2, of_four<2>(w[i][0]), of_four<2>(w[i][1]));
-                    take(4 * i + 3, of_four<3>(w[i][0]), of_four<3>(w[i][1]));
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const v4f delta = *reinterpret_cast<const v4f *>(stat + kRowsOfTile + 32 * rb + 2 * i + 4 * hf);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) dp[i + j] = p[i + j] * (dp[i + j] - delta[j]);
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const v8s pr = rounded<T>(pm, h), ds = rounded<T>(dp, h);
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i) {
-                    dV[i] = T::mma32(R::across(td, 32 * rb + 16 * h, 32 * i, lane), pr, dV[i]);
-                    dK[i] = T::mma32(R::across(tq, 32 * rb + 16 * h, 32 * i, lane), ds, dK[i]);
-                }
+            for (int d = 0; d < kBatch; ++d) {
+                p[0] = T::mma32(x[d], k[d0 + d], p[0]);
+                ds[0] = T::mma32(y[d], v[d0 + d], ds[0]);
             }
         }
     }
+    int t = begin, stage = 0, token, head;
+    place_of(t, token, head);
+    const auto step = [&](auto masked) __attribute__((always_inline)) {
+        const int next = stage == kStages - 1 ? 0 : stage + 1;
+        const uint32_t tq = lds0 + stage * kStage, tn = lds0 + next * kStage;
+        both(tq, 0, p[0], ds[0], tq, 1, p[1], ds[1], token, head, masked);
+        wait_copies<0>();
+        barrier();  // the next tile has come, and everyone is done with the last one
+        if (t + 2 < end) fetch(t + 2, next == kStages - 1 ? 0 : next + 1);
+        both(tq, 1, p[1], ds[1], tn, 0, p[0], ds[0], token, head, masked);  // (past the last tile: scores of what lies there, unused)
+        stage = next;
+        place_of(++t, token, head);
+    };
+    // (causal: the tiles that some key of the wavefront is hidden from come first; two loops, for with both kinds in one the
+    // compiler keeps the sums twice)
+    while (t < end && token < wave_token) step(std::true_type{});
+    while (t < end) step(std::false_type{});
     if (key >= seg.nk) return;
     if (todo.parts > 1) {
         float *const to = g.part + ((int64_t)((at.pair * (int64_t)a.tiles + tile) * splits + part) * 128 + key - first) * (2 * D);
@@ -395,7 +492,7 @@ __global__ __launch_bounds__(256, D == 64 && !DROP ? 3 : 2) void attention_dkv_k
 
 // dK and dV of 16 keys from their parts; a thread does eight neighbouring values
 template <typename T, int D>
-__global__ __launch_bounds__(256) void attention_dkv_join_kernel(const AttnArgs a, const GradArgs g, int splits, int most, float inv_share)
+__global__ __launch_bounds__(256) void attention_dkv_join_kernel(const AttnArgs a, const GradArgs g, const RowTiling tiling, int splits, int most, float inv_share)
 {
     constexpr int kEach = 2 * D / 8;  // threads to a key
     const int pair = blockIdx.x / (a.tiles * (128 * kEach / 256)), in_pair = blockIdx.x - pair * (a.tiles * (128 * kEach / 256));
@@ -403,10 +500,10 @@ __global__ __launch_bounds__(256) void attention_dkv_join_kernel(const AttnArgs 
     const int b = pair / a.kv_heads, kv = pair - b * a.kv_heads;
     const Segment seg = segment(a, b);
     if (key >= seg.nk) return;
-    const int rows = max(0, seg.nq) * a.group, tile = key / 128;
+    const int tile = key / 128;
     const float *const from = g.part + ((int64_t)(pair * (int64_t)a.tiles + tile) * splits * 128 + key % 128) * (2 * D) + d;
     v4f x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-    const int parts = min(splits, row_tiles(a, seg, rows, tile * 128, 0, most).parts);
+    const int parts = min(splits, row_tiles(a, tiling, seg, tile * 128, 0, most).parts);
     if (parts == 1) return;  // (written whole)
 #pragma unroll 4
     for (int p = 0; p < parts; ++p) {
@@ -427,11 +524,12 @@ struct Parts {
 };
 inline Parts row_parts(int64_t pairs, int64_t max_q, int64_t group, int64_t max_k, bool causal)
 {
-    const int64_t tiles = pairs * ((max_k + 127) / 128), rows = (max_q * group + kRowsOfTile - 1) / kRowsOfTile;
+    const RowTiling t = row_tiling((int)group);
+    const int64_t tiles = pairs * ((max_k + 127) / 128), rows = (max_q + t.tokens - 1) / t.tokens * t.chunks;
     const int64_t most = std::max<int64_t>(8, tiles * rows / (causal ? 2 : 1) / kParts);
     return {most, std::max<int64_t>(1, (rows + most - 1) / most)};
 }
-inline size_t stat_bytes(const qb_attention *p) { return ((size_t)p->total_q * p->heads * 8 + 255) / 256 * 256; }
+inline size_t stat_bytes(const qb_attention *p) { return ((size_t)(p->total_q * p->heads + 1) * 8 + 255) / 256 * 256; }
 
 template <typename T, int D>
 qb_status backward(AttnArgs a, const GradArgs &g, int64_t max_q, int64_t max_k, bool drop, hipStream_t stream)
@@ -454,9 +552,9 @@ qb_status backward(AttnArgs a, const GradArgs &g, int64_t max_q, int64_t max_k, 
         const Parts parts = row_parts(pairs, max_q, a.group, max_k, a.causal);
         const int splits = (int)parts.splits, most = (int)parts.most;
         const int64_t grid = dealt_workgroups(pairs, (int64_t)a.tiles * splits);
-        if (drop) attention_dkv_kernel<T, D, true><<<(int)grid, 256, 0, stream>>>(a, g, splits, most, by_xcd);
-        else attention_dkv_kernel<T, D, false><<<(int)grid, 256, 0, stream>>>(a, g, splits, most, by_xcd);
-        if (splits > 1) attention_dkv_join_kernel<T, D><<<(int)(pairs * a.tiles * (128 * 2 * D / 8 / 256)), 256, 0, stream>>>(a, g, splits, most, drop ? a.inv_share : 1.0f);
+        if (drop) attention_dkv_kernel<T, D, true><<<(int)grid, 256, 0, stream>>>(a, g, row_tiling(a.group), splits, most, by_xcd);
+        else attention_dkv_kernel<T, D, false><<<(int)grid, 256, 0, stream>>>(a, g, row_tiling(a.group), splits, most, by_xcd);
+        if (splits > 1) attention_dkv_join_kernel<T, D><<<(int)(pairs * a.tiles * (128 * 2 * D / 8 / 256)), 256, 0, stream>>>(a, g, row_tiling(a.group), splits, most, drop ? a.inv_share : 1.0f);
     }
     return launch_status();
 }

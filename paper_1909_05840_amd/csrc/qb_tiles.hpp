@@ -40,6 +40,16 @@ struct Fp16 {
     static __device__ __forceinline__ float hi(uint32_t w) { return (float)__builtin_bit_cast(v2, w)[1]; }
 };
 
+// f(0), .., f(N - 1) with the number as a constant (vector elements whose number is one only after unrolling end up in memory)
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void each(const F &f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        each<N, I + 1>(f);
+    }
+}
+
 template <int N>
 __device__ __forceinline__ void wait_copies()  // until at most N of this wavefront's vector memory operations are under way
 {
@@ -62,7 +72,9 @@ __device__ __forceinline__ void copy16(const void *from, uint32_t lds)
 // the same with the address as a base that the wavefront shares and an offset in bytes
 __device__ __forceinline__ void copy16(const void *base, uint32_t offset, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory", "m0");
+    const uint64_t at = reinterpret_cast<uint64_t>(base);  // (a quotient of uniform values lies in a vector register)
+    const uint64_t uniform = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)) << 32;
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(uniform), "s"(lds) : "memory", "m0");
 }
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p; }
 
@@ -82,20 +94,36 @@ struct Rows {
     // which row of a copy's rows, and which chunk of the row in memory, the lane fetches (row0: first row of the copy)
     static __device__ __forceinline__ int copy_row(int lane) { return lane / kChunks; }
     static __device__ __forceinline__ int copy_chunk(int row, int lane) { return (lane % kChunks) ^ key(row); }
-    // Operand with the contraction along the rows, 32 x 16: the lane's row (lane % 32 of `row0`), values 16 * c + 8 * (lane / 32) ..
-    static __device__ __forceinline__ v8s along(const uint8_t *tile, int row0, int c, int lane)
+};
+
+// Operands out of such tiles.  The lane's places in a tile are formed once; rows further on by a multiple of 32 (16) are an offset in the instruction.
+template <int D>
+struct Operands {
+    typedef Rows<D> R;
+    uint32_t along_at[D / 16], across_at[D / 32][2];
+    __device__ __forceinline__ explicit Operands(int lane)
     {
-        return *reinterpret_cast<const v8s *>(tile + at(row0 + (lane & 31), 2 * c + (lane >> 5)));
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) along_at[c] = R::at(lane & 31, 2 * c + (lane >> 5));
+        const int row = 4 * (lane >> 5) + ((lane >> 2) & 3), col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int part = 0; part < 2; ++part) across_at[i][part] = R::at(row + 8 * part, (32 * i + col) >> 3) + 2 * (col & 7);
     }
-    // Operand with the contraction across the rows, 32 x 16: the lane's column is col0 + lane % 32, its eight values are rows
-    // row0 + 4 * (lane / 32) + 0..3 and 8 further on: the order in which a product's result holds its rows.  The transposing read
-    // hands lane i of sixteen the four rows of column i; lane i points at row i / 4, columns 4 * (i % 4)..
-    static __device__ __forceinline__ v8s across(const uint8_t *tile, int row0, int col0, int lane)
+    // Contraction along the rows, 32 x 16: the lane's row (lane % 32 of `row0`), values 16 * c + 8 * (lane / 32) ..
+    __device__ __forceinline__ v8s along(uint32_t tile, int row0, int c) const
+    {
+        return *(const __attribute__((address_space(3))) v8s *)(tile + along_at[c] + row0 * R::kBytes);
+    }
+    // Contraction across the rows, 32 x 16: the lane's column is 32 * i + lane % 32, its eight values are rows row0 + 4 * (lane / 32) + 0..3
+    // and 8 further on: the order in which a product's result holds its rows.  The transposing read hands lane i of sixteen the
+    // four rows of column i; lane i points at row i / 4, columns 4 * (i % 4)..
+    __device__ __forceinline__ v8s across(uint32_t tile, int row0, int i) const
     {
         typedef __attribute__((address_space(3))) v4s *turned;
-        const int row = row0 + 4 * (lane >> 5) + ((lane >> 2) & 3), col = col0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-        const uint8_t *first = tile + at(row, col >> 3) + 2 * (col & 7), *second = tile + at(row + 8, col >> 3) + 2 * (col & 7);
-        const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((turned)first), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((turned)second);
+        const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((turned)(tile + across_at[i][0] + row0 * R::kBytes));
+        const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((turned)(tile + across_at[i][1] + row0 * R::kBytes));
         return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     }
 };

@@ -135,7 +135,7 @@ template <bool ACROSS>
 __device__ __forceinline__ v8s operand(const uint8_t *tile, int result, int sub, int lane)
 {
     if constexpr (ACROSS) return across_in_order(tile + (result >> 6) * 8192, 16 * sub, result & 63, lane);
-    else return Rows<64>::along(tile, result, sub, lane);
+    else return *reinterpret_cast<const v8s *>(tile + Rows<64>::at(result + (lane & 31), 2 * sub + (lane >> 5)));
 }
 
 // acc += A B^T over steps [s0, s1); row_a(r, s) is the address of LDS row r of step s: of result r (along), or for r = 64 * block + k of
