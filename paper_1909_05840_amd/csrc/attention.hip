@@ -241,7 +241,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uin
         copy_rows<D, kKeys, 4>(to + kTile, wave, lane, [&](int r) { return V + (int64_t)min(tile * kKeys + r, seg.nk - 1) * a.v_row; });
     };
     const Threefry bits(DROP ? (uint64_t)*a.seed : 0);
-    const Operands<D> op(lane);
+    const Operands<D> op(lane, lds0);
     Softmax<D> x;
     x.clear();
     if (tiles) fetch(0, 0);
@@ -250,7 +250,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uin
         barrier();
         if (t + 1 < tiles) fetch(t + 1, (t + 1) & 1);
         if (t * kKeys < wave_most)
-            attend<T, D, DROP>(x, q, op, lds0 + (t & 1) * 2 * kTile, lds0 + (t & 1) * 2 * kTile + kTile, t * kKeys, limit, (t + 1) * kKeys > wave_least, a.c, bits, a.threshold, row_q, head, lane);
+            attend<T, D, DROP>(x, q, op, (t & 1) * 2 * kTile, (t & 1) * 2 * kTile + kTile, t * kKeys, limit, (t + 1) * kKeys > wave_least, a.c, bits, a.threshold, row_q, head, lane);
     }
     if (row >= rows) return;
     const float l = halves_sum(x.l);
@@ -297,7 +297,7 @@ __global__ __launch_bounds__(256, 1) void attention_cache_kernel(const AttnArgs 
         copy_rows<D, kTileKeys, 1>(to, 0, lane, [&](int r) { return K + (int64_t)min(key0 + r, seg.nk - 1) * a.k_row; });
         copy_rows<D, kTileKeys, 1>(to + kTile, 0, lane, [&](int r) { return V + (int64_t)min(key0 + r, seg.nk - 1) * a.v_row; });
     };
-    const Operands<D> op(lane);
+    const Operands<D> op(lane, lds0);
     Softmax<D> x;
     x.clear();
     const int step = 4 * kTileKeys, mine = begin + wave * kTileKeys;
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(256, 1) void attention_cache_kernel(const AttnArgs 
             wait_copies<0>();
         }
         asm volatile("" ::: "memory");
-        attend<T, D, false, KB>(x, q, op, lds0 + stage * 2 * kTile, lds0 + stage * 2 * kTile + kTile, key0, limit, key0 + kTileKeys > least, a.c, bits, 0, row_q, head, lane);
+        attend<T, D, false, KB>(x, q, op, stage * 2 * kTile, stage * 2 * kTile + kTile, key0, limit, key0 + kTileKeys > least, a.c, bits, 0, row_q, head, lane);
         __builtin_amdgcn_s_waitcnt(0xC07F);  // this stage's reads have returned before the next copies into it
         asm volatile("" ::: "memory");
     }

@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
         copy_rows<D, kKeys, 4>(to + kTile, wave, lane, [&](int r) { return V + (int64_t)min(tile * kKeys + r, seg.nk - 1) * a.v_row; });
     };
     const Threefry bits(DROP ? (uint64_t)*a.seed : 0);
-    const Operands<D> op(lane);
+    const Operands<D> op(lane, lds0);
     v16f A[D / 32], B[EXACT ? D / 32 : 1];
     clear(A);
     clear(B);
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
         barrier();
         if (t + 1 < tiles) fetch(t + 1, (t + 1) & 1);
         if (t * kKeys >= wave_most) continue;
-        const uint32_t tk = lds0 + (t & 1) * 2 * kTile, tv = tk + kTile;
+        const uint32_t tk = (t & 1) * 2 * kTile, tv = tk + kTile;
         const bool masked = (t + 1) * kKeys > wave_least;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
@@ -236,8 +236,9 @@ inline RowTiling row_tiling(int group)
     const int heads = group < kRowsOfTile ? group : kRowsOfTile;
     return {heads, kRowsOfTile / heads, (group + heads - 1) / heads};
 }
-// The tiles that a tile of 128 keys is seen by are cut into parts of about the same number, at most `most` of them to a part
-// (with causal masks the first keys are seen by many more rows than the last).
+// The tiles that a tile of 128 keys is seen by are cut into parts of `most` tiles, from the last row on (with causal masks the first keys
+// are seen by many more rows than the last, but all by the last rows): part p of every tile of keys is the same rows, and the
+// workgroups that are at work together, which take the parts in turn, find them in their L2.
 struct RowTiles {
     int begin, end, parts;
 };
@@ -245,8 +246,8 @@ __device__ __forceinline__ RowTiles row_tiles(const AttnArgs &a, const RowTiling
 {
     const int nq = max(0, seg.nq), token = a.causal ? min(nq, max(0, first_key - (seg.nk - seg.nq))) : 0;  // causal: key <= token + nk - nq
     const int all = (nq + r.tokens - 1) / r.tokens, first = token < nq ? token / r.tokens : all;
-    const int n = (all - first) * r.chunks, parts = max(1, (n + most - 1) / most);
-    return {first * r.chunks + (int)((int64_t)n * part / parts), first * r.chunks + (int)((int64_t)n * (part + 1) / parts), parts};
+    const int n = (all - first) * r.chunks, end = all * r.chunks - part * most;
+    return {max(first * r.chunks, end - most), end, max(1, (n + most - 1) / most)};
 }
 
 // dK and dV; 128 keys to a workgroup, 32 to a wavefront: a lane's results all of one key.  Where tiles of keys are few, a workgroup does
@@ -264,9 +265,8 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
     if (at.pair >= a.n_seqs * a.kv_heads) return;
     const int b = at.pair / a.kv_heads, kv = at.pair - b * a.kv_heads;
     const Segment seg = segment(a, b);
-    // `splits`: the most parts that a tile of keys has (the first keys are seen by the most rows: they come first)
-    const int back = a.tiles * splits - 1 - at.tile, tile = back / splits, part = back - tile * splits;
-    const int first = tile * 128;
+    const int rank = a.tiles * splits - 1 - at.tile, part = rank / a.tiles, key_tile = rank - part * a.tiles;  // part after part
+    const int first = key_tile * 128;
     if (first >= seg.nk) return;
     const RowTiles todo = row_tiles(a, tiling, seg, first, part, most);
     if (part >= todo.parts) return;
@@ -333,15 +333,17 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
     v16f dK[D / 32], dV[D / 32];
     clear(dK);
     clear(dV);
-    const Operands<D> op(lane);
+    const Operands<D> op(lane, lds0);
     typedef const __attribute__((address_space(3))) v4f *lds_v4f;
+    const uint32_t stat_at = lds0 + 2 * kTile + 16 * hf;
 
     // A block of 32 rows goes through three steps: its operands are read; scores and dP are formed; P, dS and their products.  The
-    // second step of a block runs next to the exponentials of the block before it, which do not depend on it: the matrix cores work
-    // on the one while the vector units work on the other.  (sched_barrier: the compiler keeps to the order written here.)
+    // second step of a block runs next to the exponentials of the block before it, the first next to that one's products: the matrix
+    // cores work on the one while the vector units and the LDS work on the other.  (sched_barrier: the compiler keeps to the order
+    // written here.)  The stage is a constant of the code, and with it every place in LDS.
     // The sums start from -lse / scale and -delta, as they lie in LDS: exp(S - lse) and dP - delta take a multiplication each.
     const auto start = [&](uint32_t tq, int rb, v16f &p, v16f &ds) __attribute__((always_inline)) {
-        const uint32_t stat = tq + 2 * kTile + 4 * (32 * rb) + 16 * hf;
+        const uint32_t stat = stat_at + tq + 4 * (32 * rb);
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const v4f x = *(lds_v4f)(stat + 8 * i);
@@ -354,12 +356,10 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
             }
         }
     };
-    constexpr int kBatch = 4;  // operands of a product that are read at a time
-    const auto read = [&](uint32_t tq, int rb, int d0, v8s (&x)[kBatch], v8s (&y)[kBatch]) {
-#pragma unroll
-        for (int d = 0; d < kBatch; ++d) x[d] = op.along(tq, 32 * rb, d0 + d);
-#pragma unroll
-        for (int d = 0; d < kBatch; ++d) y[d] = op.along(tq + kTile, 32 * rb, d0 + d);
+    constexpr int kAhead = 2;  // operands that are read ahead of their products
+    const auto read = [&](uint32_t tq, int rb, int d, v8s &x, v8s &y) __attribute__((always_inline)) {
+        x = op.along(tq, 32 * rb, d);
+        y = op.along(tq + kTile, 32 * rb, d);
     };
     const auto turn = [&](uint32_t tq, int rb, int h, v8s (&x)[D / 32], v8s (&y)[D / 32]) {
 #pragma unroll
@@ -392,7 +392,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
 #pragma unroll
             for (int j = 0; j < 4; ++j) ds[i0 + j] *= p[i0 + j];
         } else {
-            const v4f minus_delta = *(lds_v4f)(tq + 2 * kTile + 4 * (kRowsOfTile + 32 * rb + 8 * q4) + 16 * hf);
+            const v4f minus_delta = *(lds_v4f)(stat_at + tq + 4 * (kRowsOfTile + 32 * rb + 8 * q4));
             const auto take = [&](int j, uint32_t w0, uint32_t w1) {
                 const uint32_t word = (lane & 2) ? w1 : w0;
                 const bool in = ((lane & 1) ? word >> 16 : word & 0xFFFFu) >= a.threshold;
@@ -406,77 +406,89 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
             take(3, of_four<3>(w[0]), of_four<3>(w[1]));
         }
     };
-    // block (tq, rb), whose scores are in p, ds, next to the scores of block (tn, rn), into pn, dsn
-    const auto both = [&](uint32_t tq, int rb, v16f &p, v16f &ds, uint32_t tn, int rn, v16f &pn, v16f &dsn, int token, int head, auto masked) __attribute__((always_inline)) {
-        v8s x[kBatch], y[kBatch], tx[D / 32], ty[D / 32];
-        start(tn, rn, pn, dsn);
-        read(tn, rn, 0, x, y);
-        if constexpr (decltype(masked)::value) hide(rb, token, p);
+    v16f p[2], ds[2];
+    v8s x[kAhead], y[kAhead], tx[D / 32], ty[D / 32];
+    int t = begin, token, head;
+    // block rb of the tile at tq, whose scores are in p[rb] and ds[rb], next to the scores of the other block, whose operands are in x and y
+    const auto exponentials = [&](uint32_t tq, auto block, uint32_t tn) __attribute__((always_inline)) {
+        constexpr int rb = decltype(block)::value;
+        int hidden = wave_token;
+        asm volatile("" : "+s"(hidden));  // (or the compiler makes two copies of all that follows, for the tiles with and those without)
+        if (token < hidden) hide(rb, token, p[rb]);
         if constexpr (DROP) draw(rb, token, head);
         __builtin_amdgcn_sched_barrier(0);
-        each<D / 16>([&](auto number) {
+        each<D / 16>([&](auto number) __attribute__((always_inline)) {
             constexpr int d = decltype(number)::value;
-            if constexpr (d > 0 && d % kBatch == 0) {
-                read(tn, rn, d, x, y);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            pn = T::mma32(x[d % kBatch], k[d], pn);
-            dsn = T::mma32(y[d % kBatch], v[d], dsn);
-            if constexpr (d % (D / 64) == 0) weights(tq, rb, std::integral_constant<int, d / (D / 64)>{}, p, ds);
+            p[1 - rb] = T::mma32(x[d % kAhead], k[d], p[1 - rb]);
+            ds[1 - rb] = T::mma32(y[d % kAhead], v[d], ds[1 - rb]);
+            if constexpr (d + kAhead < D / 16) read(tn, 1 - rb, d + kAhead, x[d % kAhead], y[d % kAhead]);
+            if constexpr (d % (D / 64) == 0) weights(tq, rb, std::integral_constant<int, d / (D / 64)>{}, p[rb], ds[rb]);
             if constexpr (d == D / 16 - 1) turn(tq, rb, 0, tx, ty);
             __builtin_amdgcn_sched_barrier(0);
         });
+    };
+    // its products; meanwhile the operands of block rn of the tile at tn are read
+    const auto products = [&](uint32_t tq, auto block, uint32_t tn, const auto &in_between) __attribute__((always_inline)) {
+        constexpr int rb = decltype(block)::value;
+        v8s pr[2] = {rounded<T>(p[rb], 0), rounded<T>(p[rb], 1)}, dr[2] = {rounded<T>(ds[rb], 0), rounded<T>(ds[rb], 1)};
+        asm volatile("" : "+v"(pr[0]), "+v"(pr[1]), "+v"(dr[0]), "+v"(dr[1]));  // (formed here, and not moved behind the branch below)
+        in_between();
+        __builtin_amdgcn_sched_barrier(0);
+        start(tn, rb, p[rb], ds[rb]);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const v8s pr = rounded<T>(p, h), dr = rounded<T>(ds, h);
+        for (int d = 0; d < kAhead; ++d) read(tn, rb, d, x[d], y[d]);
+        each<2>([&](auto half) __attribute__((always_inline)) {
+            constexpr int h = decltype(half)::value;
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) {
-                dV[i] = T::mma32(tx[i], pr, dV[i]);
-                dK[i] = T::mma32(ty[i], dr, dK[i]);
+                dV[i] = T::mma32(tx[i], pr[h], dV[i]);
+                dK[i] = T::mma32(ty[i], dr[h], dK[i]);
             }
-            if (h == 0) turn(tq, rb, 1, tx, ty);
-        }
+            if constexpr (h == 0) turn(tq, rb, 1, tx, ty);
+        });
         __builtin_amdgcn_sched_barrier(0);
     };
-    if (begin < end) fetch(begin, 0);
-    if (begin + 1 < end) fetch(begin + 1, 1);
-    v16f p[2], ds[2];
-    if (begin < end) {
-        if (begin + 1 < end) wait_copies<2 * decltype(copy_q)::N>();  // (the first tile's; the second's may be under way)
-        else wait_copies<0>();
-        barrier();
-        v8s x[kBatch], y[kBatch];
-        start(lds0, 0, p[0], ds[0]);
-#pragma unroll
-        for (int d0 = 0; d0 < D / 16; d0 += kBatch) {
-            read(lds0, 0, d0, x, y);
-#pragma unroll
-            for (int d = 0; d < kBatch; ++d) {
-                p[0] = T::mma32(x[d], k[d0 + d], p[0]);
-                ds[0] = T::mma32(y[d], v[d0 + d], ds[0]);
-            }
-        }
-    }
-    int t = begin, stage = 0, token, head;
     place_of(t, token, head);
-    const auto step = [&](auto masked) __attribute__((always_inline)) {
+    if (begin < end) {
+        fetch(begin, 0);
+        if (begin + 1 < end) {
+            fetch(begin + 1, 1);
+            wait_copies<2 * decltype(copy_q)::N>();  // (the first tile's; the second's may be under way)
+        } else {
+            wait_copies<0>();
+        }
+        barrier();
+        start(0, 0, p[0], ds[0]);
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) {
+            read(0, 0, d, x[0], y[0]);
+            p[0] = T::mma32(x[0], k[d], p[0]);
+            ds[0] = T::mma32(y[0], v[d], ds[0]);
+        }
+        start(0, 1, p[1], ds[1]);
+#pragma unroll
+        for (int d = 0; d < kAhead; ++d) read(0, 1, d, x[d], y[d]);
+    }
+    int stage = 0;
+    while (t < end) {
         const int next = stage == kStages - 1 ? 0 : stage + 1;
-        const uint32_t tq = lds0 + stage * kStage, tn = lds0 + next * kStage;
-        both(tq, 0, p[0], ds[0], tq, 1, p[1], ds[1], token, head, masked);
-        wait_copies<0>();
-        barrier();  // the next tile has come, and everyone is done with the last one
-        if (t + 2 < end) fetch(t + 2, next == kStages - 1 ? 0 : next + 1);
-        both(tq, 1, p[1], ds[1], tn, 0, p[0], ds[0], token, head, masked);  // (past the last tile: scores of what lies there, unused)
-        stage = next;
+        const uint32_t tq = stage * kStage, tn = next * kStage;
+        const std::integral_constant<int, 0> upper;
+        const std::integral_constant<int, 1> lower;
+        exponentials(tq, upper, tq);
+        products(tq, upper, tn, [&]() __attribute__((always_inline)) {
+            wait_copies<0>();
+            barrier();  // the next tile has come, and everyone is done with the last one
+            if (t + 2 < end) fetch(t + 2, next == kStages - 1 ? 0 : next + 1);
+        });
+        exponentials(tq, lower, tn);
+        products(tq, lower, tn, []() {});  // (past the last tile: scores of what lies there, unused)
         place_of(++t, token, head);
-    };
-    // (causal: the tiles that some key of the wavefront is hidden from come first; two loops, for with both kinds in one the
-    // compiler keeps the sums twice)
-    while (t < end && token < wave_token) step(std::true_type{});
-    while (t < end) step(std::false_type{});
+        stage = next;
+    }
     if (key >= seg.nk) return;
     if (todo.parts > 1) {
-        float *const to = g.part + ((int64_t)((at.pair * (int64_t)a.tiles + tile) * splits + part) * 128 + key - first) * (2 * D);
+        float *const to = g.part + ((int64_t)((at.pair * (int64_t)a.tiles + key_tile) * splits + part) * 128 + key - first) * (2 * D);
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll

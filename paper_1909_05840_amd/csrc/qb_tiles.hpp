@@ -101,15 +101,16 @@ template <int D>
 struct Operands {
     typedef Rows<D> R;
     uint32_t along_at[D / 16], across_at[D / 32][2];
-    __device__ __forceinline__ explicit Operands(int lane)
+    // base: the tiles' place in LDS
+    __device__ __forceinline__ Operands(int lane, uint32_t base)
     {
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) along_at[c] = R::at(lane & 31, 2 * c + (lane >> 5));
+        for (int c = 0; c < D / 16; ++c) along_at[c] = base + R::at(lane & 31, 2 * c + (lane >> 5));
         const int row = 4 * (lane >> 5) + ((lane >> 2) & 3), col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-            for (int part = 0; part < 2; ++part) across_at[i][part] = R::at(row + 8 * part, (32 * i + col) >> 3) + 2 * (col & 7);
+            for (int part = 0; part < 2; ++part) across_at[i][part] = base + R::at(row + 8 * part, (32 * i + col) >> 3) + 2 * (col & 7);
     }
     // Contraction along the rows, 32 x 16: the lane's row (lane % 32 of `row0`), values 16 * c + 8 * (lane / 32) ..
     __device__ __forceinline__ v8s along(uint32_t tile, int row0, int c) const
