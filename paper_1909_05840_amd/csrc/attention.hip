@@ -220,7 +220,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uin
     const auto token_of = [&](int r) { return min(r / a.group, seg.nq - 1); };
     const int limit = sees(token);
     const int wave_least = __builtin_amdgcn_readfirstlane(sees(token_of(first + wave * 32)));
-    const int wave_most = __builtin_amdgcn_readfirstlane(sees(token_of(first + wave * 32 + 31)));
+    const int wave_most = first + wave * 32 < rows ? __builtin_amdgcn_readfirstlane(sees(token_of(first + wave * 32 + 31))) : 0;  // (a wavefront without rows only copies)
     const int most = __builtin_amdgcn_readfirstlane(sees(token_of(first + 127)));
     const int tiles = (most + kKeys - 1) / kKeys;
 
@@ -249,8 +249,11 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uin
         wait_copies<0>();
         barrier();
         if (t + 1 < tiles) fetch(t + 1, (t + 1) & 1);
-        if (t * kKeys < wave_most)
-            attend<T, D, DROP>(x, q, op, (t & 1) * 2 * kTile, (t & 1) * 2 * kTile + kTile, t * kKeys, limit, (t + 1) * kKeys > wave_least, a.c, bits, a.threshold, row_q, head, lane);
+        const int left = wave_most - t * kKeys;
+        const uint32_t tk = (t & 1) * 2 * kTile;
+        constexpr bool kHalves = D == 64 || !DROP;  // (else there are no registers left for both)
+        if (left > (kHalves ? 32 : 0)) attend<T, D, DROP>(x, q, op, tk, tk + kTile, t * kKeys, limit, (t + 1) * kKeys > wave_least, a.c, bits, a.threshold, row_q, head, lane);
+        else if (kHalves && left > 0) attend<T, D, DROP, 1>(x, q, op, tk, tk + kTile, t * kKeys, limit, t * kKeys + 32 > wave_least, a.c, bits, a.threshold, row_q, head, lane);
     }
     if (row >= rows) return;
     const float l = halves_sum(x.l);

@@ -101,7 +101,7 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
     const auto token_of = [&](int r) { return min(r / a.group, seg.nq - 1); };
     const int limit = sees(token);
     const int wave_least = __builtin_amdgcn_readfirstlane(sees(token_of(first + wave * 32)));
-    const int wave_most = __builtin_amdgcn_readfirstlane(sees(token_of(first + wave * 32 + 31)));
+    const int wave_most = first + wave * 32 < rows ? __builtin_amdgcn_readfirstlane(sees(token_of(first + wave * 32 + 31))) : 0;  // (a wavefront without rows only copies)
     const int most = __builtin_amdgcn_readfirstlane(sees(token_of(first + 127)));
     if (EXACT != (most <= kExactKeys)) return;
     const int tiles = (most + kKeys - 1) / kKeys;
@@ -137,6 +137,7 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
         const bool masked = (t + 1) * kKeys > wave_least;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
+            if (kb == 1 && t * kKeys + 32 >= wave_most) break;
             // (all operands are read in front of their products, those turned for the last one in front of the exponentials)
             v16f s, dp;
             {
@@ -469,18 +470,26 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
 #pragma unroll
         for (int d = 0; d < kAhead; ++d) read(0, 1, d, x[d], y[d]);
     }
+    const auto turn_over = [&](int next) __attribute__((always_inline)) {
+        wait_copies<0>();
+        barrier();  // the next tile has come, and everyone is done with the last one
+        if (t + 2 < end) fetch(t + 2, next == kStages - 1 ? 0 : next + 1);
+    };
     int stage = 0;
+    if (first + wave * 32 >= seg.nk) {  // a wavefront without keys only copies
+        for (; t < end; ++t) {
+            stage = stage == kStages - 1 ? 0 : stage + 1;
+            turn_over(stage);
+        }
+        return;
+    }
     while (t < end) {
         const int next = stage == kStages - 1 ? 0 : stage + 1;
         const uint32_t tq = stage * kStage, tn = next * kStage;
         const std::integral_constant<int, 0> upper;
         const std::integral_constant<int, 1> lower;
         exponentials(tq, upper, tq);
-        products(tq, upper, tn, [&]() __attribute__((always_inline)) {
-            wait_copies<0>();
-            barrier();  // the next tile has come, and everyone is done with the last one
-            if (t + 2 < end) fetch(t + 2, next == kStages - 1 ? 0 : next + 1);
-        });
+        products(tq, upper, tn, [&]() __attribute__((always_inline)) { turn_over(next); });
         exponentials(tq, lower, tn);
         products(tq, lower, tn, []() {});  // (past the last tile: scores of what lies there, unused)
         place_of(++t, token, head);
