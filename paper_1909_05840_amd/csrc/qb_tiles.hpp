@@ -143,6 +143,15 @@ __device__ __forceinline__ float halves_sum(float v)
     return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
+// Eight bytes of each of two quads of results, one quad in the lower and one in the upper half of the wavefront, to sixteen neighbouring bytes a lane: a
+// product's result holds four neighbours in a lane and the next four in the lane 32 further on.  first, second: the lane's words of
+// rows 8 * q + 4 * (lane / 32) .. of quads q and q + 1; the lane is given the eight rows of quad q + (lane / 32).
+__device__ __forceinline__ v4u join_halves(v2u first, v2u second)
+{
+    const auto a = __builtin_amdgcn_permlane32_swap(first[0], second[0], false, false), b = __builtin_amdgcn_permlane32_swap(first[1], second[1], false, false);
+    return v4u{a[0], b[0], a[1], b[1]};
+}
+
 // Dropout's random bits: Threefry-2x32 with 13 rounds (J. Salmon, M. Moraes, R. Dror, D. Shaw, "Parallel random numbers: as
 // easy as 1, 2, 3", SC 2011; 13 rounds is the least that passed the authors' tests), key: the caller's 64-bit seed.  Additions,
 // rotations and exclusive ors run at the full rate, the multiplications of the same paper's other generators at a quarter.

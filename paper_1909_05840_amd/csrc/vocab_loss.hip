@@ -15,7 +15,7 @@ namespace qb {
 namespace {
 
 constexpr int64_t kMost = 1 << 24;              // tokens, words
-constexpr int64_t kPieceBytes = 512ll << 20;    // d of a piece
+constexpr int64_t kPieceBytes = 1024ll << 20;   // d of a piece, at most (16384 tokens: 32768 words)
 constexpr float kLow = -1.0e30f;               // the maximum of no words (finite, also in powers of two)
 constexpr int kRowPad = 256;                    // the list of tokens is padded to this
 constexpr int kSlices = 32;                     // most slices that a tile of dX is cut into
@@ -26,14 +26,20 @@ struct Counted {
     int pad[62];
 };
 
+struct RowInfo {
+    int token, target;
+    float lse2, weight;  // backward: lse / ln 2, dloss
+};
+
 struct LossArgs {
     const uint16_t *X, *W;
     const float *bias, *dloss;
     const int64_t *targets;
     int T, V, K;
     Counted *counted;
-    int *list;       // [Tp] token of every counted row; padded with the last one
-    int *place;      // [T] the other way round; -1 where a token has no target
+    RowInfo *info;   // [Tp] of every counted row; padded
+    int *place;      // [T] the row of a token; -1 where it has no target
+    float *start;    // [Vp] the bias, -infinity behind the last word
     // forward
     float *loss, *lse;
     v2f *part;       // [vocabulary tiles][Tp] maximum, sum
@@ -46,7 +52,7 @@ struct LossArgs {
     float *dXs;      // tiles of dX: [tile][slice], binary32
     uint16_t *dX, *dW;
     float *dbias;
-    int Tp;
+    int Tp, Vp;
 };
 
 __device__ __forceinline__ bool is_word(int64_t t, int V) { return t >= 0 && t < V; }
@@ -57,8 +63,14 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossArgs a)
 {
     __shared__ int sums[16];
     __shared__ float tops[16];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, first = blockIdx.x * 1024, t = first + tid;
-    const bool last = blockIdx.x == gridDim.x - 1;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, groups = (a.T + 1023) / 1024;
+    if ((int)blockIdx.x >= groups) {  // the further workgroups: where the sums start
+        const int v = ((int)blockIdx.x - groups) * 1024 + tid;
+        if (v < a.Vp) a.start[v] = v >= a.V ? -__builtin_inff() : a.bias ? a.bias[v] : 0.0f;
+        return;
+    }
+    const int first = blockIdx.x * 1024, t = first + tid;
+    const bool last = (int)blockIdx.x == groups - 1;
     int before = 0;
     float top = 0.0f;
     for (int i = tid; i < first; i += 1024) {
@@ -89,7 +101,14 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossArgs a)
     all += start;
     const int at = before + __builtin_popcountll(who & ((1ull << lane) - 1));
     if (t < a.T) {
-        if (mine) a.list[at] = t;
+        if (mine) {
+            RowInfo r = {t, (int)a.targets[t], 0.0f, 0.0f};
+            if constexpr (BACKWARD) {
+                r.lse2 = a.lse[t] * 1.44269504088896341f;
+                r.weight = a.dloss[t];
+            }
+            a.info[at] = r;
+        }
         if constexpr (BACKWARD) {
             a.place[t] = mine ? at : -1;
         } else if (!mine) {
@@ -105,7 +124,7 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossArgs a)
         a.counted->scale = s;
     }
     const int end = min(a.Tp, (all + kRowPad - 1) / kRowPad * kRowPad);
-    if (all + tid < end) a.list[all + tid] = 0;
+    if (all + tid < end) a.info[all + tid] = RowInfo{0, -1, __builtin_inff(), 0.0f};  // (exponentials of zero)
 }
 
 // ---- products ------------------------------------------------------------------------------------------------------
@@ -138,12 +157,31 @@ __device__ __forceinline__ v8s operand(const uint8_t *tile, int result, int sub,
     else return *reinterpret_cast<const v8s *>(tile + Rows<64>::at(result + (lane & 31), 2 * sub + (lane >> 5)));
 }
 
+// acc += A B^T over one step, whose operands lie in a stage
+template <typename S, bool A_ACROSS, bool B_ACROSS>
+__device__ __forceinline__ void step(v16f (&acc)[S::TM][S::TN], const uint8_t *ta, int wave, int lane)
+{
+    const int wm = wave / S::WN, wn = wave - wm * S::WN;
+    const uint8_t *const tb = ta + S::BM * 128;
+#pragma unroll
+    for (int sub = 0; sub < 4; ++sub) {
+        v8s x[S::TM], y[S::TN];
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i) x[i] = operand<A_ACROSS>(ta, (wm * S::TM + i) * 32, sub, lane);
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) y[j] = operand<B_ACROSS>(tb, (wn * S::TN + j) * 32, sub, lane);
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j) acc[i][j] = Bf16::mma32(x[i], y[j], acc[i][j]);
+    }
+}
+
 // acc += A B^T over steps [s0, s1); row_a(r, s) is the address of LDS row r of step s: of result r (along), or for r = 64 * block + k of
 // step k, result block `block` (across).  The addresses must not come from memory: a load between the copies waits for those before it.
 template <typename S, bool A_ACROSS, bool B_ACROSS, typename FA, typename FB>
 __device__ __forceinline__ void multiply(v16f (&acc)[S::TM][S::TN], uint8_t *lds, int s0, int s1, int wave, int lane, const FA &row_a, const FB &row_b)
 {
-    const int wm = wave / S::WN, wn = wave - wm * S::WN;
     const uint32_t lds0 = lds_address(lds);
     constexpr int NA = S::BM / 8 / S::kWaves, NB = S::BN / 8 / S::kWaves, kAhead = S::kStages - 1;
     static_assert(NA * 8 * S::kWaves == S::BM && NB * 8 * S::kWaves == S::BN, "every wavefront copies the same number of times");
@@ -170,19 +208,7 @@ __device__ __forceinline__ void multiply(v16f (&acc)[S::TM][S::TN], uint8_t *lds
         else wait_copies<0>();
         barrier();
         if (s + kAhead < s1) fetch(s + kAhead, stage == 0 ? kAhead : stage - 1);  // (into the stage that the last step was multiplied from)
-        const uint8_t *const ta = lds + stage * S::kStage, *const tb = ta + S::BM * 128;
-#pragma unroll
-        for (int sub = 0; sub < 4; ++sub) {
-            v8s x[S::TM], y[S::TN];
-#pragma unroll
-            for (int i = 0; i < S::TM; ++i) x[i] = operand<A_ACROSS>(ta, (wm * S::TM + i) * 32, sub, lane);
-#pragma unroll
-            for (int j = 0; j < S::TN; ++j) y[j] = operand<B_ACROSS>(tb, (wn * S::TN + j) * 32, sub, lane);
-#pragma unroll
-            for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-                for (int j = 0; j < S::TN; ++j) acc[i][j] = Bf16::mma32(x[i], y[j], acc[i][j]);
-        }
+        step<S, A_ACROSS, B_ACROSS>(acc, lds + stage * S::kStage, wave, lane);
         stage = stage == kAhead ? 0 : stage + 1;
     }
     barrier();  // the stages are free again
@@ -213,44 +239,113 @@ __device__ __forceinline__ float half_sum(float x)
 }
 
 // Logits, a tile of words by tokens at a time: a lane's results belong to one token.  The sums start from the bias, and from
-// -infinity for words past the end, which so have no weight.
+// -infinity for words past the end, which so have no weight.  A workgroup's tiles are one stream of steps: the first steps of a tile,
+// what is known of its rows and where its sums start are on their way while the tile before is ended.  All of it comes
+// through copies to LDS: a load into registers would have to wait for the copies in front of it.
 template <typename S, bool BACKWARD>
 __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_logits_kernel(const LossArgs a)
 {
+    constexpr int kAhead = S::kStages - 1, kRing = S::kStages + 2;  // the tile at work, those ahead (of one step), and the next one's rows on their way
+    constexpr int NA = S::BM / 8 / S::kWaves, NB = S::BN / 8 / S::kWaves;
+    constexpr int kBoth = BACKWARD ? S::WN * S::BM * 4 : S::WM * S::BN * 8;
     __shared__ __align__(1024) uint8_t lds[S::kStages * S::kStage];
+    __shared__ __align__(1024) RowInfo info[kRing][S::BN];
+    __shared__ __align__(1024) float begin[kRing][S::BM > 256 ? S::BM : 256];  // (a copy fills 256)
+    __shared__ __align__(16) uint8_t shared[kBoth];
+    typedef Rows<64> R;
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave - wm * S::WN;
-    const int n = a.counted->n, K = a.K;
+    const int n = a.counted->n, K = a.K, steps = K / 64, grid = (int)gridDim.x;
     const float scale = BACKWARD ? a.counted->scale : 0.0f, inv = scale > 0.0f ? 1.0f / scale : 0.0f;
     const int words = BACKWARD ? a.piece / S::BM : (a.V + S::BM - 1) / S::BM, tiles = words * ((n + S::BN - 1) / S::BN);
+    const int tile0 = first_tile();
     if (BACKWARD && a.v0 == 0) {  // the rows that take part, side by side, for dW
         const int64_t chunks = (int64_t)((n + S::BN - 1) / S::BN * S::BN) * (K / 8);
-        for (int64_t c = (int64_t)blockIdx.x * (64 * S::kWaves) + threadIdx.x; c < chunks; c += (int64_t)gridDim.x * (64 * S::kWaves)) {
+        for (int64_t c = (int64_t)blockIdx.x * (64 * S::kWaves) + threadIdx.x; c < chunks; c += (int64_t)grid * (64 * S::kWaves)) {
             const int row = (int)(c / (K / 8)), k = (int)(c - (int64_t)row * (K / 8)) * 8;
-            *reinterpret_cast<v4u *>(a.Xc + (int64_t)row * K + k) = *reinterpret_cast<const v4u *>(a.X + (int64_t)a.list[row] * K + k);
+            *reinterpret_cast<v4u *>(a.Xc + (int64_t)row * K + k) = *reinterpret_cast<const v4u *>(a.X + (int64_t)a.info[row].token * K + k);
         }
     }
-    for (int tile = first_tile(); tile < tiles; tile += gridDim.x) {
-        const int tt = tile / words, tv = tile - tt * words, t0 = tt * S::BN, v0 = (BACKWARD ? a.v0 : 0) + tv * S::BM;
+    if (tile0 >= tiles) return;
+    const auto words_of = [&](int tile) { return (BACKWARD ? a.v0 : 0) + tile % words * S::BM; };
+    const auto rows_of = [&](int tile) { return tile / words * S::BN; };
+    // a tile's rows and starts on their way (64 entries of 16 bytes a copy)
+    const auto announce = [&](int tile, int ring) {
+        constexpr int kInfo = S::BN / 64, kBegin = S::BM / 256 > 0 ? S::BM / 256 : 1;
+        static_assert(kInfo + kBegin <= S::kWaves, "a copy to a wavefront");
+        if (wave < kInfo) copy16(a.info + rows_of(tile) + wave * 64 + lane, lds_address(info[ring]) + wave * 1024);
+        else if (wave < kInfo + kBegin) {  // (tiles of 64 words: a quarter of the copy is used)
+            const int at = words_of(tile) + (wave - kInfo) * 256 + 4 * (S::BM >= 256 ? lane : lane & 15);
+            copy16(a.start + at, lds_address(begin[ring]) + (wave - kInfo) * 1024);
+        }
+    };
+    // ---- the copies' side of the stream: step `cs` of tile `ct`, the `cn`-th of this workgroup
+    int ct = tile0, cs = 0, cn = 0;
+    const uint16_t *x[NB], *w[NA];
+    const auto enter = [&]() {
+        const int v0 = words_of(ct);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) x[i] = a.X + (int64_t)info[cn % kRing][S::row(i, wave, lane)].token * K + 8 * R::copy_chunk(S::row(i, wave, lane), lane);
+#pragma unroll
+        for (int i = 0; i < NA; ++i) w[i] = a.W + (int64_t)min(v0 + S::row(i, wave, lane), a.V - 1) * K + 8 * R::copy_chunk(S::row(i, wave, lane), lane);
+        if (ct + grid < tiles) announce(ct + grid, (cn + 1) % kRing);
+    };
+    const uint32_t lds0 = lds_address(lds);
+    const auto fetch = [&](int stage) {
+        if (ct >= tiles) return;
+        const uint32_t to = lds0 + stage * S::kStage;
+#pragma unroll
+        for (int i = 0; i < NA; ++i) copy16(w[i] + cs * 64, to + (i * S::kWaves + wave) * 1024);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) copy16(x[i] + cs * 64, to + S::BM * 128 + (i * S::kWaves + wave) * 1024);
+        if (++cs < steps) return;
+        cs = 0;
+        ct += grid;
+        ++cn;
+        if (ct >= tiles) return;
+        if (steps <= kAhead) {  // the next tile's rows may not have come yet
+            wait_copies<0>();
+            barrier();
+        }
+        enter();
+    };
+    announce(ct, 0);
+    wait_copies<0>();
+    barrier();
+    enter();
+    for (int u = 0; u < kAhead; ++u) fetch(u);
+
+    const int mine = (tiles - tile0 + grid - 1) / grid;  // tiles of this workgroup
+    int stage = 0, left = mine * steps;
+    constexpr float kLog2e = 1.44269504088896341f;
+    for (int number = 0, tile = tile0; tile < tiles; tile += grid, ++number) {
+        const int tt = tile / words, tv = tile - tt * words, t0 = tt * S::BN, v0 = words_of(tile), ring = number % kRing;
         v16f z[S::TM][S::TN];
+        for (int s = 0; s < steps; ++s, --left) {
+            constexpr int kStores = BACKWARD && kAhead == 1 ? S::TM * S::TN * 2 : 0;  // of d, at a tile's end, behind the copies that are waited for
+            asm volatile("" ::: "memory");  // (the stores stay in front of the wait that counts them)
+            if (kAhead == 1 && kStores > 0 && s == 0 && number > 0) wait_copies<kStores>();
+            else if (left >= kAhead) wait_copies<(kAhead - 1) * (NA + NB)>();  // (younger steps' stay under way)
+            else wait_copies<0>();
+            barrier();
+            fetch(stage == 0 ? kAhead : stage - 1);  // (into the stage that the last step was multiplied from)
+            if (s == 0) {
 #pragma unroll
-        for (int i = 0; i < S::TM; ++i)
+                for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const int v = v0 + (wm * S::TM + i) * 32 + 8 * (k >> 2) + 4 * hf + (k & 3);
-                const float start = v >= a.V ? -__builtin_inff() : a.bias ? a.bias[v] : 0.0f;
+                    for (int k = 0; k < 16; k += 4) {
+                        const v4f b = *reinterpret_cast<const v4f *>(&begin[ring][(wm * S::TM + i) * 32 + 2 * k + 4 * hf]);
 #pragma unroll
-                for (int j = 0; j < S::TN; ++j) z[i][j][k] = start;
+                        for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) z[i][j][k + e] = b[e];
+                    }
             }
-        const uint16_t *x[S::BN / 8 / S::kWaves];
-#pragma unroll
-        for (int i = 0; i < S::BN / 8 / S::kWaves; ++i) x[i] = a.X + (int64_t)a.list[t0 + S::row(i, wave, lane)] * K;
-        multiply<S, false, false>(z, lds, 0, K / 64, wave, lane,
-            [&](int, int r, int s) { return a.W + (int64_t)min(v0 + r, a.V - 1) * K + s * 64; },
-            [&](int i, int, int s) { return x[i] + s * 64; });
-        constexpr float kLog2e = 1.44269504088896341f;
+            step<S, false, false>(z, lds + stage * S::kStage, wave, lane);
+            stage = stage == kAhead ? 0 : stage + 1;
+        }
         if constexpr (!BACKWARD) {
-            v2f *const both = reinterpret_cast<v2f *>(lds);  // [WM][BN] maximum, sum of a wavefront's words
+            v2f *const both = reinterpret_cast<v2f *>(shared);  // [WM][BN] maximum, sum of a wavefront's words
 #pragma unroll
             for (int j = 0; j < S::TN; ++j) {
                 float m = z[0][j][0];
@@ -266,9 +361,9 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_logits_kernel(const Lo
 #pragma unroll
                     for (int k = 0; k < 16; ++k) l += __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][j][k], kLog2e, -m2));
                 l = halves_sum(l);
-                if (hf == 0) both[wm * S::BN + (wn * S::TN + j) * 32 + l32] = v2f{m, l};
-                const int row = t0 + (wn * S::TN + j) * 32 + l32;
-                const int target = row < n ? (int)a.targets[a.list[row]] - v0 - wm * S::TM * 32 : -1;
+                const int row = (wn * S::TN + j) * 32 + l32;
+                if (hf == 0) both[wm * S::BN + row] = v2f{m, l};
+                const int target = info[ring][row].target - v0 - wm * S::TM * 32;
                 if (__builtin_amdgcn_ballot_w64(target >= 0 && target < S::TM * 32)) {  // (one wavefront in four at 30522 words)
                     bool have = false;
                     float hit = 0.0f;
@@ -280,7 +375,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_logits_kernel(const Lo
                                 hit = z[i][j][k];
                                 have = true;
                             }
-                    if (have) a.hit[row] = hit;
+                    if (have) a.hit[t0 + row] = hit;
                 }
             }
             barrier();
@@ -294,33 +389,34 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_logits_kernel(const Lo
                 }
                 a.part[(int64_t)tv * a.Tp + t0 + r] = x;
             }
-            barrier();
         } else {
-            float *const sums = reinterpret_cast<float *>(lds);  // [WN][BM] of d over a wavefront's tokens
 #pragma unroll
             for (int j = 0; j < S::TN; ++j) {
-                const int row = t0 + (wn * S::TN + j) * 32 + l32, token = a.list[row];
-                const bool in = row < n;  // (a padding row has weight 0 and exponentials of 0)
-                const float lse2 = in ? a.lse[token] * kLog2e : __builtin_inff(), w = in ? a.dloss[token] * inv : 0.0f;
-                const int target = in ? (int)a.targets[token] - v0 - wm * S::TM * 32 : -1;
+                const int row = (wn * S::TN + j) * 32 + l32;
+                const RowInfo r = info[ring][row];
+                const float w = r.weight * inv;
+                const int target = r.target - v0 - wm * S::TM * 32;
 #pragma unroll
                 for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) z[i][j][k] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][j][k], kLog2e, -lse2)) * w;
+                    for (int k = 0; k < 16; ++k) z[i][j][k] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][j][k], kLog2e, -r.lse2)) * w;
                 if (__builtin_amdgcn_ballot_w64(target >= 0 && target < S::TM * 32)) {
 #pragma unroll
                     for (int i = 0; i < S::TM; ++i)
 #pragma unroll
                         for (int k = 0; k < 16; ++k) z[i][j][k] -= target - 4 * hf == i * 32 + 8 * (k >> 2) + (k & 3) ? w : 0.0f;
                 }
-                uint16_t *const to = a.d + (int64_t)row * a.piece + tv * S::BM + wm * S::TM * 32 + 4 * hf;
+                uint16_t *const to = a.d + (int64_t)(t0 + row) * a.piece + tv * S::BM + wm * S::TM * 32 + 8 * hf;
 #pragma unroll
                 for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-                    for (int k = 0; k < 16; k += 4)
-                        *reinterpret_cast<v2u *>(to + i * 32 + 2 * k) = v2u{Bf16::pair(z[i][j][k], z[i][j][k + 1]), Bf16::pair(z[i][j][k + 2], z[i][j][k + 3])};
+                    for (int k = 0; k < 16; k += 8)
+                        *reinterpret_cast<v4u *>(to + i * 32 + 2 * k) =
+                            join_halves(v2u{Bf16::pair(z[i][j][k], z[i][j][k + 1]), Bf16::pair(z[i][j][k + 2], z[i][j][k + 3])},
+                                        v2u{Bf16::pair(z[i][j][k + 4], z[i][j][k + 5]), Bf16::pair(z[i][j][k + 6], z[i][j][k + 7])});
             }
             if (a.db) {  // (uniform)
+                float *const sums = reinterpret_cast<float *>(shared);  // [WN][BM] of d over a wavefront's tokens
 #pragma unroll
                 for (int i = 0; i < S::TM; ++i)
 #pragma unroll
@@ -338,9 +434,9 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_logits_kernel(const Lo
                     for (int i = 0; i < S::WN; ++i) x += sums[i * S::BM + v];
                     if (v0 + v < a.V) a.db[(int64_t)tt * a.V + v0 + v] = x;
                 }
-                barrier();
             }
         }
+        // (the next step's barrier stands between these reads of `shared` and the next tile's writes)
     }
 }
 
@@ -373,7 +469,7 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const LossArgs a, int wo
 #pragma unroll
     for (int i = 1; i < 16; ++i) add(both[i][r]);
     const float lse = m + logf(l);
-    const int token = a.list[row];
+    const int token = a.info[row].token;
     a.lse[token] = lse;
     a.loss[token] = lse - a.hit[row];
 }
@@ -388,22 +484,25 @@ __device__ __host__ inline int dx_slices(int tiles, int steps)
 
 // The piece's share of both gradients: results lie transposed in the products (hidden units by tokens or words), so that a lane
 // holds neighbours of a row of dX or dW.
-template <typename S>
+template <typename S, typename SW>  // tiles of dX, of dW
 __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_grads_kernel(const LossArgs a)
 {
-    __shared__ __align__(1024) uint8_t lds[S::kStages * S::kStage];
+    static_assert(S::kWaves == SW::kWaves, "the same workgroups");
+    constexpr int kX = S::kStages * S::kStage, kW = SW::kStages * SW::kStage;
+    __shared__ __align__(1024) uint8_t lds[kX > kW ? kX : kW];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave - wm * S::WN;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = a.counted->n, K = a.K;
     const float scale = a.counted->scale;
-    const int kt = (K + S::BM - 1) / S::BM;
+    const int kt = (K + S::BM - 1) / S::BM, kt_w = (K + SW::BM - 1) / SW::BM;
     const int words = min(a.piece, (a.V - a.v0 + 63) / 64 * 64);                 // of this piece, in whole steps
     const int x_tiles = kt * ((n + S::BN - 1) / S::BN), slices = dx_slices(x_tiles, a.piece / 64), x_steps = words / 64;
-    const int w_tiles = kt * ((words + S::BN - 1) / S::BN), w_steps = (n + 63) / 64;
+    const int w_tiles = kt_w * ((words + SW::BN - 1) / SW::BN), w_steps = (n + 63) / 64;
     for (int id = first_tile(); id < x_tiles * slices + w_tiles; id += gridDim.x) {
-        v16f acc[S::TM][S::TN];
-        clear(acc);
         if (id < x_tiles * slices) {
+            const int wm = wave / S::WN, wn = wave - wm * S::WN;
+            v16f acc[S::TM][S::TN];
+            clear(acc);
             const int tile = id / slices, slice = id - tile * slices, tt = tile / kt, k0 = (tile - tt * kt) * S::BM, t0 = tt * S::BN;
             const int s0 = x_steps * slice / slices, s1 = x_steps * (slice + 1) / slices;
             if (s0 < s1)
@@ -423,23 +522,27 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_grads_kernel(const Los
                         *p = x;
                     }
         } else {
-            const int tile = id - x_tiles * slices, tv = tile / kt, k0 = (tile - tv * kt) * S::BM, v0 = tv * S::BN;
+            const int wm = wave / SW::WN, wn = wave - wm * SW::WN;
+            v16f acc[SW::TM][SW::TN];
+            clear(acc);
+            const int tile = id - x_tiles * slices, tv = tile / kt_w, k0 = (tile - tv * kt_w) * SW::BM, v0 = tv * SW::BN;
             if (w_steps > 0)
-                multiply<S, true, true>(acc, lds, 0, w_steps, wave, lane,
+                multiply<SW, true, true>(acc, lds, 0, w_steps, wave, lane,
                     [&](int, int r, int s) { return a.Xc + (int64_t)(s * 64 + (r & 63)) * K + min(k0 + (r & ~63), K - 64); },
                     [&](int, int r, int s) { return a.d + (int64_t)(s * 64 + (r & 63)) * a.piece + v0 + (r & ~63); });
 #pragma unroll
-            for (int j = 0; j < S::TN; ++j) {
-                const int v = a.v0 + v0 + (wn * S::TN + j) * 32 + l32;
-                if (v >= a.V) continue;
+            for (int j = 0; j < SW::TN; ++j) {
+                const int v = a.v0 + v0 + (wn * SW::TN + j) * 32 + l32;  // (words past the end are exchanged too, not written)
 #pragma unroll
-                for (int i = 0; i < S::TM; ++i) {
-                    const int k1 = k0 + (wm * S::TM + i) * 32;
+                for (int i = 0; i < SW::TM; ++i) {
+                    const int k1 = k0 + (wm * SW::TM + i) * 32;
                     if (k1 >= K) continue;
 #pragma unroll
-                    for (int k = 0; k < 16; k += 4)
-                        *reinterpret_cast<v2u *>(a.dW + (int64_t)v * K + k1 + 2 * k + 4 * hf) =
-                            v2u{Bf16::pair(acc[i][j][k] * scale, acc[i][j][k + 1] * scale), Bf16::pair(acc[i][j][k + 2] * scale, acc[i][j][k + 3] * scale)};
+                    for (int k = 0; k < 16; k += 8) {
+                        const auto pairs = [&](int e) { return v2u{Bf16::pair(acc[i][j][e] * scale, acc[i][j][e + 1] * scale), Bf16::pair(acc[i][j][e + 2] * scale, acc[i][j][e + 3] * scale)}; };
+                        const v4u w = join_halves(pairs(k), pairs(k + 4));
+                        if (v < a.V) *reinterpret_cast<v4u *>(a.dW + (int64_t)v * K + k1 + 2 * k + 8 * hf) = w;
+                    }
                 }
             }
         }
@@ -479,6 +582,9 @@ __global__ __launch_bounds__(256) void loss_ends_kernel(const LossArgs a, int x_
 // 48 KB of them under way on every CU, two workgroups to a CU
 typedef Shape<2, 4, 4, 2, 2> Large;
 typedef Shape<2, 2, 1, 1, 4> Small;
+typedef Shape<4, 1, 2, 2, 2> SmallW;  // dW of few tokens: one or two steps a tile, so larger ones
+template <typename S> struct ForW { typedef S type; };
+template <> struct ForW<Small> { typedef SmallW type; };
 inline bool few(int64_t T) { return T <= 512; }
 
 inline size_t up(size_t v) { return (v + 255) / 256 * 256; }
@@ -495,17 +601,20 @@ size_t lay_out(LossArgs &a, uint8_t *base, bool backward)
     const int bm = few(a.T) ? Small::BM : Large::BM, bn = few(a.T) ? Small::BN : Large::BN;
     a.Tp = (int)((a.T + kRowPad - 1) / kRowPad * kRowPad);
     a.counted = reinterpret_cast<Counted *>(take(sizeof(Counted)));
-    a.list = reinterpret_cast<int *>(take((size_t)a.Tp * 4));
+    a.Vp = (int)(((int64_t)a.V + kRowPad - 1) / kRowPad * kRowPad);
+    if (backward) {  // pieces of about one size
+        const int64_t most = std::max<int64_t>(1, kPieceBytes / (2ll * a.Tp) / kRowPad), pieces = (a.Vp / kRowPad + most - 1) / most;
+        a.piece = (int)((a.Vp / kRowPad + pieces - 1) / pieces * kRowPad);
+        a.Vp = (int)(pieces * a.piece);
+    }
+    a.info = reinterpret_cast<RowInfo *>(take((size_t)a.Tp * sizeof(RowInfo)));
+    a.start = reinterpret_cast<float *>(take((size_t)a.Vp * 4));
     if (!backward) {
         a.part = reinterpret_cast<v2f *>(take((size_t)((a.V + bm - 1) / bm) * a.Tp * 8));
         a.hit = reinterpret_cast<float *>(take((size_t)a.Tp * 4));
         return at;
     }
     a.place = reinterpret_cast<int *>(take((size_t)a.T * 4));
-    const int64_t widest = ((int64_t)a.V + kRowPad - 1) / kRowPad * kRowPad;
-    a.piece = (int)std::min(widest, std::max<int64_t>(kRowPad, kPieceBytes / (2ll * a.Tp) / kRowPad * kRowPad));
-    const int64_t pieces = (widest + a.piece - 1) / a.piece;
-    a.piece = (int)((widest / kRowPad + pieces - 1) / pieces * kRowPad);  // pieces of about one size
     a.d = reinterpret_cast<uint16_t *>(take((size_t)a.Tp * a.piece * 2));
     a.Xc = reinterpret_cast<uint16_t *>(take((size_t)a.Tp * a.K * 2));
     a.db = reinterpret_cast<float *>(take((size_t)(a.Tp / bn) * a.V * 4));
@@ -524,7 +633,7 @@ qb_status forward(const LossArgs &a, hipStream_t st)
 {
     const int words = (a.V + S::BM - 1) / S::BM;
     const int64_t tiles = (int64_t)words * (a.Tp / S::BN);
-    loss_rows_kernel<false><<<(a.T + 1023) / 1024, 1024, 0, st>>>(a);
+    loss_rows_kernel<false><<<(a.T + 1023) / 1024 + (a.Vp + 1023) / 1024, 1024, 0, st>>>(a);
     loss_logits_kernel<S, false><<<(int)std::min<int64_t>(tiles, kAtWork<S>), 64 * S::kWaves, 0, st>>>(a);
     loss_join_kernel<<<(a.T + 15) / 16, 256, 0, st>>>(a, words);
     return launch_status();
@@ -533,11 +642,11 @@ qb_status forward(const LossArgs &a, hipStream_t st)
 template <typename S>
 qb_status backward(LossArgs a, hipStream_t st)
 {
-    loss_rows_kernel<true><<<(a.T + 1023) / 1024, 1024, 0, st>>>(a);
+    loss_rows_kernel<true><<<(a.T + 1023) / 1024 + (a.Vp + 1023) / 1024, 1024, 0, st>>>(a);
     for (a.v0 = 0; a.v0 < a.V; a.v0 += a.piece) {
         const int64_t tiles = (int64_t)(a.piece / S::BM) * (a.Tp / S::BN);
         loss_logits_kernel<S, true><<<(int)std::min<int64_t>(tiles, kAtWork<S>), 64 * S::kWaves, 0, st>>>(a);
-        loss_grads_kernel<S><<<kAtWork<S>, 64 * S::kWaves, 0, st>>>(a);
+        loss_grads_kernel<S, typename ForW<S>::type><<<kAtWork<S>, 64 * S::kWaves, 0, st>>>(a);
     }
     const int x_groups = (int)std::min<int64_t>(4096, ((int64_t)a.T * (a.K / 4) + 255) / 256);
     loss_ends_kernel<S><<<x_groups + (a.dbias ? (a.V + 255) / 256 : 0), 256, 0, st>>>(a, x_groups);
