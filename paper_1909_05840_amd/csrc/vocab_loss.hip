@@ -18,13 +18,32 @@ constexpr int64_t kMost = 1 << 24;              // tokens, words
 constexpr int64_t kPieceBytes = 1024ll << 20;   // d of a piece, at most (16384 tokens: 32768 words)
 constexpr float kLow = -1.0e30f;               // the maximum of no words (finite, also in powers of two)
 constexpr int kRowPad = 256;                    // the list of tokens is padded to this
-constexpr int kSlices = 32;                     // most slices that a tile of dX is cut into
 
 struct Counted {
     int n;        // tokens that have a target
     float scale;  // the largest |dloss| among them
-    int pad[62];
+    int slices;   // that the contraction of a tile of dX is cut into
+    int pad[61];
 };
+
+// the shapes of the gradients' tiles and the number of workgroups at work
+struct Work {
+    int bm, bn, wbm, wbn, groups;
+};
+// Tiles of dX (x) and dW (w) come one after the other, id by id, to workgroups in turn.  A tile of dX runs over all words of the
+// piece; it is cut into as many slices as make the longest share of a workgroup shortest, a tile counted as its steps and four more.
+__device__ __host__ inline int most_slices(int x_tiles, int groups) { return x_tiles * 64 <= 2 * groups ? 64 : 2 * groups / x_tiles > 1 ? 2 * groups / x_tiles : 1; }
+__device__ inline int best_slices(const Work &k, int n, int K, int words, int lane)  // (of one wavefront: a lane to a number)
+{
+    const int x_tiles = max(1, (n + k.bn - 1) / k.bn * ((K + k.bm - 1) / k.bm)), w_tiles = (words + k.wbn - 1) / k.wbn * ((K + k.wbm - 1) / k.wbm);
+    const int steps = words / 64, most = min(most_slices(x_tiles, k.groups), max(1, steps / 4)), w = (n + 63) / 64 + 4;
+    const int s = min(lane + 1, most), all = x_tiles * s, x = (steps + s - 1) / s + 4, full = all / k.groups, mixed = all % k.groups ? 1 : 0;
+    const int64_t share = (int64_t)full * x + mixed * max(x, w) + (int64_t)max(0, (all + w_tiles + k.groups - 1) / k.groups - full - mixed) * w;
+    int64_t best = share * 64 + s - 1;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) best = min(best, __shfl_xor(best, o));
+    return (int)(best & 63) + 1;
+}
 
 struct RowInfo {
     int token, target;
@@ -53,6 +72,7 @@ struct LossArgs {
     uint16_t *dX, *dW;
     float *dbias;
     int Tp, Vp;
+    Work work;
 };
 
 __device__ __forceinline__ bool is_word(int64_t t, int V) { return t >= 0 && t < V; }
@@ -73,6 +93,7 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossArgs a)
     const bool last = (int)blockIdx.x == groups - 1;
     int before = 0;
     float top = 0.0f;
+#pragma unroll 8
     for (int i = tid; i < first; i += 1024) {
         const bool word = is_word(a.targets[i], a.V);
         before += word;
@@ -122,6 +143,10 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossArgs a)
         float s = 0.0f;
         for (int i = 0; i < 16; ++i) s = fmaxf(s, tops[i]);
         a.counted->scale = s;
+    }
+    if (BACKWARD && wave == 1) {
+        const int slices = best_slices(a.work, all, a.K, min(a.piece, (a.V + 63) / 64 * 64), lane);
+        if (lane == 0) a.counted->slices = slices;
     }
     const int end = min(a.Tp, (all + kRowPad - 1) / kRowPad * kRowPad);
     if (all + tid < end) a.info[all + tid] = RowInfo{0, -1, __builtin_inff(), 0.0f};  // (exponentials of zero)
@@ -474,14 +499,6 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const LossArgs a, int wo
     a.loss[token] = lse - a.hit[row];
 }
 
-// A tile of dX is cut into slices of the contraction, the same number whoever asks.
-__device__ __host__ inline int dx_slices(int tiles, int steps)
-{
-    int s = 512 / (tiles > 0 ? tiles : 1);
-    s = s < steps / 8 ? s : steps / 8;
-    return s < 1 ? 1 : s < kSlices ? s : kSlices;
-}
-
 // The piece's share of both gradients: results lie transposed in the products (hidden units by tokens or words), so that a lane
 // holds neighbours of a row of dX or dW.
 template <typename S, typename SW>  // tiles of dX, of dW
@@ -496,20 +513,21 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_grads_kernel(const Los
     const float scale = a.counted->scale;
     const int kt = (K + S::BM - 1) / S::BM, kt_w = (K + SW::BM - 1) / SW::BM;
     const int words = min(a.piece, (a.V - a.v0 + 63) / 64 * 64);                 // of this piece, in whole steps
-    const int x_tiles = kt * ((n + S::BN - 1) / S::BN), slices = dx_slices(x_tiles, a.piece / 64), x_steps = words / 64;
+    const int x_tiles = kt * ((n + S::BN - 1) / S::BN), slices = a.counted->slices, x_steps = words / 64;
     const int w_tiles = kt_w * ((words + SW::BN - 1) / SW::BN), w_steps = (n + 63) / 64;
     for (int id = first_tile(); id < x_tiles * slices + w_tiles; id += gridDim.x) {
         if (id < x_tiles * slices) {
             const int wm = wave / S::WN, wn = wave - wm * S::WN;
             v16f acc[S::TM][S::TN];
             clear(acc);
-            const int tile = id / slices, slice = id - tile * slices, tt = tile / kt, k0 = (tile - tt * kt) * S::BM, t0 = tt * S::BN;
+            const int slice = id / x_tiles, tile = id - slice * x_tiles, tt = tile / kt,  // (neighbours read the same rows of W)
+                      k0 = (tile - tt * kt) * S::BM, t0 = tt * S::BN;
             const int s0 = x_steps * slice / slices, s1 = x_steps * (slice + 1) / slices;
             if (s0 < s1)
                 multiply<S, true, false>(acc, lds, s0, s1, wave, lane,
                     [&](int, int r, int s) { return a.W + (int64_t)min(a.v0 + s * 64 + (r & 63), a.V - 1) * K + min(k0 + (r & ~63), K - 64); },
                     [&](int, int r, int s) { return a.d + (int64_t)(t0 + r) * a.piece + s * 64; });
-            float *const to = a.dXs + (int64_t)id * S::BM * S::BN;
+            float *const to = a.dXs + (int64_t)(tile * slices + slice) * S::BM * S::BN;
 #pragma unroll
             for (int i = 0; i < S::TM; ++i)
 #pragma unroll
@@ -564,7 +582,7 @@ __global__ __launch_bounds__(256) void loss_ends_kernel(const LossArgs a, int x_
         a.dbias[v] = x * scale;
         return;
     }
-    const int kt = (K + S::BM - 1) / S::BM, slices = dx_slices(kt * ((n + S::BN - 1) / S::BN), a.piece / 64);
+    const int kt = (K + S::BM - 1) / S::BM, slices = a.counted->slices;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)a.T * quads; i += (int64_t)x_groups * 256) {
         const int t = (int)(i / quads), k = (int)(i - (int64_t)t * quads) * 4, row = a.place[t];
         v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -587,6 +605,9 @@ template <typename S> struct ForW { typedef S type; };
 template <> struct ForW<Small> { typedef SmallW type; };
 inline bool few(int64_t T) { return T <= 512; }
 
+template <typename S>
+constexpr int kAtWork = S::kWaves == 8 ? 256 : 512;  // workgroups of a launch: as many as are resident
+
 inline size_t up(size_t v) { return (v + 255) / 256 * 256; }
 
 // where everything lies in the workspace; returns its size
@@ -599,6 +620,7 @@ size_t lay_out(LossArgs &a, uint8_t *base, bool backward)
         return p;
     };
     const int bm = few(a.T) ? Small::BM : Large::BM, bn = few(a.T) ? Small::BN : Large::BN;
+    a.work = few(a.T) ? Work{bm, bn, SmallW::BM, SmallW::BN, kAtWork<Small>} : Work{bm, bn, bm, bn, kAtWork<Large>};
     a.Tp = (int)((a.T + kRowPad - 1) / kRowPad * kRowPad);
     a.counted = reinterpret_cast<Counted *>(take(sizeof(Counted)));
     a.Vp = (int)(((int64_t)a.V + kRowPad - 1) / kRowPad * kRowPad);
@@ -619,14 +641,20 @@ size_t lay_out(LossArgs &a, uint8_t *base, bool backward)
     a.Xc = reinterpret_cast<uint16_t *>(take((size_t)a.Tp * a.K * 2));
     a.db = reinterpret_cast<float *>(take((size_t)(a.Tp / bn) * a.V * 4));
     const int64_t x_tiles = (int64_t)(a.Tp / bn) * ((a.K + bm - 1) / bm);
-    a.dXs = reinterpret_cast<float *>(take((size_t)std::max(x_tiles, std::min<int64_t>(512, x_tiles * kSlices)) * bm * bn * 4));
+    int64_t slots = 0;  // the most tiles and slices that any number of counted tokens gives
+    for (int64_t t = 1; t <= a.Tp / bn; ++t) {
+        const int64_t tiles = t * ((a.K + bm - 1) / bm);
+        slots = std::max(slots, tiles * most_slices((int)tiles, a.work.groups));
+        if (tiles > 2 * a.work.groups) {
+            slots = std::max(slots, x_tiles);
+            break;
+        }
+    }
+    a.dXs = reinterpret_cast<float *>(take((size_t)slots * bm * bn * 4));
     return at;
 }
 
 bool shape_ok(int64_t T, int64_t V, int64_t K) { return T >= 1 && T <= kMost && V >= 1 && V <= kMost && k_ok(K); }
-
-template <typename S>
-constexpr int kAtWork = S::kWaves == 8 ? 256 : 512;  // workgroups of a launch: as many as are resident
 
 template <typename S>
 qb_status forward(const LossArgs &a, hipStream_t st)
