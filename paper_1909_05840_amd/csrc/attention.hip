@@ -90,21 +90,22 @@ __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], co
     // All operands of a product are read before its first multiplication (left to itself the compiler reads each just in front of its
     // use, and every multiplication waits for the LDS): the keys here, the values in front of the exponentials.
     v16f s[KB];
-    {
-        v8s k[KB][D / 16];
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d)
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) k[kb][d] = op.along(tk, 32 * kb, d);
+        for (int i = 0; i < 16; ++i) s[kb][i] = 0.0f;
+#pragma unroll
+    for (int d0 = 0; d0 < D / 16; d0 += 4) {
+        v8s k[KB][4];
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) k[kb][d] = op.along(tk, 32 * kb, d0 + d);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
+        for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[kb][i] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < D / 16; ++d)
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) s[kb] = T::mma32(k[kb][d], q[d], s[kb]);
+            for (int kb = 0; kb < KB; ++kb) s[kb] = T::mma32(k[kb][d], q[d0 + d], s[kb]);
     }
     v8s v[D == 64 ? KB : 1][2][D / 32];
     const auto read_values = [&](int kb, v8s (&to)[2][D / 32]) {
@@ -136,9 +137,11 @@ __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], co
 #pragma unroll
             for (int j = 0; j < 16; ++j) x.o[i][j] *= f;
     }
-    read_values(0, v[0]);
-    if constexpr (D == 64 && KB == 2) read_values(1, v[KB - 1]);
-    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (D == 64) {
+        read_values(0, v[0]);
+        if constexpr (KB == 2) read_values(1, v[KB - 1]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
     const float mc = x.m * c;
     float sum = 0.0f;
 #pragma unroll
@@ -163,7 +166,7 @@ __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], co
     }
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-        if (D != 64 && kb > 0) read_values(kb, v[0]);
+        if constexpr (D != 64) read_values(kb, v[0]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             v4u w;
@@ -201,8 +204,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uin
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place at = place(blockIdx.x, a.n_seqs * a.kv_heads, a.tiles, by_xcd);
     if (at.pair >= a.n_seqs * a.kv_heads) return;
-    const int b = at.pair / a.kv_heads, kv = at.pair - b * a.kv_heads;
-    const Segment seg = segment(a, b);
+    const int nth = at.pair / a.kv_heads, kv = at.pair - nth * a.kv_heads;
+    const Segment seg = segment(a, nth_longest(a, nth, lane));
     const int rows = seg.nq * a.group, first = at.tile * 128;
     if (first >= rows) return;
     const int row = first + wave * 32 + l32;
@@ -251,7 +254,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uin
         if (t + 1 < tiles) fetch(t + 1, (t + 1) & 1);
         const int left = wave_most - t * kKeys;
         const uint32_t tk = (t & 1) * 2 * kTile;
-        constexpr bool kHalves = D == 64 || !DROP;  // (else there are no registers left for both)
+constexpr bool kHalves = D == 64 && DROP;  // (without dropout's arithmetic to save, both in the kernel cost more: 177 -> 190 us for 8192 causal keys)
         if (left > (kHalves ? 32 : 0)) attend<T, D, DROP>(x, q, op, tk, tk + kTile, t * kKeys, limit, (t + 1) * kKeys > wave_least, a.c, bits, a.threshold, row_q, head, lane);
         else if (kHalves && left > 0) attend<T, D, DROP, 1>(x, q, op, tk, tk + kTile, t * kKeys, limit, t * kKeys + 32 > wave_least, a.c, bits, a.threshold, row_q, head, lane);
     }

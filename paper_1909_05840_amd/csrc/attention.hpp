@@ -45,6 +45,20 @@ __device__ __forceinline__ Segment segment(const AttnArgs &a, int b)
     return s;
 }
 
+// The nth longest sequence (of up to 64; of more, the nth): workgroups take the sequences in that order, so that those with the most tiles are
+// at work first and every CU gets some of either kind.
+__device__ __forceinline__ int nth_longest(const AttnArgs &a, int nth, int lane)
+{
+    if (a.n_seqs == 1 || a.n_seqs > 64) return nth;
+    const int i = min(lane, a.n_seqs - 1), length = a.cu_q[i + 1] - a.cu_q[i] + a.cu_k[i + 1] - a.cu_k[i];
+    int before = 0;
+    for (int j = 0; j < a.n_seqs; ++j) {
+        const int other = __builtin_amdgcn_readlane(length, j);
+        before += other > length || (other == length && j < lane);
+    }
+    return __builtin_ctzll(__builtin_amdgcn_ballot_w64(before == nth && lane < a.n_seqs));
+}
+
 // Which tile of which (sequence, key head) a workgroup does.  Workgroups are dealt to the eight XCDs in turn, each with an L2
 // of its own: where there are pairs enough, all tiles of a pair go to one XCD, which fetches its keys once.  Tiles of the largest number
 // come first: with causal masks they see the most keys.

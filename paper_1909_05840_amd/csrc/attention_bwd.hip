@@ -71,8 +71,8 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
     if (EXACT && blockIdx.x == 0 && threadIdx.x < 2) g.stat[threadIdx.x ? 2 * (int64_t)a.total_q * a.heads + 1 : (int64_t)a.total_q * a.heads] = threadIdx.x ? 0.0f : -__builtin_inff();
     const Place at = place(blockIdx.x, a.n_seqs * a.kv_heads, a.tiles, by_xcd);
     if (at.pair >= a.n_seqs * a.kv_heads) return;
-    const int b = at.pair / a.kv_heads, kv = at.pair - b * a.kv_heads;
-    const Segment seg = segment(a, b);
+    const int nth = at.pair / a.kv_heads, kv = at.pair - nth * a.kv_heads;
+    const Segment seg = segment(a, nth_longest(a, nth, lane));
     const int rows = seg.nq * a.group, first = at.tile * 128;
     if (first >= rows) return;
     const int row = first + wave * 32 + l32;
@@ -264,8 +264,8 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place at = place(blockIdx.x, a.n_seqs * a.kv_heads, a.tiles * splits, by_xcd);
     if (at.pair >= a.n_seqs * a.kv_heads) return;
-    const int b = at.pair / a.kv_heads, kv = at.pair - b * a.kv_heads;
-    const Segment seg = segment(a, b);
+    const int nth = at.pair / a.kv_heads, kv = at.pair - nth * a.kv_heads;
+    const Segment seg = segment(a, nth_longest(a, nth, lane));
     const int rank = a.tiles * splits - 1 - at.tile, part = rank / a.tiles, key_tile = rank - part * a.tiles;  // part after part
     const int first = key_tile * 128;
     if (first >= seg.nk) return;
@@ -518,8 +518,8 @@ __global__ __launch_bounds__(256) void attention_dkv_join_kernel(const AttnArgs 
     constexpr int kEach = 2 * D / 8;  // threads to a key
     const int pair = blockIdx.x / (a.tiles * (128 * kEach / 256)), in_pair = blockIdx.x - pair * (a.tiles * (128 * kEach / 256));
     const int id = in_pair * 256 + threadIdx.x, key = id / kEach, d = (id - key * kEach) * 8;
-    const int b = pair / a.kv_heads, kv = pair - b * a.kv_heads;
-    const Segment seg = segment(a, b);
+    const int nth = pair / a.kv_heads, kv = pair - nth * a.kv_heads;
+    const Segment seg = segment(a, nth_longest(a, nth, threadIdx.x & 63));
     if (key >= seg.nk) return;
     const int tile = key / 128;
     const float *const from = g.part + ((int64_t)(pair * (int64_t)a.tiles + tile) * splits * 128 + key % 128) * (2 * D) + d;
