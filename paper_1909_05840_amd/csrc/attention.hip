@@ -192,14 +192,14 @@ __device__ __forceinline__ void write_row(uint16_t *row, const v16f (&o)[D / 32]
         }
 }
 
-// A workgroup does 128 rows, a wavefront 32 of them; tiles of 64 keys and values go through two stages in LDS, one under way
-// while the other is used.
+// A workgroup does 128 rows, a wavefront 32 of them; tiles of 64 keys and values go through a ring of stages in LDS, one used while the
+// others are under way (three where three workgroups fit a CU all the same).
 template <typename T, int D, bool DROP>
 __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uint16_t *O, float *lse, bool by_xcd)
 {
     typedef Rows<D> R;
-    constexpr int kTile = kKeys * R::kBytes;
-    __shared__ __align__(1024) uint8_t lds[2][2 * kTile];
+    constexpr int kTile = kKeys * R::kBytes, kStages = D == 64 ? 3 : 2, kCopies = 2 * kKeys / R::kPerCopy / 4;
+    __shared__ __align__(1024) uint8_t lds[kStages][2 * kTile];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place at = place(blockIdx.x, a.n_seqs * a.kv_heads, a.tiles, by_xcd);
@@ -247,13 +247,14 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uin
     const Operands<D> op(lane, lds0);
     Softmax<D> x;
     x.clear();
-    if (tiles) fetch(0, 0);
-    for (int t = 0; t < tiles; ++t) {
-        wait_copies<0>();
+    for (int t = 0; t < kStages - 1 && t < tiles; ++t) fetch(t, t);
+    for (int t = 0, stage = 0; t < tiles; ++t, stage = stage == kStages - 1 ? 0 : stage + 1) {
+        if (t + kStages - 1 <= tiles) wait_copies<(kStages - 2) * kCopies>();  // (the tiles behind this one may be under way)
+        else wait_copies<0>();
         barrier();
-        if (t + 1 < tiles) fetch(t + 1, (t + 1) & 1);
+        if (t + kStages - 1 < tiles) fetch(t + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
         const int left = wave_most - t * kKeys;
-        const uint32_t tk = (t & 1) * 2 * kTile;
+        const uint32_t tk = stage * 2 * kTile;
 constexpr bool kHalves = D == 64 && DROP;  // (without dropout's arithmetic to save, both in the kernel cost more: 177 -> 190 us for 8192 causal keys)
         if (left > (kHalves ? 32 : 0)) attend<T, D, DROP>(x, q, op, tk, tk + kTile, t * kKeys, limit, (t + 1) * kKeys > wave_least, a.c, bits, a.threshold, row_q, head, lane);
         else if (kHalves && left > 0) attend<T, D, DROP, 1>(x, q, op, tk, tk + kTile, t * kKeys, limit, t * kKeys + 32 > wave_least, a.c, bits, a.threshold, row_q, head, lane);

@@ -64,8 +64,8 @@ template <typename T, int D, bool DROP, bool EXACT>
 __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_kernel(const AttnArgs a, const GradArgs g, bool by_xcd)
 {
     typedef Rows<D> R;
-    constexpr int kTile = kKeys * R::kBytes;
-    __shared__ __align__(1024) uint8_t lds[2][2 * kTile];
+    constexpr int kTile = kKeys * R::kBytes, kStages = D == 64 ? 3 : 2, kCopies = 2 * kKeys / R::kPerCopy / 4;
+    __shared__ __align__(1024) uint8_t lds[kStages][2 * kTile];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (EXACT && blockIdx.x == 0 && threadIdx.x < 2) g.stat[threadIdx.x ? 2 * (int64_t)a.total_q * a.heads + 1 : (int64_t)a.total_q * a.heads] = threadIdx.x ? 0.0f : -__builtin_inff();
@@ -127,13 +127,14 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
     clear(A);
     clear(B);
     float eps = 0.0f;
-    if (tiles) fetch(0, 0);
-    for (int t = 0; t < tiles; ++t) {
-        wait_copies<0>();
+    for (int t = 0; t < kStages - 1 && t < tiles; ++t) fetch(t, t);
+    for (int t = 0, stage = 0; t < tiles; ++t, stage = stage == kStages - 1 ? 0 : stage + 1) {
+        if (t + kStages - 1 <= tiles) wait_copies<(kStages - 2) * kCopies>();  // (the tiles behind this one may be under way)
+        else wait_copies<0>();
         barrier();
-        if (t + 1 < tiles) fetch(t + 1, (t + 1) & 1);
+        if (t + kStages - 1 < tiles) fetch(t + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
         if (t * kKeys >= wave_most) continue;
-        const uint32_t tk = (t & 1) * 2 * kTile, tv = tk + kTile;
+        const uint32_t tk = stage * 2 * kTile, tv = tk + kTile;
         const bool masked = (t + 1) * kKeys > wave_least;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
