@@ -179,19 +179,6 @@ __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], co
     }
 }
 
-// O^T / l to a row of O: the lane holds four neighbouring values of its row at a time
-template <typename T, int D>
-__device__ __forceinline__ void write_row(uint16_t *row, const v16f (&o)[D / 32], float f, int hf)
-{
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int j = 0; j < 16; j += 4) {
-            const v2u w = {T::pair(o[i][j] * f, o[i][j + 1] * f), T::pair(o[i][j + 2] * f, o[i][j + 3] * f)};
-            *reinterpret_cast<v2u *>(row + 32 * i + 2 * j + 4 * hf) = w;
-        }
-}
-
 // A workgroup does 128 rows, a wavefront 32 of them; tiles of 64 keys and values go through a ring of stages in LDS, one used while the
 // others are under way (three where three workgroups fit a CU all the same).
 template <typename T, int D, bool DROP>
@@ -202,21 +189,16 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uin
     __shared__ __align__(1024) uint8_t lds[kStages][2 * kTile];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Place at = place(blockIdx.x, a.n_seqs * a.kv_heads, a.tiles, by_xcd);
-    if (at.pair >= a.n_seqs * a.kv_heads) return;
-    const int nth = at.pair / a.kv_heads, kv = at.pair - nth * a.kv_heads;
-    const Segment seg = segment(a, nth_longest(a, nth, lane));
+    const Place at = place<false>(a, blockIdx.x, a.tiles, by_xcd, true, lane);
+    if (at.none) return;
+    const int kv = at.kv;
+    const Segment &seg = at.seg;
     const int rows = seg.nq * a.group, first = at.tile * 128;
     if (first >= rows) return;
     const int row = first + wave * 32 + l32;
     const int token = min((unsigned)row / (unsigned)a.group, (unsigned)seg.nq - 1u);  // rows past the end compute the last token's, unstored
     const int head = kv * a.group + (row - (int)((unsigned)row / (unsigned)a.group) * a.group);
     const int row_q = seg.q0 + token;
-
-    v8s q[D / 16];
-    const uint16_t *const from = a.Q + (int64_t)row_q * a.q_row + (int64_t)head * a.q_head + 8 * hf;
-#pragma unroll
-    for (int d = 0; d < D / 16; ++d) q[d] = *reinterpret_cast<const v8s *>(from + 16 * d);
 
     // the keys that the lane's row, the wavefront's first and last row, and the workgroup's last row see
     const auto sees = [&](int t) { return a.causal ? min(seg.nk, max(0, seg.first_hidden(t))) : seg.nk; };
@@ -243,11 +225,17 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uin
         copy_rows<D, kKeys, 4>(to, wave, lane, [&](int r) { return K + (int64_t)min(tile * kKeys + r, seg.nk - 1) * a.k_row; });
         copy_rows<D, kKeys, 4>(to + kTile, wave, lane, [&](int r) { return V + (int64_t)min(tile * kKeys + r, seg.nk - 1) * a.v_row; });
     };
+    if (tiles > 0) fetch(0, 0);
+    v8s q[D / 16];
+    const uint16_t *const from = a.Q + (int64_t)row_q * a.q_row + (int64_t)head * a.q_head + 8 * hf;
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) q[d] = *reinterpret_cast<const v8s *>(from + 16 * d);
     const Threefry bits(DROP ? (uint64_t)*a.seed : 0);
     const Operands<D> op(lane, lds0);
     Softmax<D> x;
     x.clear();
-    for (int t = 0; t < kStages - 1 && t < tiles; ++t) fetch(t, t);
+    wait_copies<0>();  // the first products wait for Q and the first tile, not for what follows them
+    for (int t = 1; t < kStages - 1 && t < tiles; ++t) fetch(t, t);
     for (int t = 0, stage = 0; t < tiles; ++t, stage = stage == kStages - 1 ? 0 : stage + 1) {
         if (t + kStages - 1 <= tiles) wait_copies<(kStages - 2) * kCopies>();  // (the tiles behind this one may be under way)
         else wait_copies<0>();
@@ -259,10 +247,10 @@ constexpr bool kHalves = D == 64 && DROP;  // (without dropout's arithmetic to s
         if (left > (kHalves ? 32 : 0)) attend<T, D, DROP>(x, q, op, tk, tk + kTile, t * kKeys, limit, (t + 1) * kKeys > wave_least, a.c, bits, a.threshold, row_q, head, lane);
         else if (kHalves && left > 0) attend<T, D, DROP, 1>(x, q, op, tk, tk + kTile, t * kKeys, limit, t * kKeys + 32 > wave_least, a.c, bits, a.threshold, row_q, head, lane);
     }
-    if (row >= rows) return;
     const float l = halves_sum(x.l);
     const int64_t at_row = (int64_t)row_q * a.heads + head;
-    write_row<T, D>(O + at_row * D, x.o, l > 0.0f ? (DROP ? a.inv_share : 1.0f) / l : 0.0f, hf);
+    write_row<T, D>(O + at_row * D, x.o, l > 0.0f ? (DROP ? a.inv_share : 1.0f) / l : 0.0f, hf, row < rows);
+    if (row >= rows) return;
     if (hf == 0) lse[at_row] = l > 0.0f ? x.m * a.scale + __logf(l) : -__builtin_inff();
 }
 

@@ -39,42 +39,89 @@ __device__ __forceinline__ Segment segment(const AttnArgs &a, int b)
     // (whatever the arrays say, nothing outside the tensors is touched)
     s.q0 = s.q0 > 0 ? s.q0 : 0;
     s.k0 = s.k0 > 0 ? s.k0 : 0;
-    s.nq = (s.nq < a.total_q ? s.nq : a.total_q) - s.q0;
-    s.nk = (s.nk < a.total_k ? s.nk : a.total_k) - s.k0;
-    s.nk = s.nk > 0 ? s.nk : 0;
+    s.nq = max(0, (s.nq < a.total_q ? s.nq : a.total_q) - s.q0);
+    s.nk = max(0, (s.nk < a.total_k ? s.nk : a.total_k) - s.k0);
     return s;
 }
 
-// The nth longest sequence (of up to 64; of more, the nth): workgroups take the sequences in that order, so that those with the most tiles are
-// at work first and every CU gets some of either kind.
-__device__ __forceinline__ int nth_longest(const AttnArgs &a, int nth, int lane)
+// Which tile of which (sequence, key head) a workgroup does.  Workgroups are dealt to the eight XCDs in turn, each with an L2
+// of its own: where there are pairs enough, all tiles of a pair go to one XCD, which fetches its keys once.  Tiles with the
+// most work under a causal mask come first: the last rows, the first keys.  With 2 to 64 sequences a wavefront's lanes hold one
+// each: sequences come by their lengths, the longest first, and the tiles that there are take the first workgroups, so that
+// the empty ones of a ragged batch come last and cost next to nothing.
+struct Place {
+    int pair, tile;  // (pair: the sequence, or its rank by length, times kv_heads, and the key head)
+    Segment seg;
+    int kv;
+    bool none;
+};
+// KEYS: tiles of 128 keys, else of 128 rows; by_length: there is one workgroup to such a tile
+template <bool KEYS>
+__device__ __forceinline__ Place place(const AttnArgs &a, int id, int tiles, bool by_xcd, bool by_length, int lane)
 {
-    if (a.n_seqs == 1 || a.n_seqs > 64) return nth;
-    const int i = min(lane, a.n_seqs - 1), length = a.cu_q[i + 1] - a.cu_q[i] + a.cu_k[i + 1] - a.cu_k[i];
-    int before = 0;
+    Place p;
+    const int pairs = a.n_seqs * a.kv_heads;
+    if (a.n_seqs > 64 || a.n_seqs == 1 || !by_xcd || !by_length) {
+        const int i = by_xcd ? id >> 3 : id;
+        p.pair = by_xcd ? (i / tiles) * 8 + (id & 7) : id % pairs;
+        p.tile = by_xcd ? i % tiles : id / pairs;
+        if (!KEYS) p.tile = tiles - 1 - p.tile;
+        p.none = p.pair >= pairs;
+        const int b = p.none ? 0 : p.pair / a.kv_heads;
+        p.kv = p.pair - b * a.kv_heads;
+        p.seg = segment(a, b);
+        return p;
+    }
+    const Segment mine = segment(a, min(lane, a.n_seqs - 1));
+    const int length = mine.nq + mine.nk;
+    int rank = 0;
     for (int j = 0; j < a.n_seqs; ++j) {
         const int other = __builtin_amdgcn_readlane(length, j);
-        before += other > length || (other == length && j < lane);
+        rank += other > length || (other == length && j < lane);
     }
-    return __builtin_ctzll(__builtin_amdgcn_ballot_w64(before == nth && lane < a.n_seqs));
-}
-
-// Which tile of which (sequence, key head) a workgroup does.  Workgroups are dealt to the eight XCDs in turn, each with an L2
-// of its own: where there are pairs enough, all tiles of a pair go to one XCD, which fetches its keys once.  Tiles of the largest number
-// come first: with causal masks they see the most keys.
-struct Place {
-    int pair, tile;
-};
-__device__ __forceinline__ Place place(int id, int pairs, int tiles, bool by_xcd)
-{
-    if (by_xcd) {
-        const int i = id >> 3;
-        return {(i / tiles) * 8 + (id & 7), tiles - 1 - i % tiles};
+    const bool in = lane < a.n_seqs;
+    rank = in ? rank : lane;
+    const int count = !in ? 0 : KEYS ? (mine.nk + 127) >> 7 : (mine.nq * a.group + 127) >> 7;
+    // from here on a lane stands for a rank
+    const int n = __builtin_amdgcn_ds_permute(rank << 2, count), who = __builtin_amdgcn_ds_permute(rank << 2, lane);
+    const int xcd = id & 7, first = (xcd - lane * a.kv_heads) & 7, heads = first < a.kv_heads ? (a.kv_heads - first + 7) >> 3 : 0;  // of the rank's key heads on this XCD
+    const int items = n * heads;
+    int sum = items;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int before = __shfl_up(sum, o);
+        sum += lane >= o ? before : 0;
     }
-    return {id % pairs, tiles - 1 - id / pairs};
+    const int slot = id >> 3;
+    const uint64_t beyond = __builtin_amdgcn_ballot_w64(sum > slot);
+    p.none = beyond == 0;
+    if (p.none) return p;
+    const int r = __builtin_ctzll(beyond), of = __builtin_amdgcn_readlane(n, r), rest = slot - __builtin_amdgcn_readlane(sum - items, r);
+    const int nth = __builtin_amdgcn_readfirstlane(rest / of), seq = __builtin_amdgcn_readlane(who, r);
+    p.tile = KEYS ? rest - nth * of : of - 1 - (rest - nth * of);
+    p.kv = __builtin_amdgcn_readlane(first, r) + 8 * nth;
+    p.pair = r * a.kv_heads + p.kv;
+    p.seg = {__builtin_amdgcn_readlane(mine.q0, seq), __builtin_amdgcn_readlane(mine.nq, seq), __builtin_amdgcn_readlane(mine.k0, seq), __builtin_amdgcn_readlane(mine.nk, seq)};
+    return p;
 }
 inline bool deal_by_xcd(int64_t pairs) { return pairs % 8 == 0 || pairs >= 64; }
 inline int64_t dealt_workgroups(int64_t pairs, int64_t tiles) { return (deal_by_xcd(pairs) ? (pairs + 7) / 8 * 8 : pairs) * tiles; }
+
+// f times a row's D values, held as products hold them (value d of the row in the lane pair's result d), rounded to 16 bits, 16 bytes a store;
+// every lane of the wavefront calls it, and `write` is the same for both lanes of a row
+template <typename T, int D>
+__device__ __forceinline__ void write_row(uint16_t *row, const v16f (&o)[D / 32], float f, int hf, bool write)
+{
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; j += 8) {
+            const v2u low = {T::pair(o[i][j] * f, o[i][j + 1] * f), T::pair(o[i][j + 2] * f, o[i][j + 3] * f)};
+            const v2u high = {T::pair(o[i][j + 4] * f, o[i][j + 5] * f), T::pair(o[i][j + 6] * f, o[i][j + 7] * f)};
+            const v4u w = join_halves(low, high);
+            if (write) *reinterpret_cast<v4u *>(row + 32 * i + 2 * j + 8 * hf) = w;
+        }
+}
 
 qb_status attention_args(const qb_attention *p, AttnArgs &a);  // checks and converts
 

@@ -24,17 +24,6 @@ struct GradArgs {
     float *part;  // [pairs][tiles of keys][splits][128][dK, dV] of tiles in parts
 };
 
-template <typename T, int D>
-__device__ __forceinline__ void write_scaled(uint16_t *row, const v16f (&o)[D / 32], float f, int hf)
-{
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int j = 0; j < 16; j += 4) {
-            const v2u w = {T::pair(o[i][j] * f, o[i][j + 1] * f), T::pair(o[i][j + 2] * f, o[i][j + 3] * f)};
-            *reinterpret_cast<v2u *>(row + 32 * i + 2 * j + 4 * hf) = w;
-        }
-}
 template <int N>
 __device__ __forceinline__ void clear(v16f (&x)[N])
 {
@@ -69,10 +58,10 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (EXACT && blockIdx.x == 0 && threadIdx.x < 2) g.stat[threadIdx.x ? 2 * (int64_t)a.total_q * a.heads + 1 : (int64_t)a.total_q * a.heads] = threadIdx.x ? 0.0f : -__builtin_inff();
-    const Place at = place(blockIdx.x, a.n_seqs * a.kv_heads, a.tiles, by_xcd);
-    if (at.pair >= a.n_seqs * a.kv_heads) return;
-    const int nth = at.pair / a.kv_heads, kv = at.pair - nth * a.kv_heads;
-    const Segment seg = segment(a, nth_longest(a, nth, lane));
+    const Place at = place<false>(a, blockIdx.x, a.tiles, by_xcd, true, lane);
+    if (at.none) return;
+    const int kv = at.kv;
+    const Segment &seg = at.seg;
     const int rows = seg.nq * a.group, first = at.tile * 128;
     if (first >= rows) return;
     const int row = first + wave * 32 + l32;
@@ -211,8 +200,8 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
 #pragma unroll
             for (int j = 0; j < 16; ++j) A[i][j] -= eps * B[i][j];
     }
+    write_row<T, D>(g.dQ + (int64_t)row_q * g.q_row + (int64_t)head * g.q_head, A, a.scale, hf, row < rows);
     if (row >= rows) return;
-    write_scaled<T, D>(g.dQ + (int64_t)row_q * g.q_row + (int64_t)head * g.q_head, A, a.scale, hf);
     if (hf == 0) {
         g.stat[at_row] = lse > -__builtin_inff() ? -lse / a.scale : -__builtin_inff();
         g.stat[(int64_t)a.total_q * a.heads + 1 + at_row] = -delta;
@@ -263,11 +252,11 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
     __shared__ __align__(1024) uint8_t lds[kStages][kStage];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Place at = place(blockIdx.x, a.n_seqs * a.kv_heads, a.tiles * splits, by_xcd);
-    if (at.pair >= a.n_seqs * a.kv_heads) return;
-    const int nth = at.pair / a.kv_heads, kv = at.pair - nth * a.kv_heads;
-    const Segment seg = segment(a, nth_longest(a, nth, lane));
-    const int rank = a.tiles * splits - 1 - at.tile, part = rank / a.tiles, key_tile = rank - part * a.tiles;  // part after part
+    const Place at = place<true>(a, blockIdx.x, a.tiles * splits, by_xcd, splits == 1, lane);
+    if (at.none) return;
+    const int kv = at.kv;
+    const Segment &seg = at.seg;
+    const int part = splits == 1 ? 0 : at.tile / a.tiles, key_tile = at.tile - part * a.tiles;  // part after part
     const int first = key_tile * 128;
     if (first >= seg.nk) return;
     const RowTiles todo = row_tiles(a, tiling, seg, first, part, most);
@@ -496,8 +485,8 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
         place_of(++t, token, head);
         stage = next;
     }
-    if (key >= seg.nk) return;
     if (todo.parts > 1) {
+        if (key >= seg.nk) return;
         float *const to = g.part + ((int64_t)((at.pair * (int64_t)a.tiles + key_tile) * splits + part) * 128 + key - first) * (2 * D);
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
@@ -508,8 +497,8 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
             }
         return;
     }
-    write_scaled<T, D>(g.dK + (int64_t)(seg.k0 + key) * g.k_row + (int64_t)kv * g.k_head, dK, a.scale, hf);
-    write_scaled<T, D>(g.dV + (int64_t)(seg.k0 + key) * g.v_row + (int64_t)kv * g.v_head, dV, DROP ? a.inv_share : 1.0f, hf);
+    write_row<T, D>(g.dK + (int64_t)(seg.k0 + key) * g.k_row + (int64_t)kv * g.k_head, dK, a.scale, hf, key < seg.nk);
+    write_row<T, D>(g.dV + (int64_t)(seg.k0 + key) * g.v_row + (int64_t)kv * g.v_head, dV, DROP ? a.inv_share : 1.0f, hf, key < seg.nk);
 }
 
 // dK and dV of 16 keys from their parts; a thread does eight neighbouring values
@@ -519,8 +508,8 @@ __global__ __launch_bounds__(256) void attention_dkv_join_kernel(const AttnArgs 
     constexpr int kEach = 2 * D / 8;  // threads to a key
     const int pair = blockIdx.x / (a.tiles * (128 * kEach / 256)), in_pair = blockIdx.x - pair * (a.tiles * (128 * kEach / 256));
     const int id = in_pair * 256 + threadIdx.x, key = id / kEach, d = (id - key * kEach) * 8;
-    const int nth = pair / a.kv_heads, kv = pair - nth * a.kv_heads;
-    const Segment seg = segment(a, nth_longest(a, nth, threadIdx.x & 63));
+    const int b = pair / a.kv_heads, kv = pair - b * a.kv_heads;
+    const Segment seg = segment(a, b);
     if (key >= seg.nk) return;
     const int tile = key / 128;
     const float *const from = g.part + ((int64_t)(pair * (int64_t)a.tiles + tile) * splits * 128 + key % 128) * (2 * D) + d;
