@@ -507,8 +507,9 @@ qb_status qb_attention_bwd(const qb_attention *a, const void *dO, const void *O,
  *   dX[t] = sum_v d[t,v] W[v],  dW[v] = sum_t d[t,v] X[t],  dbias[v] = sum_t d[t,v]
  *   lse as the forward wrote it, dloss [T] fp32 (finite);  dX [T,K], dW [V,K] bfloat16, dbias [V] fp32 or NULL; overwritten
  * d is held in bfloat16, relative to the largest |dloss| and so exact in the weight of a mean over tokens.
- * Base pointers and the workspace (qb_vocab_loss_workspace_nbytes(T,V,K, 0 forward / 1 backward) bytes): 16- and 256-byte aligned.  The backward
- * works through the vocabulary in pieces, d of one piece at a time.  The same call gives the same bits every time.
+ * X, W, dX, dW are 16-byte aligned, the workspace (qb_vocab_loss_workspace_nbytes(T,V,K, 0 forward / 1 backward) bytes) 256-byte aligned, the
+ * rest as their types.  The backward works through the vocabulary in pieces, d of one piece at a time.  The same call gives the
+ * same bits every time.
  * QB_ERR_SHAPE: T or V below 1 or above 2^24, K no multiple of QB_K_ALIGN or above QB_MAX_K.
  */
 size_t qb_vocab_loss_workspace_nbytes(int64_t T, int64_t V, int64_t K, int backward);

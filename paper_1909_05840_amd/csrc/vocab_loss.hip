@@ -701,7 +701,7 @@ extern "C" qb_status qb_vocab_loss_fwd(const uint16_t *X, const uint16_t *W, con
 {
     if (!shape_ok(T, V, K)) return QB_ERR_SHAPE;
     if (!X || !W || !targets || !loss || !lse) return QB_ERR_NULL;
-    if (!aligned16(X) || !aligned16(W) || !aligned16(bias) || !aligned16(targets)) return QB_ERR_VALUE;
+    if (!aligned16(X) || !aligned16(W) || (reinterpret_cast<uintptr_t>(targets) & 7)) return QB_ERR_VALUE;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255)) return QB_ERR_WORKSPACE;
     LossArgs a = {};
     a.X = X; a.W = W; a.bias = bias; a.targets = targets;
@@ -718,7 +718,7 @@ extern "C" qb_status qb_vocab_loss_bwd(const float *dloss, const uint16_t *X, co
 {
     if (!shape_ok(T, V, K)) return QB_ERR_SHAPE;
     if (!dloss || !X || !W || !targets || !lse || !dX || !dW) return QB_ERR_NULL;
-    if (!aligned16(X) || !aligned16(W) || !aligned16(bias) || !aligned16(targets) || !aligned16(dX) || !aligned16(dW)) return QB_ERR_VALUE;
+    if (!aligned16(X) || !aligned16(W) || !aligned16(dX) || !aligned16(dW) || (reinterpret_cast<uintptr_t>(targets) & 7)) return QB_ERR_VALUE;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255)) return QB_ERR_WORKSPACE;
     LossArgs a = {};
     a.X = X; a.W = W; a.bias = bias; a.targets = targets; a.dloss = dloss;

@@ -192,3 +192,16 @@ def test_refusals(qb):
                 lambda: qb.qb_vocab_loss_fwd(c.X, c.W, c.targets, workspace=torch.empty(8, dtype=torch.uint8, device=DEV))):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_targets_and_bias_from_any_place(qb):
+    """A part of a longer tensor of targets (the next words of a text) starts anywhere."""
+    c = Case(20, 50, 64)
+    inside = lambda x: torch.cat([x[:1], x])[1:]  # noqa: E731
+    targets, bias = inside(c.targets), inside(c.bias)
+    assert targets.data_ptr() % 16 and bias.data_ptr() % 16
+    want = qb.qb_vocab_loss_fwd(c.X, c.W, c.targets, bias=c.bias)
+    got = qb.qb_vocab_loss_fwd(c.X, c.W, targets, bias=bias)
+    want += qb.qb_vocab_loss_bwd(c.dloss, c.X, c.W, c.targets, want[1], bias=c.bias)
+    got += qb.qb_vocab_loss_bwd(c.dloss, c.X, c.W, targets, got[1], bias=bias)
+    assert all(torch.equal(x, y) for x, y in zip(want, got))
