@@ -43,12 +43,12 @@ __device__ __forceinline__ v8s rounded(const v16f &x, int half)
 
 // dQ and delta; 128 rows to a workgroup, 32 to a wavefront, a lane's results all of one row (as in the forward).
 //
-// delta = dO.O takes O as the forward rounded it.  Where few keys carry a row's weight that error is as large as the rounding
-// of dS (384 keys of random scores of deviation 2: together 1.5 times the error of exact arithmetic rounded once).  EXACT therefore
-// sums eps = sum_k P (dP - delta) on the way, which is what delta lacks, and B = sum_k P K beside A = sum_k dS K: dQ = scale (A - eps B),
-// and the second launch gets delta + eps.  With many keys |O| is small beside |V|, and the rounding with it: tiles of rows that see more than
-// kExactKeys are left to the other variant, which needs two thirds of the registers and six sevenths of the products.
-constexpr int kExactKeys = 1024;
+// delta = dO.O takes O as the forward rounded it, which moves dQ by -eps sum_k P K.  EXACT therefore sums eps = sum_k P (dP - delta)
+// on the way, which is what delta lacks, and B = sum_k P K beside A = sum_k dS K: dQ = scale (A - eps B), and the second launch gets
+// delta + eps.  Without it dQ is 1.5 to 1.6 times as far from exact as exact arithmetic rounded once at dim 64, whatever the number
+// of keys (dS in 16 bits alone makes 1.41), and so at dim 128 with few; with many keys it is 1.43 to 1.49 times there, and tiles of rows that see
+// more than kExactKeys are left to the other variant, which needs two thirds of the registers and six sevenths of the products.
+template <int D> constexpr int kExactKeys = D == 64 ? INT32_MAX : 1024;
 template <typename T, int D, bool DROP, bool EXACT>
 __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_kernel(const AttnArgs a, const GradArgs g, bool by_xcd)
 {
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
     const int wave_least = __builtin_amdgcn_readfirstlane(sees(token_of(first + wave * 32)));
     const int wave_most = first + wave * 32 < rows ? __builtin_amdgcn_readfirstlane(sees(token_of(first + wave * 32 + 31))) : 0;  // (a wavefront without rows only copies)
     const int most = __builtin_amdgcn_readfirstlane(sees(token_of(first + 127)));
-    if (EXACT != (most <= kExactKeys)) return;
+    if (EXACT != (most <= kExactKeys<D>)) return;
     const int tiles = (most + kKeys - 1) / kKeys;
 
     const uint16_t *const K = a.K + (int64_t)seg.k0 * a.k_row + (int64_t)kv * a.k_head;
@@ -553,7 +553,7 @@ qb_status backward(AttnArgs a, const GradArgs &g, int64_t max_q, int64_t max_k, 
         if (grid > INT32_MAX / 256) return QB_ERR_SHAPE;
         if (drop) attention_dq_kernel<T, D, true, true><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
         else attention_dq_kernel<T, D, false, true><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
-        if (max_k > kExactKeys) {
+        if constexpr (D == 128) if (max_k > kExactKeys<D>) {
             if (drop) attention_dq_kernel<T, D, true, false><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
             else attention_dq_kernel<T, D, false, false><<<(int)grid, 256, 0, stream>>>(a, g, by_xcd);
         }

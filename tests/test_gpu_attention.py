@@ -337,3 +337,20 @@ def test_refusals(qb):
         c.backward(qb, O, lse, dK=c.V[:-1])
     with pytest.raises(TypeError):
         c.backward(qb, O.half(), lse)
+
+
+def test_rounding_of_o_does_not_reach_dq(qb):
+    """dS in 16 bits and dQ in 16 bits: two roundings of equal size, sqrt(2) of one.  delta takes the rounded O, and what that does to dQ would
+    add a tenth more at dim 64 (in squares: a quarter) with keys of any number; it is taken out, up to a twentieth."""
+    torch.manual_seed(11)
+    n, heads, dim = 1500, 4, 64
+    q, k, v, do = (torch.randn(n, heads, dim, device="cuda").bfloat16() for _ in range(4))
+    cu = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    O, lse = qb.qb_attention_fwd(q, k, v, cu, cu, n, n)
+    dQ = qb.qb_attention_bwd(do, q, k, v, O, lse, cu, cu, n, n)[0]
+    x, y, z, g = (t.double().transpose(0, 1) for t in (q, k, v, do))
+    p = torch.softmax(x @ y.transpose(1, 2).contiguous() * dim ** -0.5, -1)
+    dp = g @ z.transpose(1, 2).contiguous()
+    want = ((p * (dp - (p * dp).sum(-1, keepdim=True))) @ y * dim ** -0.5).transpose(0, 1)
+    once = (want.bfloat16().double() - want).norm()
+    assert (dQ.double() - want).norm() < 1.05 * 2 ** 0.5 * once
