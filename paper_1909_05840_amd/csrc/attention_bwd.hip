@@ -527,17 +527,21 @@ __global__ __launch_bounds__(256) void attention_dkv_join_kernel(const AttnArgs 
     *reinterpret_cast<v4u *>(to) = v4u{T::pair(x[0][0] * f, x[0][1] * f), T::pair(x[0][2] * f, x[0][3] * f), T::pair(x[1][0] * f, x[1][1] * f), T::pair(x[1][2] * f, x[1][3] * f)};
 }
 
-// How many tiles of rows a part has at most: such that the longest sequences' parts come to about kParts workgroups (three fit a CU:
-// two rounds of them even out what differs), but eight or more; and the most parts of a tile of keys
-constexpr int64_t kParts = 1536;
+// How many tiles of rows a part has at most: such that the parts come to about as many workgroups as this, but eight or more; and the
+// most parts of a tile of keys.  Parts even out what tiles of keys have to do, and fill the CUs (two workgroups to each) where tiles are few:
+// 8192 causal keys, 4 key heads of 64, whole backward: unsplit 842 us, for 256 workgroups 705, 512 668, 768 614, 1536 614.  But each part's sums are
+// written and read again, 4 * 128 * 2 * dim bytes: 8 heads of 128 over 4000 keys 244 us unsplit and for 256, for 512 274, 768 287; 2 x 4000 causal, 4 key heads
+// of 128: 719 unsplit, 576 for 256, 645 for 512.
+inline int64_t parts_wanted(int dim) { return dim == 64 ? 768 : 256; }
 struct Parts {
     int64_t most, splits;
 };
-inline Parts row_parts(int64_t pairs, int64_t max_q, int64_t group, int64_t max_k, bool causal)
+inline Parts row_parts(int64_t pairs, int64_t max_q, int64_t group, int64_t max_k, bool causal, int dim)
 {
     const RowTiling t = row_tiling((int)group);
-    const int64_t tiles = pairs * ((max_k + 127) / 128), rows = (max_q + t.tokens - 1) / t.tokens * t.chunks;
-    const int64_t most = std::max<int64_t>(8, tiles * rows / (causal ? 2 : 1) / kParts);
+    const int64_t tiles = pairs * ((max_k + 127) / 128), rows = (max_q + t.tokens - 1) / t.tokens * t.chunks, wanted = parts_wanted(dim);
+    if (tiles > INT32_MAX / 256) return {rows, 1};  // (more than a launch takes: refused)
+    const int64_t most = std::max<int64_t>(8, (tiles * rows / (causal ? 2 : 1) + wanted - 1) / wanted);
     return {most, std::max<int64_t>(1, (rows + most - 1) / most)};
 }
 inline size_t stat_bytes(const qb_attention *p) { return ((size_t)(p->total_q * p->heads + 1) * 8 + 255) / 256 * 256; }
@@ -560,7 +564,7 @@ qb_status backward(AttnArgs a, const GradArgs &g, int64_t max_q, int64_t max_k, 
     }
     if (max_k > 0) {
         a.tiles = (int)((max_k + 127) / 128);
-        const Parts parts = row_parts(pairs, max_q, a.group, max_k, a.causal);
+        const Parts parts = row_parts(pairs, max_q, a.group, max_k, a.causal, D);
         const int splits = (int)parts.splits, most = (int)parts.most;
         const int64_t grid = dealt_workgroups(pairs, (int64_t)a.tiles * splits);
         if (drop) attention_dkv_kernel<T, D, true><<<(int)grid, 256, 0, stream>>>(a, g, row_tiling(a.group), splits, most, by_xcd);
@@ -579,7 +583,7 @@ extern "C" size_t qb_attention_bwd_workspace_nbytes(const qb_attention *p)
 {
     AttnArgs a;
     if (attention_args(p, a) != QB_OK) return 0;
-    const int64_t pairs = (int64_t)a.n_seqs * a.kv_heads, splits = row_parts(pairs, p->max_q, a.group, p->max_k, p->causal).splits;
+    const int64_t pairs = (int64_t)a.n_seqs * a.kv_heads, splits = row_parts(pairs, p->max_q, a.group, p->max_k, p->causal, p->dim).splits;
     return stat_bytes(p) + (splits > 1 ? (size_t)(pairs * ((p->max_k + 127) / 128) * splits) * 128 * 2 * p->dim * 4 : 0);
 }
 
@@ -597,7 +601,7 @@ extern "C" qb_status qb_attention_bwd(const qb_attention *p, const void *dO, con
     if (!aligned16(dO) || !aligned16(O) || !aligned16(grads->dQ) || !aligned16(grads->dK) || !aligned16(grads->dV)) return QB_ERR_VALUE;
     if (p->total_q > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255))) return QB_ERR_WORKSPACE;
     const int64_t pairs = (int64_t)p->n_seqs * p->kv_heads;
-    if (dealt_workgroups(pairs, (p->max_q * a.group + 127) / 128) > INT32_MAX / 256 || dealt_workgroups(pairs, (p->max_k + 127) / 128 * row_parts(pairs, p->max_q, a.group, p->max_k, p->causal).splits) > INT32_MAX / 256) return QB_ERR_SHAPE;
+    if (dealt_workgroups(pairs, (p->max_q * a.group + 127) / 128) > INT32_MAX / 256 || dealt_workgroups(pairs, (p->max_k + 127) / 128 * row_parts(pairs, p->max_q, a.group, p->max_k, p->causal, p->dim).splits) > INT32_MAX / 256) return QB_ERR_SHAPE;
     const GradArgs g = {static_cast<const uint16_t *>(dO), static_cast<const uint16_t *>(O), lse, static_cast<uint16_t *>(grads->dQ), static_cast<uint16_t *>(grads->dK),
                         static_cast<uint16_t *>(grads->dV), grads->q_row, grads->q_head, grads->k_row, grads->k_head, grads->v_row, grads->v_head, static_cast<float *>(workspace), reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + stat_bytes(p))};
     const hipStream_t st = static_cast<hipStream_t>(stream);
