@@ -18,7 +18,8 @@ qb_status attention_args(const qb_attention *p, AttnArgs &a)
     if (!p) return QB_ERR_NULL;
     if (p->total_q < 0 || p->total_k < 0 || p->total_q > INT32_MAX - 4096 || p->total_k > INT32_MAX - 4096 || p->n_seqs < 0 || p->heads <= 0 ||
         p->kv_heads <= 0 || p->heads % p->kv_heads != 0 || p->heads > (1 << 16) || (p->dim != 64 && p->dim != 128) || p->max_q < 0 || p->max_k < 0 ||
-        p->max_q > INT32_MAX || p->max_k > INT32_MAX - 4096 || p->max_q * (p->heads / p->kv_heads) >= (1 << 30))
+        p->max_q > INT32_MAX || p->max_k > INT32_MAX - 4096 || p->max_q * (p->heads / p->kv_heads) >= (1 << 30) ||
+        (int64_t)p->n_seqs * p->kv_heads > INT32_MAX)
         return QB_ERR_SHAPE;
     if ((p->type != QB_TYPE_BF16 && p->type != QB_TYPE_FP16) || !(p->scale > 0.0f) || !std::isfinite(p->scale * 1.5f) || !(p->p >= 0.0f && p->p < 1.0f) ||
         (p->q_row | p->q_head | p->k_row | p->k_head | p->v_row | p->v_head) % 8 != 0)
@@ -398,9 +399,11 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a, u
     if (lane == 0) lse[at_row] = l > 0.0f ? m * a.scale + __logf(l) : -__builtin_inff();
 }
 
-// Few rows (without dropout, which serving has none of): up to kFewRows of a key head.  The chunks: as many as fill the GPU with
-// about 2048 workgroups, half of which find no keys where lengths differ, of 512 keys or more.
-constexpr int64_t kFewRows = 64;
+// Few rows (without dropout, which serving has none of): up to 32 of a key head, or more where the other kernel would leave most CUs idle: it
+// reads the keys once for 128 rows but has one workgroup for them.  16 sequences of 4096 keys, 8 key heads of 128: 32 rows 64 us here, 80 there; 64 rows 120
+// here, 82 there, and 128 rows 222 and 82.  What it takes is that of one workgroup, what this one takes grows with the tiles of 32 rows: even at about 170.
+// The chunks: as many as fill the GPU with about 2048 workgroups, half of which find no keys where lengths differ, of 512 keys or more.
+constexpr int64_t kFewTiles = 160;
 struct Chunks {
     int64_t size, count;
 };
@@ -412,7 +415,11 @@ inline Chunks chunks_of(int64_t pairs, int64_t max_k)
     c.count = std::max<int64_t>(1, (max_k + c.size - 1) / c.size);
     return c;
 }
-inline bool few_rows(const AttnArgs &a, const qb_attention *p) { return p->max_q * a.group <= kFewRows && !(p->p > 0.0f); }
+inline bool few_rows(const AttnArgs &a, const qb_attention *p)
+{
+    const int64_t tiles = (p->max_q * a.group + 31) / 32;
+    return (tiles <= 1 || tiles * a.n_seqs * a.kv_heads <= kFewTiles) && !(p->p > 0.0f);
+}
 
 template <typename T, int D>
 qb_status forward_few(AttnArgs a, int64_t max_q, int64_t max_k, void *O, float *lse, void *workspace, hipStream_t stream)
