@@ -3,14 +3,14 @@
 //   Y[i] = X[i] * m[i] (+ residual[i]),  dX[i] = dY[i] * m[i],  m[i] = 0 or 65536 / (65536 - t)
 //
 // Bound by memory: three tensors of traffic forward, two backward.  A counter's four draws cost about 60 instructions, 15 a
-// value, against the 2 to 12 bytes that it moves.
+// value, against the 2 to 12 bytes that it moves.  32768 x 1024 bfloat16: 35 us with the residual (5.8 TB/s), 25 us without (5.4).
 #include "qb_tiles.hpp"
 #include <cmath>
 
 namespace qb {
 namespace {
 
-constexpr int kAtOnce = 4;  // chunks of sixteen bytes that a thread has under way
+constexpr int kAtOnce = 4;  // chunks of sixteen bytes that a thread has under way, so that the loads' latency is hidden
 
 struct DropArgs {
     const void *X, *residual;
