@@ -69,12 +69,14 @@ __device__ __forceinline__ void copy16(const void *from, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory", "m0");
 }
-// the same with the address as a base that the wavefront shares and an offset in bytes
+// the same with the address as a base that the wavefront shares and an offset in bytes (the base is moved into registers of the block's
+// own by a scalar instruction: a vector memory instruction may read what a VALU instruction wrote five wait states later only)
 __device__ __forceinline__ void copy16(const void *base, uint32_t offset, uint32_t lds)
 {
     const uint64_t at = reinterpret_cast<uint64_t>(base);  // (a quotient of uniform values lies in a vector register)
     const uint64_t uniform = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)) << 32;
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(uniform), "s"(lds) : "memory", "m0");
+    uint64_t own;
+    asm volatile("s_mov_b32 m0, %3\n\ts_mov_b64 %0, %1\n\tglobal_load_lds_dwordx4 %2, %0" : "=&s"(own) : "s"(uniform), "v"(offset), "s"(lds) : "memory", "m0");
 }
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p; }
 
