@@ -354,3 +354,31 @@ def test_rounding_of_o_does_not_reach_dq(qb):
     want = ((p * (dp - (p * dp).sum(-1, keepdim=True))) @ y * dim ** -0.5).transpose(0, 1)
     once = (want.bfloat16().double() - want).norm()
     assert (dQ.double() - want).norm() < 1.05 * 2 ** 0.5 * once
+
+
+def crowd(type, dim, heads, kv_heads, q_lens, k_lens=None, **more):
+    """The same sequences again and again, until there are tiles enough for the kernel of many rows."""
+    tiles = (max(q_lens) * heads // kv_heads + 31) // 32
+    times = 160 // (len(q_lens) * kv_heads * tiles) + 1
+    return dict(type=type, dim=dim, heads=heads, kv_heads=kv_heads, q_lens=q_lens * times, k_lens=k_lens and k_lens * times, **more)
+
+
+CROWDS = {"crowd: " + n: crowd(**FORWARD[n]) for n in ("lengths round a tile", "the same, causal", "wide heads, groups of three", "groups of seven, fp16", "empty sequences",
+                                                       "more queries than keys, causal", "more keys than queries, causal", "large scores", "many short sequences")}
+CROWDS["one sequence, many heads"] = dict(type="bf16", dim=64, heads=24, kv_heads=24, q_lens=[300], causal=True, fused=True)
+CROWDS["one sequence, many heads, wide"] = dict(type="fp16", dim=128, heads=48, kv_heads=12, q_lens=[131], k_lens=[270])
+CROWDS["cache, a prompt in pieces"] = dict(type="bf16", dim=64, heads=8, kv_heads=4, q_lens=[129, 1, 200, 64], k_lens=[129, 700, 333, 64], cap=710, causal=True)
+
+
+@pytest.mark.parametrize("name", CROWDS)
+def test_forward_of_many_rows(qb, name):
+    say("attention forward:", name)
+    c = Case(**CROWDS[name])
+    O = torch.full(c.Q.shape, float("nan"), dtype=c.dtype, device=DEV)
+    lse = torch.full(c.Q.shape[:2], float("nan"), device=DEV)
+    c.forward(qb, O=O, lse=lse)
+    val, tol = c.exact()
+    check("O", O, val["O"], tol["O"])
+    check("lse", lse, val["lse"], tol["lse"])
+    again = c.forward(qb)
+    assert torch.equal(again[0], O) and torch.equal(again[1], lse)
