@@ -231,16 +231,17 @@ inline RowTiling row_tiling(int group)
 }
 // The tiles that a tile of 128 keys is seen by are cut into parts of `most` tiles, from the last row on (with causal masks the first keys
 // are seen by many more rows than the last, but all by the last rows): part p of every tile of keys is the same rows, and the
-// workgroups that are at work together, which take the parts in turn, find them in their L2.
+// workgroups that are at work together, which take the parts in turn, find them in their L2.  There are at most `splits` parts, for which the
+// workspace has room, however long the sequence is.
 struct RowTiles {
     int begin, end, parts;
 };
-__device__ __forceinline__ RowTiles row_tiles(const AttnArgs &a, const RowTiling &r, const Segment &seg, int first_key, int part, int most)
+__host__ __device__ __forceinline__ RowTiles row_tiles(bool causal, const RowTiling &r, int nq, int nk, int first_key, int part, int most, int splits)
 {
-    const int nq = max(0, seg.nq), token = a.causal ? min(nq, max(0, first_key - (seg.nk - seg.nq))) : 0;  // causal: key <= token + nk - nq
+    const int token = causal ? min(nq, max(0, first_key - (nk - nq))) : 0;  // causal: key <= token + nk - nq
     const int all = (nq + r.tokens - 1) / r.tokens, first = token < nq ? token / r.tokens : all;
     const int n = (all - first) * r.chunks, end = all * r.chunks - part * most;
-    return {max(first * r.chunks, end - most), end, max(1, (n + most - 1) / most)};
+    return {max(first * r.chunks, end - most), end, max(1, min(splits, (n + most - 1) / most))};
 }
 
 // dK and dV; 128 keys to a workgroup, 32 to a wavefront: a lane's results all of one key.  Where tiles of keys are few, a workgroup does
@@ -263,7 +264,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
     const int part = splits == 1 ? 0 : at.tile / a.tiles, key_tile = at.tile - part * a.tiles;  // part after part
     const int first = key_tile * 128;
     if (first >= seg.nk) return;
-    const RowTiles todo = row_tiles(a, tiling, seg, first, part, most);
+    const RowTiles todo = row_tiles(a.causal, tiling, seg.nq, seg.nk, first, part, most, splits);
     if (part >= todo.parts) return;
     const int begin = __builtin_amdgcn_readfirstlane(todo.begin), end = __builtin_amdgcn_readfirstlane(todo.end);
     const int key = first + wave * 32 + l32, key_in = min(key, seg.nk - 1);
@@ -518,7 +519,7 @@ __global__ __launch_bounds__(256) void attention_dkv_join_kernel(const AttnArgs 
     const int tile = key / 128;
     const float *const from = g.part + ((int64_t)(pair * (int64_t)a.tiles + tile) * splits * 128 + key % 128) * (2 * D) + d;
     v4f x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-    const int parts = min(splits, row_tiles(a, tiling, seg, tile * 128, 0, most).parts);
+    const int parts = row_tiles(a.causal, tiling, seg.nq, seg.nk, tile * 128, 0, most, splits).parts;
     if (parts == 1) return;  // (written whole)
 #pragma unroll 4
     for (int p = 0; p < parts; ++p) {
@@ -579,6 +580,16 @@ qb_status backward(AttnArgs a, const GradArgs &g, int64_t max_q, int64_t max_k, 
 }
 
 }  // namespace
+
+// Parts that the dK and dV of a tile of keys are written in, for a sequence of nq queries and nk keys in a call of these sizes; `reserved`:
+// the parts that its workspace has room for.
+int attention_row_parts(int64_t pairs, int64_t group, int64_t max_q, int64_t max_k, bool causal, int dim, int nq, int nk, int first_key, int *reserved)
+{
+    const Parts p = row_parts(pairs, max_q, group, max_k, causal, dim);
+    *reserved = (int)p.splits;
+    return row_tiles(causal, row_tiling((int)group), nq, nk, first_key, 0, (int)p.most, (int)p.splits).parts;
+}
+
 }  // namespace qb
 
 using namespace qb;

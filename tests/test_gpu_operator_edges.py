@@ -1,0 +1,35 @@
+"""Attention, vocabulary loss and dropout where a call goes to an edge of what its interface allows."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def offsets(*lens):
+    return torch.tensor([sum(lens[:i]) for i in range(len(lens) + 1)], dtype=torch.int32, device=DEV)
+
+
+@pytest.mark.parametrize("max_q", [0, 500])
+def test_sequences_longer_than_named_leave_the_memory_behind_the_workspace(qb, max_q):
+    """their results are undefined, but nothing is written beyond the workspace that belongs to the call"""
+    say("attention backward, 700 queries where", max_q, "were named")
+    import ctypes
+    n, heads, dim = 700, 12, 64
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    q, k, v, do = (torch.randn(n, heads, dim, generator=g, device=DEV).bfloat16() for _ in range(4))
+    cu = offsets(n)
+    O, lse = qb.qb_attention_fwd(q, k, v, cu, cu, n, n)
+    a = qb.binding.Attention(Q=q.data_ptr(), K=k.data_ptr(), V=v.data_ptr(), q_row=768, q_head=64, k_row=768, k_head=64, v_row=768, v_head=64, type=0, heads=heads, kv_heads=heads,
+                             dim=dim, total_q=n, total_k=n, n_seqs=1, cu_q=cu.data_ptr(), cu_k=cu.data_ptr(), max_q=max_q, max_k=n, scale=0.125)
+    room = qb.load_library().qb_attention_bwd_workspace_nbytes(ctypes.byref(a))
+    parts = 6 * heads * 2 * 128 * 2 * dim * 4  # of two parts of every tile of keys
+    workspace = torch.full((room + parts,), 77, dtype=torch.uint8, device=DEV)
+    for x in qb.qb_attention_bwd(do, q, k, v, O, lse, cu, cu, max_q, n, workspace=workspace):
+        assert x.shape == q.shape
+    assert (workspace[room:] == 77).all()
