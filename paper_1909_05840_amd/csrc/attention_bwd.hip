@@ -614,7 +614,7 @@ extern "C" qb_status qb_attention_bwd(const qb_attention *p, const void *dO, con
     if (p->total_q > 0 && (!dO || !O || !lse || !grads->dQ)) return QB_ERR_NULL;
     if (p->total_k > 0 && (!grads->dK || !grads->dV)) return QB_ERR_NULL;
     if (!aligned16(dO) || !aligned16(O) || !aligned16(grads->dQ) || !aligned16(grads->dK) || !aligned16(grads->dV)) return QB_ERR_VALUE;
-    if (p->total_q > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255))) return QB_ERR_WORKSPACE;
+    if ((p->total_q > 0 || p->max_q > 0) && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255))) return QB_ERR_WORKSPACE;
     const int64_t pairs = (int64_t)p->n_seqs * p->kv_heads;
     if (dealt_workgroups(pairs, (p->max_q * a.group + 127) / 128) > INT32_MAX / 256 || dealt_workgroups(pairs, (p->max_k + 127) / 128 * row_parts(pairs, p->max_q, a.group, p->max_k, p->causal, p->dim).splits) > INT32_MAX / 256) return QB_ERR_SHAPE;
     const GradArgs g = {static_cast<const uint16_t *>(dO), static_cast<const uint16_t *>(O), lse, static_cast<uint16_t *>(grads->dQ), static_cast<uint16_t *>(grads->dK),

@@ -33,3 +33,14 @@ def test_sequences_longer_than_named_leave_the_memory_behind_the_workspace(qb, m
     for x in qb.qb_attention_bwd(do, q, k, v, O, lse, cu, cu, max_q, n, workspace=workspace):
         assert x.shape == q.shape
     assert (workspace[room:] == 77).all()
+
+
+def test_keys_without_queries_have_no_gradient(qb):
+    """no query in the whole tensor, with max_q as an upper bound"""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    q, k, v = (torch.randn(n, 4, 64, generator=g, device=DEV).bfloat16() for n in (0, 100, 100))
+    O, lse = qb.qb_attention_fwd(q, k, v, offsets(0, 0), offsets(70, 30), 40, 70)
+    grads = [torch.full_like(x, float("nan")) for x in (q, k, v)]
+    qb.qb_attention_bwd(q, q, k, v, O, lse, offsets(0, 0), offsets(70, 30), 40, 70, dQ=grads[0], dK=grads[1], dV=grads[2])
+    assert O.shape == q.shape and (grads[1] == 0).all() and (grads[2] == 0).all()
