@@ -77,12 +77,14 @@ struct LossArgs {
 
 __device__ __forceinline__ bool is_word(int64_t t, int V) { return t >= 0 && t < V; }
 
-// Numbers the tokens that have a target, in order.  A workgroup does 1024 tokens; it counts those before them itself.
+// Numbers the tokens that have a target, in order.  A workgroup does 1024 tokens; it counts those before them itself.  The list is padded with
+// one of them: a row of X that has no target may hold anything, and even with a weight of zero it would reach dW and dbias.
 template <bool BACKWARD>
 __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossArgs a)
 {
     __shared__ int sums[16];
     __shared__ float tops[16];
+    __shared__ int someone[16];  // a token that has a target, or -1
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, groups = (a.T + 1023) / 1024;
     if ((int)blockIdx.x >= groups) {  // the further workgroups: where the sums start
         const int v = ((int)blockIdx.x - groups) * 1024 + tid;
@@ -91,22 +93,33 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossArgs a)
     }
     const int first = blockIdx.x * 1024, t = first + tid;
     const bool last = (int)blockIdx.x == groups - 1;
-    int before = 0;
+    int before = 0, counted = -1;
     float top = 0.0f;
 #pragma unroll 8
     for (int i = tid; i < first; i += 1024) {
         const bool word = is_word(a.targets[i], a.V);
         before += word;
-        if (BACKWARD && last && word) top = fmaxf(top, fabsf(a.dloss[i]));
+        if (BACKWARD && last && word) {
+            top = fmaxf(top, fabsf(a.dloss[i]));
+            counted = i;
+        }
     }
     const bool mine = t < a.T && is_word(a.targets[t], a.V);
-    if (BACKWARD && last && mine) top = fmaxf(top, fabsf(a.dloss[t]));
+    if (BACKWARD && last && mine) {
+        top = fmaxf(top, fabsf(a.dloss[t]));
+        counted = t;
+    }
     const uint64_t who = __builtin_amdgcn_ballot_w64(mine);
     before = wave_sum(before);
-    if constexpr (BACKWARD) top = wave_max(top);
+    if constexpr (BACKWARD) {
+        top = wave_max(top);
+        const uint64_t any = __builtin_amdgcn_ballot_w64(counted >= 0);
+        if (any) counted = __builtin_amdgcn_readlane(counted, __builtin_ctzll(any));
+    }
     if (lane == 0) {
         sums[wave] = before;
         tops[wave] = top;
+        someone[wave] = counted;
     }
     __syncthreads();
     int start = 0;
@@ -149,7 +162,10 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossArgs a)
         if (lane == 0) a.counted->slices = slices;
     }
     const int end = min(a.Tp, (all + kRowPad - 1) / kRowPad * kRowPad);
-    if (all + tid < end) a.info[all + tid] = RowInfo{0, -1, __builtin_inff(), 0.0f};  // (exponentials of zero)
+    int pad = 0;  // (forward: what padding gives is not written)
+    if constexpr (BACKWARD)
+        for (int i = 0; i < 16; ++i) pad = max(pad, someone[i]);
+    if (all + tid < end) a.info[all + tid] = RowInfo{pad, -1, __builtin_inff(), 0.0f};  // (exponentials of zero)
 }
 
 // ---- products ------------------------------------------------------------------------------------------------------

@@ -44,3 +44,26 @@ def test_keys_without_queries_have_no_gradient(qb):
     grads = [torch.full_like(x, float("nan")) for x in (q, k, v)]
     qb.qb_attention_bwd(q, q, k, v, O, lse, offsets(0, 0), offsets(70, 30), 40, 70, dQ=grads[0], dK=grads[1], dV=grads[2])
     assert O.shape == q.shape and (grads[1] == 0).all() and (grads[2] == 0).all()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), 3e38])
+@pytest.mark.parametrize("T,labelled", [(77, 20), (1500, 700), (1500, 1)])
+def test_hidden_states_of_tokens_without_a_target_do_not_reach_the_gradients(qb, T, labelled, value):
+    say("vocabulary loss, the first and the last token without a target:", T, labelled, value)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(T)
+    X, W = torch.randn(T, 128, generator=g, device=DEV).bfloat16(), (torch.randn(333, 128, generator=g, device=DEV) * 0.1).bfloat16()
+    bias = torch.randn(333, generator=g, device=DEV)
+    targets = torch.full((T,), -100, dtype=torch.int64, device=DEV)
+    at = 1 + torch.randperm(T - 2, generator=g, device=DEV)[:labelled]
+    targets[at] = torch.randint(0, 333, (labelled,), generator=g, device=DEV)
+    dloss = torch.full((T,), 1.0 / labelled, device=DEV)
+
+    def outputs():
+        loss, lse = qb.qb_vocab_loss_fwd(X, W, targets, bias=bias)
+        return (loss, lse) + tuple(qb.qb_vocab_loss_bwd(dloss, X, W, targets, lse, bias=bias))
+
+    want = outputs()
+    assert all(torch.isfinite(x).all() for x in want)
+    X[0] = X[-1] = value
+    assert all(torch.equal(x, y) for x, y in zip(outputs(), want))
