@@ -21,7 +21,7 @@ constexpr int kRowPad = 256;                    // the list of tokens is padded 
 
 struct Counted {
     int n;        // tokens that have a target
-    float scale;  // the largest |dloss| among them
+    float scale;  // the largest |dloss| among them, and a normal number
     int slices;   // that the contraction of a tile of dX is cut into
     int pad[61];
 };
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossArgs a)
     if (!last) return;
     if (tid == 0) {
         a.counted->n = all;
-        float s = 0.0f;
+        float s = 1.17549435e-38f;  // (one over less would be infinite)
         for (int i = 0; i < 16; ++i) s = fmaxf(s, tops[i]);
         a.counted->scale = s;
     }
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 1) void loss_logits_kernel(const Lo
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave - wm * S::WN;
     const int n = a.counted->n, K = a.K, steps = K / 64, grid = (int)gridDim.x;
-    const float scale = BACKWARD ? a.counted->scale : 0.0f, inv = scale > 0.0f ? 1.0f / scale : 0.0f;
+    const float inv = BACKWARD ? 1.0f / a.counted->scale : 0.0f;
     const int words = BACKWARD ? a.piece / S::BM : (a.V + S::BM - 1) / S::BM, tiles = words * ((n + S::BN - 1) / S::BN);
     const int tile0 = first_tile();
     if (BACKWARD && a.v0 == 0) {  // the rows that take part, side by side, for dW

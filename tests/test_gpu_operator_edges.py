@@ -67,3 +67,27 @@ def test_hidden_states_of_tokens_without_a_target_do_not_reach_the_gradients(qb,
     assert all(torch.isfinite(x).all() for x in want)
     X[0] = X[-1] = value
     assert all(torch.equal(x, y) for x, y in zip(outputs(), want))
+
+
+@pytest.mark.parametrize("T", [60, 1100])
+@pytest.mark.parametrize("power", [127, 100, -100, -126, -130, -149])
+def test_weights_of_the_loss_of_any_size(qb, T, power):
+    """dloss of a power of two moves the gradients by that power, up to the spacing of the types' least numbers (2^-133, 2^-149)"""
+    say("vocabulary loss: gradients of", T, "tokens for a weight of 2 to the", power)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(T)
+    X, W = torch.randn(T, 128, generator=g, device=DEV).bfloat16(), (torch.randn(333, 128, generator=g, device=DEV) * 0.1).bfloat16()
+    targets = torch.randint(0, 333, (T,), generator=g, device=DEV)
+    bias = torch.randn(333, generator=g, device=DEV)
+    lse = qb.qb_vocab_loss_fwd(X, W, targets, bias=bias)[1]
+    weight = torch.ones(T, device=DEV)
+    weight[::3] = 0.0
+    one = [x.double() * 2.0 ** power for x in qb.qb_vocab_loss_bwd(weight, X, W, targets, lse, bias=bias)]
+    got = qb.qb_vocab_loss_bwd(weight * 2.0 ** power, X, W, targets, lse, bias=bias)
+    for x, want in zip(got, one):
+        over = want.abs() > torch.finfo(x.dtype).max
+        assert torch.equal(torch.isfinite(x), ~over)
+        least = 2.0 ** -149 if x.dtype == torch.float32 else 2.0 ** -133
+        # (below the least normal number a result is rounded a second time here)
+        off = (x.double() - want).abs()[~over]
+        assert (off <= torch.where(want.abs()[~over] < 2.0 ** -125, 0.51 * least, 0.0)).all()
