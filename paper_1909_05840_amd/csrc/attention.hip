@@ -251,11 +251,11 @@ constexpr bool kHalves = D == 64 && DROP;  // (without dropout's arithmetic to s
         if (left > (kHalves ? 32 : 0)) attend<T, D, DROP>(x, q, op, tk, tk + kTile, t * kKeys, limit, (t + 1) * kKeys > wave_least, a.c, bits, a.threshold, row_q, head, lane);
         else if (kHalves && left > 0) attend<T, D, DROP, 1>(x, q, op, tk, tk + kTile, t * kKeys, limit, t * kKeys + 32 > wave_least, a.c, bits, a.threshold, row_q, head, lane);
     }
-    const float l = halves_sum(x.l);
+    const float l = halves_sum(x.l);  // (zero where no key is seen; NaN stays NaN, in O and lse)
     const int64_t at_row = (int64_t)row_q * a.heads + head;
-    write_row<T, D>(O + at_row * D, x.o, l > 0.0f ? (DROP ? a.inv_share : 1.0f) / l : 0.0f, hf, row < rows);
+    write_row<T, D>(O + at_row * D, x.o, l == 0.0f ? 0.0f : (DROP ? a.inv_share : 1.0f) / l, hf, row < rows);
     if (row >= rows) return;
-    if (hf == 0) lse[at_row] = l > 0.0f ? x.m * a.scale + __logf(l) : -__builtin_inff();
+    if (hf == 0) lse[at_row] = l == 0.0f ? -__builtin_inff() : x.m * a.scale + __logf(l);
 }
 
 // ---- few rows: the new tokens over a cache
@@ -361,10 +361,10 @@ __global__ __launch_bounds__(256, 1) void attention_cache_kernel(const AttnArgs 
                 to[D + 1] = l;
             }
         } else {
-            const float f = l > 0.0f ? 1.0f / l : 0.0f;
+            const float f = l == 0.0f ? 0.0f : 1.0f / l;
             const int64_t at_row = (int64_t)(seg.q0 + t) * a.heads + h;
             *reinterpret_cast<v4u *>(O + at_row * D + d) = v4u{T::pair(o[0][0] * f, o[0][1] * f), T::pair(o[0][2] * f, o[0][3] * f), T::pair(o[1][0] * f, o[1][1] * f), T::pair(o[1][2] * f, o[1][3] * f)};
-            if (d == 0) lse[at_row] = l > 0.0f ? m * a.scale + __logf(l) : -__builtin_inff();
+            if (d == 0) lse[at_row] = l == 0.0f ? -__builtin_inff() : m * a.scale + __logf(l);
         }
     }
 }
@@ -396,11 +396,11 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a, u
 #pragma unroll
         for (int i = 0; i < N; ++i) o[i] = o[i] * f + p[N * lane + i] * g;
     }
-    const float f = l > 0.0f ? 1.0f / l : 0.0f;
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;
     const int64_t at_row = (int64_t)(seg.q0 + t) * a.heads + h;
     if constexpr (N == 2) *reinterpret_cast<uint32_t *>(O + at_row * D + 2 * lane) = T::pair(o[0] * f, o[N - 1] * f);
     else O[at_row * D + lane] = (uint16_t)T::pair(o[0] * f, 0.0f);
-    if (lane == 0) lse[at_row] = l > 0.0f ? m * a.scale + __logf(l) : -__builtin_inff();
+    if (lane == 0) lse[at_row] = l == 0.0f ? -__builtin_inff() : m * a.scale + __logf(l);
 }
 
 // Few rows (without dropout, which serving has none of): up to 32 of a key head, or more where the other kernel would leave most CUs idle: it

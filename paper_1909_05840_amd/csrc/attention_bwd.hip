@@ -86,7 +86,7 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
     }
     delta = halves_sum(delta);
     const float lse = g.lse[at_row];
-    const float lse2 = lse > -__builtin_inff() ? lse * 1.44269504088896341f : __builtin_inff();
+    const float lse2 = lse == -__builtin_inff() ? __builtin_inff() : lse * 1.44269504088896341f;
 
     const auto sees = [&](int t) { return a.causal ? min(seg.nk, max(0, seg.first_hidden(t))) : seg.nk; };
     const auto token_of = [&](int r) { return min(r / a.group, seg.nq - 1); };
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
     write_row<T, D>(g.dQ + (int64_t)row_q * g.q_row + (int64_t)head * g.q_head, A, a.scale, hf, row < rows);
     if (row >= rows) return;
     if (hf == 0) {
-        g.stat[at_row] = lse > -__builtin_inff() ? -lse / a.scale : -__builtin_inff();
+        g.stat[at_row] = lse == -__builtin_inff() ? -__builtin_inff() : -lse / a.scale;
         g.stat[(int64_t)a.total_q * a.heads + 1 + at_row] = -delta;
     }
 }

@@ -91,3 +91,25 @@ def test_weights_of_the_loss_of_any_size(qb, T, power):
         # (below the least normal number a result is rounded a second time here)
         off = (x.double() - want).abs()[~over]
         assert (off <= torch.where(want.abs()[~over] < 2.0 ** -125, 0.51 * least, 0.0)).all()
+
+
+@pytest.mark.parametrize("name,heads,kv,q_lens,k_lens", [("one launch over a cache", 4, 2, [1, 1, 1], [40, 200, 7]), ("a cache in chunks", 4, 2, [1, 1, 1], [5000, 3000, 7]),
+                                                         ("many rows", 24, 24, [300, 257], [300, 400])])
+def test_a_query_that_is_no_number_is_not_one_that_sees_no_key(qb, name, heads, kv, q_lens, k_lens):
+    say("attention, NaN in a query:", name)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(5)
+    q, k, v = (torch.randn(sum(n), h, 64, generator=g, device=DEV).bfloat16() for n, h in ((q_lens, heads), (k_lens, kv), (k_lens, kv)))
+    call = (k, v, offsets(*q_lens), offsets(*k_lens), max(q_lens), max(k_lens))
+    want = qb.qb_attention_fwd(q, *call)
+    at = q_lens[0] - 1
+    q[at, 1, 3] = float("nan")
+    O, lse = qb.qb_attention_fwd(q, *call)
+    assert torch.isnan(O[at, 1]).all() and torch.isnan(lse[at, 1])
+    dQ, dK, dV = qb.qb_attention_bwd(torch.ones_like(q), q, k, v, O, lse, *call[2:])
+    of = 1 // (heads // kv)  # the key head that it reads
+    assert torch.isnan(dQ[at, 1]).all() and torch.isnan(dK[0, of]).all() and torch.isnan(dV[0, of]).all()
+    assert torch.isfinite(dQ[at, 0]).all() and torch.isfinite(dK[:, -1]).all() and torch.isfinite(dV[:, -1]).all()
+    for x, y in ((O, want[0]), (lse, want[1])):
+        x[at, 1] = y[at, 1]
+        assert torch.equal(x, y)
