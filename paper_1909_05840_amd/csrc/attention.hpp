@@ -52,7 +52,7 @@ __device__ __forceinline__ Segment segment(const AttnArgs &a, int b)
 struct Place {
     int pair, tile;  // (pair: the sequence, or its rank by length, times kv_heads, and the key head)
     Segment seg;
-    int kv;
+    int seq, kv;
     bool none;
 };
 // KEYS: tiles of 128 keys, else of 128 rows; by_length: there is one workgroup to such a tile
@@ -68,6 +68,7 @@ __device__ __forceinline__ Place place(const AttnArgs &a, int id, int tiles, boo
         if (!KEYS) p.tile = tiles - 1 - p.tile;
         p.none = p.pair >= pairs;
         const int b = p.none ? 0 : p.pair / a.kv_heads;
+        p.seq = b;
         p.kv = p.pair - b * a.kv_heads;
         p.seg = segment(a, b);
         return p;
@@ -100,6 +101,7 @@ __device__ __forceinline__ Place place(const AttnArgs &a, int id, int tiles, boo
     const int nth = __builtin_amdgcn_readfirstlane(rest / of), seq = __builtin_amdgcn_readlane(who, r);
     p.tile = KEYS ? rest - nth * of : of - 1 - (rest - nth * of);
     p.kv = __builtin_amdgcn_readlane(first, r) + 8 * nth;
+    p.seq = seq;
     p.pair = r * a.kv_heads + p.kv;
     p.seg = {__builtin_amdgcn_readlane(mine.q0, seq), __builtin_amdgcn_readlane(mine.nq, seq), __builtin_amdgcn_readlane(mine.k0, seq), __builtin_amdgcn_readlane(mine.nk, seq)};
     return p;

@@ -7,6 +7,14 @@
 // of a tile of keys (dK, dV; shared heads of keys sum over their queries there).  Seven products instead of the five
 // that one launch would need, but nothing is added to memory by several workgroups: no atomics, the same bits every time.
 // dS and P are rounded to the inputs' type for the last products only.
+//
+// float16 has normal numbers from 2^-14 on, and P is about 1 / keys, dS that times gradients of any size.  Both are rounded lifted by powers of two,
+// which the binary32 results are taken back by: P 2^14 times, and dS that and a power for dP - delta besides, which keeps that at one or below.  dQ has such a
+// power for every row, lowered when a block of keys has a larger |dP - delta| than those before, and the sums with it.  dK and dV sum over rows:
+// theirs follows from |dP - delta| <= |dO| |V| / share + |delta|, norms over a row's values, with the largest of V among a wavefront's keys and the largest
+// of dO and of delta that the launch for dQ leaves for the rows of the sequence and key head.  (A bound by the differences themselves would not do: where they
+// vanish in the one launch, they are rounding errors in the other, which sums in another order.)  Unlifted, at 8192 keys and a spread of dO of
+// 1e-4 dQ and dK were 11 times as far from exact as exact arithmetic rounded once; so 1.0 times, and 1.4 at a spread of 1e-2 and more.
 #include "attention.hpp"
 #include <algorithm>
 
@@ -22,7 +30,13 @@ struct GradArgs {
     int64_t q_row, q_head, k_row, k_head, v_row, v_head;
     float *stat;  // [2][total_q * heads + 1]: -lse / scale (-infinity for a row that sees nothing, and for the last entry: P is zero), -delta
     float *part;  // [pairs][tiles of keys][splits][128][dK, dV] of tiles in parts
+    v2f *most;    // float16: [pairs][tiles_q][4] of a wavefront's rows the largest squared norm of dO, the largest |delta|
+    int tiles_q;  // tiles of 128 rows of the longest sequence
 };
+
+constexpr int kLift = 14;  // of P in float16, in powers of two: a weight that rounding has put a little above one, and any dS, stays below 65504
+
+constexpr int kMostLift = 40;  // of dS besides, a row's before it has seen a key
 
 template <int N>
 __device__ __forceinline__ void clear(v16f (&x)[N])
@@ -39,6 +53,16 @@ __device__ __forceinline__ v8s rounded(const v16f &x, int half)
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = T::pair(x[8 * half + 2 * i], x[8 * half + 2 * i + 1]);
     return __builtin_bit_cast(v8s, w);
+}
+
+template <typename T>
+__device__ __forceinline__ float squares(v8s x)
+{
+    const v4u w = __builtin_bit_cast(v4u, x);
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += T::lo(w[i]) * T::lo(w[i]) + T::hi(w[i]) * T::hi(w[i]);
+    return sum;
 }
 
 // dQ and delta; 128 rows to a workgroup, 32 to a wavefront, a lane's results all of one row (as in the forward).
@@ -75,7 +99,7 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
     v8s q[D / 16], dO[D / 16];
     const uint16_t *const q_from = a.Q + (int64_t)row_q * a.q_row + (int64_t)head * a.q_head + 8 * hf;
     const uint16_t *const do_from = g.dO + at_row * D + 8 * hf, *const o_from = g.O + at_row * D + 8 * hf;
-    float delta = 0.0f;
+    float delta = 0.0f, norm = 0.0f;
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) {
         q[d] = *reinterpret_cast<const v8s *>(q_from + 16 * d);
@@ -83,10 +107,11 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
         const v4u x = __builtin_bit_cast(v4u, dO[d]), y = *reinterpret_cast<const v4u *>(o_from + 16 * d);
 #pragma unroll
         for (int i = 0; i < 4; ++i) delta += T::lo(x[i]) * T::lo(y[i]) + T::hi(x[i]) * T::hi(y[i]);
+        if constexpr (T::kNarrow) norm += squares<T>(dO[d]);
     }
     delta = halves_sum(delta);
     const float lse = g.lse[at_row];
-    const float lse2 = lse == -__builtin_inff() ? __builtin_inff() : lse * 1.44269504088896341f;
+    const float lse2 = lse == -__builtin_inff() ? __builtin_inff() : lse * 1.44269504088896341f - (T::kNarrow ? kLift : 0);
 
     const auto sees = [&](int t) { return a.causal ? min(seg.nk, max(0, seg.first_hidden(t))) : seg.nk; };
     const auto token_of = [&](int r) { return min(r / a.group, seg.nq - 1); };
@@ -114,6 +139,8 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
     };
     const Threefry bits(DROP ? (uint64_t)*a.seed : 0);
     const Operands<D> op(lane, lds0);
+    int lift = kMostLift;
+    float lifted = __builtin_ldexpf(1.0f, kMostLift), lifted_delta = delta * lifted;
     v16f A[D / 32], B[EXACT ? D / 32 : 1];
     clear(A);
     clear(B);
@@ -175,9 +202,35 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
                     dp[i + 3] = kept_high(w[1], a.threshold) ? dp[i + 3] * a.inv_share : 0.0f;
                 }
             }
+            if constexpr (T::kNarrow) {
+                float top = 0.0f, other = 0.0f;  // (two chains)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) dp[i] = __builtin_fmaf(dp[i], lifted, -lifted_delta);
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    top = max3(top, __builtin_fabsf(dp[i]), __builtin_fabsf(dp[i + 1]));
+                    other = max3(other, __builtin_fabsf(dp[i + 2]), __builtin_fabsf(dp[i + 3]));
+                }
+                top = fmaxf(top, other);
+                if (__builtin_amdgcn_ballot_w64(top > 1.0f)) {
+                    top = halves_max(top);
+                    const int down = top > 1.0f && top < __builtin_inff() ? __builtin_amdgcn_frexp_expf(top) + 2 : 0;  // (two powers of two to spare)
+                    const float f = __builtin_ldexpf(1.0f, -down);
+                    lift -= down;
+                    lifted *= f;
+                    lifted_delta *= f;
+                    eps *= f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) dp[i] *= f;
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) A[i][j] *= f;
+                }
+            }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                dp[i] = s[i] * (dp[i] - delta);
+                dp[i] = s[i] * (T::kNarrow ? dp[i] : dp[i] - delta);
                 if constexpr (EXACT) eps += dp[i];
             }
 #pragma unroll
@@ -196,13 +249,20 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
     }
     if constexpr (EXACT) {
         eps = halves_sum(eps);
-        delta += eps;
+        if constexpr (T::kNarrow) eps = __builtin_ldexpf(eps, -kLift);  // (B is as P is)
+        delta += T::kNarrow ? __builtin_ldexpf(eps, -lift) : eps;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll
             for (int j = 0; j < 16; ++j) A[i][j] -= eps * B[i][j];
     }
-    write_row<T, D>(g.dQ + (int64_t)row_q * g.q_row + (int64_t)head * g.q_head, A, a.scale, hf, row < rows);
+    if constexpr (T::kNarrow) {  // (rows that see no key have no gradient; one with infinities or NaN gives those whatever it is multiplied by)
+        const float squared = halves_sum(norm);
+        const bool counts = limit > 0 && squared < __builtin_inff() && __builtin_fabsf(delta) < __builtin_inff();
+        const v2f most = {wave_max(counts ? squared : 0.0f), wave_max(counts ? __builtin_fabsf(delta) : 0.0f)};
+        if (lane == 0) g.most[(((int64_t)at.seq * a.kv_heads + kv) * g.tiles_q + at.tile) * 4 + wave] = most;
+    }
+    write_row<T, D>(g.dQ + (int64_t)row_q * g.q_row + (int64_t)head * g.q_head, A, T::kNarrow ? __builtin_ldexpf(a.scale, -kLift - lift) : a.scale, hf, row < rows);
     if (row >= rows) return;
     if (hf == 0) {
         g.stat[at_row] = lse == -__builtin_inff() ? -__builtin_inff() : -lse / a.scale;
@@ -326,6 +386,8 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
         }
     };
     const Threefry bits(DROP ? (uint64_t)*a.seed : 0);
+    int lift = 0;
+    float lifted = 1.0f;
     v16f dK[D / 32], dV[D / 32];
     clear(dK);
     clear(dV);
@@ -383,16 +445,16 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
     const auto weights = [&](uint32_t tq, int rb, auto quarter, v16f &p, v16f &ds) __attribute__((always_inline)) {
         constexpr int q4 = decltype(quarter)::value, i0 = 4 * q4;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) p[i0 + j] = __builtin_amdgcn_exp2f(p[i0 + j] * a.c);
+        for (int j = 0; j < 4; ++j) p[i0 + j] = __builtin_amdgcn_exp2f(T::kNarrow ? __builtin_fmaf(p[i0 + j], a.c, (float)kLift) : p[i0 + j] * a.c);
         if constexpr (!DROP) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) ds[i0 + j] *= p[i0 + j];
+            for (int j = 0; j < 4; ++j) ds[i0 + j] *= T::kNarrow ? p[i0 + j] * lifted : p[i0 + j];
         } else {
             const v4f minus_delta = *(lds_v4f)(stat_at + tq + 4 * (kRowsOfTile + 32 * rb + 8 * q4));
             const auto take = [&](int j, uint32_t w0, uint32_t w1) {
                 const uint32_t word = (lane & 2) ? w1 : w0;
                 const bool in = ((lane & 1) ? word >> 16 : word & 0xFFFFu) >= a.threshold;
-                ds[i0 + j] = p[i0 + j] * ((in ? ds[i0 + j] * a.inv_share : 0.0f) + minus_delta[j]);
+                ds[i0 + j] = (T::kNarrow ? p[i0 + j] * lifted : p[i0 + j]) * ((in ? ds[i0 + j] * a.inv_share : 0.0f) + minus_delta[j]);
                 p[i0 + j] = in ? p[i0 + j] : 0.0f;
             };
             const v2u w = bits_of[q4];
@@ -447,6 +509,19 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
     place_of(t, token, head);
     if (begin < end) {
         fetch(begin, 0);
+        if constexpr (T::kNarrow) {
+            const v2f *const from = g.most + ((int64_t)at.seq * a.kv_heads + kv) * g.tiles_q * 4;
+            v2f most = {0.0f, 0.0f};
+            for (int i = lane, n = min(g.tiles_q, (seg.nq * a.group + 127) >> 7) * 4; i < n; i += 64) most = v2f{fmaxf(most[0], from[i][0]), fmaxf(most[1], from[i][1])};
+            float norm = 0.0f;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) norm += squares<T>(v[d]);
+            norm = halves_sum(norm);
+            norm = wave_max(norm < __builtin_inff() ? norm : 0.0f);
+            const float bound = __builtin_sqrtf(wave_max(most[0])) * __builtin_sqrtf(norm) * (DROP ? a.inv_share : 1.0f) + wave_max(most[1]);
+            if (bound > 0.0f) lift = __builtin_amdgcn_readfirstlane(-__builtin_amdgcn_frexp_expf(bound));
+            lifted = __builtin_ldexpf(1.0f, lift);
+        }
         if (begin + 1 < end) {
             fetch(begin + 1, 1);
             wait_copies<2 * decltype(copy_q)::N>();  // (the first tile's; the second's may be under way)
@@ -489,6 +564,16 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a,
         products(tq, lower, tn, []() {});  // (past the last tile: scores of what lies there, unused)
         place_of(++t, token, head);
         stage = next;
+    }
+    if constexpr (T::kNarrow) {
+        const float of_k = __builtin_ldexpf(1.0f, -kLift - lift), of_v = __builtin_ldexpf(1.0f, -kLift);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                dK[i][j] *= of_k;
+                dV[i][j] *= of_v;
+            }
     }
     if (todo.parts > 1) {
         if (key >= seg.nk) return;
@@ -550,6 +635,11 @@ inline Parts row_parts(int64_t pairs, int64_t max_q, int64_t group, int64_t max_
     return {most, std::max<int64_t>(1, (rows + most - 1) / most)};
 }
 inline size_t stat_bytes(const qb_attention *p) { return ((size_t)(p->total_q * p->heads + 1) * 8 + 255) / 256 * 256; }
+inline size_t most_bytes(const qb_attention *p)  // (four wavefronts to a tile)
+{
+    const int64_t tiles = (p->max_q * (p->heads / p->kv_heads) + 127) / 128;
+    return p->type == QB_TYPE_FP16 ? ((size_t)((int64_t)p->n_seqs * p->kv_heads * tiles) * 32 + 255) / 256 * 256 : 0;
+}
 
 template <typename T, int D>
 qb_status backward(AttnArgs a, const GradArgs &g, int64_t max_q, int64_t max_k, bool drop, hipStream_t stream)
@@ -599,7 +689,7 @@ extern "C" size_t qb_attention_bwd_workspace_nbytes(const qb_attention *p)
     AttnArgs a;
     if (attention_args(p, a) != QB_OK) return 0;
     const int64_t pairs = (int64_t)a.n_seqs * a.kv_heads, splits = row_parts(pairs, p->max_q, a.group, p->max_k, p->causal, p->dim).splits;
-    return stat_bytes(p) + (splits > 1 ? (size_t)(pairs * ((p->max_k + 127) / 128) * splits) * 128 * 2 * p->dim * 4 : 0);
+    return stat_bytes(p) + most_bytes(p) + (splits > 1 ? (size_t)(pairs * ((p->max_k + 127) / 128) * splits) * 128 * 2 * p->dim * 4 : 0);
 }
 
 extern "C" qb_status qb_attention_bwd(const qb_attention *p, const void *dO, const void *O, const float *lse,
@@ -617,8 +707,10 @@ extern "C" qb_status qb_attention_bwd(const qb_attention *p, const void *dO, con
     if ((p->total_q > 0 || p->max_q > 0) && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255))) return QB_ERR_WORKSPACE;
     const int64_t pairs = (int64_t)p->n_seqs * p->kv_heads;
     if (dealt_workgroups(pairs, (p->max_q * a.group + 127) / 128) > INT32_MAX / 256 || dealt_workgroups(pairs, (p->max_k + 127) / 128 * row_parts(pairs, p->max_q, a.group, p->max_k, p->causal, p->dim).splits) > INT32_MAX / 256) return QB_ERR_SHAPE;
+    uint8_t *const ws = static_cast<uint8_t *>(workspace);
     const GradArgs g = {static_cast<const uint16_t *>(dO), static_cast<const uint16_t *>(O), lse, static_cast<uint16_t *>(grads->dQ), static_cast<uint16_t *>(grads->dK),
-                        static_cast<uint16_t *>(grads->dV), grads->q_row, grads->q_head, grads->k_row, grads->k_head, grads->v_row, grads->v_head, static_cast<float *>(workspace), reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + stat_bytes(p))};
+                        static_cast<uint16_t *>(grads->dV), grads->q_row, grads->q_head, grads->k_row, grads->k_head, grads->v_row, grads->v_head, reinterpret_cast<float *>(ws),
+                        reinterpret_cast<float *>(ws + stat_bytes(p) + most_bytes(p)), reinterpret_cast<v2f *>(ws + stat_bytes(p)), (int)((p->max_q * a.group + 127) / 128)};
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool drop = p->p > 0.0f;
     if (p->type == QB_TYPE_BF16) return p->dim == 64 ? backward<Bf16, 64>(a, g, p->max_q, p->max_k, drop, st) : backward<Bf16, 128>(a, g, p->max_q, p->max_k, drop, st);

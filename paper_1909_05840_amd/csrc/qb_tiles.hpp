@@ -14,7 +14,9 @@ typedef unsigned int v2u __attribute__((ext_vector_type(2)));
 typedef unsigned int v4u __attribute__((ext_vector_type(4)));
 
 // A 16-bit type: eight values as a matrix operand, two floats rounded to nearest even (the first in the low half), and back.
+// kNarrow: the exponents of binary32 do not fit.
 struct Bf16 {
+    static constexpr bool kNarrow = false;
     typedef __bf16 v8 __attribute__((ext_vector_type(8)));
     static __device__ __forceinline__ v16f mma32(v8s a, v8s b, v16f c)
     {
@@ -29,6 +31,7 @@ struct Bf16 {
     static __device__ __forceinline__ float hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 };
 struct Fp16 {
+    static constexpr bool kNarrow = true;
     typedef _Float16 v8 __attribute__((ext_vector_type(8)));
     typedef _Float16 v2 __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ v16f mma32(v8s a, v8s b, v16f c)
