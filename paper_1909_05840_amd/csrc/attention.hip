@@ -63,6 +63,12 @@ constexpr float kNothing = -1.0e30f;  // m before a row has seen a key (finite: 
 // The accumulators are rescaled only when a maximum has grown by more than this (powers of two): until then the
 // exponentials stay below 2^8, which costs no precision in either type.
 constexpr float kLazy = 8.0f;
+// In float16 exponentials, and with them l and O's sums, are held 2^7 times as large (so below 2^15): its normal numbers end at 2^-14, and keys
+// of less weight count where those of more have little value.  A first key of 2^20 times the others' weight and no value had O 9 to 11 times
+// as far from exact as exact arithmetic rounded once.
+template <typename T> constexpr float kLift = T::kNarrow ? 7.0f : 0.0f;
+template <typename T>
+__device__ __forceinline__ float lse_of(float m, float l, float scale) { return l == 0.0f ? -__builtin_inff() : m * scale + __logf(T::kNarrow ? l * 0.0078125f : l); }
 
 template <int D>
 struct Softmax {
@@ -143,7 +149,7 @@ __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], co
         if constexpr (KB == 2) read_values(1, v[KB - 1]);
         __builtin_amdgcn_sched_barrier(0);
     }
-    const float mc = x.m * c;
+    const float mc = x.m * c - kLift<T>;
     float sum = 0.0f;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
@@ -255,7 +261,7 @@ constexpr bool kHalves = D == 64 && DROP;  // (without dropout's arithmetic to s
     const int64_t at_row = (int64_t)row_q * a.heads + head;
     write_row<T, D>(O + at_row * D, x.o, l == 0.0f ? 0.0f : (DROP ? a.inv_share : 1.0f) / l, hf, row < rows);
     if (row >= rows) return;
-    if (hf == 0) lse[at_row] = l == 0.0f ? -__builtin_inff() : x.m * a.scale + __logf(l);
+    if (hf == 0) lse[at_row] = lse_of<T>(x.m, l, a.scale);
 }
 
 // ---- few rows: the new tokens over a cache
@@ -364,7 +370,7 @@ __global__ __launch_bounds__(256, 1) void attention_cache_kernel(const AttnArgs 
             const float f = l == 0.0f ? 0.0f : 1.0f / l;
             const int64_t at_row = (int64_t)(seg.q0 + t) * a.heads + h;
             *reinterpret_cast<v4u *>(O + at_row * D + d) = v4u{T::pair(o[0][0] * f, o[0][1] * f), T::pair(o[0][2] * f, o[0][3] * f), T::pair(o[1][0] * f, o[1][1] * f), T::pair(o[1][2] * f, o[1][3] * f)};
-            if (d == 0) lse[at_row] = l == 0.0f ? -__builtin_inff() : m * a.scale + __logf(l);
+            if (d == 0) lse[at_row] = lse_of<T>(m, l, a.scale);
         }
     }
 }
@@ -400,7 +406,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a, u
     const int64_t at_row = (int64_t)(seg.q0 + t) * a.heads + h;
     if constexpr (N == 2) *reinterpret_cast<uint32_t *>(O + at_row * D + 2 * lane) = T::pair(o[0] * f, o[N - 1] * f);
     else O[at_row * D + lane] = (uint16_t)T::pair(o[0] * f, 0.0f);
-    if (lane == 0) lse[at_row] = l == 0.0f ? -__builtin_inff() : m * a.scale + __logf(l);
+    if (lane == 0) lse[at_row] = lse_of<T>(m, l, a.scale);
 }
 
 // Few rows (without dropout, which serving has none of): up to 32 of a key head, or more where the other kernel would leave most CUs idle: it

@@ -86,3 +86,22 @@ def test_what_is_not_finite_stays_with_its_sequence(qb):
     assert not torch.isfinite(got[1][:300]).any()
     c.dO[:300] = 0.0  # and nothing at all
     assert all((x[:300] == 0).all() and torch.equal(x[300:], y) for x, y in zip(c.backward(qb, O, lse), want))
+
+
+@pytest.mark.parametrize("rows,heads,keys", [(1, 2, 500), (1, 2, 4096), (128, 32, 3000)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_weights_far_below_the_largest(qb, dim, rows, heads, keys):
+    """The first key takes nearly all of the weight and has no value, as often in trained models; O is what the others give, each 2^-20 of it."""
+    print("float16 attention: a first key of 2^20 times the weight", rows, heads, keys, dim, flush=True)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(dim)
+    Q = 1.0 + 0.01 * torch.randn(rows, heads, dim, generator=g, device=DEV)
+    K, V = 0.3 * torch.randn(keys, heads, dim, generator=g, device=DEV), torch.randn(keys, heads, dim, generator=g, device=DEV)
+    K[0], V[0] = 20 * math.log(2) / math.sqrt(dim), 0.0
+    Q, K, V = Q.half(), K.half(), V.half()
+    cu = [torch.tensor([0, n], dtype=torch.int32, device=DEV) for n in (rows, keys)]
+    O, lse = qb.qb_attention_fwd(Q, K, V, *cu, rows, keys)
+    q, k, v = (x.double().transpose(0, 1).contiguous() for x in (Q, K, V))
+    s = torch.matmul(q, k.transpose(1, 2).contiguous()) / math.sqrt(dim)
+    check("O", O.transpose(0, 1), torch.matmul(torch.softmax(s, 2), v))
+    assert ((lse.t() - torch.logsumexp(s, 2)).abs() < 1e-5).all()
