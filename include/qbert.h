@@ -465,7 +465,7 @@ qb_status qb_dropout_bwd(const void *dY, int64_t n, int type, float p, const int
  *   k_len       device [n_seqs] int32 or NULL; forward only
  *   max_q, max_k  host: no sequence has more queries, keys; max_q * heads / kv_heads < 2^30.  Results of sequences that
  *   have more are undefined
- *   scale positive and finite; 0 <= p < 1, and where p > 0: seed, heads <= 512, max_k <= 2^24
+ *   scale from 1e-36 to 2e8; 0 <= p < 1, and where p > 0: seed, heads <= 512, max_k <= 2^24
  *   O, dO [total_q, heads, dim] dense; lse [total_q, heads] fp32.  Rows outside all sequences are not written.
  *   What lies in K and V outside the sequences is not read; inside it must be finite.
  *

@@ -9,10 +9,10 @@
 // them unrounded.
 #include "attention.hpp"
 #include <algorithm>
-#include <cmath>
 
 namespace qb {
 
+// scale: lse / scale, which the backward's sums start from, and kNothing * scale, which a row's exponentials start from, have to be finite
 qb_status attention_args(const qb_attention *p, AttnArgs &a)
 {
     if (!p) return QB_ERR_NULL;
@@ -21,7 +21,7 @@ qb_status attention_args(const qb_attention *p, AttnArgs &a)
         p->max_q > INT32_MAX || p->max_k > INT32_MAX - 4096 || p->max_q * (p->heads / p->kv_heads) >= (1 << 30) ||
         (int64_t)p->n_seqs * p->kv_heads > INT32_MAX)
         return QB_ERR_SHAPE;
-    if ((p->type != QB_TYPE_BF16 && p->type != QB_TYPE_FP16) || !(p->scale > 0.0f) || !std::isfinite(p->scale * 1.5f) || !(p->p >= 0.0f && p->p < 1.0f) ||
+    if ((p->type != QB_TYPE_BF16 && p->type != QB_TYPE_FP16) || !(p->scale >= 1e-36f && p->scale <= 2e8f) || !(p->p >= 0.0f && p->p < 1.0f) ||
         (p->q_row | p->q_head | p->k_row | p->k_head | p->v_row | p->v_head) % 8 != 0)
         return QB_ERR_VALUE;
     if (p->p > 0.0f) {
