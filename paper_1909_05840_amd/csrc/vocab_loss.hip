@@ -45,6 +45,12 @@ __device__ inline int best_slices(const Work &k, int n, int K, int words, int la
     return (int)(best & 63) + 1;
 }
 
+// of 1024 tokens
+struct Count {
+    int n, someone;  // that have a target, and one of them or -1
+    float top;       // the largest |dloss| among them
+};
+
 struct RowInfo {
     int token, target;
     float lse2, weight;  // backward: lse / ln 2, dloss
@@ -56,6 +62,7 @@ struct LossArgs {
     const int64_t *targets;
     int T, V, K;
     Counted *counted;
+    Count *counts;   // of every 1024 tokens, or null where these are few
     RowInfo *info;   // [Tp] of every counted row; padded
     int *place;      // [T] the row of a token; -1 where it has no target
     float *start;    // [Vp] the bias, -infinity behind the last word
@@ -77,8 +84,34 @@ struct LossArgs {
 
 __device__ __forceinline__ bool is_word(int64_t t, int V) { return t >= 0 && t < V; }
 
-// Numbers the tokens that have a target, in order.  A workgroup does 1024 tokens; it counts those before them itself.  The list is padded with
-// one of them: a row of X that has no target may hold anything, and even with a weight of zero it would reach dW and dbias.
+// Of many tokens a launch before the next counts every 1024.
+template <bool BACKWARD>
+__global__ __launch_bounds__(256) void loss_count_kernel(const LossArgs a)
+{
+    __shared__ Count each[4];
+    const int tid = threadIdx.x, wave = tid >> 6;
+    int n = 0, someone = -1;
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int t = (int)blockIdx.x * 1024 + i * 256 + tid;
+        if (t >= a.T || !is_word(a.targets[t], a.V)) continue;
+        ++n;
+        someone = t;
+        if constexpr (BACKWARD) top = fmaxf(top, fabsf(a.dloss[t]));
+    }
+    const uint64_t any = __builtin_amdgcn_ballot_w64(someone >= 0);
+    const Count mine = {wave_sum(n), any ? __builtin_amdgcn_readlane(someone, __builtin_ctzll(any)) : -1, wave_max(top)};
+    if ((tid & 63) == 0) each[wave] = mine;
+    __syncthreads();
+    if (tid != 0) return;
+    Count c = each[0];
+    for (int i = 1; i < 4; ++i) c = {c.n + each[i].n, max(c.someone, each[i].someone), fmaxf(c.top, each[i].top)};
+    a.counts[blockIdx.x] = c;
+}
+
+// Numbers the tokens that have a target, in order.  A workgroup does 1024 tokens; it counts those before them itself, or adds up the counts.  The list
+// is padded with one of them: a row of X that has no target may hold anything, and even with a weight of zero it would reach dW and dbias.
 template <bool BACKWARD>
 __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossArgs a)
 {
@@ -95,8 +128,17 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossArgs a)
     const bool last = (int)blockIdx.x == groups - 1;
     int before = 0, counted = -1;
     float top = 0.0f;
+    if (a.counts) {
+#pragma unroll 4
+        for (int i = tid; i < (int)blockIdx.x; i += 1024) {
+            const Count c = a.counts[i];
+            before += c.n;
+            counted = max(counted, c.someone);
+            top = fmaxf(top, c.top);
+        }
+    }
 #pragma unroll 8
-    for (int i = tid; i < first; i += 1024) {
+    for (int i = tid; i < (a.counts ? 0 : first); i += 1024) {
         const bool word = is_word(a.targets[i], a.V);
         before += word;
         if (BACKWARD && last && word) {
@@ -630,6 +672,10 @@ constexpr int kAtWork = S::kWaves == 8 ? 256 : 512;  // workgroups of a launch: 
 
 inline size_t up(size_t v) { return (v + 255) / 256 * 256; }
 
+// A workgroup that counts the tokens before its own reads all of their targets: work that grows with the square of T.  One launch and two, us: 32768
+// tokens forward 6.9 and 3.6 + 3.9, backward 13.7 and 4.0 + 3.9; 4 194 304 tokens 6300 and 29 + 12.
+inline bool count_apart(int64_t T) { return T > 32768; }
+
 // where everything lies in the workspace; returns its size
 size_t lay_out(LossArgs &a, uint8_t *base, bool backward)
 {
@@ -649,6 +695,7 @@ size_t lay_out(LossArgs &a, uint8_t *base, bool backward)
         a.piece = (int)((a.Vp / kRowPad + pieces - 1) / pieces * kRowPad);
         a.Vp = (int)(pieces * a.piece);
     }
+    a.counts = count_apart(a.T) ? reinterpret_cast<Count *>(take((size_t)((a.T + 1023) / 1024) * sizeof(Count))) : nullptr;
     a.info = reinterpret_cast<RowInfo *>(take((size_t)a.Tp * sizeof(RowInfo)));
     a.start = reinterpret_cast<float *>(take((size_t)a.Vp * 4));
     if (!backward) {
@@ -681,6 +728,7 @@ qb_status forward(const LossArgs &a, hipStream_t st)
 {
     const int words = (a.V + S::BM - 1) / S::BM;
     const int64_t tiles = (int64_t)words * (a.Tp / S::BN);
+    if (a.counts) loss_count_kernel<false><<<(a.T + 1023) / 1024, 256, 0, st>>>(a);
     loss_rows_kernel<false><<<(a.T + 1023) / 1024 + (a.Vp + 1023) / 1024, 1024, 0, st>>>(a);
     loss_logits_kernel<S, false><<<(int)std::min<int64_t>(tiles, kAtWork<S>), 64 * S::kWaves, 0, st>>>(a);
     loss_join_kernel<<<(a.T + 15) / 16, 256, 0, st>>>(a, words);
@@ -690,6 +738,7 @@ qb_status forward(const LossArgs &a, hipStream_t st)
 template <typename S>
 qb_status backward(LossArgs a, hipStream_t st)
 {
+    if (a.counts) loss_count_kernel<true><<<(a.T + 1023) / 1024, 256, 0, st>>>(a);
     loss_rows_kernel<true><<<(a.T + 1023) / 1024 + (a.Vp + 1023) / 1024, 1024, 0, st>>>(a);
     for (a.v0 = 0; a.v0 < a.V; a.v0 += a.piece) {
         const int64_t tiles = (int64_t)(a.piece / S::BM) * (a.Tp / S::BN);

@@ -113,3 +113,44 @@ def test_a_query_that_is_no_number_is_not_one_that_sees_no_key(qb, name, heads, 
     for x, y in ((O, want[0]), (lse, want[1])):
         x[at, 1] = y[at, 1]
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("T,labelled", [(32768, 700), (32769, 700), (40_000, 1), (70_001, 70_001), (262_145, 3000), (40_000, 0)])
+def test_many_tokens_are_numbered_in_order(qb, T, labelled):
+    """beyond some tens of thousands the counting of tokens is a launch of its own"""
+    from test_gpu_vocab_loss import Case, check
+    say("vocabulary loss:", labelled, "of", T, "tokens")
+    c = Case(T, 300, 64, labelled=labelled, weights=True)
+    c.X[c.targets < 0] = float("nan")
+    loss, lse = qb.qb_vocab_loss_fwd(c.X, c.W, c.targets, bias=c.bias)
+    dX, dW, db = qb.qb_vocab_loss_bwd(c.dloss, c.X, c.W, c.targets, lse, bias=c.bias)
+    rows, rest = torch.nonzero(c.targets >= 0)[:, 0], c.targets < 0
+    assert (loss[rest] == 0).all() and (lse[rest] == 0).all() and (dX[rest] == 0).all()
+    if labelled == 0:
+        assert (dW == 0).all() and (db == 0).all()
+        return
+    few = Case(1, 1, 64)
+    few.X, few.W, few.bias, few.targets, few.dloss = c.X[rows], c.W, c.bias, c.targets[rows], c.dloss[rows]
+    val, tol = few.exact()
+    for n, x in (("loss", loss[rows]), ("lse", lse[rows]), ("dX", dX[rows]), ("dW", dW), ("dbias", db)):
+        check(n, x, val[n], tol[n])
+
+
+def test_the_time_of_many_tokens_grows_with_them(qb):
+    """four times the tokens, most of them without a target: not sixteen times the work"""
+    def least(T):
+        X, W = torch.zeros(T, 64, dtype=torch.bfloat16, device=DEV), torch.zeros(100, 64, dtype=torch.bfloat16, device=DEV)
+        targets = torch.full((T,), -100, dtype=torch.int64, device=DEV)
+        targets[::100] = 5
+        times = []
+        for _ in range(5):
+            begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            begin.record()
+            qb.qb_vocab_loss_fwd(X, W, targets)
+            end.record()
+            torch.cuda.synchronize()
+            times.append(begin.elapsed_time(end))
+        return min(times)
+    few, many = least(1 << 20), least(1 << 22)
+    say("vocabulary loss of 2^20 and 2^22 tokens:", few, many, "ms")
+    assert many < 8 * few
