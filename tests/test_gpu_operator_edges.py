@@ -154,3 +154,59 @@ def test_the_time_of_many_tokens_grows_with_them(qb):
     few, many = least(1 << 20), least(1 << 22)
     say("vocabulary loss of 2^20 and 2^22 tokens:", few, many, "ms")
     assert many < 8 * few
+
+
+GUARD = 1 << 16
+
+
+def guarded(bytes_):
+    """a workspace of that size, and whether what lies round it is untouched"""
+    held = torch.full((bytes_ + 2 * GUARD,), 77, dtype=torch.uint8, device=DEV)
+    return held[GUARD:GUARD + bytes_], lambda: bool((held[:GUARD] == 77).all() and (held[GUARD + bytes_:] == 77).all())
+
+
+ATTENTION = {
+    "one launch over a cache": dict(heads=4, kv_heads=2, q_lens=[1, 2], k_lens=[300, 40], causal=True),
+    "a cache in chunks": dict(heads=16, kv_heads=2, q_lens=[5, 1, 0], k_lens=[9000, 700, 40], causal=True),
+    "sequences by length": dict(heads=8, kv_heads=8, q_lens=[300, 1, 0, 129, 128, 70]),
+    "keys in parts": dict(heads=6, kv_heads=2, q_lens=[2500], causal=True),
+    "more keys than queries": dict(heads=3, kv_heads=1, q_lens=[70, 200], k_lens=[3000, 200], causal=True),
+    "groups of eighty in parts": dict(heads=80, kv_heads=1, q_lens=[300, 20], k_lens=[300, 400]),
+    "many sequences": dict(heads=2, kv_heads=1, q_lens=[(i * 37) % 140 for i in range(70)], p=0.1),
+}
+
+
+@pytest.mark.parametrize("type", ["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("name", ATTENTION)
+def test_attention_stays_in_its_workspace(qb, name, dim, type):
+    import ctypes
+    from test_gpu_attention import Case
+    say("attention in a workspace of the size asked for:", name, dim, type)
+    c = Case(type, dim, **ATTENTION[name])
+    a = ctypes.byref(qb.binding.Attention(Q=c.Q.data_ptr(), K=c.K.data_ptr(), V=c.V.data_ptr(), type=("bf16", "fp16").index(type), heads=c.heads, kv_heads=c.kv, dim=dim, total_q=c.Q.shape[0],
+                                          total_k=c.K.shape[0], n_seqs=len(c.q_lens), causal=c.causal, cu_q=c.cu_q.data_ptr(), cu_k=c.cu_k.data_ptr(), max_q=c.max_q, max_k=c.max_k,
+                                          scale=c.scale, p=c.p, seed=c.seed.data_ptr() if c.p else None))
+    lib = qb.load_library()
+    space, untouched = guarded(lib.qb_attention_fwd_workspace_nbytes(a))
+    O, lse = c.forward(qb, workspace=space)
+    assert untouched()
+    space, untouched = guarded(lib.qb_attention_bwd_workspace_nbytes(a))
+    grads = c.backward(qb, O, lse, workspace=space)
+    assert untouched()
+    assert all(torch.equal(x, y) for x, y in zip((O, lse) + tuple(grads), tuple(c.forward(qb)) + tuple(c.backward(qb, O, lse))))
+
+
+@pytest.mark.parametrize("T,V,K,labelled", [(1, 1, 64, 1), (300, 1003, 128, 300), (512, 30522, 768, 77), (513, 700, 64, 513), (3000, 2600, 320, 1300), (40_000, 3000, 64, 9000), (40_000, 257, 128, 0)])
+def test_vocabulary_loss_stays_in_its_workspace(qb, T, V, K, labelled):
+    from test_gpu_vocab_loss import Case
+    say("vocabulary loss in a workspace of the size asked for:", T, V, K, labelled)
+    c, lib = Case(T, V, K, labelled=labelled), qb.load_library()
+    space, untouched = guarded(lib.qb_vocab_loss_workspace_nbytes(T, V, K, 0))
+    loss, lse = qb.qb_vocab_loss_fwd(c.X, c.W, c.targets, bias=c.bias, workspace=space)
+    assert untouched()
+    space, untouched = guarded(lib.qb_vocab_loss_workspace_nbytes(T, V, K, 1))
+    grads = qb.qb_vocab_loss_bwd(c.dloss, c.X, c.W, c.targets, lse, bias=c.bias, workspace=space)
+    assert untouched()
+    again = qb.qb_vocab_loss_fwd(c.X, c.W, c.targets, bias=c.bias) + qb.qb_vocab_loss_bwd(c.dloss, c.X, c.W, c.targets, lse, bias=c.bias)
+    assert all(torch.equal(x, y) for x, y in zip((loss, lse) + tuple(grads), again))
