@@ -464,16 +464,22 @@ qb_status qb_dropout_bwd(const void *dY, int64_t n, int type, float p, const int
  *   cu_q, cu_k  device [n_seqs + 1] int32, ascending, within total_q and total_k (clamped on the device to stay inside);
  *   k_len       device [n_seqs] int32 or NULL; forward only
  *   max_q, max_k  host: no sequence has more queries, keys; max_q * heads / kv_heads < 2^30.  Results of sequences that
- *   have more are undefined
+ *   have more are undefined (nothing but the outputs and the workspace is written for them either)
  *   scale from 1e-36 to 2e8; 0 <= p < 1, and where p > 0: seed, heads <= 512, max_k <= 2^24
- *   O, dO [total_q, heads, dim] dense; lse [total_q, heads] fp32.  Rows outside all sequences are not written.
- *   What lies in K and V outside the sequences is not read; inside it must be finite.
+ *   O, dO [total_q, heads, dim] dense; lse [total_q, heads] fp32.  Rows outside all sequences are not written, neither of O and lse nor of the
+ *   gradients: where a tensor has room behind its last sequence and is used whole, clear the outputs before their first use.
+ *   What lies in K and V outside the sequences is not read; inside it must be finite, and so must dO, in rows that see no key too.
+ *   NaN in a row of Q makes its O and lse NaN.  A key whose q.k is below -10^30 counts as hidden.
+ *
+ * P, and in the backward dS = P (dP - delta), are rounded to the tensors' type for the last products (in fp16 multiplied by powers of two that are
+ * taken back, so that small ones are no subnormal numbers); results are rounded once more.  Scores |scale q.k| beyond 10^4 cost the backward bits of P
+ * in binary32 themselves.
  *
  * Workspace: qb_attention_fwd_workspace_nbytes / qb_attention_bwd_workspace_nbytes (0: NULL will do), 256-byte aligned, contents undefined before and
  * after.  Refused before anything is enqueued: QB_ERR_NULL, _SHAPE (dims, sizes), _VALUE (strides, types, scale, p), _WORKSPACE.
  *
- * qb_attention_bwd: O and lse as the forward wrote them.  dQ, dK, dV have the type of Q, with strides of their own (g_*),
- * and are overwritten.  The same call gives the same bits every time.
+ * qb_attention_bwd: O and lse as the forward wrote them.  dQ, dK, dV have the type of Q, with strides of their own; the sequences' rows of them
+ * are overwritten.  The same call gives the same bits every time.
  */
 typedef struct {
     const void *Q, *K, *V;
@@ -508,8 +514,8 @@ qb_status qb_attention_bwd(const qb_attention *a, const void *dO, const void *O,
  *   lse as the forward wrote it, dloss [T] fp32 (finite);  dX [T,K], dW [V,K] bfloat16, dbias [V] fp32 or NULL; overwritten
  * d is held in bfloat16, relative to the largest |dloss| and so exact in the weight of a mean over tokens.
  * X, W, dX, dW are 16-byte aligned, the workspace (qb_vocab_loss_workspace_nbytes(T,V,K, 0 forward / 1 backward) bytes) 256-byte aligned, the
- * rest as their types.  The backward works through the vocabulary in pieces, d of one piece at a time.  The same call gives the
- * same bits every time.
+ * rest as their types.  The backward works through the vocabulary in pieces, d of one piece at a time: up to 1 GiB, or of 256 words where those take more
+ * (beyond 2^21 tokens).  Its workspace has room for dbias's sums whether dbias is given or not.  The same call gives the same bits every time.
  * QB_ERR_SHAPE: T or V below 1 or above 2^24, K no multiple of QB_K_ALIGN or above QB_MAX_K.
  */
 size_t qb_vocab_loss_workspace_nbytes(int64_t T, int64_t V, int64_t K, int backward);

@@ -439,14 +439,16 @@ def qb_attention_fwd(Q, K, V, cu_q, cu_k, max_q, max_k, causal=False, scale=None
     """Attention of packed sequences: Q[total_q,heads,dim], K, V[total_k,kv_heads,dim] bf16 or fp16 with any strides that are multiples
     of 8 between rows and heads; cu_q, cu_k int32 offsets of the sequences, k_len int32 lengths where a cache has room to grow.
     max_q, max_k: at least the longest sequence's queries and keys.  scale: 1 / sqrt(dim) if None.  p, seed: dropout of the weights.
-    Returns (O[total_q,heads,dim], lse[total_q,heads] fp32)."""
+    Rows outside all sequences are not written: uninitialised in outputs made here, so pass cleared ones (O, lse) where a tensor has room
+    behind its last sequence.  Returns (O[total_q,heads,dim], lse[total_q,heads] fp32)."""
     return _native().attention_fwd(Q, K, V, cu_q, cu_k, max_q, max_k, causal, scale, k_len, p, seed, O, lse, workspace)
 
 
 def qb_attention_bwd(dO, Q, K, V, O, lse, cu_q, cu_k, max_q, max_k, causal=False, scale=None, p=0.0, seed=None, dQ=None, dK=None,
                      dV=None, workspace=None):
     """Gradients of qb_attention_fwd called with the same arguments, which gave O and lse.  dQ, dK, dV may be parts of one wider
-    tensor (the gradient of a projection that gives queries, keys and values).  Returns (dQ, dK, dV)."""
+    tensor (the gradient of a projection that gives queries, keys and values).  Rows outside all sequences are not written, as in the
+    forward: pass cleared gradients where what takes them reads such rows.  Returns (dQ, dK, dV)."""
     return _native().attention_bwd(Q, K, V, cu_q, cu_k, max_q, max_k, causal, scale, None, p, seed, dO, O, lse, dQ, dK, dV, workspace)
 
 

@@ -190,7 +190,7 @@ __device__ __forceinline__ void attend(Softmax<D> &x, const v8s (&q)[D / 16], co
 // others are under way (three where three workgroups fit a CU all the same).  Bound by the matrix cores and the vector unit in turn: a
 // wavefront's products wait for its exponentials, and the two or three wavefronts of a SIMD overlap them in part.  8192 causal keys, 16
 // heads of 64: 176 us, 0.78 PFLOP/s; sequences of up to 3999, 16 heads of 128: 108 us, 0.87.  Short sequences are bound by a workgroup's
-// start: 32 of up to 512, 12 heads of 64: 26 us, of which 11 go without any keys (places, first loads, outputs).
+// start: 32 of up to 512, 12 heads of 64: 26 us, and 12 without any keys (places, first loads, outputs).
 template <typename T, int D, bool DROP>
 __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uint16_t *O, float *lse, bool by_xcd)
 {
@@ -253,7 +253,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a, uin
         if (t + kStages - 1 < tiles) fetch(t + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
         const int left = wave_most - t * kKeys;
         const uint32_t tk = stage * 2 * kTile;
-constexpr bool kHalves = D == 64 && DROP;  // (without dropout's arithmetic to save, both in the kernel cost more: 177 -> 190 us for 8192 causal keys)
+        constexpr bool kHalves = D == 64 && DROP;  // (without dropout's arithmetic to save, both in the kernel cost more: 177 -> 190 us for 8192 causal keys)
         if (left > (kHalves ? 32 : 0)) attend<T, D, DROP>(x, q, op, tk, tk + kTile, t * kKeys, limit, (t + 1) * kKeys > wave_least, a.c, bits, a.threshold, row_q, head, lane);
         else if (kHalves && left > 0) attend<T, D, DROP, 1>(x, q, op, tk, tk + kTile, t * kKeys, limit, t * kKeys + 32 > wave_least, a.c, bits, a.threshold, row_q, head, lane);
     }

@@ -307,8 +307,8 @@ __host__ __device__ __forceinline__ RowTiles row_tiles(bool causal, const RowTil
 // dK and dV; 128 keys to a workgroup, 32 to a wavefront: a lane's results all of one key.  Where tiles of keys are few, a workgroup does
 // a part of the rows, and its binary32 sums go to the workspace for a third launch to join.  Scores are taken as S = Q K^T, so that a
 // lane holds sixteen rows of its key and P and dS are, as they lie, the operands of dV^T = dO^T P and dK^T = Q^T dS.  8192 causal keys, 16 heads
-// and 4 key heads of 64: 345 us and 11 to join the parts, 0.77 PFLOP/s of four products; a block of 32 x 32 takes about 1030 cycles of a SIMD, of
-// which its products are 512 and its vector instructions 520: one after the other.  32 sequences of up to 384 with dropout: 43 us.
+// and 4 key heads of 64: 340 us and 11 to join the parts, 0.78 PFLOP/s of four products; a block of 32 x 32 takes about 1000 cycles of a SIMD, of
+// which its products are 512 and its vector instructions 490: one after the other (counters of a run).  32 sequences of up to 384 with dropout: 43 us.
 template <typename T, int D, bool DROP>
 __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(const AttnArgs a, const GradArgs g, const RowTiling tiling, int splits, int most, bool by_xcd)
 {

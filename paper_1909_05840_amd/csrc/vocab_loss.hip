@@ -15,7 +15,7 @@ namespace qb {
 namespace {
 
 constexpr int64_t kMost = 1 << 24;              // tokens, words
-constexpr int64_t kPieceBytes = 1024ll << 20;   // d of a piece, at most (16384 tokens: 32768 words)
+constexpr int64_t kPieceBytes = 1024ll << 20;   // d of a piece, at most (16384 tokens: 32768 words), or of kRowPad words
 constexpr float kLow = -1.0e30f;               // the maximum of no words (finite, also in powers of two)
 constexpr int kRowPad = 256;                    // the list of tokens is padded to this
 

@@ -210,3 +210,34 @@ def test_vocabulary_loss_stays_in_its_workspace(qb, T, V, K, labelled):
     assert untouched()
     again = qb.qb_vocab_loss_fwd(c.X, c.W, c.targets, bias=c.bias) + qb.qb_vocab_loss_bwd(c.dloss, c.X, c.W, c.targets, lse, bias=c.bias)
     assert all(torch.equal(x, y) for x, y in zip((loss, lse) + tuple(grads), again))
+
+
+@pytest.mark.parametrize("low", [float("-inf"), -3.4028234e38])
+@pytest.mark.parametrize("T", [70, 700])
+def test_words_masked_by_their_bias(qb, T, low):
+    """words that nothing may choose, whole tiles of them among those, as padding of the vocabulary has it"""
+    say("vocabulary loss: words masked by a bias of", low, T)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(T)
+    X, W = torch.randn(T, 128, generator=g, device=DEV).bfloat16(), (torch.randn(1500, 128, generator=g, device=DEV) * 0.1).bfloat16()
+    bias = torch.full((1500,), low, device=DEV)
+    free = torch.cat([torch.arange(3, 200), torch.arange(1290, 1499)]).to(DEV)
+    bias[free] = 0.1
+    targets = free[torch.randint(0, len(free), (T,), generator=g, device=DEV)]
+    dloss = torch.full((T,), 1.0 / T, device=DEV)
+    place = torch.full((1500,), -1, device=DEV)
+    place[free] = torch.arange(len(free), device=DEV)
+    loss, lse = qb.qb_vocab_loss_fwd(X, W, targets, bias=bias)
+    want = qb.qb_vocab_loss_fwd(X, W[free], place[targets], bias=bias[free])
+    assert all(((x - y).abs() < 1e-5).all() for x, y in zip((loss, lse), want))
+    dX, dW, db = qb.qb_vocab_loss_bwd(dloss, X, W, targets, lse, bias=bias)
+    dX1, dW1, db1 = qb.qb_vocab_loss_bwd(dloss, X, W[free], place[targets], want[1], bias=bias[free])
+    for x, y in ((dX, dX1), (dW[free], dW1), (db[free], db1)):  # (lse and sums in another order: 2^-16, then bfloat16's rounding)
+        assert ((x.float() - y.float()).abs() <= 2.0 ** -7 * y.float().abs() + 2.0 ** -16 * y.float().abs().max()).all()
+    hidden = torch.ones(1500, dtype=torch.bool, device=DEV)
+    hidden[free] = False
+    assert (dW[hidden] == 0).all() and (db[hidden] == 0).all()
+    targets[5] = 0  # a target that is masked: a loss without bound, a gradient all the same
+    loss, lse = qb.qb_vocab_loss_fwd(X, W, targets, bias=bias)
+    assert loss[5] > 1e38 and torch.isfinite(loss[:5]).all() and torch.isfinite(lse).all()
+    assert all(torch.isfinite(x).all() for x in qb.qb_vocab_loss_bwd(dloss, X, W, targets, lse, bias=bias))
