@@ -31,7 +31,7 @@ struct GradArgs {
     float *stat;  // [2][total_q * heads + 1]: -lse / scale (-infinity for a row that sees nothing, and for the last entry: P is zero), -delta
     float *part;  // [pairs][tiles of keys][splits][128][dK, dV] of tiles in parts
     v2f *most;    // float16: [pairs][tiles_q][4] of a wavefront's rows the largest squared norm of dO, the largest |delta|
-    int tiles_q;  // tiles of 128 rows of the longest sequence
+    int tiles_q;  // tiles of 128 rows of a sequence of max_q (a longer one may have more, which there is no room for)
 };
 
 constexpr int kLift = 14;  // of P in float16, in powers of two: a weight that rounding has put a little above one, and any dS, stays below 65504
@@ -260,7 +260,7 @@ __global__ __launch_bounds__(256, D == 128 && EXACT ? 1 : 2) void attention_dq_k
         const float squared = halves_sum(norm);
         const bool counts = limit > 0 && squared < __builtin_inff() && __builtin_fabsf(delta) < __builtin_inff();
         const v2f most = {wave_max(counts ? squared : 0.0f), wave_max(counts ? __builtin_fabsf(delta) : 0.0f)};
-        if (lane == 0) g.most[(((int64_t)at.seq * a.kv_heads + kv) * g.tiles_q + at.tile) * 4 + wave] = most;
+        if (lane == 0 && at.tile < g.tiles_q) g.most[(((int64_t)at.seq * a.kv_heads + kv) * g.tiles_q + at.tile) * 4 + wave] = most;
     }
     write_row<T, D>(g.dQ + (int64_t)row_q * g.q_row + (int64_t)head * g.q_head, A, T::kNarrow ? __builtin_ldexpf(a.scale, -kLift - lift) : a.scale, hf, row < rows);
     if (row >= rows) return;

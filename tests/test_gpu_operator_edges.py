@@ -241,3 +241,25 @@ def test_words_masked_by_their_bias(qb, T, low):
     loss, lse = qb.qb_vocab_loss_fwd(X, W, targets, bias=bias)
     assert loss[5] > 1e38 and torch.isfinite(loss[:5]).all() and torch.isfinite(lse).all()
     assert all(torch.isfinite(x).all() for x in qb.qb_vocab_loss_bwd(dloss, X, W, targets, lse, bias=bias))
+
+
+@pytest.mark.parametrize("type", ["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("max_q,max_k", [(100, 900), (900, 100), (100, 100), (1, 1)])
+def test_batches_longer_than_named_stay_in_their_workspace(qb, max_q, max_k, dim, type):
+    """sequences in the order of their lengths: workgroups find their tiles by the device's lengths"""
+    import ctypes
+    from test_gpu_attention import Case
+    say("attention of up to 900 queries and keys,", max_q, "and", max_k, "named", dim, type)
+    c = Case(type, dim, 8, 8, [900, 100, 640], [700, 900, 640])
+    O, lse = c.forward(qb)
+    c.max_q, c.max_k = max_q, max_k
+    a = ctypes.byref(qb.binding.Attention(Q=c.Q.data_ptr(), K=c.K.data_ptr(), V=c.V.data_ptr(), type=("bf16", "fp16").index(type), heads=8, kv_heads=8, dim=dim, total_q=c.Q.shape[0],
+                                          total_k=c.K.shape[0], n_seqs=3, cu_q=c.cu_q.data_ptr(), cu_k=c.cu_k.data_ptr(), max_q=max_q, max_k=max_k, scale=c.scale))
+    lib = qb.load_library()
+    space, untouched = guarded(lib.qb_attention_fwd_workspace_nbytes(a))
+    c.forward(qb, workspace=space)
+    assert untouched()
+    space, untouched = guarded(lib.qb_attention_bwd_workspace_nbytes(a))
+    c.backward(qb, O, lse, workspace=space)
+    assert untouched()
