@@ -42,7 +42,7 @@ typedef enum {
     QB_ERR_CLIP = 4,       /* activation range not a positive finite number                  */
     QB_ERR_WORKSPACE = 5,  /* workspace NULL or misaligned although the call needs one       */
     QB_ERR_HIP = 6,        /* the HIP runtime refused a launch (its error state is cleared) */
-    QB_ERR_VALUE = 7       /* attention, loss, dropout: a type, stride, alignment, scale or probability out of range */
+    QB_ERR_VALUE = 7       /* 16-bit operators: a type, stride, alignment, scale or probability out of range, arguments that exclude each other */
 } qb_status;
 
 /* Host, pure.  Static string for a status. */
@@ -524,6 +524,100 @@ qb_status qb_vocab_loss_fwd(const uint16_t *X, const uint16_t *W, const float *b
 qb_status qb_vocab_loss_bwd(const float *dloss, const uint16_t *X, const uint16_t *W, const float *bias,
                             const int64_t *targets, const float *lse, int64_t T, int64_t V, int64_t K,
                             uint16_t *dX, uint16_t *dW, float *dbias, void *workspace, void *stream);
+
+/*
+ * Activations kept in 8 bits for the backward.  A row's values are cut into groups of QB_KEEP_GROUP, the last one possibly shorter:
+ *   scale = max |x| of the group / 127, rounded to binary32;  code = x / scale to the nearest whole number, half to even (the true quotient's; at most 127)
+ * and a code stands for code * scale.  A group of zeros has scale 0 and codes 0; one that holds an infinity or NaN reads back as NaN.
+ *   X       [T,W] of `type`, x_row values between rows (0 .. 2^22)
+ *   codes   [T,W] int8 dense, scales [T, ceil(W / QB_KEEP_GROUP)] fp32
+ * qb_restore_act writes code * scale rounded to `type`, [T,W] dense.
+ * 0 <= T <= 2^24 (0 does nothing), 1 <= W <= QB_MAX_K, else QB_ERR_SHAPE.  Pointers need the alignment of their type only.
+ */
+#define QB_KEEP_GROUP 64
+qb_status qb_checkpoint_act(const void *X, int64_t x_row, int type, int64_t T, int64_t W, int8_t *codes, float *scales, void *stream);
+qb_status qb_restore_act(const int8_t *codes, const float *scales, int64_t T, int64_t W, int type, void *X, void *stream);
+
+/*
+ * Layer norm of each row.
+ *   mean = sum_j X[t,j] / W;  rstd = 1 / sqrt(sum_j (X[t,j] - mean)^2 / W + eps);  h = (X - mean) rstd;  Y = h weight + bias
+ *   X, Y  [T,W] of `type`, X with x_row values between rows, Y dense (Y may be X);  weight, bias [W] fp32, or NULL for ones and zeros;  eps >= 0
+ *   mean, rstd  out [T] fp32;  codes, scales  out, Y in 8 bits as qb_checkpoint_act writes it (of the values before they are rounded to `type`), or both NULL
+ * qb_layer_norm_bwd, with g = dY weight:
+ *   dX = rstd (g - sum_j g / W - h sum_j g h / W) (+ residual);  dweight[j] = sum_t dY[t,j] h[t,j];  dbias[j] = sum_t dY[t,j]
+ *   X as the forward had it, or in 8 bits (x_codes, x_scales, and X NULL);  residual: the gradient that comes past the norm, or NULL
+ *   dX [T,W] dense of `type`, may be dY or residual where these are dense;  dweight, dbias [W] fp32, each may be NULL
+ * The backward's workspace (qb_layer_norm_bwd_workspace_nbytes bytes, 256-byte aligned) may be NULL where neither dweight nor dbias is asked for.  The same call gives
+ * the same bits every time.  0 <= T <= 2^24 (0: dweight and dbias are zero), 1 <= W <= QB_MAX_K, strides 0 .. 2^22.  Pointers need the alignment of their type only.
+ */
+qb_status qb_layer_norm_fwd(const void *X, int64_t x_row, int type, int64_t T, int64_t W, const float *weight, const float *bias, float eps,
+                            void *Y, float *mean, float *rstd, int8_t *codes, float *scales, void *stream);
+typedef struct {
+    const void *dY, *X;
+    const int8_t *x_codes;
+    const float *x_scales;
+    const void *residual;
+    int64_t dy_row, x_row, residual_row;
+    const float *weight, *mean, *rstd;
+    int type;
+    int64_t T, W;
+} qb_norm_grads;
+size_t qb_layer_norm_bwd_workspace_nbytes(int64_t T, int64_t W);
+qb_status qb_layer_norm_bwd(const qb_norm_grads *n, void *dX, float *dweight, float *dbias, void *workspace, void *stream);
+
+/*
+ * Linear layer in 16 bits (bf16 or fp16), with what follows it in the same launch.
+ *   z[t,n] = sum_j X[t,j] W[n,j] (+ bias[n]);  Y = act(z) (+ residual)
+ *   act  QB_ACT_NONE, _RELU, _GELU (z (1 + erf(z / sqrt 2)) / 2), _TANH
+ *   X [T,K] with x_row values between rows (a multiple of 8), W [N,K] dense, both 16-byte aligned;  bias [N] fp32 or NULL
+ *   residual [T,N] with residual_row values between rows, or NULL;  Y [T,N] dense
+ *   pre             out [T,N] dense, z in 16 bits for the backward of act, or NULL (only with an activation)
+ *   codes, scales   out, for the backward of what follows, as qb_checkpoint_act writes them: z in 8 bits where there is an activation, else Y (in both cases of
+ *                   the values in binary32, before they are rounded to `type`); or both NULL
+ * qb_linear_bwd: here act is the activation IN FRONT of the layer, X = act(pre), and dX is the gradient of pre:
+ *   dX = (dY W) act'(pre), or dY W with QB_ACT_NONE;  dW[n] = sum_t dY[t,n] X[t];  dbias[n] = sum_t dY[t,n]
+ *   dY [T,N] with dy_row values between rows (any)
+ *   X         as in the forward; or in 8 bits (x_codes, x_scales; X NULL); or, with pre given, neither: act(pre) is formed again
+ *   pre       [T,K] dense in 16 bits, or in 8 (pre_codes, pre_scales; pre NULL), where act is an activation; else both NULL
+ *   dX [T,K], dW [N,K] dense of `type`, dbias [N] fp32: each NULL where it is not wanted (W is not read without dX, X not without dW)
+ * X from 8 bits or from pre is rounded to `type`; sums are binary32, results are rounded once.  relu's derivative is 0 at 0.
+ * 0 <= T <= 2^24 (0: dW and dbias are zero), 1 <= N <= 2^20, K a multiple of QB_K_ALIGN up to QB_MAX_K, strides 0 .. 2^22.  Pointers without another word need the
+ * alignment of their type only.  Workspaces: 256-byte aligned, contents undefined before and after; 0 bytes: NULL will do.  The same call gives the same bits
+ * every time.  Y may be residual where that is dense.
+ */
+enum { QB_ACT_NONE = 0, QB_ACT_RELU = 1, QB_ACT_GELU = 2, QB_ACT_TANH = 3 };
+typedef struct {
+    int type, act;
+    int64_t T, N, K;
+    const void *X;
+    int64_t x_row;
+    const void *W;
+    const float *bias;
+    const void *residual;
+    int64_t residual_row;
+    void *Y, *pre;
+    int8_t *codes;
+    float *scales;
+} qb_linear;
+typedef struct {
+    int type, act;
+    int64_t T, N, K;
+    const void *dY;
+    int64_t dy_row;
+    const void *W, *X;
+    int64_t x_row;
+    const int8_t *x_codes;
+    const float *x_scales;
+    const void *pre;
+    const int8_t *pre_codes;
+    const float *pre_scales;
+    void *dX, *dW;
+    float *dbias;
+} qb_linear_grads;
+size_t qb_linear_fwd_workspace_nbytes(const qb_linear *l);
+qb_status qb_linear_fwd(const qb_linear *l, void *workspace, void *stream);
+size_t qb_linear_bwd_workspace_nbytes(const qb_linear_grads *l);
+qb_status qb_linear_bwd(const qb_linear_grads *l, void *workspace, void *stream);
 
 #ifdef __cplusplus
 }

@@ -33,7 +33,9 @@ EXPORTS = ("qb_status_string", "qb_packed_nbytes", "qb_bwd_workspace_nbytes", "q
            "qb_quantize_groupwise_asym", "qb_quantize_groupwise_asym_range", "qb_qlinear_fwd_asym", "qb_qlinear_fwd_asym_dyn", "qb_qlinear_bwd_ste_asym",
            "qb_power_iteration_scratch_floats", "qb_power_iteration", "qb_sensitivity_omega", "qb_rank_by_sensitivity",
            "qb_probe_mfma_i8", "qb_dropout_fwd", "qb_dropout_bwd", "qb_attention_fwd_workspace_nbytes", "qb_attention_bwd_workspace_nbytes",
-           "qb_attention_fwd", "qb_attention_bwd", "qb_vocab_loss_workspace_nbytes", "qb_vocab_loss_fwd", "qb_vocab_loss_bwd")
+           "qb_attention_fwd", "qb_attention_bwd", "qb_vocab_loss_workspace_nbytes", "qb_vocab_loss_fwd", "qb_vocab_loss_bwd",
+           "qb_checkpoint_act", "qb_restore_act", "qb_layer_norm_fwd", "qb_layer_norm_bwd_workspace_nbytes", "qb_layer_norm_bwd",
+           "qb_linear_fwd_workspace_nbytes", "qb_linear_fwd", "qb_linear_bwd_workspace_nbytes", "qb_linear_bwd")
 
 
 # int hv(void *ctx, const float *v, float *out, void *stream)
@@ -72,6 +74,28 @@ class AttentionGrads(ctypes.Structure):
     """qb_attention_grads of the C ABI"""
     _fields_ = [("dQ", ctypes.c_void_p), ("dK", ctypes.c_void_p), ("dV", ctypes.c_void_p), ("q_row", ctypes.c_int64), ("q_head", ctypes.c_int64),
                 ("k_row", ctypes.c_int64), ("k_head", ctypes.c_int64), ("v_row", ctypes.c_int64), ("v_head", ctypes.c_int64)]
+
+
+class NormGrads(ctypes.Structure):
+    """qb_norm_grads of the C ABI"""
+    _fields_ = [("dY", ctypes.c_void_p), ("X", ctypes.c_void_p), ("x_codes", ctypes.c_void_p), ("x_scales", ctypes.c_void_p), ("residual", ctypes.c_void_p),
+                ("dy_row", ctypes.c_int64), ("x_row", ctypes.c_int64), ("residual_row", ctypes.c_int64), ("weight", ctypes.c_void_p), ("mean", ctypes.c_void_p),
+                ("rstd", ctypes.c_void_p), ("type", ctypes.c_int), ("T", ctypes.c_int64), ("W", ctypes.c_int64)]
+
+
+class LinearLayer(ctypes.Structure):
+    """qb_linear of the C ABI"""
+    _fields_ = [("type", ctypes.c_int), ("act", ctypes.c_int), ("T", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("X", ctypes.c_void_p),
+                ("x_row", ctypes.c_int64), ("W", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("residual_row", ctypes.c_int64),
+                ("Y", ctypes.c_void_p), ("pre", ctypes.c_void_p), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class LinearGrads(ctypes.Structure):
+    """qb_linear_grads of the C ABI"""
+    _fields_ = [("type", ctypes.c_int), ("act", ctypes.c_int), ("T", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("dY", ctypes.c_void_p),
+                ("dy_row", ctypes.c_int64), ("W", ctypes.c_void_p), ("X", ctypes.c_void_p), ("x_row", ctypes.c_int64), ("x_codes", ctypes.c_void_p),
+                ("x_scales", ctypes.c_void_p), ("pre", ctypes.c_void_p), ("pre_codes", ctypes.c_void_p), ("pre_scales", ctypes.c_void_p), ("dX", ctypes.c_void_p),
+                ("dW", ctypes.c_void_p), ("dbias", ctypes.c_void_p)]
 
 
 class QBError(RuntimeError):
@@ -156,6 +180,24 @@ def load_library():
     lib.qb_vocab_loss_fwd.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, vp]
     lib.qb_vocab_loss_bwd.restype = ci
     lib.qb_vocab_loss_bwd.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, vp, vp]
+    lib.qb_checkpoint_act.restype = ci
+    lib.qb_checkpoint_act.argtypes = [vp, i64, ci, i64, i64, vp, vp, vp]
+    lib.qb_restore_act.restype = ci
+    lib.qb_restore_act.argtypes = [vp, vp, i64, i64, ci, vp, vp]
+    lib.qb_layer_norm_fwd.restype = ci
+    lib.qb_layer_norm_fwd.argtypes = [vp, i64, ci, i64, i64, vp, vp, cf, vp, vp, vp, vp, vp, vp]
+    lib.qb_layer_norm_bwd_workspace_nbytes.restype = ctypes.c_size_t
+    lib.qb_layer_norm_bwd_workspace_nbytes.argtypes = [i64, i64]
+    lib.qb_layer_norm_bwd.restype = ci
+    lib.qb_layer_norm_bwd.argtypes = [ctypes.POINTER(NormGrads), vp, vp, vp, vp, vp]
+    lib.qb_linear_fwd_workspace_nbytes.restype = ctypes.c_size_t
+    lib.qb_linear_fwd_workspace_nbytes.argtypes = [ctypes.POINTER(LinearLayer)]
+    lib.qb_linear_fwd.restype = ci
+    lib.qb_linear_fwd.argtypes = [ctypes.POINTER(LinearLayer), vp, vp]
+    lib.qb_linear_bwd_workspace_nbytes.restype = ctypes.c_size_t
+    lib.qb_linear_bwd_workspace_nbytes.argtypes = [ctypes.POINTER(LinearGrads)]
+    lib.qb_linear_bwd.restype = ci
+    lib.qb_linear_bwd.argtypes = [ctypes.POINTER(LinearGrads), vp, vp]
     lib.qb_unpack_codes.restype = ci
     lib.qb_unpack_codes.argtypes = [vp, i64, i64, ci, vp, vp]
     lib.qb_embedding_quantize.restype = ci
@@ -461,3 +503,51 @@ def qb_vocab_loss_fwd(X, W, targets, bias=None, loss=None, lse=None, workspace=N
 def qb_vocab_loss_bwd(dloss, X, W, targets, lse, bias=None, dX=None, dW=None, dbias=None, workspace=None):
     """Gradients for dloss[T] fp32: (dX[T,K] bf16, dW[V,K] bf16, dbias[V] fp32, or None where neither bias nor dbias is given)."""
     return _native().vocab_loss_bwd(dloss, X, W, targets, lse, bias, dX, dW, dbias, workspace)
+
+
+QB_ACTS = {None: 0, "relu": 1, "gelu": 2, "tanh": 3}
+
+
+def _act(name):
+    if name not in QB_ACTS:
+        raise ValueError("act must be one of None, 'relu', 'gelu', 'tanh'")
+    return QB_ACTS[name]
+
+
+def qb_checkpoint_act(X, codes=None, scales=None):
+    """X[T,W] fp32, bf16 or fp16 (rows may lie apart) in 8 bits: (codes[T,W] int8, scales[T,ceil(W/64)] fp32), one scale for 64 neighbours of a row."""
+    return _native().checkpoint_act(X, codes, scales)
+
+
+def qb_restore_act(codes, scales, dtype=torch.bfloat16, X=None):
+    """What qb_checkpoint_act kept, as a tensor [T,W] of `dtype` (that of X where X is given)."""
+    if X is None:
+        X = torch.empty(codes.shape, dtype=dtype, device=codes.device)
+    return _native().restore_act(codes, scales, X)
+
+
+def qb_layer_norm_fwd(X, weight=None, bias=None, eps=1e-5, keep=False, Y=None, mean=None, rstd=None, codes=None, scales=None):
+    """Layer norm of the rows of X[T,W] fp32, bf16 or fp16 (rows may lie apart); weight[W], bias[W] fp32 or None.  Returns (Y[T,W], mean[T], rstd[T]), and
+    with keep (codes, scales) of Y in 8 bits behind them."""
+    return _native().layer_norm_fwd(X, weight, bias, eps, keep, Y, mean, rstd, codes, scales)
+
+
+def qb_layer_norm_bwd(dY, X, weight, mean, rstd, residual=None, sums=True, dX=None, dweight=None, dbias=None, workspace=None):
+    """Gradients of qb_layer_norm_fwd, which gave mean and rstd: (dX[T,W], dweight[W] fp32, dbias[W] fp32).  X: the forward's, or (codes, scales) of it in 8
+    bits; weight may be None.  residual[T,W], the gradient that comes past the norm, is added to dX.  sums: whether dweight and dbias are
+    wanted; else they are None."""
+    return _native().layer_norm_bwd(dY, X, weight, mean, rstd, residual, sums, dX, dweight, dbias, workspace)
+
+
+def qb_linear_fwd(X, W, bias=None, act=None, residual=None, keep=None, Y=None, kept=None, workspace=None):
+    """Y = act(X W^T + bias) + residual: X[T,K] bf16 or fp16 (rows may lie apart by a multiple of 8), W[N,K] of its type, bias[N] fp32, act None, "relu", "gelu" or
+    "tanh", residual[T,N].  Returns Y[T,N]; with keep="codes" (Y, (codes[T,N], scales[T,ceil(N/64)])): what the backward needs in 8 bits, the values before the
+    activation, or Y where there is none; with keep="values" (Y, values): those before the activation in 16 bits.  kept: to be written into, as it is returned."""
+    return _native().linear_fwd(X, W, bias, _act(act), residual, keep, Y, kept, workspace)
+
+
+def qb_linear_bwd(dY, X, W, pre=None, act=None, need=(True, True, True), dX=None, dW=None, dbias=None, workspace=None):
+    """Gradients of qb_linear_fwd: (dX[T,K], dW[N,K], dbias[N] fp32).  X: the forward's input, or (codes, scales) of it in 8 bits.  Where the input was act(pre),
+    pre[T,K] or (codes, scales) of it gives dX the derivative of act, so that dX is the gradient of pre; X may then be None, act(pre) is formed again.
+    need: which of the three are wanted; the others are None."""
+    return _native().linear_bwd(dY, X, W, pre, _act(act), need, dX, dW, dbias, workspace)

@@ -10,7 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqbert.so")
 CALLS = os.path.join(HERE, "_calls.so")
 SOURCES = ("api.hip", "quantize.hip", "qgemm_i8.hip", "qgemm_i8_list.hip", "bwd_bf16.hip", "bwd_direct.hip", "hessian.hip",
-           "dropout.hip", "attention.hip", "attention_bwd.hip", "vocab_loss.hip")
+           "dropout.hip", "attention.hip", "attention_bwd.hip", "vocab_loss.hip",
+           "act_keep.hip", "layer_norm.hip", "linear.hip", "linear_bwd.hip")
 # packed-fp32 instructions are switched off for every device translation unit
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wno-inline-asm",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

@@ -21,18 +21,6 @@ struct DropArgs {
     float scale;
 };
 
-// sixteen bytes at any address (the load unit takes them with the same instruction, aligned or not)
-__device__ __forceinline__ v4u load16(const void *p, int64_t byte)
-{
-    struct __attribute__((packed)) Loose { v4u v; };
-    return reinterpret_cast<const Loose *>(static_cast<const uint8_t *>(p) + byte)->v;
-}
-__device__ __forceinline__ void store16(void *p, int64_t byte, v4u v)
-{
-    struct __attribute__((packed)) Loose { v4u v; };
-    reinterpret_cast<Loose *>(static_cast<uint8_t *>(p) + byte)->v = v;
-}
-
 // Sixteen bytes are a chunk: four values and one counter in 32 bits, eight values and two counters in 16.
 template <int TYPE>
 struct Chunk {

@@ -11,6 +11,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <cmath>
 #include <cstdarg>
@@ -856,6 +857,233 @@ QB_CALL(vocab_loss_bwd, 10)  // dloss, X, W, targets, lse, bias, dX, dW, dbias, 
     return tuple({dX, dW, db});
 }
 
+// ---- layer norm, 16-bit linears, activations in 8 bits
+
+// a tensor that the current stream's device can read
+const Tensor &here(PyObject *o, const char *name)
+{
+    const Tensor &t = tensor(o, name);
+    if (!t.is_cuda() || t.device().index() != c10::hip::current_device()) raise(PyExc_TypeError, "%s must be a tensor on the current GPU", name);
+    return t;
+}
+const Tensor &here(PyObject *o, at::IntArrayRef size, at::ScalarType type, const char *name)
+{
+    same_as(here(o, name), size, type, name);
+    return tensor(o, name);
+}
+// [rows, columns] with dense rows, which may lie apart
+struct Rows {
+    const Tensor *t = nullptr;
+    int64_t row = 0;
+    Rows() = default;
+    Rows(PyObject *o, const char *name) : t(&here(o, name))
+    {
+        if (t->dim() != 2 || (t->size(1) > 1 && t->stride(1) != 1)) raise(PyExc_ValueError, "%s must be [rows, columns] with dense rows", name);
+        row = t->size(0) > 1 ? t->stride(0) : t->size(1);
+    }
+    Rows(PyObject *o, at::IntArrayRef size, at::ScalarType type, const char *name) : Rows(o, name)
+    {
+        if (t->scalar_type() != type) raise(PyExc_TypeError, "%s must be a %s tensor", name, type_name(type));
+        if (t->sizes() != size) raise(PyExc_ValueError, "%s has other sizes than the call", name);
+    }
+    void *data() const { return t ? t->data_ptr() : nullptr; }
+};
+int64_t groups_of(int64_t width) { return (width + QB_KEEP_GROUP - 1) / QB_KEEP_GROUP; }
+// (codes, scales) of [rows, width]
+struct Kept {
+    Tensor codes, scales;
+    Kept() = default;
+    Kept(PyObject *o, int64_t rows, int64_t width, const char *name)
+    {
+        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 2) raise(PyExc_TypeError, "%s must be a tensor or (codes, scales)", name);
+        codes = here(PyTuple_GET_ITEM(o, 0), {rows, width}, at::kChar, "codes");
+        scales = here(PyTuple_GET_ITEM(o, 1), {rows, groups_of(width)}, at::kFloat, "scales");
+    }
+    const int8_t *code() const { return codes.defined() ? static_cast<const int8_t *>(codes.data_ptr()) : nullptr; }
+    const float *scale() const { return scales.defined() ? static_cast<const float *>(scales.data_ptr()) : nullptr; }
+};
+const float *floats(PyObject *o, int64_t n, const char *name)  // or None
+{
+    return o == Py_None ? nullptr : ptr<float>(here(o, {n}, at::kFloat, name));
+}
+bool truth(PyObject *o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw_python_error();
+    return v != 0;
+}
+Tensor here_or_new(PyObject *o, at::IntArrayRef size, at::ScalarType type, const at::Device &dev, const char *name)
+{
+    if (o != Py_None) here(o, name);
+    return result(o, size, type, dev, name);
+}
+Tensor space(PyObject *o, size_t bytes, const at::Device &dev)
+{
+    if (o != Py_None) here(o, "workspace");
+    return workspace_of(o, bytes, dev);
+}
+float *floats(const Tensor &t) { return static_cast<float *>(where(t)); }
+
+QB_CALL(checkpoint_act, 3)  // X, codes, scales
+{
+    const Rows x(a[0], "X");
+    const int type = type_code(*x.t, "X", true);
+    const int64_t T = x.t->size(0), W = x.t->size(1);
+    const at::Device dev = x.t->device();
+    const Tensor codes = here_or_new(a[1], {T, W}, at::kChar, dev, "codes"), scales = here_or_new(a[2], {T, groups_of(W)}, at::kFloat, dev, "scales");
+    call(qb_checkpoint_act, x.data(), x.row, type, T, W, static_cast<int8_t *>(codes.data_ptr()), floats(scales), stream());
+    return tuple({codes, scales});
+}
+
+QB_CALL(restore_act, 3)  // codes, scales, X
+{
+    const Tensor &codes = here(a[0], "codes");
+    if (codes.dim() != 2) raise(PyExc_ValueError, "codes must have two dimensions");
+    const int64_t T = codes.size(0), W = codes.size(1);
+    here(a[0], {T, W}, at::kChar, "codes");
+    const Tensor &scales = here(a[1], {T, groups_of(W)}, at::kFloat, "scales"), &X = here(a[2], "X");
+    const int type = type_code(X, "X", true);
+    here(a[2], {T, W}, X.scalar_type(), "X");
+    call(qb_restore_act, static_cast<const int8_t *>(codes.data_ptr()), floats(scales), T, W, type, X.data_ptr(), stream());
+    return wrapped(X);
+}
+
+QB_CALL(layer_norm_fwd, 10)  // X, weight, bias, eps, keep, Y, mean, rstd, codes, scales
+{
+    const Rows x(a[0], "X");
+    const int type = type_code(*x.t, "X", true);
+    const int64_t T = x.t->size(0), W = x.t->size(1);
+    const at::Device dev = x.t->device();
+    const float *const w = floats(a[1], W, "weight"), *const b = floats(a[2], W, "bias"), eps = real(a[3]);
+    const bool keep = truth(a[4]);
+    const Tensor Y = here_or_new(a[5], {T, W}, x.t->scalar_type(), dev, "Y"), mean = here_or_new(a[6], {T}, at::kFloat, dev, "mean"), rstd = here_or_new(a[7], {T}, at::kFloat, dev, "rstd");
+    Tensor codes, scales;
+    if (keep) {
+        codes = here_or_new(a[8], {T, W}, at::kChar, dev, "codes");
+        scales = here_or_new(a[9], {T, groups_of(W)}, at::kFloat, dev, "scales");
+    }
+    call(qb_layer_norm_fwd, x.data(), x.row, type, T, W, w, b, eps, Y.data_ptr(), floats(mean), floats(rstd), static_cast<int8_t *>(where(codes)), floats(scales), stream());
+    return keep ? tuple({Y, mean, rstd, codes, scales}) : tuple({Y, mean, rstd});
+}
+
+QB_CALL(layer_norm_bwd, 11)  // dY, X, weight, mean, rstd, residual, sums, dX, dweight, dbias, workspace
+{
+    const Rows dy(a[0], "dY");
+    qb_norm_grads n = {};
+    n.type = type_code(*dy.t, "dY", true);
+    n.T = dy.t->size(0);
+    n.W = dy.t->size(1);
+    const at::ScalarType type = dy.t->scalar_type();
+    const at::Device dev = dy.t->device();
+    const at::IntArrayRef size = dy.t->sizes();
+    Rows x, residual;
+    Kept kept;
+    if (THPVariable_Check(a[1])) x = Rows(a[1], size, type, "X");
+    else kept = Kept(a[1], n.T, n.W, "X");
+    if (a[5] != Py_None) residual = Rows(a[5], size, type, "residual");
+    n.dY = dy.data(); n.X = x.data(); n.residual = residual.data();
+    n.x_codes = kept.code(); n.x_scales = kept.scale();
+    n.dy_row = dy.row; n.x_row = x.row; n.residual_row = residual.row;
+    n.weight = floats(a[2], n.W, "weight");
+    n.mean = ptr<float>(here(a[3], {n.T}, at::kFloat, "mean"));
+    n.rstd = ptr<float>(here(a[4], {n.T}, at::kFloat, "rstd"));
+    const bool sums = truth(a[6]);
+    const Tensor dX = here_or_new(a[7], size, type, dev, "dX");
+    Tensor dw, db;
+    if (sums) {
+        dw = here_or_new(a[8], {n.W}, at::kFloat, dev, "dweight");
+        db = here_or_new(a[9], {n.W}, at::kFloat, dev, "dbias");
+    }
+    const Tensor ws = space(a[10], sums ? qb_layer_norm_bwd_workspace_nbytes(n.T, n.W) : 0, dev);
+    call(qb_layer_norm_bwd, &n, dX.data_ptr(), floats(dw), floats(db), where(ws), stream());
+    return tuple({dX, dw, db});
+}
+
+QB_CALL(linear_fwd, 9)  // X, W, bias, act, residual, keep, Y, kept, workspace
+{
+    const Rows x(a[0], "X");
+    qb_linear l = {};
+    l.type = type_code(*x.t, "X", false);
+    const at::ScalarType type = x.t->scalar_type();
+    const Tensor &W = here(a[1], "W");
+    if (W.dim() != 2 || W.size(1) != x.t->size(1)) raise(PyExc_ValueError, "W must be [N, K] with the K of X");
+    here(a[1], W.sizes(), type, "W");
+    l.T = x.t->size(0); l.K = x.t->size(1); l.N = W.size(0);
+    const at::Device dev = x.t->device();
+    l.bias = floats(a[2], l.N, "bias");
+    l.act = small(a[3]);
+    Rows residual;
+    if (a[4] != Py_None) residual = Rows(a[4], {l.T, l.N}, type, "residual");
+    const bool codes = a[5] != Py_None && PyUnicode_Check(a[5]) && PyUnicode_CompareWithASCIIString(a[5], "codes") == 0;
+    const bool values = a[5] != Py_None && PyUnicode_Check(a[5]) && PyUnicode_CompareWithASCIIString(a[5], "values") == 0;
+    if (a[5] != Py_None && !codes && !values) raise(PyExc_ValueError, "keep must be None, 'codes' or 'values'");
+    if (values && l.act == QB_ACT_NONE) raise(PyExc_ValueError, "keep='values' needs an activation");
+    const Tensor Y = here_or_new(a[6], {l.T, l.N}, type, dev, "Y");
+    Kept kept;
+    Tensor pre;
+    if (codes && a[7] != Py_None) {
+        kept = Kept(a[7], l.T, l.N, "kept");
+    } else if (codes) {
+        kept.codes = fresh({l.T, l.N}, at::kChar, dev);
+        kept.scales = fresh({l.T, groups_of(l.N)}, at::kFloat, dev);
+    } else if (values) {
+        pre = here_or_new(a[7], {l.T, l.N}, type, dev, "kept");
+    }
+    l.X = x.data(); l.x_row = x.row; l.W = W.data_ptr();
+    l.residual = residual.data(); l.residual_row = residual.row;
+    l.Y = Y.data_ptr(); l.pre = where(pre);
+    l.codes = const_cast<int8_t *>(kept.code()); l.scales = const_cast<float *>(kept.scale());
+    const Tensor ws = space(a[8], qb_linear_fwd_workspace_nbytes(&l), dev);
+    call(qb_linear_fwd, &l, where(ws), stream());
+    if (values) return tuple({Y, pre});
+    if (!codes) return wrapped(Y);
+    THPObjectPtr y(wrapped(Y)), k(tuple({kept.codes, kept.scales}));
+    PyObject *const r = PyTuple_Pack(2, y.get(), k.get());
+    if (!r) throw_python_error();
+    return r;
+}
+
+QB_CALL(linear_bwd, 10)  // dY, X, W, pre, act, need, dX, dW, dbias, workspace
+{
+    const Rows dy(a[0], "dY");
+    qb_linear_grads l = {};
+    l.type = type_code(*dy.t, "dY", false);
+    const at::ScalarType type = dy.t->scalar_type();
+    const at::Device dev = dy.t->device();
+    const Tensor &W = here(a[2], "W");
+    if (W.dim() != 2 || W.size(0) != dy.t->size(1)) raise(PyExc_ValueError, "W must be [N, K] with the N of dY");
+    here(a[2], W.sizes(), type, "W");
+    l.T = dy.t->size(0); l.N = W.size(0); l.K = W.size(1);
+    Rows x;
+    Kept x8, pre8;
+    const Tensor *pre = nullptr;
+    if (a[1] != Py_None) {
+        if (THPVariable_Check(a[1])) x = Rows(a[1], {l.T, l.K}, type, "X");
+        else x8 = Kept(a[1], l.T, l.K, "X");
+    }
+    if (a[3] != Py_None) {
+        if (THPVariable_Check(a[3])) pre = &here(a[3], {l.T, l.K}, type, "pre");
+        else pre8 = Kept(a[3], l.T, l.K, "pre");
+    }
+    l.act = small(a[4]);
+    if ((a[3] != Py_None) != (l.act != QB_ACT_NONE)) raise(PyExc_ValueError, "pre and act go together");
+    PyObject *const need = a[5];
+    if (!PyTuple_Check(need) || PyTuple_GET_SIZE(need) != 3) raise(PyExc_TypeError, "need must be a tuple of three truth values");
+    const bool nx = truth(PyTuple_GET_ITEM(need, 0)), nw = truth(PyTuple_GET_ITEM(need, 1)), nb = truth(PyTuple_GET_ITEM(need, 2));
+    if (nw && a[1] == Py_None && a[3] == Py_None) raise(PyExc_ValueError, "dW needs X or pre");
+    Tensor dX, dW, db;
+    if (nx) dX = here_or_new(a[6], {l.T, l.K}, type, dev, "dX");
+    if (nw) dW = here_or_new(a[7], {l.N, l.K}, type, dev, "dW");
+    if (nb) db = here_or_new(a[8], {l.N}, at::kFloat, dev, "dbias");
+    l.dY = dy.data(); l.dy_row = dy.row; l.W = W.data_ptr();
+    l.X = x.data(); l.x_row = x.row; l.x_codes = x8.code(); l.x_scales = x8.scale();
+    l.pre = pre ? pre->data_ptr() : nullptr; l.pre_codes = pre8.code(); l.pre_scales = pre8.scale();
+    l.dX = where(dX); l.dW = where(dW); l.dbias = floats(db);
+    const Tensor ws = space(a[9], qb_linear_bwd_workspace_nbytes(&l), dev);
+    call(qb_linear_bwd, &l, where(ws), stream());
+    return tuple({dX, dW, db});
+}
+
 PyObject *set_error(PyObject *, PyObject *cls)
 {
     Py_INCREF(cls);
@@ -872,7 +1100,8 @@ PyMethodDef g_methods[] = {
     QB_ENTRY(qlinear_fwd_q8), QB_ENTRY(qlinear_bwd_ste), QB_ENTRY(qlinear_bwd_ste_static), QB_ENTRY(qlinear_bwd_ste_masked),
     QB_ENTRY(qlinear_bwd_ste_asym), QB_ENTRY(embedding_quantize), QB_ENTRY(embedding_quantize_bits), QB_ENTRY(embedding_gather),
     QB_ENTRY(embedding_gather_bits), QB_ENTRY(dropout_fwd), QB_ENTRY(dropout_bwd), QB_ENTRY(attention_fwd), QB_ENTRY(attention_bwd),
-    QB_ENTRY(vocab_loss_fwd), QB_ENTRY(vocab_loss_bwd),
+    QB_ENTRY(vocab_loss_fwd), QB_ENTRY(vocab_loss_bwd), QB_ENTRY(checkpoint_act), QB_ENTRY(restore_act),
+    QB_ENTRY(layer_norm_fwd), QB_ENTRY(layer_norm_bwd), QB_ENTRY(linear_fwd), QB_ENTRY(linear_bwd),
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

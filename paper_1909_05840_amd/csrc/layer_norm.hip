@@ -1,0 +1,317 @@
+// Layer norm and its backward.
+//
+//   mean = sum x / W;  rstd = 1 / sqrt(sum (x - mean)^2 / W + eps);  h = (x - mean) rstd;  y = h w + b
+//   g = dy w;  dx = rstd (g - sum g / W - h sum g h / W) (+ residual);  dw = sum_t dy h;  db = sum_t dy
+//
+// A row stays in the registers of a wavefront or a workgroup between its loads and its stores; the squares are of x - mean, as the formula has
+// them.  Bound by memory.  The backward's threads keep their columns from row to row and so hold their share of dw and db; a workgroup's share
+// goes to the workspace, and a second launch adds these up in a fixed order.
+#include "qb_acts.hpp"
+#include <algorithm>
+
+namespace qb {
+namespace {
+
+struct NormArgs {
+    const void *X, *dY, *residual;
+    int64_t x_row, dy_row, residual_row;
+    const int8_t *x_codes;  // X in 8 bits, instead of X
+    const float *x_scales, *weight, *bias;
+    float eps;
+    int T, W;
+    void *Y;  // backward: dX
+    float *mean, *rstd;
+    int8_t *codes;
+    float *scales;
+    float *part;  // [workgroups][2][W]: dw, db
+    float *dweight, *dbias;
+};
+
+// R threads to a row, C chunks of eight values to a thread
+template <int R, int C>
+struct Row {
+    static constexpr int kThreads = R > 256 ? R : 256, kRows = kThreads / R, kWaves = R / 64;
+    static __device__ __forceinline__ int col(int i) { return (i * R + (int)(threadIdx.x % R)) * 8; }
+    // the sums of two values over a row's threads
+    static __device__ __forceinline__ v2f sum(float a, float b, v2f *shared)
+    {
+        a = wave_add(a);
+        b = wave_add(b);
+        if constexpr (R > 64) {
+            __syncthreads();  // (the last sum has been read)
+            if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v2f{a, b};
+            __syncthreads();
+            const int first = (int)(threadIdx.x / R) * kWaves;
+            a = b = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) {
+                a += shared[first + i][0];
+                b += shared[first + i][1];
+            }
+        }
+        return v2f{a, b};
+    }
+};
+__device__ __forceinline__ void columns(const float *p, float other, int col, int W, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = p && col + i < W ? p[col + i] : other;
+}
+
+template <int TYPE, int R, int C>
+__global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_kernel(const NormArgs a)
+{
+    typedef Row<R, C> L;
+    __shared__ v2f shared[L::kThreads / 64];
+    float w[C][8], b[C][8];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        columns(a.weight, 1.0f, L::col(i), a.W, w[i]);
+        columns(a.bias, 0.0f, L::col(i), a.W, b[i]);
+    }
+    for (int row0 = blockIdx.x * L::kRows; row0 < a.T; row0 += gridDim.x * L::kRows) {
+        const int row = row0 + (int)(threadIdx.x / R);
+        if (R == 64 && row >= a.T) break;
+        Eight<TYPE> x[C];
+        float v[C][8], s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < C; ++i) x[i].load(a.X, row * a.x_row + L::col(i), a.W - L::col(i));
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            x[i].get(v[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s += v[i][e];
+        }
+        // the differences from a mean that is rounded say what it is off, and the squares are corrected for that (equal values have no variance)
+        const float near = L::sum(s, 0.0f, shared)[0] / (float)a.W;
+        float q = 0.0f;
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[i][e] = L::col(i) + e < a.W ? v[i][e] - near : 0.0f;
+                q = __builtin_fmaf(v[i][e], v[i][e], q);
+                s += v[i][e];
+            }
+        const v2f both = L::sum(q, s, shared);
+        const float more = both[1] / (float)a.W, mean = near + more;
+        const float rstd = 1.0f / sqrtf(fmaxf(__builtin_fmaf(-more, more, both[0] / (float)a.W), 0.0f) + a.eps);
+        if (threadIdx.x % R == 0) {
+            a.mean[row] = mean;
+            a.rstd[row] = rstd;
+        }
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = __builtin_fmaf((v[i][e] - more) * rstd, w[i][e], b[i][e]);
+            if (a.codes) keep8(v[i], a.codes, a.scales, row, a.W, L::col(i));
+            x[i].set(v[i]);
+            x[i].store(a.Y, (int64_t)row * a.W + L::col(i), a.W - L::col(i));
+        }
+    }
+}
+
+template <int TYPE, int R, int C>
+__global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_bwd_kernel(const NormArgs a)
+{
+    typedef Row<R, C> L;
+    __shared__ v2f shared[L::kThreads / 64];
+    const float inv = 1.0f / (float)a.W;
+    float w[C][8], dw[C][8], db[C][8];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        columns(a.weight, 1.0f, L::col(i), a.W, w[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dw[i][e] = db[i][e] = 0.0f;
+    }
+    for (int row0 = blockIdx.x * L::kRows; row0 < a.T; row0 += gridDim.x * L::kRows) {
+        const int row = row0 + (int)(threadIdx.x / R);
+        if (R == 64 && row >= a.T) break;
+        Eight<TYPE> x[C], g[C], r[C];
+        float h[C][8], v[C][8], s = 0.0f, sh = 0.0f;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            g[i].load(a.dY, row * a.dy_row + L::col(i), a.W - L::col(i));
+            if (a.x_codes) kept8(h[i], a.x_codes, a.x_scales, row, a.W, L::col(i));
+            else x[i].load(a.X, row * a.x_row + L::col(i), a.W - L::col(i));
+            if (a.residual) r[i].load(a.residual, row * a.residual_row + L::col(i), a.W - L::col(i));
+        }
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            g[i].get(v[i]);
+            if (!a.x_codes) x[i].get(h[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                h[i][e] = (h[i][e] - mean) * rstd;  // (values past the row's end meet gradients of zero)
+                dw[i][e] = __builtin_fmaf(v[i][e], h[i][e], dw[i][e]);
+                db[i][e] += v[i][e];
+                v[i][e] *= w[i][e];
+                s += v[i][e];
+                sh = __builtin_fmaf(v[i][e], h[i][e], sh);
+            }
+        }
+        const v2f m = L::sum(s, sh, shared) * inv;
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            float past[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) past[e] = 0.0f;
+            if (a.residual) r[i].get(past);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = __builtin_fmaf(v[i][e] - __builtin_fmaf(h[i][e], m[1], m[0]), rstd, past[e]);
+            x[i].set(v[i]);
+            x[i].store(a.Y, (int64_t)row * a.W + L::col(i), a.W - L::col(i));
+        }
+    }
+    if (!a.part) return;
+    // the rows of a workgroup that worked side by side
+    if constexpr (L::kRows > 1) {
+        __shared__ float other[2][L::kRows - 1][R * 8];
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int at = (int)(threadIdx.x % R), team = (int)(threadIdx.x / R);
+            __syncthreads();
+            if (team > 0)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    other[0][team - 1][e * R + at] = dw[i][e];
+                    other[1][team - 1][e * R + at] = db[i][e];
+                }
+            __syncthreads();
+            if (team == 0)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    for (int t = 0; t < L::kRows - 1; ++t) {
+                        dw[i][e] += other[0][t][e * R + at];
+                        db[i][e] += other[1][t][e * R + at];
+                    }
+        }
+    }
+    if (threadIdx.x >= R) return;
+    float *const to = a.part + (int64_t)blockIdx.x * 2 * a.W;
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (L::col(i) + e < a.W) {
+                to[L::col(i) + e] = dw[i][e];
+                to[a.W + L::col(i) + e] = db[i][e];
+            }
+}
+
+// dw and db from the workgroups' shares: 64 columns to a workgroup, sixteen wavefronts on shares of their own
+__global__ __launch_bounds__(1024) void layer_norm_join_kernel(const NormArgs a, int parts)
+{
+    __shared__ float sums[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane, all = 2 * a.W;
+    float s = 0.0f;
+    if (col < all) {
+#pragma unroll 8
+        for (int p = wave; p < parts; p += 16) s += a.part[(int64_t)p * all + col];
+    }
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0 || col >= all) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += sums[i][lane];
+    if (col < a.W) {
+        if (a.dweight) a.dweight[col] = s;
+    } else if (a.dbias) {
+        a.dbias[col - a.W] = s;
+    }
+}
+
+// f with the threads to a row and the chunks to a thread that rows of W values take
+template <typename F>
+void by_width(int64_t W, const F &f)
+{
+    if (W <= 512) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+    else if (W <= 1024) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
+    else if (W <= 2048) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
+    else if (W <= 4096) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
+    else if (W <= 8192) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{});
+    else if (W <= 16384) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
+    else f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 4>{});
+}
+template <typename F>
+void by_type(int type, const F &f)
+{
+    if (type == QB_TYPE_BF16) f(std::integral_constant<int, QB_TYPE_BF16>{});
+    else if (type == QB_TYPE_FP16) f(std::integral_constant<int, QB_TYPE_FP16>{});
+    else f(std::integral_constant<int, QB_TYPE_FP32>{});
+}
+inline int rows_of(int64_t W) { return W <= 1024 ? 4 : 1; }  // that a workgroup works on at once
+inline int bwd_groups(int64_t T, int64_t W) { return (int)std::min<int64_t>((T + rows_of(W) - 1) / rows_of(W), W <= 4096 ? 512 : 256); }
+
+bool shape_ok(int64_t T, int64_t W) { return T >= 0 && T <= kMostRows && W >= 1 && W <= QB_MAX_K; }
+
+}  // namespace
+}  // namespace qb
+
+using namespace qb;
+
+extern "C" qb_status qb_layer_norm_fwd(const void *X, int64_t x_row, int type, int64_t T, int64_t W, const float *weight, const float *bias, float eps,
+                                       void *Y, float *mean, float *rstd, int8_t *codes, float *scales, void *stream)
+{
+    if (!shape_ok(T, W)) return QB_ERR_SHAPE;
+    if (!type_ok(type) || !stride_ok(x_row) || !(eps >= 0.0f && eps < __builtin_inff())) return QB_ERR_VALUE;
+    if (T == 0) return QB_OK;
+    if (!X || !Y || !mean || !rstd || !codes != !scales) return QB_ERR_NULL;
+    if (misaligned(X, size_of(type)) || misaligned(Y, size_of(type)) || misaligned(weight, 4) || misaligned(bias, 4) || misaligned(mean, 4) || misaligned(rstd, 4) ||
+        misaligned(scales, 4))
+        return QB_ERR_VALUE;
+    NormArgs a = {};
+    a.X = X; a.x_row = x_row; a.T = (int)T; a.W = (int)W;
+    a.weight = weight; a.bias = bias; a.eps = eps;
+    a.Y = Y; a.mean = mean; a.rstd = rstd; a.codes = codes; a.scales = scales;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    by_type(type, [&](auto t) {
+        by_width(W, [&](auto r, auto c) {
+            typedef Row<decltype(r)::value, decltype(c)::value> L;
+            const int64_t groups = (T + L::kRows - 1) / L::kRows;
+            layer_norm_kernel<decltype(t)::value, decltype(r)::value, decltype(c)::value><<<(int)std::min<int64_t>(groups, 2048), L::kThreads, 0, st>>>(a);
+        });
+    });
+    return launch_status();
+}
+
+extern "C" size_t qb_layer_norm_bwd_workspace_nbytes(int64_t T, int64_t W)
+{
+    return shape_ok(T, W) ? (size_t)bwd_groups(T, W) * 2 * (size_t)W * 4 : 0;
+}
+
+extern "C" qb_status qb_layer_norm_bwd(const qb_norm_grads *n, void *dX, float *dweight, float *dbias, void *workspace, void *stream)
+{
+    if (!n) return QB_ERR_NULL;
+    if (!shape_ok(n->T, n->W)) return QB_ERR_SHAPE;
+    if (!type_ok(n->type) || !stride_ok(n->dy_row) || !stride_ok(n->x_row) || !stride_ok(n->residual_row)) return QB_ERR_VALUE;
+    const bool sums = dweight || dbias;
+    if (n->T > 0) {
+        if (!n->dY || !n->mean || !n->rstd || !dX || (!n->X) == (!n->x_codes) || !n->x_codes != !n->x_scales) return QB_ERR_NULL;
+        const int size = size_of(n->type);
+        if (misaligned(n->dY, size) || misaligned(n->X, size) || misaligned(n->residual, size) || misaligned(dX, size) || misaligned(n->x_scales, 4) || misaligned(n->weight, 4) ||
+            misaligned(n->mean, 4) || misaligned(n->rstd, 4) || misaligned(dweight, 4) || misaligned(dbias, 4))
+            return QB_ERR_VALUE;
+        if (sums && (!workspace || misaligned(workspace, 256))) return QB_ERR_WORKSPACE;
+    }
+    NormArgs a = {};
+    a.X = n->X; a.dY = n->dY; a.residual = n->residual;
+    a.x_row = n->x_row; a.dy_row = n->dy_row; a.residual_row = n->residual_row;
+    a.x_codes = n->x_codes; a.x_scales = n->x_scales; a.weight = n->weight;
+    a.T = (int)n->T; a.W = (int)n->W;
+    a.Y = dX; a.mean = const_cast<float *>(n->mean); a.rstd = const_cast<float *>(n->rstd);
+    a.part = sums ? static_cast<float *>(workspace) : nullptr;
+    a.dweight = dweight; a.dbias = dbias;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const int groups = bwd_groups(n->T, n->W);
+    if (groups > 0)
+        by_type(n->type, [&](auto t) {
+            by_width(n->W, [&](auto r, auto c) {
+                layer_norm_bwd_kernel<decltype(t)::value, decltype(r)::value, decltype(c)::value><<<groups, Row<decltype(r)::value, decltype(c)::value>::kThreads, 0, st>>>(a);
+            });
+        });
+    if (sums) layer_norm_join_kernel<<<(2 * a.W + 63) / 64, 1024, 0, st>>>(a, groups);
+    return launch_status();
+}

@@ -1,4 +1,4 @@
-// What the kernels of attention and of the vocabulary loss share: the 16-bit types with their matrix instructions, tiles
+// What the kernels of attention, of the vocabulary loss and of the other 16-bit operators share: the 16-bit types with their matrix instructions, tiles
 // of rows in LDS, copies into them, the generator of dropout's random bits.
 #pragma once
 #include "qb_common.hpp"
@@ -195,6 +195,18 @@ inline uint32_t drop_threshold(float p)
 // (the low half of the word only adds below its last bit).
 __device__ __forceinline__ bool kept_low(uint32_t w, uint32_t threshold) { return (w & 0xFFFFu) >= threshold; }
 __device__ __forceinline__ bool kept_high(uint32_t w, uint32_t threshold) { return w >= (threshold << 16); }
+
+// Sixteen bytes at any address (the load unit takes them with the same instruction, aligned or not)
+__device__ __forceinline__ v4u load16(const void *p, int64_t byte)
+{
+    struct __attribute__((packed)) Loose { v4u v; };
+    return reinterpret_cast<const Loose *>(static_cast<const uint8_t *>(p) + byte)->v;
+}
+__device__ __forceinline__ void store16(void *p, int64_t byte, v4u v)
+{
+    struct __attribute__((packed)) Loose { v4u v; };
+    reinterpret_cast<Loose *>(static_cast<uint8_t *>(p) + byte)->v = v;
+}
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
