@@ -521,9 +521,7 @@ def qb_checkpoint_act(X, codes=None, scales=None):
 
 def qb_restore_act(codes, scales, dtype=torch.bfloat16, X=None):
     """What qb_checkpoint_act kept, as a tensor [T,W] of `dtype` (that of X where X is given)."""
-    if X is None:
-        X = torch.empty(codes.shape, dtype=dtype, device=codes.device)
-    return _native().restore_act(codes, scales, X)
+    return _native().restore_act(codes, scales, dtype, X)
 
 
 def qb_layer_norm_fwd(X, weight=None, bias=None, eps=1e-5, keep=False, Y=None, mean=None, rstd=None, codes=None, scales=None):

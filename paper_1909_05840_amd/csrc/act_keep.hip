@@ -20,32 +20,41 @@ struct KeepArgs {
     float *scales;
 };
 
-// Chunk c of eight values: group c / 8 of all rows' groups, in order; the lanes of a group are neighbours.
-template <int TYPE, bool KEEP>
+// Chunk c of eight values: group c / 8 of all rows' groups, in order; the lanes of a group are neighbours.  FLAT: rows of whole groups, side by side, need no row or
+// column (and no division).
+template <int TYPE, bool KEEP, bool FLAT>
 __global__ __launch_bounds__(256) void act_keep_kernel(const KeepArgs a)
 {
     const int64_t chunks = a.T * a.groups * 8, step = (int64_t)gridDim.x * (256 * kAtOnce);
     for (int64_t first = (int64_t)blockIdx.x * (256 * kAtOnce) + threadIdx.x; first < chunks; first += step) {
-        int64_t row[kAtOnce];
+        int64_t row[kAtOnce], at[kAtOnce];
         int col[kAtOnce];
         Eight<TYPE> x[kAtOnce];
         float v[kAtOnce][8];
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
             const int64_t c = min(first + u * 256, chunks - 8 + (threadIdx.x & 7));  // (past the end: the last group again)
-            row[u] = (c >> 3) / a.groups;
-            col[u] = (int)(c - row[u] * (a.groups * 8)) * 8;
-            if constexpr (KEEP) x[u].load(a.X, row[u] * a.x_row + col[u], a.W - col[u]);
-            else kept8(v[u], a.codes, a.scales, row[u], a.W, col[u]);
+            if constexpr (FLAT) {
+                at[u] = c;
+                if constexpr (KEEP) x[u].load(a.X, c * 8, 8);
+                else kept8(v[u], a.codes, a.scales, c);
+            } else {
+                row[u] = (c >> 3) / a.groups;
+                col[u] = (int)(c - row[u] * (a.groups * 8)) * 8;
+                if constexpr (KEEP) x[u].load(a.X, row[u] * a.x_row + col[u], a.W - col[u]);
+                else kept8(v[u], a.codes, a.scales, row[u], a.W, col[u]);
+            }
         }
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
             if constexpr (KEEP) {
                 x[u].get(v[u]);
-                keep8(v[u], a.codes, a.scales, row[u], a.W, col[u]);
+                if constexpr (FLAT) keep8(v[u], a.codes, a.scales, at[u]);
+                else keep8(v[u], a.codes, a.scales, row[u], a.W, col[u]);
             } else {
                 x[u].set(v[u]);
-                x[u].store(a.Y, row[u] * a.W + col[u], a.W - col[u]);
+                if constexpr (FLAT) x[u].store(a.Y, at[u] * 8, 8);
+                else x[u].store(a.Y, row[u] * a.W + col[u], a.W - col[u]);
             }
         }
     }
@@ -56,9 +65,13 @@ qb_status launch(const KeepArgs &a, int type, hipStream_t st)
 {
     const int64_t need = (a.T * a.groups * 8 + 256 * kAtOnce - 1) / (256 * kAtOnce);
     const int blocks = (int)std::min<int64_t>(need, 8192);
-    if (type == QB_TYPE_BF16) act_keep_kernel<QB_TYPE_BF16, KEEP><<<blocks, 256, 0, st>>>(a);
-    else if (type == QB_TYPE_FP16) act_keep_kernel<QB_TYPE_FP16, KEEP><<<blocks, 256, 0, st>>>(a);
-    else act_keep_kernel<QB_TYPE_FP32, KEEP><<<blocks, 256, 0, st>>>(a);
+    const auto go = [&](auto t) {
+        if (a.W % kGroup == 0 && a.x_row == a.W) act_keep_kernel<decltype(t)::value, KEEP, true><<<blocks, 256, 0, st>>>(a);
+        else act_keep_kernel<decltype(t)::value, KEEP, false><<<blocks, 256, 0, st>>>(a);
+    };
+    if (type == QB_TYPE_BF16) go(std::integral_constant<int, QB_TYPE_BF16>{});
+    else if (type == QB_TYPE_FP16) go(std::integral_constant<int, QB_TYPE_FP16>{});
+    else go(std::integral_constant<int, QB_TYPE_FP32>{});
     return launch_status();
 }
 

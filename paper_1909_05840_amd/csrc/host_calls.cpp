@@ -7,6 +7,7 @@
 // calls took 82 us for 8 and for 4096 tokens alike.  Here a call costs 4.2-4.6 us, of which the runtime's launch is 3.5:
 // the layer forward takes 39 us at 8 tokens, and is bound by the GPU from about a thousand tokens on.
 // binding.py keeps names, defaults and documentation; the functions below take its arguments by position.
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
@@ -935,15 +936,18 @@ QB_CALL(checkpoint_act, 3)  // X, codes, scales
     return tuple({codes, scales});
 }
 
-QB_CALL(restore_act, 3)  // codes, scales, X
+QB_CALL(restore_act, 4)  // codes, scales, dtype, X
 {
     const Tensor &codes = here(a[0], "codes");
     if (codes.dim() != 2) raise(PyExc_ValueError, "codes must have two dimensions");
     const int64_t T = codes.size(0), W = codes.size(1);
     here(a[0], {T, W}, at::kChar, "codes");
-    const Tensor &scales = here(a[1], {T, groups_of(W)}, at::kFloat, "scales"), &X = here(a[2], "X");
+    const Tensor &scales = here(a[1], {T, groups_of(W)}, at::kFloat, "scales");
+    if (a[3] == Py_None && !THPDtype_Check(a[2])) raise(PyExc_TypeError, "dtype must be a torch.dtype");
+    const at::ScalarType wanted = a[3] == Py_None ? reinterpret_cast<THPDtype *>(a[2])->scalar_type : here(a[3], "X").scalar_type();
+    if (wanted != at::kFloat && wanted != at::kBFloat16 && wanted != at::kHalf) raise(PyExc_TypeError, "activations are float32, bfloat16 or float16");
+    const Tensor X = here_or_new(a[3], {T, W}, wanted, codes.device(), "X");
     const int type = type_code(X, "X", true);
-    here(a[2], {T, W}, X.scalar_type(), "X");
     call(qb_restore_act, static_cast<const int8_t *>(codes.data_ptr()), floats(scales), T, W, type, X.data_ptr(), stream());
     return wrapped(X);
 }

@@ -55,14 +55,20 @@ struct Row {
 __device__ __forceinline__ void columns(const float *p, float other, int col, int W, float (&v)[8])
 {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = p && col + i < W ? p[col + i] : other;
+    for (int i = 0; i < 8; ++i) v[i] = other;
+    if (!p || col >= W) return;
+    Eight<QB_TYPE_FP32> x;
+    x.load(p, col, W - col);
+    x.get(v);
 }
 
-template <int TYPE, int R, int C>
+// TAIL: the width is no multiple of eight, so that a chunk may be part of a row and not only all or nothing of it.
+template <int TYPE, int R, int C, bool TAIL>
 __global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_kernel(const NormArgs a)
 {
     typedef Row<R, C> L;
     __shared__ v2f shared[L::kThreads / 64];
+    const float inv = 1.0f / (float)a.W;
     float w[C][8], b[C][8];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
@@ -83,20 +89,20 @@ __global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_kernel(const
             for (int e = 0; e < 8; ++e) s += v[i][e];
         }
         // the differences from a mean that is rounded say what it is off, and the squares are corrected for that (equal values have no variance)
-        const float near = L::sum(s, 0.0f, shared)[0] / (float)a.W;
+        const float near = L::sum(s, 0.0f, shared)[0] * inv;
         float q = 0.0f;
         s = 0.0f;
 #pragma unroll
         for (int i = 0; i < C; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                v[i][e] = L::col(i) + e < a.W ? v[i][e] - near : 0.0f;
+                v[i][e] -= L::col(i) + (TAIL ? e : 0) < a.W ? near : 0.0f;
                 q = __builtin_fmaf(v[i][e], v[i][e], q);
                 s += v[i][e];
             }
         const v2f both = L::sum(q, s, shared);
         const float more = both[1] / (float)a.W, mean = near + more;
-        const float rstd = 1.0f / sqrtf(fmaxf(__builtin_fmaf(-more, more, both[0] / (float)a.W), 0.0f) + a.eps);
+        const float rstd = 1.0f / sqrtf(fmaxf(__builtin_fmaf(-more, more, both[0] * inv), 0.0f) + a.eps);
         if (threadIdx.x % R == 0) {
             a.mean[row] = mean;
             a.rstd[row] = rstd;
@@ -271,7 +277,9 @@ extern "C" qb_status qb_layer_norm_fwd(const void *X, int64_t x_row, int type, i
         by_width(W, [&](auto r, auto c) {
             typedef Row<decltype(r)::value, decltype(c)::value> L;
             const int64_t groups = (T + L::kRows - 1) / L::kRows;
-            layer_norm_kernel<decltype(t)::value, decltype(r)::value, decltype(c)::value><<<(int)std::min<int64_t>(groups, 2048), L::kThreads, 0, st>>>(a);
+            const int grid = (int)std::min<int64_t>(groups, 2048);
+            if (W % 8) layer_norm_kernel<decltype(t)::value, decltype(r)::value, decltype(c)::value, true><<<grid, L::kThreads, 0, st>>>(a);
+            else layer_norm_kernel<decltype(t)::value, decltype(r)::value, decltype(c)::value, false><<<grid, L::kThreads, 0, st>>>(a);
         });
     });
     return launch_status();

@@ -57,97 +57,237 @@ __device__ __forceinline__ void finish(const LinearArgs &a, int row, int col, in
     B::store(a.Y, at, col + 32, a.N, inside, hf, z[1]);
 }
 
-// Tiles of neurons by tokens: a lane's results are neighbours of a row of Y.
+// Tiles of neurons by tokens: a lane's results are neighbours of a row of Y.  A workgroup's tiles are one stream of steps: the first two steps of a tile and its
+// bias are on their way while the tile before is ended, and that one's stores while the next one's first two steps are multiplied.
 template <typename T, typename S>
 __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_kernel(const LinearArgs a)
 {
     static_assert(S::TM % 2 == 0, "a wavefront holds whole groups of 64");
-    __shared__ __align__(1024) uint8_t lds[S::kStages * S::kStage];
+    constexpr int kBiases = S::kStages + 1, kBias = S::BM / 64;  // copies that bring a tile's bias, one to a wavefront (and again, where there are more wavefronts)
+    __shared__ __align__(1024) uint8_t lds[S::kLds];
+    __shared__ __align__(256) float bias[kBiases][S::BM];  // (tiles of one step: kStages further ones are under way when a tile ends)
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave - wm * S::WN;
-    const int words = (a.N + S::BM - 1) / S::BM, tiles = words * ((a.T + S::BN - 1) / S::BN);
-    const int id = tile_of(blockIdx.x, tiles * a.parts), part = id / tiles, tile = id - part * tiles;
-    const int tt = tile / words, n0 = (tile - tt * words) * S::BM, t0 = tt * S::BN;
-    const int steps = a.K / 64, s0 = (int)((int64_t)steps * part / a.parts), s1 = (int)((int64_t)steps * (part + 1) / a.parts);
-    v16f z[S::TM][S::TN];
-    clear(z);
-    constexpr int NA = S::BM / 8 / S::kWaves, NB = S::BN / 8 / S::kWaves;
-    multiply<T, S, false, false>(z, lds, s1 - s0, 64, 64, wave, lane, along<S, NA>(a.W, (int64_t)a.K * 2, n0, a.N, s0, wave, lane),
-                                 along<S, NB>(a.X, a.x_row * 2, t0, a.T, s0, wave, lane));
-    each<S::TM / 2>([&](auto half) {
-        constexpr int i = 2 * half;
-        const int col = n0 + (wm * S::TM + i) * 32;
-        if (col >= a.N) return;
-        float b[2][16];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const int n = col + 32 * u + 8 * (k >> 2) + 4 * hf + (k & 3);
-                b[u][k] = a.bias && !a.part && n < a.N ? a.bias[n] : 0.0f;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % (S::WM * S::WN) / S::WN, wn = wave % S::WN;
+    const int words = (a.N + S::BM - 1) / S::BM, rows = (a.T + S::BN - 1) / S::BN, tiles = words * rows, all = tiles * a.parts, grid = (int)gridDim.x;
+    const bool with_bias = a.bias && !a.part;
+    struct At {
+        int n0, t0, part, s0, steps;
+    };
+    const auto at = [&](int number) {  // of this workgroup's tile `number`
+        At p;
+        const int id = tile_of((int)blockIdx.x + number * grid, all);
+        int tt, tn;
+        p.part = id / tiles;
+        place_of(id - p.part * tiles, rows, words, tt, tn);
+        p.n0 = tn * S::BM;
+        p.t0 = tt * S::BN;
+        const int steps = a.K / S::KS;
+        p.s0 = (int)((int64_t)steps * p.part / a.parts);
+        p.steps = (int)((int64_t)steps * (p.part + 1) / a.parts) - p.s0;
+        return p;
+    };
+    const uint32_t lds0 = lds_address(lds);
+    const Product<T, S, false, false, false> product(lds0, wave, lane);
+    const int mine = (all - (int)blockIdx.x + grid - 1) / grid;  // tiles of this workgroup
+    // ---- the copies' side of the stream: step number `cs` of tile number `cn` is the next
+    At ahead = at(0);
+    int cn = 0, cs = 0;
+    Feed<S::NA> fw;
+    Feed<S::NB> fx;
+    const auto fetch = [&](int stage) {
+        if (cn >= mine) return;
+        if (cs == 0) {
+            fw = along<S, S::NA>(a.W, (int64_t)a.K * 2, ahead.n0, a.N, ahead.s0, wave, lane);
+            fx = along<S, S::NB>(a.X, a.x_row * 2, ahead.t0, a.T, ahead.s0, wave, lane);
+            if (with_bias) {
+                const int n = ahead.n0 + wave % kBias * 64;
+                copy4(a.bias + min(n + lane, a.N - 1), lds_address(&bias[cn % kBiases][wave % kBias * 64]));
             }
+        }
+        const uint32_t to = lds0 + stage * S::kStage;
+        copy_step<S, false>(fw, to, S::KS, wave, lane);
+        copy_step<S, false>(fx, to + S::BM * S::KS * 2, S::KS, wave, lane);
+        if (++cs < ahead.steps) return;
+        cs = 0;
+        if (++cn < mine) ahead = at(cn);
+    };
+    int stage = 0;
 #pragma unroll
-        for (int j = 0; j < S::TN; ++j) {
-            const int row = t0 + (wn * S::TN + j) * 32 + l32;
-            float v[2][16];
+    for (int u = 0; u < S::kStages; ++u) fetch(u);
+    for (int number = 0; number < mine; ++number) {
+        const At p = at(number);
+        v16f z[S::TM][S::TN];
+        float none[S::TN];
+        clear(z);
+        product.run(z, none, p.steps, stage, fetch, [&](int s) {
+            constexpr int kStep = S::NA + S::NB;  // (a bias's copy among the younger ones only makes the wait longer)
+            if (S::kStages > 2 && p.steps - s >= S::kStages) wait_copies<(S::kStages - 2) * kStep>();
+            else wait_copies<0>();
+        });
+        gather<S>(z, none, lds + S::kStages * S::kStage, wave, lane);
+        if (wave >= S::WM * S::WN) continue;
+        each<S::TM / 2>([&](auto half) {
+            constexpr int i = 2 * half;
+            const int col = p.n0 + (wm * S::TM + i) * 32;
+            if (col >= a.N) return;
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int k = 0; k < 16; ++k) v[u][k] = z[i + u][j][k] + b[u][k];
-            if (!a.part) {
-                finish<T>(a, row, col, hf, v);
-            } else if (row < a.T) {
-                float *const to = a.part + ((int64_t)part * a.T + row) * a.Np + col;
+            for (int j = 0; j < S::TN; ++j) {
+                const int row = p.t0 + (wn * S::TN + j) * 32 + l32;
+                float v[2][16];
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int k = 0; k < 16; k += 4) *reinterpret_cast<v4f *>(to + 32 * u + 2 * k + 4 * hf) = v4f{v[u][k], v[u][k + 1], v[u][k + 2], v[u][k + 3]};
+                    for (int k = 0; k < 16; k += 4) {
+                        v4f b = {0.0f, 0.0f, 0.0f, 0.0f};
+                        if (with_bias) b = *reinterpret_cast<const v4f *>(&bias[number % kBiases][(wm * S::TM + i + u) * 32 + 2 * k + 4 * hf]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[u][k + e] = z[i + u][j][k + e] + b[e];
+                    }
+                if (!a.part) {
+                    finish<T>(a, row, col, hf, v);
+                } else if (row < a.T) {
+                    float *const to = a.part + ((int64_t)p.part * a.T + row) * a.Np + col;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int k = 0; k < 16; k += 4) *reinterpret_cast<v4f *>(to + 32 * u + 2 * k + 4 * hf) = v4f{v[u][k], v[u][k + 1], v[u][k + 2], v[u][k + 3]};
+                }
             }
-        }
-    });
+        });
+    }
 }
 
-// the parts of a contraction that was cut: 32 rows by 64 columns to a wavefront, in the order in which a product's results lie
-template <typename T>
-__global__ __launch_bounds__(64) void linear_join_kernel(const LinearArgs a)
+// Few tokens: sixteen neurons to a workgroup, whose wavefronts share the contraction, or a part of it; the weights go from memory straight into the matrix cores'
+// operands, each read once.  G groups of sixteen tokens.  A CU is given about 40 GB/s, whatever it asks for: with few neurons the contraction is cut into parts, so that
+// every CU takes its share of weights and tokens.
+template <typename T, int G, int kUnits>  // kUnits: of 64 values of the contraction, under way to a wavefront
+__global__ __launch_bounds__(512) void linear_few_kernel(const LinearArgs a)
 {
-    const int lane = threadIdx.x, hf = lane >> 5, groups = a.Np / 64, tt = (int)blockIdx.x / groups, col = ((int)blockIdx.x - tt * groups) * 64, row = tt * 32 + (lane & 31);
-    float z[2][16];
+    __shared__ float sums[8][G * 16][17];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), blocks = (a.N + 15) / 16;
+    const int part = blockIdx.x / blocks, n0 = ((int)blockIdx.x - part * blocks) * 16, r = lane & 15, k0 = 8 * (lane >> 4);
+    const int units = a.K / 64, u0 = (int)((int64_t)units * part / a.parts), u1 = (int)((int64_t)units * (part + 1) / a.parts);
+    const uint16_t *const w = a.W + (int64_t)min(n0 + r, a.N - 1) * a.K + k0;
+    const uint16_t *x[G];
+    v4f z[G];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int g = 0; g < G; ++g) {
+        x[g] = a.X + min(16 * g + r, a.T - 1) * a.x_row + k0;
+        z[g] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    for (int first = u0 + wave; first < u1; first += 8 * kUnits) {
+        v8s p[kUnits][2], q[kUnits][2][G];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const int n = col + 32 * u + 8 * (k >> 2) + 4 * hf + (k & 3);
-            z[u][k] = a.bias && n < a.N ? a.bias[n] : 0.0f;
-        }
-    const float *from = a.part + (int64_t)min(row, a.T - 1) * a.Np + col + 4 * hf;
-    for (int p = 0; p < a.parts; ++p, from += (int64_t)a.T * a.Np)
+        for (int u = 0; u < kUnits; ++u) {
+            const int k = min(first + 8 * u, u1 - 1) * 64;  // (past the end: the last unit again, not multiplied)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+            for (int h = 0; h < 2; ++h) {
+                p[u][h] = *reinterpret_cast<const v8s *>(w + k + 32 * h);
 #pragma unroll
-            for (int k = 0; k < 16; k += 4) {
-                const v4f x = *reinterpret_cast<const v4f *>(from + 32 * u + 2 * k);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) z[u][k + e] += x[e];
+                for (int g = 0; g < G; ++g) q[u][h][g] = *reinterpret_cast<const v8s *>(x[g] + k + 32 * h);
             }
-    finish<T>(a, row, col, hf, z);
+        }
+        // (all loads before the first product)
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                asm volatile("" : "+v"(p[u][h]));
+#pragma unroll
+                for (int g = 0; g < G; ++g) asm volatile("" : "+v"(q[u][h][g]));
+            }
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+            if (first + 8 * u < u1) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int g = 0; g < G; ++g) z[g] = T::mma16(p[u][h], q[u][h][g], z[g]);
+            }
+    }
+    // a lane's results: token lane % 16, neurons 4 * (lane / 16) ..
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sums[wave][16 * g + r][k0 / 2 + e] = z[g][e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < G * 256; i += 512) {
+        const int row = i >> 4, n = n0 + (i & 15);
+        if (row >= a.T || n >= a.N) continue;
+        float v[1] = {a.bias && !a.part ? a.bias[n] : 0.0f};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[0] += sums[k][row][i & 15];
+        if (a.part) {
+            a.part[((int64_t)part * a.T + row) * a.Np + n] = v[0];
+            continue;
+        }
+        const int64_t at = (int64_t)row * a.N + n;
+        if (a.pre) a.pre[at] = (uint16_t)T::pair(v[0], 0.0f);
+        activate(a.act, v);
+        if (a.residual) v[0] += T::lo(a.residual[row * a.residual_row + n]);
+        a.Y[at] = (uint16_t)T::pair(v[0], 0.0f);
+    }
 }
 
-typedef Shape<2, 4, 4, 2, 2> Large;  // 256 x 256
-typedef Shape<2, 2, 2, 2, 2> Middle;  // 128 x 128
-typedef Shape<1, 4, 2, 1, 3> Small;  // 64 x 128
+// the parts of a contraction that was cut: four neighbours of a row to a thread, a group of 64 to sixteen lanes
+template <typename T>
+__global__ __launch_bounds__(256) void linear_join_kernel(const LinearArgs a)
+{
+    const uint32_t quads = (uint32_t)a.Np / 4, i = blockIdx.x * 256 + threadIdx.x;
+    const int row = (int)min(i / quads, (uint32_t)a.T - 1), col = (int)(i % quads) * 4;  // (a group's lanes stay together)
+    const bool inside = i / quads < (uint32_t)a.T;
+    float z[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = a.bias && col + e < a.N ? a.bias[col + e] : 0.0f;
+    add_parts(a.part + (int64_t)row * a.Np + col, (int64_t)a.T * a.Np, a.parts, z);
+    if (a.act != QB_ACT_NONE) {
+        if (a.codes) keep4(z, a.codes, a.scales, row, a.N, col, inside);
+        if (a.pre && inside) store4<T>(a.pre, (int64_t)row * a.N + col, a.N - col, z);
+        activate(a.act, z);
+    }
+    if (a.residual && inside) {
+        float r[4];
+        load4<T>(a.residual, row * a.residual_row + col, a.N - col, r);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] += r[e];
+    }
+    if (a.act == QB_ACT_NONE && a.codes) keep4(z, a.codes, a.scales, row, a.N, col, inside);
+    if (inside) store4<T>(a.Y, (int64_t)row * a.N + col, a.N - col, z);
+}
+
+typedef Tile<2, 4, 4, 2, 2> Large;     // 256 x 256
+typedef Tile<2, 4, 2, 2, 3> Broad;     // 128 x 256
+typedef Tile<2, 2, 2, 2, 2> Middle;    // 128 x 128
+typedef Tile<1, 4, 2, 1, 3> Small;     // 64 x 128
+typedef Tile<1, 2, 2, 1, 4, 2> Least;  // 64 x 64
+template <typename S>
+constexpr int kResident = 256 * (S::kLds > 81920 ? 1 : 2);  // workgroups that are at work at once
 
 struct Plan {
-    int size, parts;  // 0 small, 1 middle, 2 large
+    int size, parts;  // -1 few tokens, 0 least .. 4 large
 };
 template <typename S>
 int64_t tiles_of(int64_t T, int64_t N) { return ((T + S::BN - 1) / S::BN) * ((N + S::BM - 1) / S::BM); }
+// Of few tokens: the largest share of a CU, at 40 KB a microsecond, and 3 us for a second launch.
+int few_parts(const qb_linear &l)
+{
+    const int64_t blocks = (l.N + 15) / 16, rows = 16 + (l.T <= 16 ? std::min<int64_t>(l.T, 16) : l.T);
+    int best = 1;
+    double least = 0;
+    for (const int p : {1, 2, 4, 8}) {
+        if (p > l.K / 128) break;
+        const double cost = (double)((blocks * p + 255) / 256) * (double)(rows * l.K * 2 / p) / 40e3 + (p > 1 || l.codes ? 3.0 : 0.0);
+        if (p == 1 || cost < least) {
+            least = cost;
+            best = p;
+        }
+    }
+    return best;
+}
 Plan plan_of(const qb_linear &l)
 {
-    const int steps = (int)(l.K / 64);
-    if (tiles_of<Large>(l.T, l.N) >= 192) return {2, 1};
-    if (tiles_of<Middle>(l.T, l.N) >= 256) return {1, 1};
-    return {0, best_parts(tiles_of<Small>(l.T, l.N), steps, 512, 8)};
+    if (l.T <= 64) return {-1, few_parts(l)};
+    return {tiles_of<Large>(l.T, l.N) >= 192 ? 4 : tiles_of<Broad>(l.T, l.N) >= 224 ? 3 : tiles_of<Small>(l.T, l.N) > 384 ? 2 : tiles_of<Least>(l.T, l.N) > 256 ? 1 : 0, 1};
 }
 
 size_t lay_out(const qb_linear &l, LinearArgs &a)
@@ -155,22 +295,35 @@ size_t lay_out(const qb_linear &l, LinearArgs &a)
     const Plan p = plan_of(l);
     a.parts = p.parts;
     a.Np = (int)((l.N + 63) / 64 * 64);
-    return p.parts > 1 ? round_up((size_t)p.parts * l.T * a.Np * 4) : 0;
+    return p.parts > 1 || (p.size < 0 && l.codes) ? round_up((size_t)p.parts * l.T * a.Np * 4) : 0;
 }
 bool shape_ok(const qb_linear &l) { return l.T >= 0 && l.T <= kMostRows && l.N >= 1 && l.N <= kMostOutputs && k_ok(l.K); }
 
 template <typename T, typename S>
 void launch(const LinearArgs &a, hipStream_t st)
 {
-    linear_kernel<T, S><<<(int)(tiles_of<S>(a.T, a.N) * a.parts), 64 * S::kWaves, 0, st>>>(a);
+    linear_kernel<T, S><<<(int)std::min<int64_t>(tiles_of<S>(a.T, a.N) * a.parts, kResident<S>), 64 * S::kWaves, 0, st>>>(a);
 }
 template <typename T>
 qb_status launch(const LinearArgs &a, int size, hipStream_t st)
 {
-    if (size == 2) launch<T, Large>(a, st);
-    else if (size == 1) launch<T, Middle>(a, st);
-    else launch<T, Small>(a, st);
-    if (a.parts > 1) linear_join_kernel<T><<<(a.T + 31) / 32 * (a.Np / 64), 64, 0, st>>>(a);
+    if (size < 0) {
+        const int groups = (a.N + 15) / 16 * a.parts, units = (a.K / 64 + 8 * a.parts - 1) / (8 * a.parts);  // (of a wavefront)
+        const auto go = [&](auto g) {
+            constexpr int G = decltype(g)::value;
+            if (units == 1) linear_few_kernel<T, G, 1><<<groups, 512, 0, st>>>(a);
+            else if (units == 2 || G == 4) linear_few_kernel<T, G, 2><<<groups, 512, 0, st>>>(a);
+            else linear_few_kernel<T, G, 4><<<groups, 512, 0, st>>>(a);
+        };
+        if (a.T <= 16) go(std::integral_constant<int, 1>{});
+        else if (a.T <= 32) go(std::integral_constant<int, 2>{});
+        else go(std::integral_constant<int, 4>{});
+    } else if (size == 4) launch<T, Large>(a, st);
+    else if (size == 3) launch<T, Broad>(a, st);
+    else if (size == 2) launch<T, Middle>(a, st);
+    else if (size == 1) launch<T, Small>(a, st);
+    else launch<T, Least>(a, st);
+    if (a.part) linear_join_kernel<T><<<(int)(((int64_t)a.T * (a.Np / 4) + 255) / 256), 256, 0, st>>>(a);
     return launch_status();
 }
 

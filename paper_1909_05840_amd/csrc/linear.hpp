@@ -1,7 +1,6 @@
 // What the 16-bit linears' forward and backward share: the stream of steps through LDS, a product's results as rows.
 #pragma once
 #include "qb_acts.hpp"
-#include "qb_products.hpp"
 
 namespace qb {
 
@@ -16,6 +15,49 @@ __device__ __forceinline__ int tile_of(int group, int tiles)
     return xcd * each + min(xcd, rest) + (group >> 3);
 }
 
+// Tiles of BM x BN results by WM x WN wavefronts, TM x TN blocks of 32 x 32 each; the contraction goes in steps of KS through a ring of stages in LDS.  An operand lies in
+// LDS as it does in memory: rows of results with the contraction along them (KS values), or rows along the contraction (64 results; KS rows to a block of these), read
+// turned.  KG groups of wavefronts share a step's sixteens of the contraction: a small tile's step is a chain of reads and few instructions, which more wavefronts shorten.
+template <int WM_, int WN_, int TM_, int TN_, int STAGES_, int KG_ = 1>
+struct Tile {
+    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, KG = KG_, kWaves = WM * WN * KG, kStages = STAGES_, KS = 64;
+    static constexpr int BM = 32 * WM * TM, BN = 32 * WN * TN;
+    static constexpr int kStage = (BM + BN) * KS * 2, kSums = (KG - 1) * BM * BN * 4, kLds = kStages * kStage + kSums;
+    static constexpr int NA = BM * KS / 512 / kWaves, NB = BN * KS / 512 / kWaves;  // copies of 1024 bytes that a wavefront makes
+    static_assert(NA * 512 * kWaves == BM * KS && NB * 512 * kWaves == BN * KS, "every wavefront copies the same number of times");
+};
+
+// Rows of KS values along the contraction: the chunks of sixteen bytes are XORed with a key of the row such that sixteen consecutive rows at one chunk meet different banks.
+template <int KS>
+struct AlongRows {
+    static_assert(KS == 32 || KS == 64, "rows of 64 or 128 bytes");
+    static constexpr int kBytes = 2 * KS, kChunks = KS / 8, kPerCopy = 64 / kChunks;
+    static __device__ __forceinline__ int key(int row)
+    {
+        if constexpr (KS == 64) return Rows<64>::key(row);
+        else return (row >> 2) & 3;
+    }
+    static __device__ __forceinline__ int row(int copy, int lane) { return copy * kPerCopy + lane / kChunks; }
+    static __device__ __forceinline__ int chunk(int copy, int lane) { return (lane % kChunks) ^ key(row(copy, lane)); }
+};
+// Blocks of KS rows of 64 results
+template <int KS>
+struct AcrossRows {
+    static __device__ __forceinline__ int row(int copy, int lane) { return (copy * 8 + (lane >> 3)) % KS; }
+    static __device__ __forceinline__ int block(int copy) { return copy * 8 / KS; }
+    static __device__ __forceinline__ int chunk(int copy, int lane) { return (lane & 7) ^ Rows<64>::key(row(copy, lane)); }
+};
+
+// Where tile `id` of a matrix of `rows` x `columns` tiles lies: bands of four rows, a band column by column, so that the 32 workgroups that an XCD has at work read
+// the operands of 4 x 8 tiles, not of 1 x 32.  Bands of 1, 2, 4, 8 rows, us: 16384 x 4096 by 1024 151, 147, 140, 149; 8192 x 8192 by 8192 953, 890, 855, 862.
+__device__ __forceinline__ void place_of(int id, int rows, int columns, int &row, int &column)
+{
+    constexpr int kBand = 4;
+    const int band = id / (kBand * columns), in = id - band * kBand * columns, wide = min(kBand, rows - band * kBand);
+    column = in / wide;
+    row = band * kBand + in - column * wide;
+}
+
 // One operand of a product on its way to LDS.  `at` is the first step's place in memory, the same for all lanes; a lane's chunk of copy i lies `off[i]` bytes
 // further on; each step moves on by `step` bytes.
 template <int N>
@@ -28,74 +70,188 @@ struct Feed {
 template <typename S, int N>
 __device__ __forceinline__ Feed<N> along(const void *base, int64_t row, int first, int rows, int s0, int wave, int lane)
 {
-    typedef Rows<64> R;
+    typedef AlongRows<S::KS> R;
     Feed<N> f;
-    f.at = static_cast<const uint8_t *>(base) + first * row + (int64_t)s0 * 128;
-    f.step = 128;
+    f.at = static_cast<const uint8_t *>(base) + first * row + (int64_t)s0 * (2 * S::KS);
+    f.step = 2 * S::KS;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int r = S::row(i, wave, lane);
-        f.off[i] = (uint32_t)(min(r, rows - 1 - first) * row) + 16 * R::copy_chunk(r, lane);
+        const int copy = i * S::kWaves + wave;
+        f.off[i] = (uint32_t)(min(R::row(copy, lane), rows - 1 - first) * row) + 16 * R::chunk(copy, lane);
     }
     return f;
 }
-// Rows along the contraction: LDS row r holds 64 results from 64 * (r / 64) on, of step r % 64; past the last column (a multiple of eight) the last eight again.
+// Rows along the contraction; past the last column (a multiple of eight) the last eight again.
 template <typename S, int N>
 __device__ __forceinline__ Feed<N> across(const void *base, int64_t row, int first, int columns, int s0, int wave, int lane)
 {
-    typedef Rows<64> R;
+    typedef AcrossRows<S::KS> R;
     Feed<N> f;
-    f.at = static_cast<const uint8_t *>(base) + (int64_t)s0 * 64 * row;
-    f.step = 64 * row;
+    f.at = static_cast<const uint8_t *>(base) + (int64_t)s0 * S::KS * row;
+    f.step = S::KS * row;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int r = S::row(i, wave, lane);
-        f.off[i] = (uint32_t)((r & 63) * row) + 2 * min(first + (r & ~63) + 8 * R::copy_chunk(r, lane), columns - 8);
+        const int copy = i * S::kWaves + wave;
+        f.off[i] = (uint32_t)(R::row(copy, lane) * row) + 2 * min(first + 64 * R::block(copy) + 8 * R::chunk(copy, lane), columns - 8);
     }
     return f;
 }
 
-// acc += A B^T over `steps` steps.  Of the last one `left_a` and `left_b` values of the contraction are there (64, or fewer: a multiple of eight where the operand has it
-// along its rows); zeros stand for the others.
-template <typename T, typename S, bool A_ACROSS, bool B_ACROSS, int NA, int NB>
-__device__ __forceinline__ void multiply(v16f (&acc)[S::TM][S::TN], uint8_t *lds, int steps, int left_a, int left_b, int wave, int lane, Feed<NA> a, Feed<NB> b)
-{
-    constexpr int kAhead = S::kStages - 1;
-    static_assert(NA * 8 * S::kWaves == S::BM && NB * 8 * S::kWaves == S::BN, "every wavefront copies the same number of times");
-    typedef Rows<64> R;
-    const uint32_t lds0 = lds_address(lds);
-    int next = 0;
-    const auto fetch = [&](int stage) {
-        if (next >= steps) return;
-        const uint32_t to = lds0 + stage * S::kStage + wave * 1024;
-        if (++next == steps && left_a < 64) {
-            const auto there = [&](bool turned, int left, int i) {
-                const int r = S::row(i, wave, lane);
-                return turned ? (r & 63) < left : 8 * R::copy_chunk(r, lane) < left;
-            };
+// A lane's places in the tiles of one operand, formed once: everything else is an offset in the instruction.
+template <int KS, bool ACROSS>
+struct Places {
+    uint32_t at[ACROSS ? 4 : KS / 16];
+    // second: the wavefront's results start at the second half of a block
+    // sub0: the wavefront's first sixteen of a step
+    __device__ __forceinline__ Places(int lane, bool second, int sub0)
+    {
+        if constexpr (ACROSS) {
+            typedef Rows<64> R;
+            const int row = 8 * (lane >> 5) + ((lane >> 2) & 3), col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 #pragma unroll
-            for (int i = 0; i < NA; ++i) copy16(there(A_ACROSS, left_a, i) ? static_cast<const void *>(a.at + a.off[i]) : &kZeros, to + i * S::kWaves * 1024);
-#pragma unroll
-            for (int i = 0; i < NB; ++i) copy16(there(B_ACROSS, left_b, i) ? static_cast<const void *>(b.at + b.off[i]) : &kZeros, to + S::BM * 128 + i * S::kWaves * 1024);
+            for (int i = 0; i < 4; ++i) at[i] = R::at(row + 4 * (i & 1), (32 * ((i >> 1) ^ (second ? 1 : 0)) + col) >> 3) + 2 * (col & 7) + sub0 * 2048;
         } else {
+            typedef AlongRows<KS> R;
+            const int row = lane & 31;
 #pragma unroll
-            for (int i = 0; i < NA; ++i) copy16(a.at, a.off[i], to + i * S::kWaves * 1024);
-#pragma unroll
-            for (int i = 0; i < NB; ++i) copy16(b.at, b.off[i], to + S::BM * 128 + i * S::kWaves * 1024);
+            for (int c = 0; c < KS / 16; ++c) at[c] = row * R::kBytes + (((2 * ((sub0 + c) % (KS / 16)) + (lane >> 5)) ^ R::key(row)) << 4);
         }
-        a.at += a.step;
-        b.at += b.step;
-    };
+    }
+    // the operand of the 32 results from `result` on, sixteen of the contraction from 16 * sub on
+    __device__ __forceinline__ v8s get(uint32_t tile, int result, int sub) const
+    {
+        if constexpr (ACROSS) {
+            typedef __attribute__((address_space(3))) v4s *turned;
+            const uint32_t from = tile + (result >> 6) * (KS * 128) + sub * 2048;
+            const int odd = (result >> 5) & 1;
+            const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((turned)(from + at[2 * odd])), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((turned)(from + at[2 * odd + 1]));
+            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            return *(const __attribute__((address_space(3))) v8s *)(tile + at[sub] + result * AlongRows<KS>::kBytes);
+        }
+    }
+};
+
+// One step's copies of an operand; its last step may have fewer than KS values of the contraction (`left`, a multiple of eight where it runs along the rows): zeros
+// stand for the others.
+template <typename S, bool ACROSS, int N>
+__device__ __forceinline__ void copy_step(Feed<N> &f, uint32_t to, int left, int wave, int lane)
+{
+    if (left < S::KS) {
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) fetch(u);
-    int stage = 0;
-    for (int s = 0; s < steps; ++s) {
-        if (s + kAhead <= steps) wait_copies<(kAhead - 1) * (NA + NB)>();  // (younger steps' stay under way)
-        else wait_copies<0>();
+        for (int i = 0; i < N; ++i) {
+            const int copy = i * S::kWaves + wave;
+            const bool there = ACROSS ? AcrossRows<S::KS>::row(copy, lane) < left : 8 * AlongRows<S::KS>::chunk(copy, lane) < left;
+            copy16(there ? static_cast<const void *>(f.at + f.off[i]) : &kZeros, to + copy * 1024);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) copy16(f.at, f.off[i], to + (i * S::kWaves + wave) * 1024);
+    }
+    f.at += f.step;
+}
+
+// acc += A B^T over one tile's steps, which lie or will lie in the stages from `stage` on.  When the operands of a step's last instructions are in registers its stage is free:
+// `fetch(stage)` starts the copies of the step that comes kStages later, of this tile or of the one that follows.  `arrived(s)` waits for the wavefront's copies of step
+// s, behind which those of kStages - 1 further steps may be under way for s = 0, else kStages - 2.  With SUMS, sums[j] gets what B's rows add up to over the contraction, a
+// lane's share of its column of block j.
+// Of 256 x 256 tiles more than two stages (5 slots of an operand each, all of LDS) measured the same: 16384 x 1024 by 4096 112.3 us and 113.6, 8192 x 8192 by 8192 867
+// and 851; what bounds them is the rate at which a CU is given its operands, 46 GB/s each, and the clock, 1.7 to 2.1 GHz under this load.
+template <typename T, typename S, bool A_ACROSS, bool B_ACROSS, bool SUMS>
+struct Product {
+    static constexpr int KS = S::KS, kSubs = KS / 16 / S::KG;  // a wavefront's sixteens of a step
+    static_assert(S::TM % 2 == 0 && (S::TN % 2 == 0 || S::TN == 1), "a wavefront's results start at a block, or are half of one");
+    static_assert(kSubs == 1 || kSubs % 2 == 0, "the operands' two buffers");
+    const Places<KS, A_ACROSS> pa;
+    const Places<KS, B_ACROSS> pb;
+    uint32_t first_a, first_b;
+    __device__ __forceinline__ Product(uint32_t lds, int wave, int lane)
+        : pa(lane, false, wave / (S::WM * S::WN) * kSubs), pb(lane, S::TN == 1 && (wave % S::WN & 1), wave / (S::WM * S::WN) * kSubs)
+    {
+        const int wm = wave % (S::WM * S::WN) / S::WN, wn = wave % S::WN, result_b = B_ACROSS ? wn * S::TN * 32 & ~63 : wn * S::TN * 32;
+        first_a = lds + (uint32_t)(wm * S::TM * 32) * (KS * 2);
+        first_b = lds + (uint32_t)(S::BM + result_b) * (KS * 2);
+    }
+    template <typename FF, typename FA>
+    __device__ __forceinline__ void run(v16f (&acc)[S::TM][S::TN], float (&sums)[S::TN], int steps, int &stage, const FF &fetch, const FA &arrived) const
+    {
+        v8s x[2][S::TM], y[2][S::TN];
+        const auto load = [&](auto buffer, auto sub) {
+#pragma unroll
+            for (int i = 0; i < S::TM; ++i) x[buffer][i] = pa.get(first_a + stage * S::kStage, 32 * i, sub);
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j) y[buffer][j] = pb.get(first_b + stage * S::kStage, 32 * j, sub);
+        };
+        const auto step = [&](int s, auto first) {  // first: the buffer that the step's first operands are in
+            each<kSubs>([&](auto sub) {
+                constexpr int now = (first + sub) % 2, then = 1 - now;
+                if constexpr (sub + 1 < kSubs) {
+                    load(std::integral_constant<int, then>(), std::integral_constant<int, sub + 1>());
+                } else {
+                    if (s + 1 < steps) arrived(s + 1);
+                    barrier();
+                    fetch(stage);
+                    stage = stage == S::kStages - 1 ? 0 : stage + 1;
+                    if (s + 1 < steps) load(std::integral_constant<int, then>(), std::integral_constant<int, 0>());
+                }
+                if constexpr (SUMS) {
+#pragma unroll
+                    for (int j = 0; j < S::TN; ++j) {
+                        const v4u w = __builtin_bit_cast(v4u, y[now][j]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sums[j] += T::lo(w[e]) + T::hi(w[e]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < S::TN; ++j) acc[i][j] = T::mma32(x[now][i], y[now][j], acc[i][j]);
+            });
+        };
+        arrived(0);
         barrier();
-        fetch(stage == 0 ? kAhead : stage - 1);  // (into the stage that the last step was multiplied from)
-        step<T, S, A_ACROSS, B_ACROSS>(acc, lds + stage * S::kStage, wave, lane);
-        stage = stage == kAhead ? 0 : stage + 1;
+        load(std::integral_constant<int, 0>(), std::integral_constant<int, 0>());
+        for (int s = 0; s < steps; ++s) {
+            step(s, std::integral_constant<int, 0>());
+            if constexpr (kSubs % 2 != 0)
+                if (++s < steps) step(s, std::integral_constant<int, 1>());
+        }
+    }
+};
+// The groups' shares of a tile's sums (and of what SUMS adds up) come together in the first group; `room`: S::kSums bytes.
+template <typename S>
+__device__ __forceinline__ void gather(v16f (&acc)[S::TM][S::TN], float (&sums)[S::TN], uint8_t *room, int wave, int lane)
+{
+    if constexpr (S::KG > 1) {
+        constexpr int kTeam = S::WM * S::WN, kValues = S::TM * S::TN * 16;
+        const int group = wave / kTeam;
+        v4f *const mine = reinterpret_cast<v4f *>(room) + (wave % kTeam * (kValues / 4)) * 64 + lane;
+        constexpr int kNext = kTeam * (kValues / 4) * 64;
+        barrier();  // (the last tile's have been read)
+        if (group > 0) {
+#pragma unroll
+            for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+                    for (int k = 0; k < 16; k += 4)
+                        mine[(group - 1) * kNext + ((i * S::TN + j) * 4 + k / 4) * 64] = v4f{acc[i][j][k], acc[i][j][k + 1], acc[i][j][k + 2], acc[i][j][k + 3]};
+        }
+        barrier();
+        if (group == 0) {
+#pragma unroll
+            for (int g = 0; g < S::KG - 1; ++g)
+#pragma unroll
+                for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+                        for (int k = 0; k < 16; k += 4) {
+                            const v4f x = mine[g * kNext + ((i * S::TN + j) * 4 + k / 4) * 64];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][j][k + e] += x[e];
+                        }
+        }
     }
 }
 
@@ -163,9 +319,9 @@ struct Block {
     }
     static __device__ __forceinline__ void store_codes(int8_t *p, int64_t at, int col, int width, bool inside, int hf, const Coder &coder, const float (&v)[16])
     {
-        v4u w;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) w[q] = four(coder.code(v[4 * q]), coder.code(v[4 * q + 1]), coder.code(v[4 * q + 2]), coder.code(v[4 * q + 3]));
+        uint32_t q[4];
+        coder.codes(v, q);
+        v4u w = {q[0], q[1], q[2], q[3]};
         w = join_codes(w);
         const int c = col + 16 * hf;
         if (!inside) return;
@@ -187,25 +343,80 @@ __device__ __forceinline__ uint32_t halves_top(uint32_t v)
     return max(s[0], s[1]);
 }
 
+// ---- rows of sums: four neighbours to a thread, a group of 64 to sixteen lanes
+__device__ __forceinline__ void add_parts(const float *p, int64_t step, int parts, float (&z)[4])
+{
+    constexpr int kAtOnce = 8;
+    for (int first = 0; first < parts; first += kAtOnce) {
+        v4f x[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) x[u] = *reinterpret_cast<const v4f *>(p + min(first + u, parts - 1) * step);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (first + u < parts) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[e] += x[u][e];
+            }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void load4(const uint16_t *p, int64_t at, int n, float (&v)[4])
+{
+    if (n >= 4) {
+        struct __attribute__((packed)) Loose { v2u v; };
+        const v2u w = reinterpret_cast<const Loose *>(p + at)->v;
+        v[0] = T::lo(w[0]); v[1] = T::hi(w[0]); v[2] = T::lo(w[1]); v[3] = T::hi(w[1]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = e < n ? T::lo(p[at + e]) : 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store4(uint16_t *p, int64_t at, int n, const float (&v)[4])
+{
+    const v2u w = {T::pair(v[0], v[1]), T::pair(v[2], v[3])};
+    if (n >= 4) {
+        struct __attribute__((packed)) Loose { v2u v; };
+        reinterpret_cast<Loose *>(p + at)->v = w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < n) p[at + e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+    }
+}
+__device__ __forceinline__ void keep4(const float (&z)[4], int8_t *codes, float *scales, int64_t row, int width, int col, bool inside)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (col + e < width) top = max(top, magnitude(z[e]));
+    top = max8(top);
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x140, 0xF, 0xF, true));  // the other eight of sixteen
+    const Coder c(top);
+    uint32_t w[1];
+    c.codes(z, w);
+    if (!inside || col >= width) return;
+    if ((col & (kGroup - 1)) == 0) scales[row * ((width + kGroup - 1) / kGroup) + col / kGroup] = c.scale;
+    int8_t *const to = codes + row * width + col;
+    if (col + 4 <= width) {
+        struct __attribute__((packed)) Loose { uint32_t v; };
+        reinterpret_cast<Loose *>(to)->v = w[0];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < width) to[e] = (int8_t)(w[0] >> (8 * e));
+    }
+}
+__device__ __forceinline__ void kept4(float (&v)[4], const int8_t *codes, const float *scales, int64_t row, int width, int col)  // (all four inside)
+{
+    struct __attribute__((packed)) Loose { uint32_t v; };
+    const uint32_t w = reinterpret_cast<const Loose *>(codes + row * width + col)->v;
+    const float scale = scales[row * ((width + kGroup - 1) / kGroup) + col / kGroup];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (float)(int8_t)(w >> (8 * e)) * scale;
+}
+
 constexpr int64_t kMostOutputs = 1 << 20;
 inline size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
-
-// How many parts to cut a contraction of `steps` steps into, so that the longest share of `room` workgroups is shortest: a tile costs its steps and
-// about `kTileCost` more (the first copies' latency, its results' way out), and each part but a lone one is read again by a launch of its own.
-inline int best_parts(int64_t tiles, int steps, int room, int most)
-{
-    constexpr int kTileCost = 5;
-    int best = 1;
-    double least = 0;
-    for (int p = 1; p <= most && p <= steps; ++p) {
-        const int64_t rounds = (tiles * p + room - 1) / room;
-        const double cost = (double)rounds * ((steps + p - 1) / p + kTileCost) + (p > 1 ? 8 + 0.5 * p : 0);
-        if (p == 1 || cost < least) {
-            least = cost;
-            best = p;
-        }
-    }
-    return best;
-}
 
 }  // namespace qb

@@ -3,8 +3,8 @@
 //   dX = (dY W) o act'(pre)   where the input X was act(pre), or dY W;   dW = dY^T X;   dbias = sum_t dY[t]
 //
 // X is given in 16 bits, or in 8, or is formed again from pre, which is given in 16 bits or in 8.  One launch brings X and dY into the form that the
-// products read, where they are not in it, and adds up dbias; one launch forms both products, their tiles dealt to the same workgroups; one adds up the parts
-// of tiles whose contraction was cut.  Bound by the matrix cores.
+// products read, where they are not in it; one launch forms both products, their tiles dealt to the same workgroups, and adds up dbias on the way; one adds up the
+// parts of tiles whose contraction was cut.  Bound by the matrix cores.
 #include "linear.hpp"
 #include <algorithm>
 
@@ -20,13 +20,14 @@ struct GradArgs {
     uint16_t *dX, *dW;
     float *dbias;
     uint16_t *dYs, *Xs;    // dY with rows that can be copied; X in 16 bits
-    float *db;             // [row blocks][N]
+    float *db;             // [db_parts][N]: parts of dbias
     float *dXp, *dWp;      // [parts][T][K], [parts][N][K], or null
     int x_tiles, w_tiles, x_parts, w_parts, x_first;
     int x_blocks, n_blocks, t_blocks;  // of the first launch: for X; for dY, column blocks and row blocks
+    int db_parts;                      // of dbias: the first launch's row blocks, or the parts of dW's tiles, which then add it up
 };
 
-constexpr int kRowsAtOnce = 32;  // of X, to a workgroup of the first launch
+constexpr int kRowsAtOnce = 8;   // of X, to a workgroup of the first launch
 constexpr int kRowBlock = 128;   // rows of dY whose sum is one part of dbias
 
 template <typename T>
@@ -42,24 +43,31 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a)
     typedef Eight<TypeOf<T>::value> E;
     if ((int)blockIdx.x < a.x_blocks) {
         const int row0 = blockIdx.x * kRowsAtOnce, rows = min(kRowsAtOnce, a.T - row0), chunks = a.K / 8;
-        for (int c = threadIdx.x; c < rows * chunks; c += 256) {
-            const int r = c / chunks, col = (c - r * chunks) * 8;
-            const int64_t row = row0 + r;
-            float v[8];
-            E e;
-            if (a.x_codes) {
-                kept8(v, a.x_codes, a.x_scales, row, a.K, col);
-            } else {
-                if (a.pre_codes) {
-                    kept8(v, a.pre_codes, a.pre_scales, row, a.K, col);
+        constexpr int kAtOnce = 4;
+        for (int c0 = threadIdx.x; c0 < rows * chunks; c0 += 256 * kAtOnce) {
+            float v[kAtOnce][8];
+            int64_t at[kAtOnce];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const int c = min(c0 + 256 * u, rows * chunks - 1), r = c / chunks, col = (c - r * chunks) * 8;  // (past the end: the last chunk again)
+                at[u] = (int64_t)(row0 + r) * a.K + col;
+                if (a.x_codes) {
+                    kept8(v[u], a.x_codes, a.x_scales, row0 + r, a.K, col);
+                } else if (a.pre_codes) {
+                    kept8(v[u], a.pre_codes, a.pre_scales, row0 + r, a.K, col);
                 } else {
-                    e.load(a.pre, row * a.K + col, 8);
-                    e.get(v);
+                    E e;
+                    e.load(a.pre, at[u], 8);
+                    e.get(v[u]);
                 }
-                activate(a.act, v);
             }
-            e.set(v);
-            e.store(a.Xs, row * a.K + col, 8);
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                if (!a.x_codes) activate(a.act, v[u]);
+                E e;
+                e.set(v[u]);
+                e.store(a.Xs, at[u], 8);
+            }
         }
         return;
     }
@@ -81,7 +89,7 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a)
             for (int i = 0; i < 8; ++i) s[i] += v[i];
         }
     }
-    if (!a.db) return;
+    if (!a.db || a.dW) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sums[team][i * 32 + lane] = s[i];  // (lanes side by side)
     __syncthreads();
@@ -118,27 +126,76 @@ template <typename T, typename S>
 __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_grads_kernel(const GradArgs a)
 {
     static_assert(S::TM % 2 == 0, "a wavefront holds whole groups of 64");
-    __shared__ __align__(1024) uint8_t lds[S::kStages * S::kStage];
+    __shared__ __align__(1024) uint8_t lds[S::kLds];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave - wm * S::WN;
-    constexpr int NA = S::BM / 8 / S::kWaves, NB = S::BN / 8 / S::kWaves;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % (S::WM * S::WN) / S::WN, wn = wave % S::WN;
     const int kt = (a.K + S::BM - 1) / S::BM, x_all = a.x_tiles * a.x_parts, w_all = a.w_tiles * a.w_parts;
     const bool of_x = a.x_first ? (int)blockIdx.x < x_all : (int)blockIdx.x >= w_all;
     const int tiles = of_x ? a.x_tiles : a.w_tiles, parts = of_x ? a.x_parts : a.w_parts;
     const int id = tile_of(of_x == (a.x_first != 0) ? blockIdx.x : blockIdx.x - (of_x ? w_all : x_all), tiles * parts), part = id / tiles, tile = id - part * tiles;
-    const int row0 = tile / kt * S::BN, k0 = (tile - tile / kt * kt) * S::BM;  // of the results: tokens or neurons; inputs
-    const int length = of_x ? a.N : a.T, all = (length + 63) / 64, s0 = (int)((int64_t)all * part / parts), s1 = (int)((int64_t)all * (part + 1) / parts);
-    const int left = s1 == all ? length - (all - 1) * 64 : 64;
+    int tr, tk;
+    place_of(tile, tiles / kt, kt, tr, tk);
+    const int row0 = tr * S::BN, k0 = tk * S::BM;  // of the results: tokens or neurons; inputs
+    constexpr int KS = S::KS;
+    const int length = of_x ? a.N : a.T, all = (length + KS - 1) / KS, s0 = (int)((int64_t)all * part / parts), s1 = (int)((int64_t)all * (part + 1) / parts);
+    const int left = s1 == all ? length - (all - 1) * KS : KS;
     v16f g[S::TM][S::TN];
     clear(g);
+    float db[S::TN];
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) db[j] = 0.0f;
     const void *const dY = a.dYs ? a.dYs : a.dY;
     const int64_t dy_row = 2 * (a.dYs ? (int64_t)a.N8 : a.dy_row);
-    if (of_x)
-        multiply<T, S, true, false>(g, lds, s1 - s0, left, (left + 7) & ~7, wave, lane, across<S, NA>(a.W, 2ll * a.K, k0, a.K, s0, wave, lane),
-                                    along<S, NB>(dY, dy_row, row0, a.T, s0, wave, lane));
-    else
-        multiply<T, S, true, true>(g, lds, s1 - s0, left, left, wave, lane, across<S, NA>(a.Xs ? a.Xs : a.X, 2 * (a.Xs ? (int64_t)a.K : a.x_row), k0, a.K, s0, wave, lane),
-                                   across<S, NB>(dY, dy_row, row0, a.N8, s0, wave, lane));
+    const uint32_t lds0 = lds_address(lds);
+    const int steps = s1 - s0;
+    int stage = 0;
+    // f: the product, its operands on their way to LDS, how much of the last step there is
+    const auto form = [&](const auto &product, auto a_across, auto b_across, auto fa, auto fb, int left_a, int left_b) {
+        int next = 0;
+        const auto fetch = [&](int to) {
+            if (next >= steps) return;
+            const bool last = ++next == steps;
+            copy_step<S, decltype(a_across)::value>(fa, lds0 + to * S::kStage, last ? left_a : KS, wave, lane);
+            copy_step<S, decltype(b_across)::value>(fb, lds0 + to * S::kStage + S::BM * KS * 2, last ? left_b : KS, wave, lane);
+        };
+#pragma unroll
+        for (int u = 0; u < S::kStages; ++u) fetch(u);
+        product.run(g, db, steps, stage, fetch, [&](int s) {
+            if (s == 0 && steps >= S::kStages) wait_copies<(S::kStages - 1) * (S::NA + S::NB)>();
+            else if (steps - s >= S::kStages - 1) wait_copies<(S::kStages - 2) * (S::NA + S::NB)>();
+            else wait_copies<0>();
+        });
+    };
+    typedef std::true_type Across;
+    typedef std::false_type Along;
+    if (of_x) {
+        form(Product<T, S, true, false, false>(lds0, wave, lane), Across(), Along(), across<S, S::NA>(a.W, 2ll * a.K, k0, a.K, s0, wave, lane),
+             along<S, S::NB>(dY, dy_row, row0, a.T, s0, wave, lane), left, (left + 7) & ~7);
+    } else {
+        const auto x = across<S, S::NA>(a.Xs ? a.Xs : a.X, 2 * (a.Xs ? (int64_t)a.K : a.x_row), k0, a.K, s0, wave, lane);
+        const auto y = across<S, S::NB>(dY, dy_row, row0, a.N8, s0, wave, lane);
+        if (a.dbias && k0 == 0) {  // one tile of each row of tiles adds up dY on the way
+            form(Product<T, S, true, true, true>(lds0, wave, lane), Across(), Across(), x, y, left, left);
+            // the halves of the wavefront and the groups of wavefronts had shares of the contraction
+            __shared__ float shares[S::KG][S::BN];
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j) {
+                const float sum = halves_sum(db[j]);
+                if (wm == 0 && hf == 0) shares[wave / (S::WM * S::WN)][(wn * S::TN + j) * 32 + l32] = sum;
+            }
+            barrier();
+            for (int i = threadIdx.x; i < S::BN; i += 64 * S::kWaves) {
+                float sum = shares[0][i];
+#pragma unroll
+                for (int k = 1; k < S::KG; ++k) sum += shares[k][i];
+                if (row0 + i < a.N) (parts > 1 ? a.db + (int64_t)part * a.N : a.dbias)[row0 + i] = sum;
+            }
+        } else {
+            form(Product<T, S, true, true, false>(lds0, wave, lane), Across(), Across(), x, y, left, left);
+        }
+    }
+    gather<S>(g, db, lds + S::kStages * S::kStage, wave, lane);
+    if (wave >= S::WM * S::WN) return;
     float *const sums = of_x ? a.dXp : a.dWp;
     const int rows = of_x ? a.T : a.N;
     each<S::TM / 2>([&](auto half) {
@@ -171,18 +228,18 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_grads_kernel(const G
     });
 }
 
-// What was cut into parts: 32 rows by 64 columns of dX (x_blocks workgroups) or dW (w_blocks) to a wavefront; the last workgroups add up 64 columns of dbias each.
+// What was cut into parts: rows of dX (x_blocks workgroups) or of dW (w_blocks), four neighbours to a thread; the last workgroups add up 64 columns of dbias each.
 template <typename T>
 __global__ __launch_bounds__(256) void linear_ends_kernel(const GradArgs a, int x_blocks, int w_blocks)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hf = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if ((int)blockIdx.x >= x_blocks + w_blocks) {
         __shared__ float sums[4][64];
         const int n = ((int)blockIdx.x - x_blocks - w_blocks) * 64 + lane;
         float s = 0.0f;
         if (n < a.N) {
 #pragma unroll 8
-            for (int p = wave; p < a.t_blocks; p += 4) s += a.db[(int64_t)p * a.N + n];
+            for (int p = wave; p < a.db_parts; p += 4) s += a.db[(int64_t)p * a.N + n];
         }
         sums[wave][lane] = s;
         __syncthreads();
@@ -190,31 +247,20 @@ __global__ __launch_bounds__(256) void linear_ends_kernel(const GradArgs a, int 
         return;
     }
     const bool of_x = (int)blockIdx.x < x_blocks;
-    const int rows = of_x ? a.T : a.N, parts = of_x ? a.x_parts : a.w_parts, groups = a.K / 64;
-    const int64_t id = (int64_t)((int)blockIdx.x - (of_x ? 0 : x_blocks)) * 4 + wave;
-    const int block = (int)(id / groups), col = (int)(id - (int64_t)block * groups) * 64, row = block * 32 + (lane & 31);
-    if (block * 32 >= rows) return;
-    float g[2][16];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int k = 0; k < 16; ++k) g[u][k] = 0.0f;
-    const float *from = (of_x ? a.dXp : a.dWp) + (int64_t)min(row, rows - 1) * a.K + col + 4 * hf;
-    for (int p = 0; p < parts; ++p, from += (int64_t)rows * a.K)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int k = 0; k < 16; k += 4) {
-                const v4f x = *reinterpret_cast<const v4f *>(from + 32 * u + 2 * k);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) g[u][k + e] += x[e];
-            }
-    if (of_x) {
-        finish<T>(a, row, col, hf, g);
-    } else {
-        Block<T>::store(a.dW, (int64_t)row * a.K, col, a.K, row < rows, hf, g[0]);
-        Block<T>::store(a.dW, (int64_t)row * a.K, col + 32, a.K, row < rows, hf, g[1]);
+    const int rows = of_x ? a.T : a.N, quads = a.K / 4;
+    const int64_t i = (int64_t)((int)blockIdx.x - (of_x ? 0 : x_blocks)) * 256 + threadIdx.x;
+    const int row = (int)(i / quads), col = (int)(i - (int64_t)row * quads) * 4;
+    if (row >= rows) return;
+    const int64_t at = (int64_t)row * a.K + col;
+    float g[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    add_parts((of_x ? a.dXp : a.dWp) + at, (int64_t)rows * a.K, of_x ? a.x_parts : a.w_parts, g);
+    if (of_x && a.act != QB_ACT_NONE) {
+        float z[4];
+        if (a.pre_codes) kept4(z, a.pre_codes, a.pre_scales, row, a.K, col);
+        else load4<T>(a.pre, at, 4, z);
+        slope(a.act, z, g);
     }
+    store4<T>(of_x ? a.dX : a.dW, at, 4, g);
 }
 
 // no token: gradients of zero
@@ -226,55 +272,46 @@ __global__ __launch_bounds__(256) void linear_zero_kernel(uint16_t *dW, float *d
     }
 }
 
-typedef Shape<2, 4, 4, 2, 2> Large;  // 256 x 256
-typedef Shape<2, 2, 2, 2, 2> Middle;  // 128 x 128
-typedef Shape<1, 4, 2, 1, 3> Small;  // 64 x 128
+typedef Tile<2, 4, 4, 2, 2> Large;   // 256 x 256
+typedef Tile<2, 2, 2, 2, 2> Middle;  // 128 x 128
+typedef Tile<1, 4, 2, 1, 3> Small;   // 64 x 128
 
 struct Plan {
     int size, x_tiles, w_tiles, x_parts, w_parts;
 };
-// Steps until the last of `room` workgroups is done with n1 tiles of a steps and, after them, n2 of b.
-int64_t last_done(int64_t n1, int64_t a, int64_t n2, int64_t b, int room)
-{
-    const int64_t full = n1 / room, rest = n1 - full * room;
-    if (rest == 0) return full * a + (n2 + room - 1) / room * b;
-    const int64_t beside = (room - rest) * (a / b);  // tiles of b that fit beside the last round of a
-    return (full + 1) * a + (n2 > beside ? (n2 - beside + room - 1) / room * b : 0);
-}
+// Which tiles, and into how many parts their contractions are cut: the shortest time by a model in microseconds.  A CU's operands come at `rate` KB/us (more
+// small tiles are under way at once), a lone workgroup takes `step` for a step; a launch and a tile's ends 4; parts cost the launch that adds them up, 3, and their
+// bytes, twice, at 8 TB/s.  Measured and modelled: 390 x 2304 by 768, small tiles, dX in 1, 2, 3, 4 parts 18.2, 15.7, 14.4, 14.5 us (18.4, 14.6, 12.7, 13); 4000 x 1024
+// by 1024, dW in 4 parts, small 33.0, middle 29.9 (35, 30); 2000 x 1024 by 1024 small, dW in 1, 2 parts, 25, 21.5.
 template <typename S>
-void parts_of(Plan &p, bool dx, bool dw, int64_t T, int64_t N, int64_t K, int room)
+void try_tiles(Plan &best, double &least, int size, double rate, double step, bool dx, bool dw, int64_t T, int64_t N, int64_t K)
 {
-    const int64_t kt = (K + S::BM - 1) / S::BM;
-    p.x_tiles = dx ? (int)(kt * ((T + S::BN - 1) / S::BN)) : 0;
-    p.w_tiles = dw ? (int)(kt * ((N + S::BN - 1) / S::BN)) : 0;
-    constexpr int kParts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
-    constexpr int kTileCost = 5;
-    const int x_steps = (int)((N + 63) / 64), w_steps = (int)((T + 63) / 64);
-    p.x_parts = p.w_parts = 1;
-    int64_t least = INT64_MAX;
-    for (const int x : kParts)
-        for (const int w : kParts) {
+    const int64_t kt = (K + S::BM - 1) / S::BM, x_tiles = dx ? kt * ((T + S::BN - 1) / S::BN) : 0, w_tiles = dw ? kt * ((N + S::BN - 1) / S::BN) : 0;
+    const int64_t x_steps = (N + 63) / 64, w_steps = (T + 63) / 64;
+    const double kb = (x_tiles * x_steps + w_tiles * w_steps) * ((S::BM + S::BN) / 8.0);
+    for (const int x : {1, 2, 3, 4, 6, 8})
+        for (const int w : {1, 2, 3, 4, 6, 8, 12, 16}) {
             if ((x > 1 && (!dx || x > x_steps / 2)) || (w > 1 && (!dw || w > w_steps / 2))) continue;
-            const int64_t a = (x_steps + x - 1) / x + kTileCost, b = (w_steps + w - 1) / w + kTileCost, nx = (int64_t)p.x_tiles * x, nw = (int64_t)p.w_tiles * w;
-            int64_t cost = a >= b ? last_done(nx, a, nw, b, room) : last_done(nw, b, nx, a, room);
-            // the parts' sums: written and read once, at the rate at which a step's operands come
-            cost += (x > 1 || w > 1 ? 4 : 0) + ((x > 1 ? x * T * K : 0) + (w > 1 ? w * N * K : 0)) / (room * 8192ll);
+            const int64_t tasks = x_tiles * x + w_tiles * w;
+            const double chain = std::max(dx ? (x_steps + x - 1) / x : int64_t(0), dw ? (w_steps + w - 1) / w : int64_t(0)) * step;
+            double cost = 4.0 + std::max(chain, kb / (rate * std::min<int64_t>(tasks, 256)));
+            if (tasks > 256) cost += 0.5 * chain;  // (the last round is not full)
+            if (x > 1 || w > 1) cost += 3.0 + ((x > 1 ? x * T * K : 0) + (w > 1 ? w * N * K : 0)) * 8e-6 / 8.0;
             if (cost < least) {
                 least = cost;
-                p.x_parts = x;
-                p.w_parts = w;
+                best = {size, (int)x_tiles, (int)w_tiles, x, w};
             }
         }
 }
 Plan plan_of(const qb_linear_grads &l)
 {
     const bool dx = l.dX != nullptr, dw = l.dW != nullptr;
-    Plan p = {};
-    const int64_t work = (dx ? l.T * l.K * ((l.N + 63) / 64) : 0) + (dw ? l.N * l.K * ((l.T + 63) / 64) : 0);  // results by steps
-    p.size = work >= 256ll * 65536 * 16 ? 2 : work >= 256ll * 16384 * 16 ? 1 : 0;
-    if (p.size == 2) parts_of<Large>(p, dx, dw, l.T, l.N, l.K, 256);
-    else if (p.size == 1) parts_of<Middle>(p, dx, dw, l.T, l.N, l.K, 512);
-    else parts_of<Small>(p, dx, dw, l.T, l.N, l.K, 512);
+    Plan p = {0, 0, 0, 1, 1};
+    if (!dx && !dw) return p;
+    double least = 1e300;
+    try_tiles<Large>(p, least, 2, 42.0, 1.6, dx, dw, l.T, l.N, l.K);
+    try_tiles<Middle>(p, least, 1, 53.0, 0.6, dx, dw, l.T, l.N, l.K);
+    try_tiles<Small>(p, least, 0, 65.0, 0.4, dx, dw, l.T, l.N, l.K);
     return p;
 }
 
@@ -299,10 +336,11 @@ size_t lay_out(const qb_linear_grads &l, GradArgs &a, Plan &p, uint8_t *base)
     a.n_blocks = (a.N + 255) / 256;
     const bool stage = (l.dX || l.dW) && !readable(l), expand = l.dW && !l.X;
     a.x_blocks = expand ? (a.T + kRowsAtOnce - 1) / kRowsAtOnce : 0;
-    if (!stage && !l.dbias) a.t_blocks = 0;
+    a.db_parts = !l.dbias ? 0 : l.dW ? p.w_parts : a.t_blocks;
+    if (!stage && (!l.dbias || l.dW)) a.t_blocks = 0;
     if (expand) a.Xs = reinterpret_cast<uint16_t *>(take((size_t)a.T * a.K * 2));
     if (stage) a.dYs = reinterpret_cast<uint16_t *>(take((size_t)a.T * a.N8 * 2));
-    if (l.dbias) a.db = reinterpret_cast<float *>(take((size_t)a.t_blocks * a.N * 4));
+    if (l.dbias && !(l.dW && a.db_parts == 1)) a.db = reinterpret_cast<float *>(take((size_t)a.db_parts * a.N * 4));
     if (p.x_parts > 1) a.dXp = reinterpret_cast<float *>(take((size_t)p.x_parts * a.T * a.K * 4));
     if (p.w_parts > 1) a.dWp = reinterpret_cast<float *>(take((size_t)p.w_parts * a.N * a.K * 4));
     return at;
@@ -319,8 +357,8 @@ qb_status launch(const GradArgs &a, int size, hipStream_t st)
         else if (size == 1) linear_grads_kernel<T, Middle><<<groups, 64 * Middle::kWaves, 0, st>>>(a);
         else linear_grads_kernel<T, Small><<<groups, 64 * Small::kWaves, 0, st>>>(a);
     }
-    const auto blocks = [&](int64_t rows) { return (int)(((rows + 31) / 32 * (a.K / 64) + 3) / 4); };
-    const int x_blocks = a.dXp ? blocks(a.T) : 0, w_blocks = a.dWp ? blocks(a.N) : 0, ends = x_blocks + w_blocks + (a.dbias ? (a.N + 63) / 64 : 0);
+    const auto blocks = [&](int64_t rows) { return (int)((rows * (a.K / 4) + 255) / 256); };
+    const int x_blocks = a.dXp ? blocks(a.T) : 0, w_blocks = a.dWp ? blocks(a.N) : 0, ends = x_blocks + w_blocks + (a.dbias && !(a.dW && a.db_parts == 1) ? (a.N + 63) / 64 : 0);
     if (ends > 0) linear_ends_kernel<T><<<ends, 256, 0, st>>>(a, x_blocks, w_blocks);
     return launch_status();
 }

@@ -94,27 +94,42 @@ struct Coder {
     {
         scale = __fdiv_rn(__uint_as_float(top), 127.0f);
         fast = scale >= 1.0e-30f && scale <= 1.0e37f;
-        inverse = fast ? __fdiv_rn(1.0f, scale) : 0.0f;
+        inverse = fast ? __builtin_amdgcn_rcpf(scale) : 0.0f;
     }
-    // The product with the rounded reciprocal is within 127.5 * 3 * 2^-24 = 2.3e-5 of the true quotient; closer than 1e-4 to half a step the sign of
-    // x - (k + 1/2) scale decides, which one fused multiply and add gives without error.
-    __device__ __forceinline__ int code(float x) const
+    // N codes, four to a word.  Adding 1.5 * 2^23 leaves the nearest whole number in the low bits of a sum that is rounded once; the reciprocal is within one unit in
+    // the last place, so that x inverse is within 127.5 * 2^-23 = 1.6e-5 of the true quotient.  Where one of the quotients is closer than 2e-5 to half a step, all of the lane's are taken again, with care.
+    template <int N>
+    __device__ __forceinline__ void codes(const float (&x)[N], uint32_t (&w)[N / 4]) const
     {
-        const float m = fabsf(x), t = fast ? m * inverse : __fdiv_rn(m, scale);
-        float k = rintf(t);
-        if (!(fabsf(t - k) <= 0.4999f)) k = near_half(m, t);
-        k = fminf(k, 127.0f);  // (subnormal scales are far from max |x| / 127)
-        return (int)(x < 0.0f ? -k : k);
+        constexpr float kWhole = 12582912.0f;
+        float far = fast ? 0.0f : 1.0f;
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            float k[4], d[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                k[e] = __builtin_fmaf(x[i + e], inverse, kWhole);
+                d[e] = fabsf(__builtin_fmaf(x[i + e], inverse, kWhole - k[e]));
+            }
+            far = fmaxf(fmaxf(far, fmaxf(d[0], d[1])), fmaxf(d[2], d[3]));
+            const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(k[1]), __float_as_uint(k[0]), 0x0C0C0400), hi = __builtin_amdgcn_perm(__float_as_uint(k[3]), __float_as_uint(k[2]), 0x04000C0C);
+            w[i / 4] = lo | hi;
+        }
+        if (far <= 0.49998f) return;
+#pragma unroll
+        for (int i = 0; i < N; i += 4) w[i / 4] = four(careful(x[i]), careful(x[i + 1]), careful(x[i + 2]), careful(x[i + 3]));
     }
-    __device__ __forceinline__ float near_half(float m, float t) const
+    static __device__ __forceinline__ uint32_t four(int a, int b, int c, int d) { return (a & 0xFF) | (b & 0xFF) << 8 | (c & 0xFF) << 16 | (uint32_t)d << 24; }
+    // next to half a step the sign of |x| - (k + 1/2) scale decides, which one fused multiply and add gives without error
+    __device__ __forceinline__ int careful(float x) const
     {
-        if (!(scale > 0.0f && scale < __builtin_inff())) return 0.0f;
-        const float low = floorf(t), d = __builtin_fmaf(-(low + 0.5f), scale, m);
-        const bool odd = ((int)low & 1) != 0;
-        return d > 0.0f || (d == 0.0f && odd) ? low + 1.0f : low;
+        if (!(scale > 0.0f && scale < __builtin_inff())) return 0;
+        const float m = fabsf(x), t = fminf(__fdiv_rn(m, scale), 127.0f), low = floorf(t);  // (subnormal scales are far from max |x| / 127)
+        const float d = __builtin_fmaf(-(low + 0.5f), scale, m);
+        const int k = (int)low + (low < 127.0f && (d > 0.0f || (d == 0.0f && ((int)low & 1) != 0)) ? 1 : 0);
+        return x < 0.0f ? -k : k;
     }
 };
-__device__ __forceinline__ uint32_t four(int a, int b, int c, int d) { return (a & 0xFF) | (b & 0xFF) << 8 | (c & 0xFF) << 16 | (uint32_t)d << 24; }
 
 // the largest of eight neighbouring lanes, in each of them
 __device__ __forceinline__ uint32_t max8(uint32_t v)
@@ -124,7 +139,27 @@ __device__ __forceinline__ uint32_t max8(uint32_t v)
     v = max(v, other(std::integral_constant<int, 0x4E>()));   // lane ^ 2
     return max(v, other(std::integral_constant<int, 0x141>()));  // the other four of eight
 }
-// Codes of a group that lies in eight neighbouring lanes, eight values each; `n` of a lane's are inside the row.
+// Codes of a group that lies in eight neighbouring lanes, eight values each, whole groups: `chunk` counts the eights.
+__device__ __forceinline__ void keep8(const float (&v)[8], int8_t *codes, float *scales, int64_t chunk)
+{
+    uint32_t top = 0, q[2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
+    const Coder c(max8(top));
+    c.codes(v, q);
+    if ((chunk & 7) == 0) scales[chunk >> 3] = c.scale;
+    struct __attribute__((packed)) Loose { v2u v; };
+    reinterpret_cast<Loose *>(codes)[chunk].v = v2u{q[0], q[1]};
+}
+__device__ __forceinline__ void kept8(float (&v)[8], const int8_t *codes, const float *scales, int64_t chunk)
+{
+    struct __attribute__((packed)) Loose { v2u v; };
+    const v2u w = reinterpret_cast<const Loose *>(codes)[chunk].v;
+    const float scale = scales[chunk >> 3];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(w[i >> 2] >> (8 * (i & 3))) * scale;
+}
+// The same of a row of any width: eight values from column `col` on, which may be past the end.
 __device__ __forceinline__ void keep8(const float (&v)[8], int8_t *codes, float *scales, int64_t row, int width, int col)
 {
     uint32_t top = 0;
@@ -134,7 +169,9 @@ __device__ __forceinline__ void keep8(const float (&v)[8], int8_t *codes, float 
     const Coder c(max8(top));
     if (col >= width) return;
     if ((col & (kGroup - 1)) == 0) scales[row * ((width + kGroup - 1) / kGroup) + col / kGroup] = c.scale;
-    const v2u w = {four(c.code(v[0]), c.code(v[1]), c.code(v[2]), c.code(v[3])), four(c.code(v[4]), c.code(v[5]), c.code(v[6]), c.code(v[7]))};
+    uint32_t q[2];
+    c.codes(v, q);
+    const v2u w = {q[0], q[1]};
     int8_t *const to = codes + row * width + col;
     if (col + 8 <= width) {
         struct __attribute__((packed)) Loose { v2u v; };
@@ -169,23 +206,20 @@ __device__ __forceinline__ void kept8(float (&v)[8], const int8_t *codes, const 
 
 // ---- activations ------------------------------------------------------------------------------------------------------
 
-// The normal distribution's upper tail at |z| = exp(-z^2 / 2) M(|z|).  M falls like 1 / |z|; as a polynomial in u = 1 / (1 + 0.376 |z|) without a
-// constant term (the form of C. Hastings, "Approximations for Digital Computers", 1955; coefficients: least largest relative error, fitted for |z| <= 14)
-// it is within 3e-5 of itself, 2^-15, so that the share and GELU are below the 16-bit types' rounding steps, their tails included.
-struct Normal {
-    float bell, share;  // exp(-z^2 / 2); the distribution below z
-    __device__ __forceinline__ explicit Normal(float z)
-    {
-        const float u = __builtin_amdgcn_rcpf(__builtin_fmaf(0.376f, fabsf(z), 1.0f));
-        bell = __builtin_amdgcn_exp2f(z * z * -0.72134752044f);
-        float m = __builtin_fmaf(-0.0908565548694444f, u, 0.19874278238977716f);
-        m = __builtin_fmaf(m, u, 0.08471268883902303f);
-        m = __builtin_fmaf(m, u, 0.15791362939227915f);
-        m = __builtin_fmaf(m, u, 0.1494776113147777f);
-        const float tail = m * u * bell;
-        share = z < 0.0f ? tail : 1.0f - tail;
-    }
-};
+// The normal distribution's upper tail at x >= 0 is a power of two of a polynomial of degree eight: fitted to the tail's logarithm on [0, 8] for the least largest
+// error, 1.1e-5 of the tail itself with the evaluation's roundings (below 2^-16), so that GELU is below the 16-bit types' rounding steps, its tail included.  Further out, where
+// the tail is below 1e-15, it is within a quarter of itself; from 14 on it counts as that of 14, which is 0.
+__device__ __forceinline__ float normal_tail(float x)
+{
+    float p = __builtin_fmaf(7.428189558377491e-08f, x, -3.6552564920205284e-06f);
+    p = __builtin_fmaf(p, x, 7.957309408254909e-05f);
+    p = __builtin_fmaf(p, x, -0.0010219687735147222f);
+    p = __builtin_fmaf(p, x, 0.00876213643584221f);
+    p = __builtin_fmaf(p, x, -0.05433728145372735f);
+    p = __builtin_fmaf(p, x, -0.4581957365610262f);
+    p = __builtin_fmaf(p, x, -1.151321798311713f);
+    return __builtin_amdgcn_exp2f(__builtin_fmaf(p, x, -0.999992357264988f));
+}
 __device__ __forceinline__ float hyperbolic_tangent(float z)
 {
     if (fabsf(z) < 0.25f) {  // (the quotient's numerator would cancel; the next term of the series is below 2e-9)
@@ -206,7 +240,10 @@ __device__ __forceinline__ void activate(int act, float (&z)[N])
 {
     if (act == QB_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] *= Normal(z[i]).share;
+        for (int i = 0; i < N; ++i) {  // z - z tail, or below zero z tail
+            const float x = fminf(fabsf(z[i]), 14.0f);
+            z[i] = __builtin_fmaf(-x, normal_tail(x), __builtin_elementwise_maximum(z[i], 0.0f));
+        }
     } else if (act == QB_ACT_RELU) {
 #pragma unroll
         for (int i = 0; i < N; ++i) z[i] = z[i] < 0.0f ? 0.0f : z[i];
@@ -222,8 +259,8 @@ __device__ __forceinline__ void slope(int act, const float (&z)[N], float (&g)[N
     if (act == QB_ACT_GELU) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const Normal n(z[i]);
-            g[i] *= __builtin_fmaf(z[i] * n.bell, 0.3989422804f, n.share);
+            const float share = 0.5f + copysignf(0.5f - normal_tail(fminf(fabsf(z[i]), 14.0f)), z[i]);
+            g[i] *= __builtin_fmaf(z[i] * __builtin_amdgcn_exp2f(z[i] * z[i] * -0.72134752044f), 0.3989422804f, share);
         }
     } else if (act == QB_ACT_RELU) {
 #pragma unroll

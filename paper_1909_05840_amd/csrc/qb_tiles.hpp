@@ -22,6 +22,10 @@ struct Bf16 {
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
     }
+    static __device__ __forceinline__ v4f mma16(v8s a, v8s b, v4f c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    }
     static __device__ __forceinline__ uint32_t pair(float lo, float hi)
     {
         typedef __bf16 v2 __attribute__((ext_vector_type(2)));
@@ -38,6 +42,10 @@ struct Fp16 {
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
     }
+    static __device__ __forceinline__ v4f mma16(v8s a, v8s b, v4f c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    }
     static __device__ __forceinline__ uint32_t pair(float lo, float hi) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{lo, hi}, v2)); }
     static __device__ __forceinline__ float lo(uint32_t w) { return (float)__builtin_bit_cast(v2, w)[0]; }
     static __device__ __forceinline__ float hi(uint32_t w) { return (float)__builtin_bit_cast(v2, w)[1]; }
@@ -51,6 +59,17 @@ __device__ __forceinline__ void each(const F &f)
         f(std::integral_constant<int, I>{});
         each<N, I + 1>(f);
     }
+}
+
+template <int M, int N>
+__device__ __forceinline__ void clear(v16f (&x)[M][N])
+{
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) x[i][j][k] = 0.0f;
 }
 
 template <int N>
@@ -72,7 +91,12 @@ __device__ __forceinline__ void copy16(const void *from, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory", "m0");
 }
-// the same with the address as a base that the wavefront shares and an offset in bytes (the base is moved into registers of the block's
+// four bytes per lane: lane l's land at lds + 4 * l
+__device__ __forceinline__ void copy4(const void *from, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(lds) : "memory", "m0");
+}
+// sixteen with the address as a base that the wavefront shares and an offset in bytes (the base is moved into registers of the block's
 // own by a scalar instruction: a vector memory instruction may read what a VALU instruction wrote five wait states later only)
 __device__ __forceinline__ void copy16(const void *base, uint32_t offset, uint32_t lds)
 {
