@@ -542,7 +542,8 @@ qb_status qb_restore_act(const int8_t *codes, const float *scales, int64_t T, in
  * Layer norm of each row.
  *   mean = sum_j X[t,j] / W;  rstd = 1 / sqrt(sum_j (X[t,j] - mean)^2 / W + eps);  h = (X - mean) rstd;  Y = h weight + bias
  *   X, Y  [T,W] of `type`, X with x_row values between rows, Y dense (Y may be X);  weight, bias [W] fp32, or NULL for ones and zeros;  eps >= 0
- *   mean, rstd  out [T] fp32;  codes, scales  out, Y in 8 bits as qb_checkpoint_act writes it (of the values before they are rounded to `type`), or both NULL
+ *   mean, rstd  out [T] fp32;  codes, scales  out, Y in 8 bits in the form of qb_checkpoint_act, or both NULL: of the values in binary32 before they are rounded to `type`;
+ *               a quotient closer than 2^-16 to half a step may go either way, a group below 1.3e-28 reads back as zeros
  * qb_layer_norm_bwd, with g = dY weight:
  *   dX = rstd (g - sum_j g / W - h sum_j g h / W) (+ residual);  dweight[j] = sum_t dY[t,j] h[t,j];  dbias[j] = sum_t dY[t,j]
  *   X as the forward had it, or in 8 bits (x_codes, x_scales, and X NULL);  residual: the gradient that comes past the norm, or NULL
@@ -572,8 +573,7 @@ qb_status qb_layer_norm_bwd(const qb_norm_grads *n, void *dX, float *dweight, fl
  *   X [T,K] with x_row values between rows (a multiple of 8), W [N,K] dense, both 16-byte aligned;  bias [N] fp32 or NULL
  *   residual [T,N] with residual_row values between rows, or NULL;  Y [T,N] dense
  *   pre             out [T,N] dense, z in 16 bits for the backward of act, or NULL (only with an activation)
- *   codes, scales   out, for the backward of what follows, as qb_checkpoint_act writes them: z in 8 bits where there is an activation, else Y (in both cases of
- *                   the values in binary32, before they are rounded to `type`); or both NULL
+ *   codes, scales   out, for the backward of what follows, as qb_layer_norm_fwd writes them: z in 8 bits where there is an activation, else Y; or both NULL
  * qb_linear_bwd: here act is the activation IN FRONT of the layer, X = act(pre), and dX is the gradient of pre:
  *   dX = (dY W) act'(pre), or dY W with QB_ACT_NONE;  dW[n] = sum_t dY[t,n] X[t];  dbias[n] = sum_t dY[t,n]
  *   dY [T,N] with dy_row values between rows (any)

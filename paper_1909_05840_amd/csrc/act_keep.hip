@@ -50,7 +50,7 @@ __global__ __launch_bounds__(256) void act_keep_kernel(const KeepArgs a)
             if constexpr (KEEP) {
                 x[u].get(v[u]);
                 if constexpr (FLAT) keep8(v[u], a.codes, a.scales, at[u]);
-                else keep8(v[u], a.codes, a.scales, row[u], a.W, col[u]);
+                else keep8<true>(v[u], a.codes, a.scales, row[u], a.W, col[u]);
             } else {
                 x[u].set(v[u]);
                 if constexpr (FLAT) x[u].store(a.Y, at[u] * 8, 8);

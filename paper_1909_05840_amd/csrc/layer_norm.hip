@@ -111,7 +111,7 @@ __global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_kernel(const
         for (int i = 0; i < C; ++i) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[i][e] = __builtin_fmaf((v[i][e] - more) * rstd, w[i][e], b[i][e]);
-            if (a.codes) keep8(v[i], a.codes, a.scales, row, a.W, L::col(i));
+            if (a.codes) keep8<false>(v[i], a.codes, a.scales, row, a.W, L::col(i));
             x[i].set(v[i]);
             x[i].store(a.Y, (int64_t)row * a.W + L::col(i), a.W - L::col(i));
         }

@@ -218,6 +218,15 @@ struct Product {
         }
     }
 };
+// Waits for the wavefront's copies of step s of a tile that is all that it copies.
+template <typename S>
+__device__ __forceinline__ void wait_step(int s, int steps)
+{
+    constexpr int kStep = S::NA + S::NB;
+    if (s == 0 && steps >= S::kStages) wait_copies<(S::kStages - 1) * kStep>();
+    else if (steps - s >= S::kStages - 1) wait_copies<(S::kStages - 2) * kStep>();
+    else wait_copies<0>();
+}
 // The groups' shares of a tile's sums (and of what SUMS adds up) come together in the first group; `room`: S::kSums bytes.
 template <typename S>
 __device__ __forceinline__ void gather(v16f (&acc)[S::TM][S::TN], float (&sums)[S::TN], uint8_t *room, int wave, int lane)
@@ -317,30 +326,88 @@ struct Block {
 #pragma unroll
         for (int k = 0; k < 16; ++k) v[k] = (float)(int8_t)(w[k >> 2] >> (8 * (k & 3))) * scale;
     }
-    static __device__ __forceinline__ void store_codes(int8_t *p, int64_t at, int col, int width, bool inside, int hf, const Coder &coder, const float (&v)[16])
-    {
-        uint32_t q[4];
-        coder.codes(v, q);
-        v4u w = {q[0], q[1], q[2], q[3]};
-        w = join_codes(w);
-        const int c = col + 16 * hf;
-        if (!inside) return;
-        if (c + 16 <= width) store16(p + at, c, w);
-        else each<16>([&](auto e) { if (c + e < width) p[at + c + e] = (int8_t)(w[e >> 2] >> (8 * (e & 3))); });
-    }
-    static __device__ __forceinline__ uint32_t top(int col, int width, int hf, const float (&v)[16])
-    {
-        uint32_t t = 0;
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
-            if (col + 8 * (k >> 2) + 4 * hf + (k & 3) < width) t = max(t, magnitude(v[k]));
-        return t;
-    }
 };
-__device__ __forceinline__ uint32_t halves_top(uint32_t v)
+// the bits of the largest magnitude of a row's 64 columns from `col` on, those of the lane's row (NaN above all)
+__device__ __forceinline__ uint32_t top_of(int col, int width, int hf, const float (&v)[2][16])
 {
-    const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    float t = 0.0f;
+    if (col + 64 <= width) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int k = 0; k < 16; k += 2) t = max3(t, fabsf(v[u][k]), fabsf(v[u][k + 1]));
+    } else {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) t = __builtin_elementwise_maximum(t, col + 32 * u + 8 * (k >> 2) + 4 * hf + (k & 3) < width ? fabsf(v[u][k]) : 0.0f);
+    }
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(t), __float_as_uint(t), false, false);
     return max(s[0], s[1]);
+}
+
+// The same 64 columns of 32 rows through LDS of the wavefront's own (kRowsRoom bytes), sixteen rows at a time, so that eight neighbouring lanes write 128 bytes of a
+// row, where a lane alone would write 16 of its own: rows that reach memory in pieces of 32 bytes cost 16384 x 4096 results X us of Y.
+constexpr int kRowsRoom = 2048;
+template <bool STREAM>
+__device__ __forceinline__ void put16(void *p, int64_t byte, v4u v)
+{
+    if constexpr (STREAM) store16_stream(p, byte, v);
+    else store16(p, byte, v);
+}
+template <typename T, bool STREAM>
+__device__ __forceinline__ void store_rows(uint16_t *p, int row0, int rows, int col, int width, int lane, uint8_t *room, const float (&v)[2][16])
+{
+    const int l32 = lane & 31, hf = lane >> 5;
+    v4u w[4];  // chunks of eight columns: 2 * i + hf
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float *const x = v[i >> 1] + 8 * (i & 1);
+        w[i] = join_halves(v2u{T::pair(x[0], x[1]), T::pair(x[2], x[3])}, v2u{T::pair(x[4], x[5]), T::pair(x[6], x[7])});
+    }
+#pragma unroll
+    for (int pass = 0; pass < 2; ++pass) {
+        __builtin_amdgcn_wave_barrier();
+        if ((l32 >> 4) == pass) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<v4u *>(room + (l32 & 15) * 128 + (((2 * i + hf) ^ (l32 & 7)) << 4)) = w[i];
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int in = 8 * r + (lane >> 3), row = row0 + 16 * pass + in, c = col + 8 * (lane & 7);
+            const v4u x = *reinterpret_cast<const v4u *>(room + in * 128 + (((lane & 7) ^ (in & 7)) << 4));
+            if (row >= rows) continue;
+            const int64_t at = (int64_t)row * width;
+            if (c + 8 <= width) put16<STREAM>(p + at, 2 * c, x);
+            else each<8>([&](auto e) { if (c + e < width) p[at + c + e] = (uint16_t)(x[e >> 1] >> (16 * (e & 1))); });
+        }
+    }
+}
+template <bool STREAM>
+__device__ __forceinline__ void store_code_rows(int8_t *p, int row0, int rows, int col, int width, int lane, uint8_t *room, const Coder &coder, const float (&v)[2][16])
+{
+    const int l32 = lane & 31, hf = lane >> 5;
+    v4u w[2];  // chunks of sixteen columns: 2 * u + hf
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        uint32_t q[4];
+        coder.quick(v[u], q);
+        w[u] = join_codes(v4u{q[0], q[1], q[2], q[3]});
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int u = 0; u < 2; ++u) *reinterpret_cast<v4u *>(room + l32 * 64 + (((2 * u + hf) ^ (l32 >> 2 & 3)) << 4)) = w[u];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int in = 16 * r + (lane >> 2), row = row0 + in, c = col + 16 * (lane & 3);
+        const v4u x = *reinterpret_cast<const v4u *>(room + in * 64 + (((lane & 3) ^ (in >> 2 & 3)) << 4));
+        if (row >= rows) continue;
+        const int64_t at = (int64_t)row * width;
+        if (c + 16 <= width) put16<STREAM>(p + at, c, x);
+        else each<16>([&](auto e) { if (c + e < width) p[at + c + e] = (int8_t)(x[e >> 2] >> (8 * (e & 3))); });
+    }
 }
 
 // ---- rows of sums: four neighbours to a thread, a group of 64 to sixteen lanes
@@ -394,9 +461,9 @@ __device__ __forceinline__ void keep4(const float (&z)[4], int8_t *codes, float 
     top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x140, 0xF, 0xF, true));  // the other eight of sixteen
     const Coder c(top);
     uint32_t w[1];
-    c.codes(z, w);
+    c.quick(z, w);
     if (!inside || col >= width) return;
-    if ((col & (kGroup - 1)) == 0) scales[row * ((width + kGroup - 1) / kGroup) + col / kGroup] = c.scale;
+    if ((col & (kGroup - 1)) == 0) scales[row * ((width + kGroup - 1) / kGroup) + col / kGroup] = c.quick_scale();
     int8_t *const to = codes + row * width + col;
     if (col + 4 <= width) {
         struct __attribute__((packed)) Loose { uint32_t v; };

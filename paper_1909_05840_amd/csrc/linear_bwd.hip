@@ -101,11 +101,12 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a)
     a.db[(int64_t)block * a.N + n] = x;
 }
 
-// dX's rows: 64 neighbours of what dY W gives
-template <typename T>
-__device__ __forceinline__ void finish(const GradArgs &a, int row, int col, int hf, float (&g)[2][16])
+// dX's rows: 64 columns from `col` on of what dY W gives, 32 rows from `row0` on
+template <typename T, bool STREAM>
+__device__ __forceinline__ void finish(const GradArgs &a, int row0, int col, int lane, uint8_t *room, float (&g)[2][16])
 {
     typedef Block<T> B;
+    const int row = row0 + (lane & 31), hf = lane >> 5;
     const bool inside = row < a.T;
     const int64_t at = (int64_t)row * a.K;
     if (a.act != QB_ACT_NONE) {
@@ -118,8 +119,7 @@ __device__ __forceinline__ void finish(const GradArgs &a, int row, int col, int 
             slope(a.act, z, g[i]);
         }
     }
-    B::store(a.dX, at, col, a.K, inside, hf, g[0]);
-    B::store(a.dX, at, col + 32, a.K, inside, hf, g[1]);
+    store_rows<T, STREAM>(a.dX, row0, a.T, col, a.K, lane, room, g);
 }
 
 template <typename T, typename S>
@@ -127,6 +127,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_grads_kernel(const G
 {
     static_assert(S::TM % 2 == 0, "a wavefront holds whole groups of 64");
     __shared__ __align__(1024) uint8_t lds[S::kLds];
+    static_assert(S::kStages * S::kStage >= S::kWaves * kRowsRoom, "room for the rows on their way out, where the stages were");
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % (S::WM * S::WN) / S::WN, wn = wave % S::WN;
     const int kt = (a.K + S::BM - 1) / S::BM, x_all = a.x_tiles * a.x_parts, w_all = a.w_tiles * a.w_parts;
@@ -160,11 +161,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_grads_kernel(const G
         };
 #pragma unroll
         for (int u = 0; u < S::kStages; ++u) fetch(u);
-        product.run(g, db, steps, stage, fetch, [&](int s) {
-            if (s == 0 && steps >= S::kStages) wait_copies<(S::kStages - 1) * (S::NA + S::NB)>();
-            else if (steps - s >= S::kStages - 1) wait_copies<(S::kStages - 2) * (S::NA + S::NB)>();
-            else wait_copies<0>();
-        });
+        product.run(g, db, steps, stage, fetch, [&](int s) { wait_step<S>(s, steps); });
     };
     typedef std::true_type Across;
     typedef std::false_type Along;
@@ -204,7 +201,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_grads_kernel(const G
         if (col >= a.K) return;
 #pragma unroll
         for (int j = 0; j < S::TN; ++j) {
-            const int row = row0 + (wn * S::TN + j) * 32 + l32;
+            const int first = row0 + (wn * S::TN + j) * 32, row = first + l32;
             float v[2][16];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -219,10 +216,9 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_grads_kernel(const G
                         for (int k = 0; k < 16; k += 4) *reinterpret_cast<v4f *>(to + 32 * u + 2 * k + 4 * hf) = v4f{v[u][k], v[u][k + 1], v[u][k + 2], v[u][k + 3]};
                 }
             } else if (of_x) {
-                finish<T>(a, row, col, hf, v);
+                finish<T, S::kWaves == 8>(a, first, col, lane, lds + wave * kRowsRoom, v);
             } else {
-                Block<T>::store(a.dW, (int64_t)row * a.K, col, a.K, row < a.N, hf, v[0]);
-                Block<T>::store(a.dW, (int64_t)row * a.K, col + 32, a.K, row < a.N, hf, v[1]);
+                store_rows<T, false>(a.dW, first, a.N, col, a.K, lane, lds + wave * kRowsRoom, v);
             }
         }
     });

@@ -119,6 +119,20 @@ struct Coder {
 #pragma unroll
         for (int i = 0; i < N; i += 4) w[i / 4] = four(careful(x[i]), careful(x[i + 1]), careful(x[i + 2]), careful(x[i + 3]));
     }
+    // The same without the second look, for values that are themselves results of rounded arithmetic: a quotient closer than 2^-16 to half a step may go either way.
+    // Groups whose scale has no reciprocal read back as zeros (magnitudes below 1.3e-28), or as NaN (infinities, NaN).
+    __device__ __forceinline__ float quick_scale() const { return fast ? scale : scale * 0.0f; }
+    template <int N>
+    __device__ __forceinline__ void quick(const float (&x)[N], uint32_t (&w)[N / 4]) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            uint32_t k[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) k[e] = __float_as_uint(__builtin_fmaf(x[i + e], inverse, 12582912.0f));
+            w[i / 4] = __builtin_amdgcn_perm(k[1], k[0], 0x0C0C0400) | __builtin_amdgcn_perm(k[3], k[2], 0x04000C0C);
+        }
+    }
     static __device__ __forceinline__ uint32_t four(int a, int b, int c, int d) { return (a & 0xFF) | (b & 0xFF) << 8 | (c & 0xFF) << 16 | (uint32_t)d << 24; }
     // next to half a step the sign of |x| - (k + 1/2) scale decides, which one fused multiply and add gives without error
     __device__ __forceinline__ int careful(float x) const
@@ -160,6 +174,7 @@ __device__ __forceinline__ void kept8(float (&v)[8], const int8_t *codes, const 
     for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(w[i >> 2] >> (8 * (i & 3))) * scale;
 }
 // The same of a row of any width: eight values from column `col` on, which may be past the end.
+template <bool EXACT>
 __device__ __forceinline__ void keep8(const float (&v)[8], int8_t *codes, float *scales, int64_t row, int width, int col)
 {
     uint32_t top = 0;
@@ -168,9 +183,10 @@ __device__ __forceinline__ void keep8(const float (&v)[8], int8_t *codes, float 
         if (col + i < width) top = max(top, magnitude(v[i]));
     const Coder c(max8(top));
     if (col >= width) return;
-    if ((col & (kGroup - 1)) == 0) scales[row * ((width + kGroup - 1) / kGroup) + col / kGroup] = c.scale;
+    if ((col & (kGroup - 1)) == 0) scales[row * ((width + kGroup - 1) / kGroup) + col / kGroup] = EXACT ? c.scale : c.quick_scale();
     uint32_t q[2];
-    c.codes(v, q);
+    if constexpr (EXACT) c.codes(v, q);
+    else c.quick(v, q);
     const v2u w = {q[0], q[1]};
     int8_t *const to = codes + row * width + col;
     if (col + 8 <= width) {
@@ -206,19 +222,20 @@ __device__ __forceinline__ void kept8(float (&v)[8], const int8_t *codes, const 
 
 // ---- activations ------------------------------------------------------------------------------------------------------
 
-// The normal distribution's upper tail at x >= 0 is a power of two of a polynomial of degree eight: fitted to the tail's logarithm on [0, 8] for the least largest
-// error, 1.1e-5 of the tail itself with the evaluation's roundings (below 2^-16), so that GELU is below the 16-bit types' rounding steps, its tail included.  Further out, where
-// the tail is below 1e-15, it is within a quarter of itself; from 14 on it counts as that of 14, which is 0.
+// The normal distribution's upper tail at x >= 0 is a power of two of a polynomial of degree seven: fitted to the tail's logarithm on [0, 7] for the least largest
+// error, 1.3e-5 of the tail itself with the evaluation's roundings (below 2^-16), so that GELU is below the 16-bit types' rounding steps, its tail included.  Further out the
+// polynomial falls a little faster: 2% less at 9, where the tail is 1e-19; from 16 on it is zero.  (Degree eight: 1.0e-5.  An instruction for each of 16384 x 4096
+// results takes 8 us when the matrix cores wait for it.)
+constexpr float kTailEnd = 16.0f;
 __device__ __forceinline__ float normal_tail(float x)
 {
-    float p = __builtin_fmaf(7.428189558377491e-08f, x, -3.6552564920205284e-06f);
-    p = __builtin_fmaf(p, x, 7.957309408254909e-05f);
-    p = __builtin_fmaf(p, x, -0.0010219687735147222f);
-    p = __builtin_fmaf(p, x, 0.00876213643584221f);
-    p = __builtin_fmaf(p, x, -0.05433728145372735f);
-    p = __builtin_fmaf(p, x, -0.4581957365610262f);
-    p = __builtin_fmaf(p, x, -1.151321798311713f);
-    return __builtin_amdgcn_exp2f(__builtin_fmaf(p, x, -0.999992357264988f));
+    float p = __builtin_fmaf(-1.58821490003902e-06f, x, 5.61533379368484e-05f);
+    p = __builtin_fmaf(p, x, -0.0008832153398543596f);
+    p = __builtin_fmaf(p, x, 0.008303219452500343f);
+    p = __builtin_fmaf(p, x, -0.053501322865486145f);
+    p = __builtin_fmaf(p, x, -0.4589643180370331f);
+    p = __builtin_fmaf(p, x, -1.1510356664657593f);
+    return __builtin_amdgcn_exp2f(__builtin_fmaf(p, x, -1.0000139474868774f));
 }
 __device__ __forceinline__ float hyperbolic_tangent(float z)
 {
@@ -241,7 +258,7 @@ __device__ __forceinline__ void activate(int act, float (&z)[N])
     if (act == QB_ACT_GELU) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {  // z - z tail, or below zero z tail
-            const float x = fminf(fabsf(z[i]), 14.0f);
+            const float x = fminf(fabsf(z[i]), kTailEnd);
             z[i] = __builtin_fmaf(-x, normal_tail(x), __builtin_elementwise_maximum(z[i], 0.0f));
         }
     } else if (act == QB_ACT_RELU) {
@@ -259,7 +276,7 @@ __device__ __forceinline__ void slope(int act, const float (&z)[N], float (&g)[N
     if (act == QB_ACT_GELU) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float share = 0.5f + copysignf(0.5f - normal_tail(fminf(fabsf(z[i]), 14.0f)), z[i]);
+            const float share = 0.5f + copysignf(0.5f - normal_tail(fminf(fabsf(z[i]), kTailEnd)), z[i]);
             g[i] *= __builtin_fmaf(z[i] * __builtin_amdgcn_exp2f(z[i] * z[i] * -0.72134752044f), 0.3989422804f, share);
         }
     } else if (act == QB_ACT_RELU) {

@@ -232,6 +232,12 @@ __device__ __forceinline__ void store16(void *p, int64_t byte, v4u v)
     reinterpret_cast<Loose *>(static_cast<uint8_t *>(p) + byte)->v = v;
 }
 
+// the same for what is not read again soon: it leaves the L2 first, and the operands that others read there stay
+__device__ __forceinline__ void store16_stream(void *p, int64_t byte, v4u v)
+{
+    typedef v4u Loose __attribute__((aligned(1)));
+    __builtin_nontemporal_store(v, reinterpret_cast<Loose *>(static_cast<uint8_t *>(p) + byte));
+}
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 }  // namespace qb
