@@ -69,12 +69,15 @@ __global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_kernel(const
     typedef Row<R, C> L;
     __shared__ v2f shared[L::kThreads / 64];
     const float inv = 1.0f / (float)a.W;
+    constexpr bool kHold = C < 4;  // the weights stay in registers
     float w[C][8], b[C][8];
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
+    const auto weights = [&](int i) {
         columns(a.weight, 1.0f, L::col(i), a.W, w[i]);
         columns(a.bias, 0.0f, L::col(i), a.W, b[i]);
-    }
+    };
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+        if (kHold) weights(i);
     for (int row0 = blockIdx.x * L::kRows; row0 < a.T; row0 += gridDim.x * L::kRows) {
         const int row = row0 + (int)(threadIdx.x / R);
         if (R == 64 && row >= a.T) break;
@@ -109,6 +112,7 @@ __global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_kernel(const
         }
 #pragma unroll
         for (int i = 0; i < C; ++i) {
+            if (!kHold) weights(i);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[i][e] = __builtin_fmaf((v[i][e] - more) * rstd, w[i][e], b[i][e]);
             if (a.codes) keep8<false>(v[i], a.codes, a.scales, row, a.W, L::col(i));
@@ -118,16 +122,19 @@ __global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_kernel(const
     }
 }
 
+// Rows that leave no registers for that (kWide values and more) are read once again by layer_norm_sums_kernel.
+constexpr int kWide = 8192;
 template <int TYPE, int R, int C>
 __global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_bwd_kernel(const NormArgs a)
 {
     typedef Row<R, C> L;
+    constexpr bool kHold = R * C * 8 <= kWide;  // weights and sums stay in registers
     __shared__ v2f shared[L::kThreads / 64];
     const float inv = 1.0f / (float)a.W;
     float w[C][8], dw[C][8], db[C][8];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-        columns(a.weight, 1.0f, L::col(i), a.W, w[i]);
+        if (kHold) columns(a.weight, 1.0f, L::col(i), a.W, w[i]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) dw[i][e] = db[i][e] = 0.0f;
     }
@@ -148,11 +155,14 @@ __global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_bwd_kernel(c
         for (int i = 0; i < C; ++i) {
             g[i].get(v[i]);
             if (!a.x_codes) x[i].get(h[i]);
+            if (!kHold) columns(a.weight, 1.0f, L::col(i), a.W, w[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 h[i][e] = (h[i][e] - mean) * rstd;  // (values past the row's end meet gradients of zero)
-                dw[i][e] = __builtin_fmaf(v[i][e], h[i][e], dw[i][e]);
-                db[i][e] += v[i][e];
+                if (kHold) {
+                    dw[i][e] = __builtin_fmaf(v[i][e], h[i][e], dw[i][e]);
+                    db[i][e] += v[i][e];
+                }
                 v[i][e] *= w[i][e];
                 s += v[i][e];
                 sh = __builtin_fmaf(v[i][e], h[i][e], sh);
@@ -171,7 +181,7 @@ __global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_bwd_kernel(c
             x[i].store(a.Y, (int64_t)row * a.W + L::col(i), a.W - L::col(i));
         }
     }
-    if (!a.part) return;
+    if (!kHold || !a.part) return;
     // the rows of a workgroup that worked side by side
     if constexpr (L::kRows > 1) {
         __shared__ float other[2][L::kRows - 1][R * 8];
@@ -207,6 +217,47 @@ __global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_bwd_kernel(c
             }
 }
 
+// Shares of dw and db of wide rows: 512 columns to a workgroup, every kSumParts-th set of four rows, one to a wavefront.
+constexpr int kSumParts = 32;
+template <int TYPE>
+__global__ __launch_bounds__(256) void layer_norm_sums_kernel(const NormArgs a)
+{
+    __shared__ float shares[2][4][512];
+    const int blocks = (a.W + 511) / 512, part = blockIdx.x / blocks, at = (threadIdx.x & 63) * 8, col = ((int)blockIdx.x - part * blocks) * 512 + at, wave = threadIdx.x >> 6;
+    float dw[8], db[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dw[e] = db[e] = 0.0f;
+#pragma unroll 4
+    for (int row = part * 4 + wave; row < a.T; row += kSumParts * 4) {
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        Eight<TYPE> g, x;
+        float v[8], h[8];
+        g.load(a.dY, row * a.dy_row + col, a.W - col);
+        if (a.x_codes) {
+            kept8(h, a.x_codes, a.x_scales, row, a.W, col);
+        } else {
+            x.load(a.X, row * a.x_row + col, a.W - col);
+            x.get(h);
+        }
+        g.get(v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            dw[e] = __builtin_fmaf(v[e], (h[e] - mean) * rstd, dw[e]);
+            db[e] += v[e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        shares[0][wave][at + e] = dw[e];
+        shares[1][wave][at + e] = db[e];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 1024; i += 256) {
+        const int which = i >> 9, c = i & 511, to = col - at + c;
+        if (to < a.W) a.part[((int64_t)part * 2 + which) * a.W + to] = shares[which][0][c] + shares[which][1][c] + shares[which][2][c] + shares[which][3][c];
+    }
+}
+
 // dw and db from the workgroups' shares: 64 columns to a workgroup, sixteen wavefronts on shares of their own
 __global__ __launch_bounds__(1024) void layer_norm_join_kernel(const NormArgs a, int parts)
 {
@@ -214,7 +265,7 @@ __global__ __launch_bounds__(1024) void layer_norm_join_kernel(const NormArgs a,
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane, all = 2 * a.W;
     float s = 0.0f;
     if (col < all) {
-#pragma unroll 8
+#pragma unroll 16
         for (int p = wave; p < parts; p += 16) s += a.part[(int64_t)p * all + col];
     }
     sums[wave][lane] = s;
@@ -250,6 +301,8 @@ void by_type(int type, const F &f)
 }
 inline int rows_of(int64_t W) { return W <= 1024 ? 4 : 1; }  // that a workgroup works on at once
 inline int bwd_groups(int64_t T, int64_t W) { return (int)std::min<int64_t>((T + rows_of(W) - 1) / rows_of(W), W <= 4096 ? 512 : 256); }
+
+inline int sum_parts(int64_t T, int64_t W) { return W <= kWide ? bwd_groups(T, W) : T > 0 ? kSumParts : 0; }
 
 bool shape_ok(int64_t T, int64_t W) { return T >= 0 && T <= kMostRows && W >= 1 && W <= QB_MAX_K; }
 
@@ -287,7 +340,7 @@ extern "C" qb_status qb_layer_norm_fwd(const void *X, int64_t x_row, int type, i
 
 extern "C" size_t qb_layer_norm_bwd_workspace_nbytes(int64_t T, int64_t W)
 {
-    return shape_ok(T, W) ? (size_t)bwd_groups(T, W) * 2 * (size_t)W * 4 : 0;
+    return shape_ok(T, W) ? (size_t)sum_parts(T, W) * 2 * (size_t)W * 4 : 0;
 }
 
 extern "C" qb_status qb_layer_norm_bwd(const qb_norm_grads *n, void *dX, float *dweight, float *dbias, void *workspace, void *stream)
@@ -320,6 +373,8 @@ extern "C" qb_status qb_layer_norm_bwd(const qb_norm_grads *n, void *dX, float *
                 layer_norm_bwd_kernel<decltype(t)::value, decltype(r)::value, decltype(c)::value><<<groups, Row<decltype(r)::value, decltype(c)::value>::kThreads, 0, st>>>(a);
             });
         });
-    if (sums) layer_norm_join_kernel<<<(2 * a.W + 63) / 64, 1024, 0, st>>>(a, groups);
+    if (sums && groups > 0 && a.W > kWide)
+        by_type(n->type, [&](auto t) { layer_norm_sums_kernel<decltype(t)::value><<<kSumParts * ((a.W + 511) / 512), 256, 0, st>>>(a); });
+    if (sums) layer_norm_join_kernel<<<(2 * a.W + 63) / 64, 1024, 0, st>>>(a, sum_parts(n->T, n->W));
     return launch_status();
 }

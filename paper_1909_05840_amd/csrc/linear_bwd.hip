@@ -27,7 +27,7 @@ struct GradArgs {
     int db_parts;                      // of dbias: the first launch's row blocks, or the parts of dW's tiles, which then add it up
 };
 
-constexpr int kRowsAtOnce = 8;   // of X, to a workgroup of the first launch
+constexpr int kAtOnce = 2;       // chunks of eight values of X to a thread of the first launch
 constexpr int kRowBlock = 128;   // rows of dY whose sum is one part of dbias
 
 template <typename T>
@@ -42,32 +42,28 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a)
 {
     typedef Eight<TypeOf<T>::value> E;
     if ((int)blockIdx.x < a.x_blocks) {
-        const int row0 = blockIdx.x * kRowsAtOnce, rows = min(kRowsAtOnce, a.T - row0), chunks = a.K / 8;
-        constexpr int kAtOnce = 4;
-        for (int c0 = threadIdx.x; c0 < rows * chunks; c0 += 256 * kAtOnce) {
-            float v[kAtOnce][8];
-            int64_t at[kAtOnce];
+        const int64_t chunks = (int64_t)a.T * (a.K / 8);
+        int64_t at[kAtOnce];
+        float v[kAtOnce][8];
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) {
-                const int c = min(c0 + 256 * u, rows * chunks - 1), r = c / chunks, col = (c - r * chunks) * 8;  // (past the end: the last chunk again)
-                at[u] = (int64_t)(row0 + r) * a.K + col;
-                if (a.x_codes) {
-                    kept8(v[u], a.x_codes, a.x_scales, row0 + r, a.K, col);
-                } else if (a.pre_codes) {
-                    kept8(v[u], a.pre_codes, a.pre_scales, row0 + r, a.K, col);
-                } else {
-                    E e;
-                    e.load(a.pre, at[u], 8);
-                    e.get(v[u]);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) {
-                if (!a.x_codes) activate(a.act, v[u]);
+        for (int u = 0; u < kAtOnce; ++u) {
+            at[u] = min(((int64_t)blockIdx.x * kAtOnce + u) * 256 + threadIdx.x, chunks - 1);  // (past the end: the last chunk again)
+            if (a.x_codes) {
+                kept8(v[u], a.x_codes, a.x_scales, at[u]);
+            } else if (a.pre_codes) {
+                kept8(v[u], a.pre_codes, a.pre_scales, at[u]);
+            } else {
                 E e;
-                e.set(v[u]);
-                e.store(a.Xs, at[u], 8);
+                e.load(a.pre, at[u] * 8, 8);
+                e.get(v[u]);
             }
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            if (!a.x_codes) activate(a.act, v[u]);
+            E e;
+            e.set(v[u]);
+            e.store(a.Xs, at[u] * 8, 8);
         }
         return;
     }
@@ -276,11 +272,11 @@ struct Plan {
     int size, x_tiles, w_tiles, x_parts, w_parts;
 };
 // Which tiles, and into how many parts their contractions are cut: the shortest time by a model in microseconds.  A CU's operands come at `rate` KB/us (more
-// small tiles are under way at once), a lone workgroup takes `step` for a step; a launch and a tile's ends 4; parts cost the launch that adds them up, 3, and their
+// small tiles are under way at once, `room` workgroups in all), a lone workgroup takes `step` for a step; a launch and a tile's ends 4; parts cost the launch that adds them up, 3, and their
 // bytes, twice, at 8 TB/s.  Measured and modelled: 390 x 2304 by 768, small tiles, dX in 1, 2, 3, 4 parts 18.2, 15.7, 14.4, 14.5 us (18.4, 14.6, 12.7, 13); 4000 x 1024
 // by 1024, dW in 4 parts, small 33.0, middle 29.9 (35, 30); 2000 x 1024 by 1024 small, dW in 1, 2 parts, 25, 21.5.
 template <typename S>
-void try_tiles(Plan &best, double &least, int size, double rate, double step, bool dx, bool dw, int64_t T, int64_t N, int64_t K)
+void try_tiles(Plan &best, double &least, int size, int room, double rate, double step, bool dx, bool dw, int64_t T, int64_t N, int64_t K)
 {
     const int64_t kt = (K + S::BM - 1) / S::BM, x_tiles = dx ? kt * ((T + S::BN - 1) / S::BN) : 0, w_tiles = dw ? kt * ((N + S::BN - 1) / S::BN) : 0;
     const int64_t x_steps = (N + 63) / 64, w_steps = (T + 63) / 64;
@@ -291,7 +287,7 @@ void try_tiles(Plan &best, double &least, int size, double rate, double step, bo
             const int64_t tasks = x_tiles * x + w_tiles * w;
             const double chain = std::max(dx ? (x_steps + x - 1) / x : int64_t(0), dw ? (w_steps + w - 1) / w : int64_t(0)) * step;
             double cost = 4.0 + std::max(chain, kb / (rate * std::min<int64_t>(tasks, 256)));
-            if (tasks > 256) cost += 0.5 * chain;  // (the last round is not full)
+            if (tasks > room) cost += 0.5 * chain;  // (the last round is not full)
             if (x > 1 || w > 1) cost += 3.0 + ((x > 1 ? x * T * K : 0) + (w > 1 ? w * N * K : 0)) * 8e-6 / 8.0;
             if (cost < least) {
                 least = cost;
@@ -305,9 +301,9 @@ Plan plan_of(const qb_linear_grads &l)
     Plan p = {0, 0, 0, 1, 1};
     if (!dx && !dw) return p;
     double least = 1e300;
-    try_tiles<Large>(p, least, 2, 42.0, 1.6, dx, dw, l.T, l.N, l.K);
-    try_tiles<Middle>(p, least, 1, 53.0, 0.6, dx, dw, l.T, l.N, l.K);
-    try_tiles<Small>(p, least, 0, 65.0, 0.4, dx, dw, l.T, l.N, l.K);
+    try_tiles<Large>(p, least, 2, 256, 42.0, 1.6, dx, dw, l.T, l.N, l.K);
+    try_tiles<Middle>(p, least, 1, 512, 53.0, 0.6, dx, dw, l.T, l.N, l.K);
+    try_tiles<Small>(p, least, 0, 512, 65.0, 0.4, dx, dw, l.T, l.N, l.K);
     return p;
 }
 
@@ -331,7 +327,7 @@ size_t lay_out(const qb_linear_grads &l, GradArgs &a, Plan &p, uint8_t *base)
     a.t_blocks = (a.T + kRowBlock - 1) / kRowBlock;
     a.n_blocks = (a.N + 255) / 256;
     const bool stage = (l.dX || l.dW) && !readable(l), expand = l.dW && !l.X;
-    a.x_blocks = expand ? (a.T + kRowsAtOnce - 1) / kRowsAtOnce : 0;
+    a.x_blocks = expand ? (int)((l.T * (l.K / 8) + 256 * kAtOnce - 1) / (256 * kAtOnce)) : 0;
     a.db_parts = !l.dbias ? 0 : l.dW ? p.w_parts : a.t_blocks;
     if (!stage && (!l.dbias || l.dW)) a.t_blocks = 0;
     if (expand) a.Xs = reinterpret_cast<uint16_t *>(take((size_t)a.T * a.K * 2));
