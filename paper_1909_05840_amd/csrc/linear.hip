@@ -110,32 +110,36 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_kernel(const LinearA
     });
 }
 
-// Few tokens: sixteen neurons to a workgroup, whose wavefronts share the contraction, or a part of it; the weights go from memory straight into the matrix cores'
-// operands, each read once.  G groups of sixteen tokens.  A CU is given about 40 GB/s, whatever it asks for: with few neurons the contraction is cut into parts, so that
-// every CU takes its share of weights and tokens.
-template <typename T, int G, int kUnits>  // kUnits: of 64 values of the contraction, under way to a wavefront
+// Few tokens: 16 * M neurons to a workgroup, whose wavefronts share the contraction, or a part of it; the weights go from memory straight into the matrix cores'
+// operands, each read once.  G groups of sixteen tokens; kUnits of 64 values of the contraction under way to a wavefront (units that are not there cost as much as others:
+// 1 x 4096 by 1024 4.5 us with four, 3.4 with two).  A CU is given about 45 GB/s, whatever it asks for: with few neurons the contraction is cut into parts, so that every CU
+// takes its share of weights and tokens, and with many M makes the tokens' share small.
+template <typename T, int M, int G, int kUnits>
 __global__ __launch_bounds__(512) void linear_few_kernel(const LinearArgs a)
 {
-    __shared__ float sums[8][G * 16][17];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), blocks = (a.N + 15) / 16;
-    const int part = blockIdx.x / blocks, n0 = ((int)blockIdx.x - part * blocks) * 16, r = lane & 15, k0 = 8 * (lane >> 4);
+    __shared__ float sums[8][G * 16][M * 16 + 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), blocks = (a.N + 16 * M - 1) / (16 * M);
+    const int part = blockIdx.x / blocks, n0 = ((int)blockIdx.x - part * blocks) * (16 * M), r = lane & 15, k0 = 8 * (lane >> 4);
     const int units = a.K / 64, u0 = (int)((int64_t)units * part / a.parts), u1 = (int)((int64_t)units * (part + 1) / a.parts);
-    const uint16_t *const w = a.W + (int64_t)min(n0 + r, a.N - 1) * a.K + k0;
-    const uint16_t *x[G];
-    v4f z[G];
+    const uint16_t *w[M], *x[G];
+    v4f z[M][G];
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-        x[g] = a.X + min(16 * g + r, a.T - 1) * a.x_row + k0;
-        z[g] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int m = 0; m < M; ++m) {
+        w[m] = a.W + (int64_t)min(n0 + 16 * m + r, a.N - 1) * a.K + k0;
+#pragma unroll
+        for (int g = 0; g < G; ++g) z[m][g] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     }
+#pragma unroll
+    for (int g = 0; g < G; ++g) x[g] = a.X + min(16 * g + r, a.T - 1) * a.x_row + k0;
     for (int first = u0 + wave; first < u1; first += 8 * kUnits) {
-        v8s p[kUnits][2], q[kUnits][2][G];
+        v8s p[kUnits][2][M], q[kUnits][2][G];
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int k = min(first + 8 * u, u1 - 1) * 64;  // (past the end: the last unit again, not multiplied)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                p[u][h] = *reinterpret_cast<const v8s *>(w + k + 32 * h);
+#pragma unroll
+                for (int m = 0; m < M; ++m) p[u][h][m] = *reinterpret_cast<const v8s *>(w[m] + k + 32 * h);
 #pragma unroll
                 for (int g = 0; g < G; ++g) q[u][h][g] = *reinterpret_cast<const v8s *>(x[g] + k + 32 * h);
             }
@@ -145,7 +149,8 @@ __global__ __launch_bounds__(512) void linear_few_kernel(const LinearArgs a)
         for (int u = 0; u < kUnits; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                asm volatile("" : "+v"(p[u][h]));
+#pragma unroll
+                for (int m = 0; m < M; ++m) asm volatile("" : "+v"(p[u][h][m]));
 #pragma unroll
                 for (int g = 0; g < G; ++g) asm volatile("" : "+v"(q[u][h][g]));
             }
@@ -155,21 +160,25 @@ __global__ __launch_bounds__(512) void linear_few_kernel(const LinearArgs a)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int g = 0; g < G; ++g) z[g] = T::mma16(p[u][h], q[u][h][g], z[g]);
+                    for (int m = 0; m < M; ++m)
+#pragma unroll
+                        for (int g = 0; g < G; ++g) z[m][g] = T::mma16(p[u][h][m], q[u][h][g], z[m][g]);
             }
     }
     // a lane's results: token lane % 16, neurons 4 * (lane / 16) ..
 #pragma unroll
-    for (int g = 0; g < G; ++g)
+    for (int m = 0; m < M; ++m)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sums[wave][16 * g + r][k0 / 2 + e] = z[g][e];
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[wave][16 * g + r][16 * m + k0 / 2 + e] = z[m][g][e];
     __syncthreads();
-    for (int i = threadIdx.x; i < G * 256; i += 512) {
-        const int row = i >> 4, n = n0 + (i & 15);
+    for (int i = threadIdx.x; i < M * G * 256; i += 512) {
+        const int row = i / (16 * M), c = i % (16 * M), n = n0 + c;
         if (row >= a.T || n >= a.N) continue;
         float v[1] = {a.bias && !a.part ? a.bias[n] : 0.0f};
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[0] += sums[k][row][i & 15];
+        for (int k = 0; k < 8; ++k) v[0] += sums[k][row][c];
         if (a.part) {
             a.part[((int64_t)part * a.T + row) * a.Np + n] = v[0];
             continue;
@@ -214,29 +223,32 @@ typedef Tile<2, 2, 2, 2, 2> Middle;    // 128 x 128
 typedef Tile<1, 4, 2, 1, 3> Small;     // 64 x 128
 typedef Tile<1, 2, 2, 1, 4, 2> Least;  // 64 x 64
 struct Plan {
-    int size, parts;  // -1 few tokens, 0 least .. 4 large
+    int size, parts;  // 0 least .. 4 large; few tokens: -M
 };
 template <typename S>
 int64_t tiles_of(int64_t T, int64_t N) { return ((T + S::BN - 1) / S::BN) * ((N + S::BM - 1) / S::BM); }
-// Of few tokens: the largest share of a CU, at 40 KB a microsecond, and 3 us for a second launch.
-int few_parts(const qb_linear &l)
+// Of few tokens: the largest share of a CU, at 45 KB a microsecond, and what a second launch and the parts' bytes cost (3 us, twice at 8 TB/s).
+Plan few_plan(const qb_linear &l)
 {
-    const int64_t blocks = (l.N + 15) / 16, rows = 16 + (l.T <= 16 ? std::min<int64_t>(l.T, 16) : l.T);
-    int best = 1;
-    double least = 0;
-    for (const int p : {1, 2, 4, 8}) {
-        if (p > l.K / 128) break;
-        const double cost = (double)((blocks * p + 255) / 256) * (double)(rows * l.K * 2 / p) / 40e3 + (p > 1 || l.codes ? 3.0 : 0.0);
-        if (p == 1 || cost < least) {
-            least = cost;
-            best = p;
+    Plan best = {-1, 1};
+    double least = 1e300;
+    for (const int m : {1, 2}) {
+        for (const int p : {1, 2, 4, 8}) {
+            if (p > 1 && p > l.K / 128) break;
+            if (m > 1 && l.K / p < 1024) break;  // (two units for each wavefront)
+            const int64_t groups = (l.N + 16 * m - 1) / (16 * m) * p;
+            const double cost = (double)((groups + 255) / 256) * (double)((16 * m + l.T) * l.K * 2 / p) / 45e3 + (p > 1 || l.codes ? 3.0 + p * l.T * l.N * 1e-6 : 0.0);
+            if (cost < 0.9 * least) {  // (64 x 4096 by 4096: one and two of sixteen neurons 21.5, 18.3 us; 1 x 16384 by 4096 25.5, 27.6)
+                least = cost;
+                best = {-m, p};
+            }
         }
     }
     return best;
 }
 Plan plan_of(const qb_linear &l)
 {
-    if (l.T <= 64) return {-1, few_parts(l)};
+    if (l.T <= 64) return few_plan(l);
     return {tiles_of<Large>(l.T, l.N) >= 192 ? 4 : tiles_of<Broad>(l.T, l.N) >= 224 ? 3 : tiles_of<Small>(l.T, l.N) > 384 ? 2 : tiles_of<Least>(l.T, l.N) > 256 ? 1 : 0, 1};
 }
 
@@ -258,12 +270,14 @@ template <typename T>
 qb_status launch(const LinearArgs &a, int size, hipStream_t st)
 {
     if (size < 0) {
-        const int groups = (a.N + 15) / 16 * a.parts, units = (a.K / 64 + 8 * a.parts - 1) / (8 * a.parts);  // (of a wavefront)
+        const int groups = (a.N + 16 * -size - 1) / (16 * -size) * a.parts, units = (a.K / 64 + 8 * a.parts - 1) / (8 * a.parts);  // (of a wavefront)
         const auto go = [&](auto g) {
             constexpr int G = decltype(g)::value;
-            if (units == 1) linear_few_kernel<T, G, 1><<<groups, 512, 0, st>>>(a);
-            else if (units == 2 || G == 4) linear_few_kernel<T, G, 2><<<groups, 512, 0, st>>>(a);
-            else linear_few_kernel<T, G, 4><<<groups, 512, 0, st>>>(a);
+            if (size == -2) return linear_few_kernel<T, 2, G, 2><<<groups, 512, 0, st>>>(a);
+            if (units == 1) return linear_few_kernel<T, 1, G, 1><<<groups, 512, 0, st>>>(a);
+            if constexpr (G < 4)
+                if (units > 2) return linear_few_kernel<T, 1, G, 4><<<groups, 512, 0, st>>>(a);
+            linear_few_kernel<T, 1, G, 2><<<groups, 512, 0, st>>>(a);
         };
         if (a.T <= 16) go(std::integral_constant<int, 1>{});
         else if (a.T <= 32) go(std::integral_constant<int, 2>{});

@@ -50,7 +50,7 @@ def check_forward(qb, T, N, K, t, act=None, bias=True, residual=False, keep=None
 
 
 SIZES = [(1, 1, 64), (1, 4096, 1024), (2, 3, 128), (3, 65, 64), (7, 768, 768), (16, 130, 4096), (17, 1000, 192), (31, 64, 64), (32, 96, 32768), (33, 33, 128), (64, 1024, 4096),
-         (129, 127, 64), (390, 768, 768), (390, 2304, 768), (257, 511, 1024), (1500, 1100, 128), (2000, 2100, 64), (4100, 3001, 64), (3, 70000, 64), (12001, 1024, 64)]
+         (129, 127, 64), (390, 768, 768), (390, 2304, 768), (257, 511, 1024), (1500, 1100, 128), (2000, 2100, 64), (4100, 3001, 64), (3, 70000, 64), (12001, 1024, 64), (40, 4100, 4096), (64, 4097, 2048), (8190, 1000, 128)]
 
 
 @pytest.mark.parametrize("t", TYPES)
