@@ -2,8 +2,8 @@
 
 Every linear layer's master weights are quantized group by group at each step and its inputs to 8 bits
 (straight-through backward, Sec. 3.1 of arXiv 1909.05840); attention runs over packed sequences of different lengths,
-with dropout of its weights; dropout and the residual addition are one call; the loss goes from hidden states to
-the vocabulary without the logits.  Afterwards the model continues prompts word by word over a cache of keys and values.
+with dropout of its weights; dropout and the residual addition are one call, each followed by a layer norm whose input is kept in 8 bits for the
+backward; the loss goes from hidden states to the vocabulary without the logits.  Afterwards the model continues prompts word by word over a cache of keys and values.
 
 The text is synthetic: each sequence counts up by one, modulo `count`, from a random start.
 
@@ -70,6 +70,20 @@ class DropoutAdd(torch.autograd.Function):
         return qb.qb_dropout_bwd(dY.contiguous(), ctx.p, *ctx.saved_tensors), dY, None, None
 
 
+class LayerNorm(torch.autograd.Function):
+    """Without weight and bias; the backward reads its input from 8 bits."""
+    @staticmethod
+    def forward(ctx, X):
+        Y, mean, rstd = qb.qb_layer_norm_fwd(X)
+        ctx.save_for_backward(*qb.qb_checkpoint_act(X), mean, rstd)
+        return Y
+
+    @staticmethod
+    def backward(ctx, dY):
+        codes, scales, mean, rstd = ctx.saved_tensors
+        return qb.qb_layer_norm_bwd(dY.contiguous(), (codes, scales), None, mean, rstd, sums=False)[0]
+
+
 class VocabLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, W, bias, targets):
@@ -95,7 +109,7 @@ class Model(torch.nn.Module):
                                                for i in range(layers) for name, shape in shapes.items()})
 
     def norm(self, x):
-        return F.layer_norm(x, x.shape[-1:])
+        return LayerNorm.apply(x)
 
     def hidden(self, words, places, attend, p=0.0, seeds=None):
         """attend(layer, qkv) -> what the attention gives; seeds: two a layer for the dropouts here."""

@@ -367,14 +367,14 @@ extern "C" qb_status qb_layer_norm_bwd(const qb_norm_grads *n, void *dX, float *
     a.dweight = dweight; a.dbias = dbias;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int groups = bwd_groups(n->T, n->W);
+    if (sums && groups > 0 && a.W > kWide)  // (before dX, which may take dY's place)
+        by_type(n->type, [&](auto t) { layer_norm_sums_kernel<decltype(t)::value><<<kSumParts * ((a.W + 511) / 512), 256, 0, st>>>(a); });
     if (groups > 0)
         by_type(n->type, [&](auto t) {
             by_width(n->W, [&](auto r, auto c) {
                 layer_norm_bwd_kernel<decltype(t)::value, decltype(r)::value, decltype(c)::value><<<groups, Row<decltype(r)::value, decltype(c)::value>::kThreads, 0, st>>>(a);
             });
         });
-    if (sums && groups > 0 && a.W > kWide)
-        by_type(n->type, [&](auto t) { layer_norm_sums_kernel<decltype(t)::value><<<kSumParts * ((a.W + 511) / 512), 256, 0, st>>>(a); });
     if (sums) layer_norm_join_kernel<<<(2 * a.W + 63) / 64, 1024, 0, st>>>(a, sum_parts(n->T, n->W));
     return launch_status();
 }

@@ -50,7 +50,7 @@ def check_forward(qb, T, N, K, t, act=None, bias=True, residual=False, keep=None
 
 
 SIZES = [(1, 1, 64), (1, 4096, 1024), (2, 3, 128), (3, 65, 64), (7, 768, 768), (16, 130, 4096), (17, 1000, 192), (31, 64, 64), (32, 96, 32768), (33, 33, 128), (64, 1024, 4096),
-         (129, 127, 64), (390, 768, 768), (390, 2304, 768), (257, 511, 1024), (1500, 1100, 128), (2000, 2100, 64), (4100, 3001, 64), (3, 70000, 64), (12001, 1024, 64), (40, 4100, 4096), (64, 4097, 2048), (8190, 1000, 128)]
+         (129, 127, 64), (390, 768, 768), (390, 2304, 768), (257, 511, 1024), (1500, 1100, 128), (2000, 2100, 64), (4100, 3001, 64), (3, 70000, 64), (12001, 1024, 64), (40, 4100, 4096), (64, 4097, 2048), (8190, 1000, 128), (301, 2, 128), (5000, 3, 64), (70, 100, 32768)]
 
 
 @pytest.mark.parametrize("t", TYPES)
@@ -137,6 +137,15 @@ def test_gradients_with_what_was_kept(qb, T, N, K, x, pre, act):
 @pytest.mark.parametrize("T,N,K", [(1, 8, 64), (70, 128, 128), (700, 333, 320), (2051, 2104, 704)])
 def test_gradients_of_rows_apart(qb, T, N, K, wide):
     check_backward(qb, T, N, K, torch.bfloat16, wide=wide)
+
+
+def test_the_same_row_for_every_token(qb):
+    """a gradient that was broadcast, tokens that were: no stride between rows"""
+    for T, N, K in ((40, 72, 64), (300, 200, 128), (2051, 2104, 704)):
+        W, b = (v.cuda() for v in weights(N, K, torch.bfloat16))
+        g, x = ref.draw(1, N, seed=1, t=torch.bfloat16).cuda().expand(T, N), ref.draw(1, K, seed=2, t=torch.bfloat16).cuda().expand(T, K)
+        assert torch.equal(qb.qb_linear_fwd(x, W, b), qb.qb_linear_fwd(x.contiguous(), W, b))
+        assert all(torch.equal(p, q) for p, q in zip(qb.qb_linear_bwd(g, x, W), qb.qb_linear_bwd(g.contiguous(), x.contiguous(), W)))
 
 
 @pytest.mark.parametrize("need", [(True, False, False), (False, True, False), (False, False, True), (True, True, False), (False, True, True), (False, False, False)])
