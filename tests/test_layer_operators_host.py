@@ -113,7 +113,9 @@ def test_linear_backward_refuses(lib, changed, status):
 
 
 def test_linear_backward_workspace(lib):
-    assert lib.qb_linear_bwd(grads(), None, None) == WORKSPACE and lib.qb_linear_bwd(grads(), 0x1080, None) == WORKSPACE
+    kept = dict(X=None, x_codes=P, x_scales=P)  # (X in 16 bits has to lie somewhere)
+    assert lib.qb_linear_bwd_workspace_nbytes(grads(**kept)) >= 390 * 768 * 2
+    assert lib.qb_linear_bwd(grads(**kept), None, None) == WORKSPACE and lib.qb_linear_bwd(grads(**kept), 0x1080, None) == WORKSPACE
     for T, N, K in ((1, 1, 64), (390, 768, 768), (16384, 4096, 1024), (16384, 2, 1024), (1 << 24, 1, 64)):
         for more in (dict(), dict(X=None, x_codes=P, x_scales=P), dict(dX=None), dict(dW=None, X=None), dict(dX=None, dW=None), dict(dy_row=N + 1)):
             n = lib.qb_linear_bwd_workspace_nbytes(grads(T=T, N=N, K=K, dy_row=more.pop("dy_row", N), x_row=K, **more))
