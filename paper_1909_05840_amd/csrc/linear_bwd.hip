@@ -264,36 +264,43 @@ __global__ __launch_bounds__(256) void linear_zero_kernel(uint16_t *dW, float *d
     }
 }
 
-typedef Tile<2, 4, 4, 2, 2> Large;   // 256 x 256
-typedef Tile<2, 2, 2, 2, 2> Middle;  // 128 x 128
-typedef Tile<1, 4, 2, 1, 3> Small;   // 64 x 128
+typedef Tile<2, 4, 4, 2, 2> Large;     // 256 x 256
+typedef Tile<2, 2, 2, 2, 2> Middle;    // 128 x 128
+typedef Tile<1, 4, 2, 1, 3> Small;     // 64 x 128
+typedef Tile<1, 2, 2, 1, 3, 2> Least;  // 64 x 64
 
 struct Plan {
-    int size, x_tiles, w_tiles, x_parts, w_parts;
+    int size, x_tiles, w_tiles, x_parts, w_parts;  // 0 least .. 3 large
 };
-// Which tiles, and into how many parts their contractions are cut: the shortest time by a model in microseconds.  A CU's operands come at `rate` KB/us (more
-// small tiles are under way at once, `room` workgroups in all), a lone workgroup takes `step` for a step; a launch and a tile's ends 4; parts cost the launch that adds them up, 3, and their
-// bytes, twice, at 8 TB/s.  Measured and modelled: 390 x 2304 by 768, small tiles, dX in 1, 2, 3, 4 parts 18.2, 15.7, 14.4, 14.5 us (18.4, 14.6, 12.7, 13); 4000 x 1024
-// by 1024, dW in 4 parts, small 33.0, middle 29.9 (35, 30); 2000 x 1024 by 1024 small, dW in 1, 2 parts, 25, 21.5.
+// What a size of tiles costs, in microseconds: a launch with a tile's ends; a step of a lone workgroup; the KB that a CU is given in one, by all the workgroups that it has
+struct Cost {
+    int size, room;  // workgroups at work at once
+    double ends, step, rate;
+};
+// Which tiles, and into how many parts their contractions are cut: the shortest time by that.  Parts cost the launch that adds them up, 3 us, and their bytes, twice, at 8 TB/s.
+// Measured (modelled), us: 390 x 768 by 768 least 7.4 (7), small 8.3 (10), middle 10.9; 1000 x 1024 by 1024 12.0 (12), 12.9 (13), 17.2; 390 x 2304 by 768 least 14.9 (13),
+// small with dX in 3 parts 14.5 (16), middle in 6 15.7 (17); 4000 x 1024 by 1024, dW in 4 parts, small 33, middle 29.9.
 template <typename S>
-void try_tiles(Plan &best, double &least, int size, int room, double rate, double step, bool dx, bool dw, int64_t T, int64_t N, int64_t K)
+void try_tiles(Plan &best, double &least, const Cost &c, bool dx, bool dw, int64_t T, int64_t N, int64_t K)
 {
     const int64_t kt = (K + S::BM - 1) / S::BM, x_tiles = dx ? kt * ((T + S::BN - 1) / S::BN) : 0, w_tiles = dw ? kt * ((N + S::BN - 1) / S::BN) : 0;
-    const int64_t x_steps = (N + 63) / 64, w_steps = (T + 63) / 64;
-    const double kb = (x_tiles * x_steps + w_tiles * w_steps) * ((S::BM + S::BN) / 8.0);
-    for (const int x : {1, 2, 3, 4, 6, 8})
-        for (const int w : {1, 2, 3, 4, 6, 8, 12, 16}) {
-            if ((x > 1 && (!dx || x > x_steps / 2)) || (w > 1 && (!dw || w > w_steps / 2))) continue;
-            const int64_t tasks = x_tiles * x + w_tiles * w;
-            const double chain = std::max(dx ? (x_steps + x - 1) / x : int64_t(0), dw ? (w_steps + w - 1) / w : int64_t(0)) * step;
-            double cost = 4.0 + std::max(chain, kb / (rate * std::min<int64_t>(tasks, 256)));
-            if (tasks > room) cost += 0.5 * chain;  // (the last round is not full)
-            if (x > 1 || w > 1) cost += 3.0 + ((x > 1 ? x * T * K : 0) + (w > 1 ? w * N * K : 0)) * 8e-6 / 8.0;
-            if (cost < least) {
-                least = cost;
-                best = {size, (int)x_tiles, (int)w_tiles, x, w};
-            }
+    const int x_steps = dx ? (int)((N + 63) / 64) : 0, w_steps = dw ? (int)((T + 63) / 64) : 0, longest = std::max(x_steps, w_steps);
+    const double kb = ((double)x_tiles * x_steps + (double)w_tiles * w_steps) * ((S::BM + S::BN) / 8.0);
+    if (c.ends + kb / (256 * c.rate) >= least) return;
+    for (const int cut : {1, 2, 3, 4, 6, 8, 12, 16}) {  // of the longer contraction; the other one is cut to the same length
+        if (cut > 1 && cut > longest / 2) break;
+        const int length = (longest + cut - 1) / cut, x = std::max(1, (x_steps + length - 1) / length), w = std::max(1, (w_steps + length - 1) / length);
+        const double tasks = (double)(x_tiles * x + w_tiles * w), chain = length * c.step;
+        const bool rounds = tasks > 1.1 * c.room;  // (the last of several is not full; of one, a CU has a whole number of workgroups)
+        const double share = rounds ? kb / 256 : kb / tasks * (1 + (int)(tasks * (0.9 / 256)));
+        double cost = c.ends + std::max(chain, share / c.rate) + (rounds ? 0.25 * chain : 0.0);
+        if (x > 1 || w > 1) cost += 3.0 + ((x > 1 ? (double)x * T : 0.0) + (w > 1 ? (double)w * N : 0.0)) * K * 1e-6;
+        if (cost < least) {
+            least = cost;
+            best = {c.size, (int)x_tiles, (int)w_tiles, x, w};
         }
+        if (rounds && chain * c.rate < 0.5 * share) break;  // (many short tiles: cutting them gains nothing)
+    }
 }
 Plan plan_of(const qb_linear_grads &l)
 {
@@ -301,9 +308,10 @@ Plan plan_of(const qb_linear_grads &l)
     Plan p = {0, 0, 0, 1, 1};
     if (!dx && !dw) return p;
     double least = 1e300;
-    try_tiles<Large>(p, least, 2, 256, 42.0, 1.6, dx, dw, l.T, l.N, l.K);
-    try_tiles<Middle>(p, least, 1, 512, 53.0, 0.6, dx, dw, l.T, l.N, l.K);
-    try_tiles<Small>(p, least, 0, 512, 65.0, 0.4, dx, dw, l.T, l.N, l.K);
+    try_tiles<Least>(p, least, {0, 512, 4.0, 0.25, 63.0}, dx, dw, l.T, l.N, l.K);
+    try_tiles<Large>(p, least, {3, 256, 6.0, 1.6, 42.0}, dx, dw, l.T, l.N, l.K);
+    try_tiles<Middle>(p, least, {2, 512, 6.0, 0.6, 53.0}, dx, dw, l.T, l.N, l.K);
+    try_tiles<Small>(p, least, {1, 512, 5.5, 0.4, 65.0}, dx, dw, l.T, l.N, l.K);
     return p;
 }
 
@@ -345,9 +353,10 @@ qb_status launch(const GradArgs &a, int size, hipStream_t st)
     if (first > 0) linear_prepare_kernel<T><<<(int)first, 256, 0, st>>>(a);
     const int groups = a.x_tiles * a.x_parts + a.w_tiles * a.w_parts;
     if (groups > 0) {
-        if (size == 2) linear_grads_kernel<T, Large><<<groups, 64 * Large::kWaves, 0, st>>>(a);
-        else if (size == 1) linear_grads_kernel<T, Middle><<<groups, 64 * Middle::kWaves, 0, st>>>(a);
-        else linear_grads_kernel<T, Small><<<groups, 64 * Small::kWaves, 0, st>>>(a);
+        if (size == 3) linear_grads_kernel<T, Large><<<groups, 64 * Large::kWaves, 0, st>>>(a);
+        else if (size == 2) linear_grads_kernel<T, Middle><<<groups, 64 * Middle::kWaves, 0, st>>>(a);
+        else if (size == 1) linear_grads_kernel<T, Small><<<groups, 64 * Small::kWaves, 0, st>>>(a);
+        else linear_grads_kernel<T, Least><<<groups, 64 * Least::kWaves, 0, st>>>(a);
     }
     const auto blocks = [&](int64_t rows) { return (int)((rows * (a.K / 4) + 255) / 256); };
     const int x_blocks = a.dXp ? blocks(a.T) : 0, w_blocks = a.dWp ? blocks(a.N) : 0, ends = x_blocks + w_blocks + (a.dbias && !(a.dW && a.db_parts == 1) ? (a.N + 63) / 64 : 0);
