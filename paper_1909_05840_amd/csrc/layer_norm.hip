@@ -27,14 +27,30 @@ struct NormArgs {
     float *dweight, *dbias;
 };
 
+// the sum over R neighbouring lanes, in each of them
+template <int R>
+__device__ __forceinline__ float lanes_add(float x)
+{
+    const auto add = [&](auto ctrl) { x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(ctrl)::value, 0xF, 0xF, true)); };
+    add(std::integral_constant<int, 0xB1>());   // lane ^ 1
+    add(std::integral_constant<int, 0x4E>());   // lane ^ 2
+    add(std::integral_constant<int, 0x141>());  // the other four of eight
+    if constexpr (R >= 16) add(std::integral_constant<int, 0x140>());  // the other eight of sixteen
+    if constexpr (R >= 32) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    return x;
+}
 // R threads to a row, C chunks of eight values to a thread
 template <int R, int C>
 struct Row {
-    static constexpr int kThreads = R > 256 ? R : 256, kRows = kThreads / R, kWaves = R / 64;
+    static constexpr int kThreads = R > 256 ? R : 256, kRows = kThreads / R, kWaves = (R + 63) / 64;
     static __device__ __forceinline__ int col(int i) { return (i * R + (int)(threadIdx.x % R)) * 8; }
     // the sums of two values over a row's threads
     static __device__ __forceinline__ v2f sum(float a, float b, v2f *shared)
     {
+        if constexpr (R < 64) return v2f{lanes_add<R>(a), lanes_add<R>(b)};
         a = wave_add(a);
         b = wave_add(b);
         if constexpr (R > 64) {
@@ -80,7 +96,7 @@ __global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_kernel(const
         if (kHold) weights(i);
     for (int row0 = blockIdx.x * L::kRows; row0 < a.T; row0 += gridDim.x * L::kRows) {
         const int row = row0 + (int)(threadIdx.x / R);
-        if (R == 64 && row >= a.T) break;
+        if (R <= 64 && row >= a.T) break;
         Eight<TYPE> x[C];
         float v[C][8], s = 0.0f;
 #pragma unroll
@@ -140,7 +156,7 @@ __global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_bwd_kernel(c
     }
     for (int row0 = blockIdx.x * L::kRows; row0 < a.T; row0 += gridDim.x * L::kRows) {
         const int row = row0 + (int)(threadIdx.x / R);
-        if (R == 64 && row >= a.T) break;
+        if (R <= 64 && row >= a.T) break;
         Eight<TYPE> x[C], g[C], r[C];
         float h[C][8], v[C][8], s = 0.0f, sh = 0.0f;
         const float mean = a.mean[row], rstd = a.rstd[row];
@@ -182,39 +198,37 @@ __global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_bwd_kernel(c
         }
     }
     if (!kHold || !a.part) return;
-    // the rows of a workgroup that worked side by side
-    if constexpr (L::kRows > 1) {
-        __shared__ float other[2][L::kRows - 1][R * 8];
+    float *const to = a.part + (int64_t)blockIdx.x * 2 * a.W;
+    if constexpr (L::kRows > 1) {  // the rows of a workgroup that worked side by side
+        __shared__ float shares[2][L::kRows][R * 8];
+        const int at = (int)(threadIdx.x % R), team = (int)(threadIdx.x / R);
 #pragma unroll
         for (int i = 0; i < C; ++i) {
-            const int at = (int)(threadIdx.x % R), team = (int)(threadIdx.x / R);
             __syncthreads();
-            if (team > 0)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    other[0][team - 1][e * R + at] = dw[i][e];
-                    other[1][team - 1][e * R + at] = db[i][e];
-                }
-            __syncthreads();
-            if (team == 0)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    for (int t = 0; t < L::kRows - 1; ++t) {
-                        dw[i][e] += other[0][t][e * R + at];
-                        db[i][e] += other[1][t][e * R + at];
-                    }
-        }
-    }
-    if (threadIdx.x >= R) return;
-    float *const to = a.part + (int64_t)blockIdx.x * 2 * a.W;
-#pragma unroll
-    for (int i = 0; i < C; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (L::col(i) + e < a.W) {
-                to[L::col(i) + e] = dw[i][e];
-                to[a.W + L::col(i) + e] = db[i][e];
+            for (int e = 0; e < 8; ++e) {
+                shares[0][team][e * R + at] = dw[i][e];
+                shares[1][team][e * R + at] = db[i][e];
             }
+            __syncthreads();
+            for (int k = threadIdx.x; k < 2 * R * 8; k += L::kThreads) {
+                const int which = k / (R * 8), c = k % (R * 8), col = (i * R + c % R) * 8 + c / R;
+                float s = 0.0f;
+#pragma unroll
+                for (int t = 0; t < L::kRows; ++t) s += shares[which][t][c];
+                if (col < a.W) to[which * a.W + col] = s;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (L::col(i) + e < a.W) {
+                    to[L::col(i) + e] = dw[i][e];
+                    to[a.W + L::col(i) + e] = db[i][e];
+                }
+    }
 }
 
 // Shares of dw and db of wide rows: 512 columns to a workgroup, every kSumParts-th set of four rows, one to a wavefront.
@@ -284,7 +298,10 @@ __global__ __launch_bounds__(1024) void layer_norm_join_kernel(const NormArgs a,
 template <typename F>
 void by_width(int64_t W, const F &f)
 {
-    if (W <= 512) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+    if (W <= 64) f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
+    else if (W <= 128) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+    else if (W <= 256) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
+    else if (W <= 512) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
     else if (W <= 1024) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
     else if (W <= 2048) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
     else if (W <= 4096) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
@@ -299,7 +316,7 @@ void by_type(int type, const F &f)
     else if (type == QB_TYPE_FP16) f(std::integral_constant<int, QB_TYPE_FP16>{});
     else f(std::integral_constant<int, QB_TYPE_FP32>{});
 }
-inline int rows_of(int64_t W) { return W <= 1024 ? 4 : 1; }  // that a workgroup works on at once
+inline int rows_of(int64_t W) { return W <= 64 ? 32 : W <= 128 ? 16 : W <= 256 ? 8 : W <= 1024 ? 4 : 1; }  // that a workgroup works on at once
 inline int bwd_groups(int64_t T, int64_t W) { return (int)std::min<int64_t>((T + rows_of(W) - 1) / rows_of(W), W <= 4096 ? 512 : 256); }
 
 inline int sum_parts(int64_t T, int64_t W) { return W <= kWide ? bwd_groups(T, W) : T > 0 ? kSumParts : 0; }

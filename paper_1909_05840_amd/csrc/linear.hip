@@ -19,10 +19,11 @@ struct LinearArgs {
     float *scales;
     float *part;  // [parts][T][Np], or null
     int parts, Np;
+    bool stream;  // results are not kept in the L2
 };
 
 // what becomes of two blocks of sums, 64 columns from `col` on of 32 rows from `row0` on; `room`: LDS of the wavefront's own
-template <typename T, bool STREAM>
+template <typename T>
 __device__ __forceinline__ void finish(const LinearArgs &a, int row0, int col, int lane, uint8_t *room, float (&z)[2][16])
 {
     typedef Block<T> B;
@@ -31,11 +32,11 @@ __device__ __forceinline__ void finish(const LinearArgs &a, int row0, int col, i
     const auto keep = [&]() {
         const Coder c(top_of(col, a.N, hf, z));
         if (inside && hf == 0) a.scales[(int64_t)row * ((a.N + kGroup - 1) / kGroup) + col / kGroup] = c.quick_scale();
-        store_code_rows<STREAM>(a.codes, row0, a.T, col, a.N, lane, room, c, z);
+        store_code_rows(a.codes, row0, a.T, col, a.N, lane, room, a.stream, c, z);
     };
     if (a.act != QB_ACT_NONE) {
         if (a.codes) keep();
-        if (a.pre) store_rows<T, STREAM>(a.pre, row0, a.T, col, a.N, lane, room, z);
+        if (a.pre) store_rows<T>(a.pre, row0, a.T, col, a.N, lane, room, a.stream, z);
         activate(a.act, z[0]);
         activate(a.act, z[1]);
     }
@@ -49,7 +50,7 @@ __device__ __forceinline__ void finish(const LinearArgs &a, int row0, int col, i
         }
     }
     if (a.act == QB_ACT_NONE && a.codes) keep();
-    store_rows<T, STREAM>(a.Y, row0, a.T, col, a.N, lane, room, z);
+    store_rows<T>(a.Y, row0, a.T, col, a.N, lane, room, a.stream, z);
 }
 
 // Tiles of neurons by tokens: a lane's results are neighbours of a row of Y.  (Workgroups that stay and take tile after tile, the next one's first steps and this one's
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_kernel(const LinearA
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) v[u][k] = z[i + u][j][k] + b[u][k];
-            finish<T, S::kWaves == 8>(a, t0 + (wn * S::TN + j) * 32, col, lane, lds + wave * kRowsRoom, v);
+            finish<T>(a, t0 + (wn * S::TN + j) * 32, col, lane, lds + wave * kRowsRoom, v);
         }
     });
 }
@@ -221,7 +222,7 @@ typedef Tile<2, 4, 4, 2, 2> Large;     // 256 x 256
 typedef Tile<2, 4, 2, 2, 3> Broad;     // 128 x 256
 typedef Tile<2, 2, 2, 2, 2> Middle;    // 128 x 128
 typedef Tile<1, 4, 2, 1, 3> Small;     // 64 x 128
-typedef Tile<1, 2, 2, 1, 4, 2> Least;  // 64 x 64
+typedef Tile<1, 2, 2, 1, 3, 2> Least;  // 64 x 64
 struct Plan {
     int size, parts;  // 0 least .. 4 large; few tokens: -M
 };
@@ -246,10 +247,30 @@ Plan few_plan(const qb_linear &l)
     }
     return best;
 }
+// Measured (modelled), us: 390 x 768 by 768 least 7 (7), small 8.6 (10); 1000 x 1024 by 1024 9.7 (8), 10.9 (12), middle 15.6 (16); 4000 x 1024 by 1024 small 20 (17), middle
+// 17.4 (16); 8190 x 1024 by 4096 broad 76 (73), large 100 (103), middle 82 (83).
+template <typename S>
+void try_size(Plan &best, double &least, const Cost &c, const qb_linear &l)
+{
+    const int64_t tiles = tiles_of<S>(l.T, l.N), steps = l.K / 64;
+    const double share = (double)((tiles + 255) / 256 * steps) * ((S::BM + S::BN) / 8.0);
+    const double cost = c.ends * (double)((tiles + c.room - 1) / c.room) + std::max(steps * c.step, share / c.rate);
+    if (cost < least) {
+        least = cost;
+        best = {c.size, 1};
+    }
+}
 Plan plan_of(const qb_linear &l)
 {
     if (l.T <= 64) return few_plan(l);
-    return {tiles_of<Large>(l.T, l.N) >= 192 ? 4 : tiles_of<Broad>(l.T, l.N) >= 224 ? 3 : tiles_of<Small>(l.T, l.N) > 384 ? 2 : tiles_of<Least>(l.T, l.N) > 256 ? 1 : 0, 1};
+    Plan p = {0, 1};
+    double least = 1e300;
+    try_size<Least>(p, least, {0, 512, 4.0, 0.25, 63.0}, l);
+    try_size<Small>(p, least, {1, 512, 5.5, 0.4, 65.0}, l);
+    try_size<Middle>(p, least, {2, 512, 6.0, 0.6, 53.0}, l);
+    try_size<Broad>(p, least, {3, 256, 6.0, 1.0, 46.0}, l);
+    try_size<Large>(p, least, {4, 256, 6.0, 1.6, 42.0}, l);
+    return p;
 }
 
 size_t lay_out(const qb_linear &l, LinearArgs &a)
@@ -324,5 +345,6 @@ extern "C" qb_status qb_linear_fwd(const qb_linear *l, void *workspace, void *st
     }
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int size = plan_of(*l).size;
+    a.stream = size >= 3 && l->N % 64 == 0;
     return l->type == QB_TYPE_BF16 ? launch<Bf16>(a, size, st) : launch<Fp16>(a, size, st);
 }

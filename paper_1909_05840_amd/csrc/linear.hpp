@@ -347,16 +347,16 @@ __device__ __forceinline__ uint32_t top_of(int col, int width, int hf, const flo
 }
 
 // The same 64 columns of 32 rows through LDS of the wavefront's own (kRowsRoom bytes), sixteen rows at a time, so that eight neighbouring lanes write 128 bytes of a
-// row, where a lane alone would write 16 of its own: rows that reach memory in pieces of 32 bytes cost 16384 x 4096 results X us of Y.
+// row, where a lane alone would write 16 of its own.  `stream`: what is written leaves the L2 first (only whole lines may: pieces of them would
+// go to memory one by one).  16384 x 4096 results of 1024, with GELU, 159 us; without `stream` 166, 32 bytes at a time 163.
 constexpr int kRowsRoom = 2048;
-template <bool STREAM>
-__device__ __forceinline__ void put16(void *p, int64_t byte, v4u v)
+__device__ __forceinline__ void put16(void *p, int64_t byte, v4u v, bool stream)
 {
-    if constexpr (STREAM) store16_stream(p, byte, v);
+    if (stream) store16_stream(p, byte, v);
     else store16(p, byte, v);
 }
-template <typename T, bool STREAM>
-__device__ __forceinline__ void store_rows(uint16_t *p, int row0, int rows, int col, int width, int lane, uint8_t *room, const float (&v)[2][16])
+template <typename T>
+__device__ __forceinline__ void store_rows(uint16_t *p, int row0, int rows, int col, int width, int lane, uint8_t *room, bool stream, const float (&v)[2][16])
 {
     const int l32 = lane & 31, hf = lane >> 5;
     v4u w[4];  // chunks of eight columns: 2 * i + hf
@@ -379,13 +379,12 @@ __device__ __forceinline__ void store_rows(uint16_t *p, int row0, int rows, int 
             const v4u x = *reinterpret_cast<const v4u *>(room + in * 128 + (((lane & 7) ^ (in & 7)) << 4));
             if (row >= rows) continue;
             const int64_t at = (int64_t)row * width;
-            if (c + 8 <= width) put16<STREAM>(p + at, 2 * c, x);
+            if (c + 8 <= width) put16(p + at, 2 * c, x, stream);
             else each<8>([&](auto e) { if (c + e < width) p[at + c + e] = (uint16_t)(x[e >> 1] >> (16 * (e & 1))); });
         }
     }
 }
-template <bool STREAM>
-__device__ __forceinline__ void store_code_rows(int8_t *p, int row0, int rows, int col, int width, int lane, uint8_t *room, const Coder &coder, const float (&v)[2][16])
+__device__ __forceinline__ void store_code_rows(int8_t *p, int row0, int rows, int col, int width, int lane, uint8_t *room, bool stream, const Coder &coder, const float (&v)[2][16])
 {
     const int l32 = lane & 31, hf = lane >> 5;
     v4u w[2];  // chunks of sixteen columns: 2 * u + hf
@@ -405,7 +404,7 @@ __device__ __forceinline__ void store_code_rows(int8_t *p, int row0, int rows, i
         const v4u x = *reinterpret_cast<const v4u *>(room + in * 64 + (((lane & 3) ^ (in >> 2 & 3)) << 4));
         if (row >= rows) continue;
         const int64_t at = (int64_t)row * width;
-        if (c + 16 <= width) put16<STREAM>(p + at, c, x);
+        if (c + 16 <= width) put16(p + at, c, x, stream);
         else each<16>([&](auto e) { if (c + e < width) p[at + c + e] = (int8_t)(x[e >> 2] >> (8 * (e & 3))); });
     }
 }
@@ -482,6 +481,12 @@ __device__ __forceinline__ void kept4(float (&v)[4], const int8_t *codes, const 
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = (float)(int8_t)(w >> (8 * e)) * scale;
 }
+
+// What a size of tiles costs, in microseconds: a launch with a tile's ends; a step of a lone workgroup; the KB that a CU is given in one, by all the workgroups that it has
+struct Cost {
+    int size, room;  // workgroups at work at once
+    double ends, step, rate;
+};
 
 constexpr int64_t kMostOutputs = 1 << 20;
 inline size_t round_up(size_t v) { return (v + 255) / 256 * 256; }

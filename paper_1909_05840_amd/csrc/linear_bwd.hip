@@ -23,11 +23,12 @@ struct GradArgs {
     float *db;             // [db_parts][N]: parts of dbias
     float *dXp, *dWp;      // [parts][T][K], [parts][N][K], or null
     int x_tiles, w_tiles, x_parts, w_parts, x_first;
-    int x_blocks, n_blocks, t_blocks;  // of the first launch: for X; for dY, column blocks and row blocks
+    bool stream;  // dX is not kept in the L2
+    int x_blocks, y_blocks, n_blocks, t_blocks;  // of the first launch: for X; for dY's copy; for dbias where dW is not formed, column blocks and row blocks
     int db_parts;                      // of dbias: the first launch's row blocks, or the parts of dW's tiles, which then add it up
 };
 
-constexpr int kAtOnce = 2;       // chunks of eight values of X to a thread of the first launch
+constexpr int kAtOnce = 2;       // chunks of eight values of X, or of dY, to a thread of the first launch
 constexpr int kRowBlock = 128;   // rows of dY whose sum is one part of dbias
 
 template <typename T>
@@ -67,8 +68,24 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a)
         }
         return;
     }
+    if ((int)blockIdx.x < a.x_blocks + a.y_blocks) {
+        const uint32_t chunks = (uint32_t)a.N8 / 8;
+        const int64_t all = (int64_t)a.T * chunks;
+        int64_t at[kAtOnce];
+        E e[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            at[u] = min(((int64_t)(blockIdx.x - a.x_blocks) * kAtOnce + u) * 256 + threadIdx.x, all - 1);  // (past the end: the last chunk again)
+            const int64_t row = all >> 32 ? at[u] / chunks : (uint32_t)at[u] / chunks;
+            const int col = (int)(at[u] - row * chunks) * 8;
+            e[u].load(a.dY, row * a.dy_row + col, a.N - col);
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) e[u].store(a.dYs, at[u] * 8, 8);
+        return;
+    }
     __shared__ float sums[8][256];
-    const int id = blockIdx.x - a.x_blocks, block = id / a.n_blocks, lane = threadIdx.x & 31, team = threadIdx.x >> 5;
+    const int id = blockIdx.x - a.x_blocks - a.y_blocks, block = id / a.n_blocks, lane = threadIdx.x & 31, team = threadIdx.x >> 5;
     const int n0 = (id - block * a.n_blocks) * 256, col = n0 + lane * 8, row0 = block * kRowBlock, row1 = min(a.T, row0 + kRowBlock);
     float s[8];
 #pragma unroll
@@ -79,13 +96,11 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a)
             E e;
             float v[8];
             e.load(a.dY, row * a.dy_row + col, a.N - col);
-            if (a.dYs) e.store(a.dYs, (int64_t)row * a.N8 + col, 8);
             e.get(v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) s[i] += v[i];
         }
     }
-    if (!a.db || a.dW) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sums[team][i * 32 + lane] = s[i];  // (lanes side by side)
     __syncthreads();
@@ -98,7 +113,7 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a)
 }
 
 // dX's rows: 64 columns from `col` on of what dY W gives, 32 rows from `row0` on
-template <typename T, bool STREAM>
+template <typename T>
 __device__ __forceinline__ void finish(const GradArgs &a, int row0, int col, int lane, uint8_t *room, float (&g)[2][16])
 {
     typedef Block<T> B;
@@ -115,7 +130,7 @@ __device__ __forceinline__ void finish(const GradArgs &a, int row0, int col, int
             slope(a.act, z, g[i]);
         }
     }
-    store_rows<T, STREAM>(a.dX, row0, a.T, col, a.K, lane, room, g);
+    store_rows<T>(a.dX, row0, a.T, col, a.K, lane, room, a.stream, g);
 }
 
 template <typename T, typename S>
@@ -212,9 +227,9 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_grads_kernel(const G
                         for (int k = 0; k < 16; k += 4) *reinterpret_cast<v4f *>(to + 32 * u + 2 * k + 4 * hf) = v4f{v[u][k], v[u][k + 1], v[u][k + 2], v[u][k + 3]};
                 }
             } else if (of_x) {
-                finish<T, S::kWaves == 8>(a, first, col, lane, lds + wave * kRowsRoom, v);
+                finish<T>(a, first, col, lane, lds + wave * kRowsRoom, v);
             } else {
-                store_rows<T, false>(a.dW, first, a.N, col, a.K, lane, lds + wave * kRowsRoom, v);
+                store_rows<T>(a.dW, first, a.N, col, a.K, lane, lds + wave * kRowsRoom, false, v);
             }
         }
     });
@@ -272,11 +287,6 @@ typedef Tile<1, 2, 2, 1, 3, 2> Least;  // 64 x 64
 struct Plan {
     int size, x_tiles, w_tiles, x_parts, w_parts;  // 0 least .. 3 large
 };
-// What a size of tiles costs, in microseconds: a launch with a tile's ends; a step of a lone workgroup; the KB that a CU is given in one, by all the workgroups that it has
-struct Cost {
-    int size, room;  // workgroups at work at once
-    double ends, step, rate;
-};
 // Which tiles, and into how many parts their contractions are cut: the shortest time by that.  Parts cost the launch that adds them up, 3 us, and their bytes, twice, at 8 TB/s.
 // Measured (modelled), us: 390 x 768 by 768 least 7.4 (7), small 8.3 (10), middle 10.9; 1000 x 1024 by 1024 12.0 (12), 12.9 (13), 17.2; 390 x 2304 by 768 least 14.9 (13),
 // small with dX in 3 parts 14.5 (16), middle in 6 15.7 (17); 4000 x 1024 by 1024, dW in 4 parts, small 33, middle 29.9.
@@ -293,7 +303,7 @@ void try_tiles(Plan &best, double &least, const Cost &c, bool dx, bool dw, int64
         const double tasks = (double)(x_tiles * x + w_tiles * w), chain = length * c.step;
         const bool rounds = tasks > 1.1 * c.room;  // (the last of several is not full; of one, a CU has a whole number of workgroups)
         const double share = rounds ? kb / 256 : kb / tasks * (1 + (int)(tasks * (0.9 / 256)));
-        double cost = c.ends + std::max(chain, share / c.rate) + (rounds ? 0.25 * chain : 0.0);
+        double cost = c.ends * std::max(1.0, tasks / c.room) + std::max(chain, share / c.rate) + (rounds ? 0.25 * chain : 0.0);
         if (x > 1 || w > 1) cost += 3.0 + ((x > 1 ? (double)x * T : 0.0) + (w > 1 ? (double)w * N : 0.0)) * K * 1e-6;
         if (cost < least) {
             least = cost;
@@ -337,7 +347,8 @@ size_t lay_out(const qb_linear_grads &l, GradArgs &a, Plan &p, uint8_t *base)
     const bool stage = (l.dX || l.dW) && !readable(l), expand = l.dW && !l.X;
     a.x_blocks = expand ? (int)((l.T * (l.K / 8) + 256 * kAtOnce - 1) / (256 * kAtOnce)) : 0;
     a.db_parts = !l.dbias ? 0 : l.dW ? p.w_parts : a.t_blocks;
-    if (!stage && (!l.dbias || l.dW)) a.t_blocks = 0;
+    if (!l.dbias || l.dW) a.t_blocks = 0;
+    a.y_blocks = stage ? (int)((l.T * (a.N8 / 8) + 256 * kAtOnce - 1) / (256 * kAtOnce)) : 0;
     if (expand) a.Xs = reinterpret_cast<uint16_t *>(take((size_t)a.T * a.K * 2));
     if (stage) a.dYs = reinterpret_cast<uint16_t *>(take((size_t)a.T * a.N8 * 2));
     if (l.dbias && !(l.dW && a.db_parts == 1)) a.db = reinterpret_cast<float *>(take((size_t)a.db_parts * a.N * 4));
@@ -349,7 +360,7 @@ size_t lay_out(const qb_linear_grads &l, GradArgs &a, Plan &p, uint8_t *base)
 template <typename T>
 qb_status launch(const GradArgs &a, int size, hipStream_t st)
 {
-    const int64_t first = (int64_t)a.x_blocks + (int64_t)a.n_blocks * a.t_blocks;
+    const int64_t first = (int64_t)a.x_blocks + a.y_blocks + (int64_t)a.n_blocks * a.t_blocks;
     if (first > 0) linear_prepare_kernel<T><<<(int)first, 256, 0, st>>>(a);
     const int groups = a.x_tiles * a.x_parts + a.w_tiles * a.w_parts;
     if (groups > 0) {
@@ -403,5 +414,6 @@ extern "C" qb_status qb_linear_bwd(const qb_linear_grads *l, void *workspace, vo
     a.dX = static_cast<uint16_t *>(l->dX); a.dW = static_cast<uint16_t *>(l->dW); a.dbias = l->dbias;
     const int64_t x_steps = (l->N + 63) / 64 / a.x_parts, w_steps = (l->T + 63) / 64 / a.w_parts;
     a.x_first = x_steps >= w_steps;
+    a.stream = p.size == 3;
     return l->type == QB_TYPE_BF16 ? launch<Bf16>(a, p.size, st) : launch<Fp16>(a, p.size, st);
 }
