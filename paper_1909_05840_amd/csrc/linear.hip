@@ -19,11 +19,10 @@ struct LinearArgs {
     float *scales;
     float *part;  // [parts][T][Np], or null
     int parts, Np;
-    bool stream;  // results are not kept in the L2
 };
 
 // what becomes of two blocks of sums, 64 columns from `col` on of 32 rows from `row0` on; `room`: LDS of the wavefront's own
-template <typename T>
+template <typename T, bool STREAM>
 __device__ __forceinline__ void finish(const LinearArgs &a, int row0, int col, int lane, uint8_t *room, float (&z)[2][16])
 {
     typedef Block<T> B;
@@ -32,11 +31,11 @@ __device__ __forceinline__ void finish(const LinearArgs &a, int row0, int col, i
     const auto keep = [&]() {
         const Coder c(top_of(col, a.N, hf, z));
         if (inside && hf == 0) a.scales[(int64_t)row * ((a.N + kGroup - 1) / kGroup) + col / kGroup] = c.quick_scale();
-        store_code_rows(a.codes, row0, a.T, col, a.N, lane, room, a.stream, c, z);
+        store_code_rows<STREAM>(a.codes, row0, a.T, col, a.N, lane, room, c, z);
     };
     if (a.act != QB_ACT_NONE) {
         if (a.codes) keep();
-        if (a.pre) store_rows<T>(a.pre, row0, a.T, col, a.N, lane, room, a.stream, z);
+        if (a.pre) store_rows<T, STREAM>(a.pre, row0, a.T, col, a.N, lane, room, z);
         activate(a.act, z[0]);
         activate(a.act, z[1]);
     }
@@ -50,12 +49,12 @@ __device__ __forceinline__ void finish(const LinearArgs &a, int row0, int col, i
         }
     }
     if (a.act == QB_ACT_NONE && a.codes) keep();
-    store_rows<T>(a.Y, row0, a.T, col, a.N, lane, room, a.stream, z);
+    store_rows<T, STREAM>(a.Y, row0, a.T, col, a.N, lane, room, z);
 }
 
 // Tiles of neurons by tokens: a lane's results are neighbours of a row of Y.  (Workgroups that stay and take tile after tile, the next one's first steps and this one's
 // rows on their way meanwhile, measured the same: 16384 x 4096 by 1024 143 us and 140, with GELU and codes 201 and 197; they need the registers.)
-template <typename T, typename S>
+template <typename T, typename S, bool STREAM>
 __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_kernel(const LinearArgs a)
 {
     static_assert(S::TM % 2 == 0, "a wavefront holds whole groups of 64");
@@ -106,7 +105,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_kernel(const LinearA
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) v[u][k] = z[i + u][j][k] + b[u][k];
-            finish<T>(a, t0 + (wn * S::TN + j) * 32, col, lane, lds + wave * kRowsRoom, v);
+            finish<T, STREAM>(a, t0 + (wn * S::TN + j) * 32, col, lane, lds + wave * kRowsRoom, v);
         }
     });
 }
@@ -285,7 +284,10 @@ bool shape_ok(const qb_linear &l) { return l.T >= 0 && l.T <= kMostRows && l.N >
 template <typename T, typename S>
 void launch(const LinearArgs &a, hipStream_t st)
 {
-    linear_kernel<T, S><<<(int)tiles_of<S>(a.T, a.N), 64 * S::kWaves, 0, st>>>(a);
+    const int tiles = (int)tiles_of<S>(a.T, a.N);
+    if constexpr (S::kWaves == 8)  // (large results, which the L2 would not keep anyway)
+        if (a.N % 64 == 0) return linear_kernel<T, S, true><<<tiles, 64 * S::kWaves, 0, st>>>(a);
+    linear_kernel<T, S, false><<<tiles, 64 * S::kWaves, 0, st>>>(a);
 }
 template <typename T>
 qb_status launch(const LinearArgs &a, int size, hipStream_t st)
@@ -345,6 +347,5 @@ extern "C" qb_status qb_linear_fwd(const qb_linear *l, void *workspace, void *st
     }
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int size = plan_of(*l).size;
-    a.stream = size >= 3 && l->N % 64 == 0;
     return l->type == QB_TYPE_BF16 ? launch<Bf16>(a, size, st) : launch<Fp16>(a, size, st);
 }

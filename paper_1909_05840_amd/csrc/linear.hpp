@@ -347,16 +347,17 @@ __device__ __forceinline__ uint32_t top_of(int col, int width, int hf, const flo
 }
 
 // The same 64 columns of 32 rows through LDS of the wavefront's own (kRowsRoom bytes), sixteen rows at a time, so that eight neighbouring lanes write 128 bytes of a
-// row, where a lane alone would write 16 of its own.  `stream`: what is written leaves the L2 first (only whole lines may: pieces of them would
-// go to memory one by one).  16384 x 4096 results of 1024, with GELU, 159 us; without `stream` 166, 32 bytes at a time 163.
+// row, where a lane alone would write 16 of its own.  STREAM: what is written leaves the L2 first (only whole lines may: pieces of them would
+// go to memory one by one).  16384 x 4096 results of 1024, with GELU and codes, 176 us; without STREAM 187, chosen by a branch 195.
 constexpr int kRowsRoom = 2048;
-__device__ __forceinline__ void put16(void *p, int64_t byte, v4u v, bool stream)
+template <bool STREAM>
+__device__ __forceinline__ void put16(void *p, int64_t byte, v4u v)
 {
-    if (stream) store16_stream(p, byte, v);
+    if constexpr (STREAM) store16_stream(p, byte, v);
     else store16(p, byte, v);
 }
-template <typename T>
-__device__ __forceinline__ void store_rows(uint16_t *p, int row0, int rows, int col, int width, int lane, uint8_t *room, bool stream, const float (&v)[2][16])
+template <typename T, bool STREAM>
+__device__ __forceinline__ void store_rows(uint16_t *p, int row0, int rows, int col, int width, int lane, uint8_t *room, const float (&v)[2][16])
 {
     const int l32 = lane & 31, hf = lane >> 5;
     v4u w[4];  // chunks of eight columns: 2 * i + hf
@@ -379,12 +380,13 @@ __device__ __forceinline__ void store_rows(uint16_t *p, int row0, int rows, int 
             const v4u x = *reinterpret_cast<const v4u *>(room + in * 128 + (((lane & 7) ^ (in & 7)) << 4));
             if (row >= rows) continue;
             const int64_t at = (int64_t)row * width;
-            if (c + 8 <= width) put16(p + at, 2 * c, x, stream);
+            if (c + 8 <= width) put16<STREAM>(p + at, 2 * c, x);
             else each<8>([&](auto e) { if (c + e < width) p[at + c + e] = (uint16_t)(x[e >> 1] >> (16 * (e & 1))); });
         }
     }
 }
-__device__ __forceinline__ void store_code_rows(int8_t *p, int row0, int rows, int col, int width, int lane, uint8_t *room, bool stream, const Coder &coder, const float (&v)[2][16])
+template <bool STREAM>
+__device__ __forceinline__ void store_code_rows(int8_t *p, int row0, int rows, int col, int width, int lane, uint8_t *room, const Coder &coder, const float (&v)[2][16])
 {
     const int l32 = lane & 31, hf = lane >> 5;
     v4u w[2];  // chunks of sixteen columns: 2 * u + hf
@@ -404,7 +406,7 @@ __device__ __forceinline__ void store_code_rows(int8_t *p, int row0, int rows, i
         const v4u x = *reinterpret_cast<const v4u *>(room + in * 64 + (((lane & 3) ^ (in >> 2 & 3)) << 4));
         if (row >= rows) continue;
         const int64_t at = (int64_t)row * width;
-        if (c + 16 <= width) put16(p + at, c, x, stream);
+        if (c + 16 <= width) put16<STREAM>(p + at, c, x);
         else each<16>([&](auto e) { if (c + e < width) p[at + c + e] = (int8_t)(x[e >> 2] >> (8 * (e & 3))); });
     }
 }

@@ -23,7 +23,6 @@ struct GradArgs {
     float *db;             // [db_parts][N]: parts of dbias
     float *dXp, *dWp;      // [parts][T][K], [parts][N][K], or null
     int x_tiles, w_tiles, x_parts, w_parts, x_first;
-    bool stream;  // dX is not kept in the L2
     int x_blocks, y_blocks, n_blocks, t_blocks;  // of the first launch: for X; for dY's copy; for dbias where dW is not formed, column blocks and row blocks
     int db_parts;                      // of dbias: the first launch's row blocks, or the parts of dW's tiles, which then add it up
 };
@@ -113,7 +112,7 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a)
 }
 
 // dX's rows: 64 columns from `col` on of what dY W gives, 32 rows from `row0` on
-template <typename T>
+template <typename T, bool STREAM>
 __device__ __forceinline__ void finish(const GradArgs &a, int row0, int col, int lane, uint8_t *room, float (&g)[2][16])
 {
     typedef Block<T> B;
@@ -130,7 +129,7 @@ __device__ __forceinline__ void finish(const GradArgs &a, int row0, int col, int
             slope(a.act, z, g[i]);
         }
     }
-    store_rows<T>(a.dX, row0, a.T, col, a.K, lane, room, a.stream, g);
+    store_rows<T, STREAM>(a.dX, row0, a.T, col, a.K, lane, room, g);
 }
 
 template <typename T, typename S>
@@ -227,9 +226,9 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_grads_kernel(const G
                         for (int k = 0; k < 16; k += 4) *reinterpret_cast<v4f *>(to + 32 * u + 2 * k + 4 * hf) = v4f{v[u][k], v[u][k + 1], v[u][k + 2], v[u][k + 3]};
                 }
             } else if (of_x) {
-                finish<T>(a, first, col, lane, lds + wave * kRowsRoom, v);
+                finish<T, S::kWaves == 8>(a, first, col, lane, lds + wave * kRowsRoom, v);
             } else {
-                store_rows<T>(a.dW, first, a.N, col, a.K, lane, lds + wave * kRowsRoom, false, v);
+                store_rows<T, false>(a.dW, first, a.N, col, a.K, lane, lds + wave * kRowsRoom, v);
             }
         }
     });
@@ -414,6 +413,5 @@ extern "C" qb_status qb_linear_bwd(const qb_linear_grads *l, void *workspace, vo
     a.dX = static_cast<uint16_t *>(l->dX); a.dW = static_cast<uint16_t *>(l->dW); a.dbias = l->dbias;
     const int64_t x_steps = (l->N + 63) / 64 / a.x_parts, w_steps = (l->T + 63) / 64 / a.w_parts;
     a.x_first = x_steps >= w_steps;
-    a.stream = p.size == 3;
     return l->type == QB_TYPE_BF16 ? launch<Bf16>(a, p.size, st) : launch<Fp16>(a, p.size, st);
 }
