@@ -30,13 +30,9 @@ struct Tile {
 // Rows of KS values along the contraction: the chunks of sixteen bytes are XORed with a key of the row such that sixteen consecutive rows at one chunk meet different banks.
 template <int KS>
 struct AlongRows {
-    static_assert(KS == 32 || KS == 64, "rows of 64 or 128 bytes");
+    static_assert(KS == 64, "rows of 128 bytes");
     static constexpr int kBytes = 2 * KS, kChunks = KS / 8, kPerCopy = 64 / kChunks;
-    static __device__ __forceinline__ int key(int row)
-    {
-        if constexpr (KS == 64) return Rows<64>::key(row);
-        else return (row >> 2) & 3;
-    }
+    static __device__ __forceinline__ int key(int row) { return Rows<64>::key(row); }
     static __device__ __forceinline__ int row(int copy, int lane) { return copy * kPerCopy + lane / kChunks; }
     static __device__ __forceinline__ int chunk(int copy, int lane) { return (lane % kChunks) ^ key(row(copy, lane)); }
 };
@@ -301,17 +297,6 @@ struct Block {
             part_halves(w, a, b);
             v[k] = T::lo(a[0]); v[k + 1] = T::hi(a[0]); v[k + 2] = T::lo(a[1]); v[k + 3] = T::hi(a[1]);
             v[k + 4] = T::lo(b[0]); v[k + 5] = T::hi(b[0]); v[k + 6] = T::lo(b[1]); v[k + 7] = T::hi(b[1]);
-        }
-    }
-    static __device__ __forceinline__ void store(uint16_t *p, int64_t at, int col, int width, bool inside, int hf, const float (&v)[16])
-    {
-#pragma unroll
-        for (int k = 0; k < 16; k += 8) {
-            const v4u w = join_halves(v2u{T::pair(v[k], v[k + 1]), T::pair(v[k + 2], v[k + 3])}, v2u{T::pair(v[k + 4], v[k + 5]), T::pair(v[k + 6], v[k + 7])});
-            const int c = col + 2 * k + 8 * hf;
-            if (!inside) continue;
-            if (c + 8 <= width) store16(p + at, 2 * c, w);
-            else each<8>([&](auto e) { if (c + e < width) p[at + c + e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1))); });
         }
     }
     static __device__ __forceinline__ void load_codes(const int8_t *p, int64_t at, int col, int width, bool inside, int hf, float scale, float (&v)[16])

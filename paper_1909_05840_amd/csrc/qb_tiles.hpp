@@ -91,11 +91,6 @@ __device__ __forceinline__ void copy16(const void *from, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory", "m0");
 }
-// four bytes per lane: lane l's land at lds + 4 * l
-__device__ __forceinline__ void copy4(const void *from, uint32_t lds)
-{
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(lds) : "memory", "m0");
-}
 // sixteen with the address as a base that the wavefront shares and an offset in bytes (the base is moved into registers of the block's
 // own by a scalar instruction: a vector memory instruction may read what a VALU instruction wrote five wait states later only)
 __device__ __forceinline__ void copy16(const void *base, uint32_t offset, uint32_t lds)
