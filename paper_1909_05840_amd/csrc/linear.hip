@@ -52,6 +52,7 @@ __device__ __forceinline__ void finish(const LinearArgs &a, int row0, int col, i
     store_rows<T, STREAM>(a.Y, row0, a.T, col, a.N, lane, room, z);
 }
 
+constexpr int kMostCut = 128 * 128;  // results of a tile whose contraction may be cut; the parts are added up by a second launch
 // Tiles of neurons by tokens: a lane's results are neighbours of a row of Y.  (Workgroups that stay and take tile after tile, the next one's first steps and this one's
 // rows on their way meanwhile, measured the same: 16384 x 4096 by 1024 143 us and 140, with GELU and codes 201 and 197; they need the registers.)
 template <typename T, typename S, bool STREAM>
@@ -63,17 +64,18 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_kernel(const LinearA
     static_assert(S::kStages * S::kStage >= kTeam * kRowsRoom, "room for the rows on their way out, where the stages were");
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % kTeam / S::WN, wn = wave % S::WN;
-    const int words = (a.N + S::BM - 1) / S::BM, rows = (a.T + S::BN - 1) / S::BN, steps = a.K / S::KS;
+    const int words = (a.N + S::BM - 1) / S::BM, rows = (a.T + S::BN - 1) / S::BN, tiles = words * rows, all = a.K / S::KS;
+    const int id = tile_of(blockIdx.x, tiles * a.parts), part = id / tiles, s0 = all * part / a.parts, steps = all * (part + 1) / a.parts - s0;
     int tt, tn, stage = 0, next = 0;
-    place_of(tile_of(blockIdx.x, words * rows), rows, words, tt, tn);
+    place_of(id - part * tiles, rows, words, tt, tn);
     const int n0 = tn * S::BM, t0 = tt * S::BN;
     const uint32_t lds0 = lds_address(lds);
     v16f z[S::TM][S::TN];
     float none[S::TN];
     clear(z);
     {
-        Feed<S::NA> w = along<S, S::NA>(a.W, (int64_t)a.K * 2, n0, a.N, 0, wave, lane);
-        Feed<S::NB> x = along<S, S::NB>(a.X, a.x_row * 2, t0, a.T, 0, wave, lane);
+        Feed<S::NA> w = along<S, S::NA>(a.W, (int64_t)a.K * 2, n0, a.N, s0, wave, lane);
+        Feed<S::NB> x = along<S, S::NB>(a.X, a.x_row * 2, t0, a.T, s0, wave, lane);
         const auto fetch = [&](int to) {
             if (next >= steps) return;
             ++next;
@@ -90,6 +92,22 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_kernel(const LinearA
         constexpr int i = 2 * half;
         const int col = n0 + (wm * S::TM + i) * 32;
         if (col >= a.N) return;
+        if constexpr (S::BM * S::BN <= kMostCut) {
+            if (a.part) {  // (its rows have room for whole groups)
+#pragma unroll
+                for (int j = 0; j < S::TN; ++j) {
+                    const int row = t0 + (wn * S::TN + j) * 32 + l32;
+                    if (row >= a.T) continue;
+                    float *const to = a.part + ((int64_t)part * a.T + row) * a.Np + col;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int k = 0; k < 16; k += 4)
+                            *reinterpret_cast<v4f *>(to + 32 * u + 2 * k + 4 * hf) = v4f{z[i + u][j][k], z[i + u][j][k + 1], z[i + u][j][k + 2], z[i + u][j][k + 3]};
+                }
+                return;
+            }
+        }
         float b[2][16];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -227,18 +245,21 @@ struct Plan {
 };
 template <typename S>
 int64_t tiles_of(int64_t T, int64_t N) { return ((T + S::BN - 1) / S::BN) * ((N + S::BM - 1) / S::BM); }
-// Of few tokens: the largest share of a CU, at 45 KB a microsecond, and what a second launch and the parts' bytes cost (3 us, twice at 8 TB/s).
-Plan few_plan(const qb_linear &l)
+// Few tokens: a launch's ends and the rounds of a wavefront's units, the largest share of a CU, at 45 KB a microsecond (with registers for 64 tokens 32), and what a second
+// launch and the parts' bytes cost.  Measured (modelled), us: 1 x 1024 by 4096 uncut 7.1 (7.0), in 4 parts 6.5 (6.6); 32 x 1024 by 4096 13.2 (12.7), 8.2 (8.0); 16 x 4096 by
+// 4096 10.3 (9.8); 64 x 768 by 768 7.1 (7.8).
+Plan few_plan(const qb_linear &l, double &least)
 {
     Plan best = {-1, 1};
-    double least = 1e300;
     for (const int m : {1, 2}) {
         for (const int p : {1, 2, 4, 8}) {
             if (p > 1 && p > l.K / 128) break;
             if (m > 1 && l.K / p < 1024) break;  // (two units for each wavefront)
-            const int64_t groups = (l.N + 16 * m - 1) / (16 * m) * p;
-            const double cost = (double)((groups + 255) / 256) * (double)((16 * m + l.T) * l.K * 2 / p) / 45e3 + (p > 1 || l.codes ? 3.0 + p * l.T * l.N * 1e-6 : 0.0);
-            if (cost < 0.9 * least) {  // (64 x 4096 by 4096: one and two of sixteen neurons 21.5, 18.3 us; 1 x 16384 by 4096 25.5, 27.6)
+            const int64_t groups = (l.N + 16 * m - 1) / (16 * m) * p, units = (l.K / 64 + 8 * p - 1) / (8 * p), at_once = m > 1 || l.T > 32 ? 2 : 4;
+            const double share = (double)((groups + 255) / 256) * (double)((16 * m + l.T) * l.K * 2 / p) * 1e-3;
+            double cost = (l.T > 32 ? 4.0 + share / 32.0 : 3.0 + share / 45.0) + (double)((units - 1) / at_once);
+            if (p > 1 || l.codes) cost += 2.8 + p * l.T * l.N * 1e-6;
+            if (cost < 0.95 * least) {  // (1 x 16384 by 4096, one and two of sixteen neurons: 25.5, 27.6 us)
                 least = cost;
                 best = {-m, p};
             }
@@ -246,25 +267,31 @@ Plan few_plan(const qb_linear &l)
     }
     return best;
 }
-// Measured (modelled), us: 390 x 768 by 768 least 7 (7), small 8.6 (10); 1000 x 1024 by 1024 9.7 (8), 10.9 (12), middle 15.6 (16); 4000 x 1024 by 1024 small 20 (17), middle
-// 17.4 (16); 8190 x 1024 by 4096 broad 76 (73), large 100 (103), middle 82 (83).
+// Tiles, and into how many parts their contraction is cut.  Measured (modelled), us: 390 x 768 by 768 least 6.8 (7.2), small 8.6 (10); 1000 x 1024 by 1024 9.1 (8.3), 10.9 (12),
+// middle 15.6 (16); 4000 x 1024 by 1024 small 20 (17), middle 17.4 (16); 8190 x 1024 by 4096 broad 76 (73), large 100 (103), middle 82 (83).  Least in parts: 65 x 1024 by 4096
+// uncut 18.5 (20.5), in 4 9.7 (10.5), in 8 8.5 (9.2); 390 x 768 by 3008 15.2 (16.1), in 2 12.7 (13.5); 24 x 1024 by 4096 16.0 (20), in 8 7.2 (7.9).
 template <typename S>
 void try_size(Plan &best, double &least, const Cost &c, const qb_linear &l)
 {
     const int64_t tiles = tiles_of<S>(l.T, l.N), steps = l.K / 64;
-    const double share = (double)((tiles + 255) / 256 * steps) * ((S::BM + S::BN) / 8.0);
-    const double cost = c.ends * (double)((tiles + c.room - 1) / c.room) + std::max(steps * c.step, share / c.rate);
-    if (cost < least) {
-        least = cost;
-        best = {c.size, 1};
+    for (const int p : {1, 2, 3, 4, 6, 8, 12, 16}) {
+        if (p > 1 && (p > steps / 4 || S::BM * S::BN > kMostCut)) break;
+        const int64_t length = (steps + p - 1) / p;
+        const double share = (double)((tiles * p + 255) / 256 * length) * ((S::BM + S::BN) / 8.0);
+        double cost = c.ends * (double)((tiles * p + c.room - 1) / c.room) + std::max(length * c.step, share / c.rate);
+        if (p > 1) cost += 1.5 + p * (double)l.T * l.N * 2.8e-6;
+        if (cost < least) {
+            least = cost;
+            best = {c.size, p};
+        }
     }
 }
 Plan plan_of(const qb_linear &l)
 {
-    if (l.T <= 64) return few_plan(l);
     Plan p = {0, 1};
     double least = 1e300;
-    try_size<Least>(p, least, {0, 512, 4.0, 0.25, 63.0}, l);
+    if (l.T <= 64) p = few_plan(l, least);
+    try_size<Least>(p, least, {0, 512, 4.2, 0.2, 63.0}, l);
     try_size<Small>(p, least, {1, 512, 5.5, 0.4, 65.0}, l);
     try_size<Middle>(p, least, {2, 512, 6.0, 0.6, 53.0}, l);
     try_size<Broad>(p, least, {3, 256, 6.0, 1.0, 46.0}, l);
@@ -284,10 +311,10 @@ bool shape_ok(const qb_linear &l) { return l.T >= 0 && l.T <= kMostRows && l.N >
 template <typename T, typename S>
 void launch(const LinearArgs &a, hipStream_t st)
 {
-    const int tiles = (int)tiles_of<S>(a.T, a.N);
+    const int groups = (int)tiles_of<S>(a.T, a.N) * a.parts;
     if constexpr (S::kWaves == 8)  // (large results, which the L2 would not keep anyway)
-        if (a.N % 64 == 0) return linear_kernel<T, S, true><<<tiles, 64 * S::kWaves, 0, st>>>(a);
-    linear_kernel<T, S, false><<<tiles, 64 * S::kWaves, 0, st>>>(a);
+        if (a.N % 64 == 0) return linear_kernel<T, S, true><<<groups, 64 * S::kWaves, 0, st>>>(a);
+    linear_kernel<T, S, false><<<groups, 64 * S::kWaves, 0, st>>>(a);
 }
 template <typename T>
 qb_status launch(const LinearArgs &a, int size, hipStream_t st)

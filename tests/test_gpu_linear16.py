@@ -53,6 +53,16 @@ SIZES = [(1, 1, 64), (1, 4096, 1024), (2, 3, 128), (3, 65, 64), (7, 768, 768), (
          (129, 127, 64), (390, 768, 768), (390, 2304, 768), (257, 511, 1024), (1500, 1100, 128), (2000, 2100, 64), (4100, 3001, 64), (3, 70000, 64), (12001, 1024, 64), (40, 4100, 4096), (64, 4097, 2048), (8190, 1000, 128), (301, 2, 128), (5000, 3, 64), (70, 100, 32768)]
 
 
+# tiles whose contraction is cut into parts: steps that do not come out even, a last group that is not whole, rows behind the last tile's
+CUT = [(65, 1024, 4096), (390, 768, 3008), (200, 770, 4032), (70, 65, 32768), (65, 1, 576), (700, 200, 8192)]
+
+
+@pytest.mark.parametrize("T,N,K", CUT)
+@pytest.mark.parametrize("act,residual,keep,wide", [(None, False, None, False), ("gelu", True, "codes", True), (None, True, "codes", False), ("tanh", False, "values", False)])
+def test_contractions_in_parts(qb, T, N, K, act, residual, keep, wide):
+    check_forward(qb, T, N, K, torch.bfloat16 if N % 2 else torch.float16, act=act, residual=residual, keep=keep, wide=wide)
+
+
 @pytest.mark.parametrize("t", TYPES)
 @pytest.mark.parametrize("T,N,K", SIZES)
 def test_sizes(qb, t, T, N, K):
@@ -199,7 +209,7 @@ def test_nothing_behind_the_outputs_is_written(qb):
         assert (dx[T * K:] == 5).all() and (dw[N * K:] == 5).all() and (db[N:] == 5).all()
 
 
-@pytest.mark.parametrize("T,N,K", [(24, 1024, 4096), (390, 768, 768), (200, 130, 2048), (2051, 2101, 704)])
+@pytest.mark.parametrize("T,N,K", [(2, 1030, 4096), (24, 1024, 4096), (65, 1030, 4032), (390, 768, 768), (200, 130, 2048), (2051, 2101, 704)])
 def test_workspaces_of_exactly_the_size(qb, T, N, K):
     import ctypes
     from paper_1909_05840_amd.binding import LinearGrads, LinearLayer
@@ -264,7 +274,7 @@ def test_residual_in_place(qb):
         assert torch.equal(qb.qb_linear_fwd(X, W.cuda(), b.cuda(), residual=R, Y=R), want)
 
 
-@pytest.mark.parametrize("T,N,K", [(1, 4096, 1024), (24, 1024, 4096), (390, 768, 768), (2051, 2101, 704)])
+@pytest.mark.parametrize("T,N,K", [(1, 4096, 1024), (2, 1024, 4096), (24, 1024, 4096), (390, 768, 768), (390, 768, 3008), (2051, 2101, 704)])
 def test_graphs_and_streams(qb, T, N, K):
     W, b = (v.cuda() for v in weights(N, K, torch.bfloat16))
     X, dY = ref.draw(T, K, seed=1, t=torch.bfloat16).cuda(), ref.draw(T, N, seed=2, t=torch.bfloat16).cuda()
