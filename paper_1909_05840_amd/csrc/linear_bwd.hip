@@ -7,6 +7,7 @@
 // parts of tiles whose contraction was cut.  Bound by the matrix cores.
 #include "linear.hpp"
 #include <algorithm>
+#include <cmath>
 
 namespace qb {
 namespace {
@@ -286,12 +287,28 @@ typedef Tile<1, 2, 2, 1, 3, 2> Least;  // 64 x 64
 struct Plan {
     int size, x_tiles, w_tiles, x_parts, w_parts;  // 0 least .. 3 large
 };
-// Which tiles, and into how many parts their contractions are cut: the shortest time by that.  Parts cost the launch that adds them up, 3 us, and their bytes, twice, at 8 TB/s.
-// Measured (modelled), us: 390 x 768 by 768 least 7.4 (7), small 8.3 (10), middle 10.9; 1000 x 1024 by 1024 12.0 (12), 12.9 (13), 17.2; 390 x 2304 by 768 least 14.9 (13),
-// small with dX in 3 parts 14.5 (16), middle in 6 15.7 (17); 4000 x 1024 by 1024, dW in 4 parts, small 33, middle 29.9.
+// When `places` workgroups have done `n1` tasks of time `t1` and then `n2` shorter ones of `t2`, each taking the next as it gets free.
+double done_at(int64_t n1, double t1, int64_t n2, double t2, int64_t places)
+{
+    const int64_t late = n1 % places;  // places with one long task more than the others
+    const double early = (double)(n1 / places) * t1;
+    int64_t a = 0, b = 0;  // short tasks behind the long ones of a late place, and of an early one
+    double end = early + (late ? t1 : 0.0);
+    while (late * a + (places - late) * b < n2) {
+        const double next_a = early + t1 + (double)(a + 1) * t2, next_b = early + (double)(b + 1) * t2;
+        if (late && next_a <= next_b) ++a, end = std::max(end, next_a);
+        else ++b, end = std::max(end, next_b);
+    }
+    return end;
+}
+// Which tiles, and into how many parts their contractions are cut: the shortest time by that.  Parts cost the launch that adds them up, 3 us, and their bytes, twice, at 3 TB/s
+// (4 where they leave the L2).  Measured (modelled), us: 390 x 768 by 768 least 7.4 (7), small 8.3 (10), middle 10.9; 1000 x 1024 by 1024 12.0 (12), 12.9 (13), 17.2;
+// 390 x 2304 by 768 least 14.9 (13), small with dX in 3 parts 14.5 (18).  Large, dW in 2, 3 and 4 parts: 8190 x 1024 by 4096 148 (156), 166 (173), 159 (161);
+// 16384 x 4096 by 1024 265 (257), 267 (289), 255 (253).
 template <typename S>
 void try_tiles(Plan &best, double &least, const Cost &c, bool dx, bool dw, int64_t T, int64_t N, int64_t K)
 {
+    constexpr bool kAlone = S::kWaves == 8;  // one workgroup to a CU
     const int64_t kt = (K + S::BM - 1) / S::BM, x_tiles = dx ? kt * ((T + S::BN - 1) / S::BN) : 0, w_tiles = dw ? kt * ((N + S::BN - 1) / S::BN) : 0;
     const int x_steps = dx ? (int)((N + 63) / 64) : 0, w_steps = dw ? (int)((T + 63) / 64) : 0, longest = std::max(x_steps, w_steps);
     const double kb = ((double)x_tiles * x_steps + (double)w_tiles * w_steps) * ((S::BM + S::BN) / 8.0);
@@ -301,9 +318,16 @@ void try_tiles(Plan &best, double &least, const Cost &c, bool dx, bool dw, int64
         const int length = (longest + cut - 1) / cut, x = std::max(1, (x_steps + length - 1) / length), w = std::max(1, (w_steps + length - 1) / length);
         const double tasks = (double)(x_tiles * x + w_tiles * w), chain = length * c.step;
         const bool rounds = tasks > 1.1 * c.room;  // (the last of several is not full; of one, a CU has a whole number of workgroups)
-        const double share = rounds ? kb / 256 : kb / tasks * (1 + (int)(tasks * (0.9 / 256)));
-        double cost = c.ends * std::max(1.0, tasks / c.room) + std::max(chain, share / c.rate) + (rounds ? 0.25 * chain : 0.0);
-        if (x > 1 || w > 1) cost += 3.0 + ((x > 1 ? (double)x * T : 0.0) + (w > 1 ? (double)w * N : 0.0)) * K * 1e-6;
+        const double share = rounds ? kb / 256 : kb / tasks * (1 + (int)(tasks * (0.97 / 256)));
+        double cost;
+        if (kAlone && tasks < 64.0 * c.room) {
+            const double tx = c.ends + (double)((x_steps + x - 1) / x) * c.step, tw = c.ends + (double)((w_steps + w - 1) / w) * c.step;
+            cost = tx >= tw ? done_at(x_tiles * x, tx, w_tiles * w, tw, c.room) : done_at(w_tiles * w, tw, x_tiles * x, tx, c.room);
+            if (dx && dw) cost += 0.1 * std::abs(tx - tw);  // (tiles of both kinds at once have less in common in the L2)
+        } else {
+            cost = c.ends * std::max(1.0, tasks / c.room) + std::max(chain, share / c.rate) + (rounds ? 0.25 * chain : 0.0);
+        }
+        if (x > 1 || w > 1) cost += 3.0 + ((x > 1 ? (double)x * T : 0.0) + (w > 1 ? (double)w * N : 0.0)) * K * (kAlone ? 2e-6 : 2.8e-6);
         if (cost < least) {
             least = cost;
             best = {c.size, (int)x_tiles, (int)w_tiles, x, w};
