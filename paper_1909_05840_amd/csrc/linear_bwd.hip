@@ -303,8 +303,8 @@ double done_at(int64_t n1, double t1, int64_t n2, double t2, int64_t places)
 }
 // Which tiles, and into how many parts their contractions are cut: the shortest time by that.  Parts cost the launch that adds them up, 3 us, and their bytes, twice, at 3 TB/s
 // (4 where they leave the L2).  Measured (modelled), us: 390 x 768 by 768 least 7.4 (7), small 8.3 (10), middle 10.9; 1000 x 1024 by 1024 12.0 (12), 12.9 (13), 17.2;
-// 390 x 2304 by 768 least 14.9 (13), small with dX in 3 parts 14.5 (18).  Large, dW in 2, 3 and 4 parts: 8190 x 1024 by 4096 148 (156), 166 (173), 159 (161);
-// 16384 x 4096 by 1024 265 (257), 267 (289), 255 (253).
+// 390 x 2304 by 768 least 14.9 (13), small with dX in 3 parts 14.5 (18).  Large, dW in 2, 3 and 4 parts: 8190 x 1024 by 4096 148 (154), 166 (171), 159 (159);
+// 16384 x 4096 by 1024 251 (247), 267 (284), 255 (253).
 template <typename S>
 void try_tiles(Plan &best, double &least, const Cost &c, bool dx, bool dw, int64_t T, int64_t N, int64_t K)
 {
