@@ -583,8 +583,8 @@ qb_status qb_layer_norm_bwd(const qb_norm_grads *n, void *dX, float *dweight, fl
  * X from 8 bits or from pre is rounded to `type`; sums are binary32, results are rounded once.  relu's derivative is 0 at 0.
  * 0 <= T <= 2^24 (0: dW and dbias are zero), 1 <= N <= 2^20, K a multiple of QB_K_ALIGN up to QB_MAX_K, strides 0 .. 2^22.  Pointers without another word need the
  * alignment of their type only.  Workspaces: 256-byte aligned, contents undefined before and after; 0 bytes: NULL will do.  The same call gives the same bits
- * every time.  Y may be residual where that is dense; no other output may overlap what the call reads.  The backward's workspace depends on which pointers are NULL and on
- * dY's alignment: ask with those of the call.
+ * every time.  Y may be residual where that is dense; no other output may overlap what the call reads.  The workspaces depend on which pointers are NULL, the backward's on
+ * dY's alignment too: ask with those of the call.
  */
 enum { QB_ACT_NONE = 0, QB_ACT_RELU = 1, QB_ACT_GELU = 2, QB_ACT_TANH = 3 };
 typedef struct {

@@ -274,6 +274,7 @@ template <typename S>
 void try_size(Plan &best, double &least, const Cost &c, const qb_linear &l)
 {
     const int64_t tiles = tiles_of<S>(l.T, l.N), steps = l.K / 64;
+    if (c.ends + (double)(tiles * steps) * ((S::BM + S::BN) / 8.0) / (256 * c.rate) >= least) return;
     for (const int p : {1, 2, 3, 4, 6, 8, 12, 16}) {
         if (p > 1 && (p > steps / 4 || S::BM * S::BN > kMostCut)) break;
         const int64_t length = (steps + p - 1) / p;
@@ -292,6 +293,7 @@ Plan plan_of(const qb_linear &l)
     double least = 1e300;
     if (l.T <= 64) p = few_plan(l, least);
     try_size<Least>(p, least, {0, 512, 4.2, 0.2, 63.0}, l);
+    if (l.T <= 64) return p;
     try_size<Small>(p, least, {1, 512, 5.5, 0.4, 65.0}, l);
     try_size<Middle>(p, least, {2, 512, 6.0, 0.6, 53.0}, l);
     try_size<Broad>(p, least, {3, 256, 6.0, 1.0, 46.0}, l);
@@ -299,9 +301,9 @@ Plan plan_of(const qb_linear &l)
     return p;
 }
 
-size_t lay_out(const qb_linear &l, LinearArgs &a)
+size_t lay_out(const qb_linear &l, LinearArgs &a, Plan &p)
 {
-    const Plan p = plan_of(l);
+    p = plan_of(l);
     a.parts = p.parts;
     a.Np = (int)((l.N + 63) / 64 * 64);
     return p.parts > 1 || (p.size < 0 && l.codes) ? round_up((size_t)p.parts * l.T * a.Np * 4) : 0;
@@ -349,7 +351,8 @@ using namespace qb;
 extern "C" size_t qb_linear_fwd_workspace_nbytes(const qb_linear *l)
 {
     LinearArgs a = {};
-    return l && shape_ok(*l) && l->T > 0 ? lay_out(*l, a) : 0;
+    Plan p;
+    return l && shape_ok(*l) && l->T > 0 ? lay_out(*l, a, p) : 0;
 }
 
 extern "C" qb_status qb_linear_fwd(const qb_linear *l, void *workspace, void *stream)
@@ -368,11 +371,11 @@ extern "C" qb_status qb_linear_fwd(const qb_linear *l, void *workspace, void *st
     a.T = (int)l->T; a.N = (int)l->N; a.K = (int)l->K; a.act = l->act;
     a.Y = static_cast<uint16_t *>(l->Y); a.pre = static_cast<uint16_t *>(l->pre);
     a.codes = l->codes; a.scales = l->scales;
-    if (lay_out(*l, a)) {
+    Plan p;
+    if (lay_out(*l, a, p)) {
         if (!workspace || misaligned(workspace, 256)) return QB_ERR_WORKSPACE;
         a.part = static_cast<float *>(workspace);
     }
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const int size = plan_of(*l).size;
-    return l->type == QB_TYPE_BF16 ? launch<Bf16>(a, size, st) : launch<Fp16>(a, size, st);
+    return l->type == QB_TYPE_BF16 ? launch<Bf16>(a, p.size, st) : launch<Fp16>(a, p.size, st);
 }
