@@ -120,8 +120,8 @@ __global__ __launch_bounds__((Row<R, C>::kThreads)) void layer_norm_kernel(const
                 s += v[i][e];
             }
         const v2f both = L::sum(q, s, shared);
-        const float more = both[1] / (float)a.W, mean = near + more;
-        const float rstd = 1.0f / sqrtf(fmaxf(__builtin_fmaf(-more, more, both[0] * inv), 0.0f) + a.eps);
+        const float more = both[1] / (float)a.W, mean = fabsf(near) < __builtin_inff() ? near + more : near;  // (infinity stays: there is no difference from it)
+        const float rstd = 1.0f / sqrtf(__builtin_elementwise_maximum(__builtin_fmaf(-more, more, both[0] * inv), 0.0f) + a.eps);  // (NaN stays)
         if (threadIdx.x % R == 0) {
             a.mean[row] = mean;
             a.rstd[row] = rstd;
