@@ -276,7 +276,7 @@ __device__ __forceinline__ void slope(int act, const float (&z)[N], float (&g)[N
     if (act == QB_ACT_GELU) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float share = 0.5f + copysignf(0.5f - normal_tail(fminf(fabsf(z[i]), kTailEnd)), z[i]);
+            const float tail = normal_tail(fminf(fabsf(z[i]), kTailEnd)), share = z[i] < 0.0f ? tail : 1.0f - tail;  // (left of zero the tail itself: 1 / 2 - (1 / 2 - tail) would lose it)
             g[i] *= __builtin_fmaf(z[i] * __builtin_amdgcn_exp2f(z[i] * z[i] * -0.72134752044f), 0.3989422804f, share);
         }
     } else if (act == QB_ACT_RELU) {

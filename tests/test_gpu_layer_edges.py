@@ -28,3 +28,39 @@ def test_norm_rows_that_are_no_numbers(qb, t, W, eps):
     assert rstd[bad].isnan().all() and Y[bad].isnan().all() and dX[bad].isnan().all()
     assert qb.qb_restore_act(codes, scales, torch.float32)[bad].isnan().all()
     assert dw.isnan().all() and db.isfinite().all()
+
+
+def tail_off(z):
+    """what the kernels' normal distribution is off, relative to its smaller tail: fitted up to 7; further out it falls faster than the true one"""
+    return torch.where(z.abs() <= 7, ref.NORMAL, torch.where(z.abs() <= 9, 0.02, 1.0))
+
+
+def from_minus_to_plus(T, t):
+    """[T, 64] values of `t` from -16 to 16, most of them between -9 and 9"""
+    z = torch.cat([torch.linspace(-9, 9, T * 64 - 64, dtype=torch.float64), torch.linspace(-16, 16, 64, dtype=torch.float64)])
+    return z[torch.randperm(T * 64, generator=torch.Generator().manual_seed(T))].view(T, 64).to(t)
+
+
+FLUSHED = 2.0 ** -126  # the hardware's power of two has no subnormal results: below this it is zero
+
+
+def rounded(t, value):
+    return ref.half_step(t) * value.abs() * (1 + 2 * ref.half_step(t)) + torch.finfo(t).tiny * torch.finfo(t).eps
+
+
+@pytest.mark.parametrize("t", TYPES[1:])
+@pytest.mark.parametrize("T", [40, 700, 9000])
+def test_gelu_derivative_and_its_tail(qb, t, T):
+    """dX of a layer whose product is one, so that what is left is the derivative at each value: relative to its two terms, however small"""
+    pre = from_minus_to_plus(T, t)
+    dY, W = torch.zeros(T, 8, dtype=t), torch.zeros(8, 64, dtype=t)
+    dY[:, 3] = W[3] = 1
+    dX = qb.qb_linear_bwd(dY.cuda(), None, W.cuda(), pre=pre.cuda(), act="gelu", need=(True, False, False))[0]
+    z = pre.double()
+    bell, tail = torch.exp(-z * z / 2) / math.sqrt(2 * math.pi), ref.phi(-z.abs())
+    want = ref.phi(z) + z * bell
+    # the exponent is rounded three times, to half a step each, and so is relative 1.5 z^2 half steps off; the exponential, the products and the last sum have eight between
+    # them; right of zero the sum is of the order of one, with two of its own
+    # (and where the exponential is below the normal numbers, at 13 and beyond, it is zero)
+    off = (1 + z.abs()) * FLUSHED + tail_off(z) * tail + (1.5 * z * z + 8) * ref.STEP * z.abs() * bell + 2 * ref.STEP * torch.where(z < 0, 0.0, 1.0 + z.abs() * bell)
+    ref.near(dX, want, rounded(t, want) + off, "GELU's derivative")
