@@ -223,9 +223,10 @@ __device__ __forceinline__ void kept8(float (&v)[8], const int8_t *codes, const 
 // ---- activations ------------------------------------------------------------------------------------------------------
 
 // The normal distribution's upper tail at x >= 0 is a power of two of a polynomial of degree seven: fitted to the tail's logarithm on [0, 7] for the least largest
-// error, 1.3e-5 of the tail itself with the evaluation's roundings (below 2^-16), so that GELU is below the 16-bit types' rounding steps, its tail included.  Further out the
-// polynomial falls a little faster: 2% less at 9, where the tail is 1e-19; from 16 on it is zero.  (Degree eight: 1.0e-5.  An instruction for each of 16384 x 4096
-// results takes 8 us when the matrix cores wait for it.)
+// error, 1.4e-5 of the tail itself with the evaluation's roundings (below 2^-16).  Up to there, 7, GELU and the tail's share of its derivative are relative to themselves below the 16-bit types' half
+// steps, 2^-9 and 2^-12, also where they are small.  Further out the polynomial falls faster than the tail: by 3.4e-4 of it at 7.5, 0.2% at 8, 0.6% at 8.5, 1.8% at 9, 9% at 10,
+// most of it from 12 on, and from 16 on it is zero; GELU is -9e-12 at -7, zero in float16 from -6 on, and -5e-15 at -8, where bf16 begins to tell the difference.  (Degree eight: 1.0e-5 up to
+// 7, or 4e-5 up to 6 and 6e-4 up to 13.  An instruction for each of 16384 x 4096 results takes 8 us when the matrix cores wait for it.)
 constexpr float kTailEnd = 16.0f;
 __device__ __forceinline__ float normal_tail(float x)
 {
@@ -239,7 +240,7 @@ __device__ __forceinline__ float normal_tail(float x)
 }
 __device__ __forceinline__ float hyperbolic_tangent(float z)
 {
-    if (fabsf(z) < 0.25f) {  // (the quotient's numerator would cancel; the next term of the series is below 2e-9)
+    if (fabsf(z) < 0.25f) {  // (the quotient's numerator would cancel; the next term of the series is 2.1e-9 at most)
         const float s = z * z;
         float p = __builtin_fmaf(s, 62.0f / 2835.0f, -17.0f / 315.0f);
         p = __builtin_fmaf(p, s, 2.0f / 15.0f);

@@ -64,3 +64,17 @@ def test_gelu_derivative_and_its_tail(qb, t, T):
     # (and where the exponential is below the normal numbers, at 13 and beyond, it is zero)
     off = (1 + z.abs()) * FLUSHED + tail_off(z) * tail + (1.5 * z * z + 8) * ref.STEP * z.abs() * bell + 2 * ref.STEP * torch.where(z < 0, 0.0, 1.0 + z.abs() * bell)
     ref.near(dX, want, rounded(t, want) + off, "GELU's derivative")
+
+
+@pytest.mark.parametrize("t", TYPES[1:])
+@pytest.mark.parametrize("T,N", [(40, 8), (700, 8), (9000, 8), (2000, 520)])
+def test_gelu_and_its_tail(qb, t, T, N):
+    """GELU at values that are known exactly: relative to itself, however small"""
+    z = from_minus_to_plus(T, t)[:, 0].contiguous()
+    X, W = torch.zeros(T, 64, dtype=t), torch.zeros(N, 64, dtype=t)
+    X[:, 5], W[:, 5] = z, 1
+    Y = qb.qb_linear_fwd(X.cuda(), W.cuda(), act="gelu")
+    z = z.double()[:, None].expand(T, N)
+    want = z * ref.phi(z)
+    off = z.abs() * (FLUSHED + tail_off(z) * ref.phi(-z.abs()) + 2 * ref.STEP * torch.where(z < 0, ref.phi(z), 1.0))
+    ref.near(Y, want, rounded(t, want) + off, "GELU")
