@@ -134,12 +134,13 @@ struct Coder {
         }
     }
     static __device__ __forceinline__ uint32_t four(int a, int b, int c, int d) { return (a & 0xFF) | (b & 0xFF) << 8 | (c & 0xFF) << 16 | (uint32_t)d << 24; }
-    // next to half a step the sign of |x| - (k + 1/2) scale decides, which one fused multiply and add gives without error
+    // next to half a step the sign of |x| - (k + 1/2) scale decides, which one fused multiply and add gives without error (of small scales both are
+    // taken larger: half a subnormal step would be rounded to nothing)
     __device__ __forceinline__ int careful(float x) const
     {
         if (!(scale > 0.0f && scale < __builtin_inff())) return 0;
-        const float m = fabsf(x), t = fminf(__fdiv_rn(m, scale), 127.0f), low = floorf(t);  // (subnormal scales are far from max |x| / 127)
-        const float d = __builtin_fmaf(-(low + 0.5f), scale, m);
+        const float up = scale < 1.0e-30f ? 0x1p60f : 1.0f, s = scale * up, m = fabsf(x) * up, t = fminf(__fdiv_rn(m, s), 127.0f), low = floorf(t);  // (subnormal scales are far from max |x| / 127)
+        const float d = __builtin_fmaf(-(low + 0.5f), s, m);
         const int k = (int)low + (low < 127.0f && (d > 0.0f || (d == 0.0f && ((int)low & 1) != 0)) ? 1 : 0);
         return x < 0.0f ? -k : k;
     }

@@ -78,3 +78,18 @@ def test_gelu_and_its_tail(qb, t, T, N):
     want = z * ref.phi(z)
     off = z.abs() * (FLUSHED + tail_off(z) * ref.phi(-z.abs()) + 2 * ref.STEP * torch.where(z < 0, ref.phi(z), 1.0))
     ref.near(Y, want, rounded(t, want) + off, "GELU")
+
+
+def test_codes_of_subnormal_scales(qb):
+    """every multiple of the least subnormal number over scales of 1 to 41 of them: quotients next to half a step, whose distance from it is less than a subnormal step"""
+    for n in range(1, 42):
+        k = torch.arange(127 * n + 1, dtype=torch.int32)
+        k = torch.cat([k, k.new_zeros(-len(k) % 63)]).view(-1, 63)
+        k = torch.cat([torch.full((len(k), 1), 127 * n, dtype=torch.int32), k], 1)
+        x = k.view(torch.float32) * torch.where(torch.arange(64) % 3 == 1, -1.0, 1.0)
+        codes, scales = qb.qb_checkpoint_act(x.cuda())
+        assert (scales.cpu().view(torch.int32) == n).all()
+        # a quotient of whole numbers, rounded half to even in whole numbers
+        low, rest = k // n, 2 * (k % n)
+        want = (low + ((rest > n) | ((rest == n) & (low % 2 == 1))).int()) * torch.where(torch.arange(64) % 3 == 1, -1, 1)
+        assert torch.equal(codes.cpu().int(), want)
