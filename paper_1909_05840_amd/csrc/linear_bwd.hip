@@ -24,12 +24,14 @@ struct GradArgs {
     float *db;             // [db_parts][N]: parts of dbias
     float *dXp, *dWp;      // [parts][T][K], [parts][N][K], or null
     int x_tiles, w_tiles, x_parts, w_parts, x_first;
-    int x_blocks, y_blocks, n_blocks, t_blocks;  // of the first launch: for X; for dY's copy; for dbias where dW is not formed, column blocks and row blocks
+    int64_t x_blocks, y_blocks;        // of the first launch: for X; for dY's copy
+    int n_blocks, t_blocks;            // for dbias where dW is not formed, column blocks and row blocks
     int db_parts;                      // of dbias: the first launch's row blocks, or the parts of dW's tiles, which then add it up
 };
 
 constexpr int kAtOnce = 2;       // chunks of eight values of X, or of dY, to a thread of the first launch
 constexpr int kRowBlock = 128;   // rows of dY whose sum is one part of dbias
+constexpr int64_t kMostBlocks = (1 << 24) - 1;  // of 256 threads: a launch has less than 2^32 of them
 
 template <typename T>
 struct TypeOf;
@@ -38,17 +40,18 @@ struct TypeOf<Bf16> { static constexpr int value = QB_TYPE_BF16; };
 template <>
 struct TypeOf<Fp16> { static constexpr int value = QB_TYPE_FP16; };
 
+// block `at_block` of the first launch's work
 template <typename T>
-__global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a)
+__device__ __forceinline__ void prepare(const GradArgs &a, int64_t at_block, float (&sums)[8][256])
 {
     typedef Eight<TypeOf<T>::value> E;
-    if ((int)blockIdx.x < a.x_blocks) {
+    if (at_block < a.x_blocks) {
         const int64_t chunks = (int64_t)a.T * (a.K / 8);
         int64_t at[kAtOnce];
         float v[kAtOnce][8];
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
-            at[u] = min(((int64_t)blockIdx.x * kAtOnce + u) * 256 + threadIdx.x, chunks - 1);  // (past the end: the last chunk again)
+            at[u] = min((at_block * kAtOnce + u) * 256 + threadIdx.x, chunks - 1);  // (past the end: the last chunk again)
             if (a.x_codes) {
                 kept8(v[u], a.x_codes, a.x_scales, at[u]);
             } else if (a.pre_codes) {
@@ -68,14 +71,14 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a)
         }
         return;
     }
-    if ((int)blockIdx.x < a.x_blocks + a.y_blocks) {
+    if (at_block < a.x_blocks + a.y_blocks) {
         const uint32_t chunks = (uint32_t)a.N8 / 8;
         const int64_t all = (int64_t)a.T * chunks;
         int64_t at[kAtOnce];
         E e[kAtOnce];
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
-            at[u] = min(((int64_t)(blockIdx.x - a.x_blocks) * kAtOnce + u) * 256 + threadIdx.x, all - 1);  // (past the end: the last chunk again)
+            at[u] = min(((at_block - a.x_blocks) * kAtOnce + u) * 256 + threadIdx.x, all - 1);  // (past the end: the last chunk again)
             const int64_t row = all >> 32 ? at[u] / chunks : (uint32_t)at[u] / chunks;
             const int col = (int)(at[u] - row * chunks) * 8;
             e[u].load(a.dY, row * a.dy_row + col, a.N - col);
@@ -84,8 +87,7 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a)
         for (int u = 0; u < kAtOnce; ++u) e[u].store(a.dYs, at[u] * 8, 8);
         return;
     }
-    __shared__ float sums[8][256];
-    const int id = blockIdx.x - a.x_blocks - a.y_blocks, block = id / a.n_blocks, lane = threadIdx.x & 31, team = threadIdx.x >> 5;
+    const int id = (int)(at_block - a.x_blocks - a.y_blocks), block = id / a.n_blocks, lane = threadIdx.x & 31, team = threadIdx.x >> 5;
     const int n0 = (id - block * a.n_blocks) * 256, col = n0 + lane * 8, row0 = block * kRowBlock, row1 = min(a.T, row0 + kRowBlock);
     float s[8];
 #pragma unroll
@@ -110,6 +112,17 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a)
 #pragma unroll
     for (int i = 0; i < 8; ++i) x += sums[i][threadIdx.x];
     a.db[(int64_t)block * a.N + n] = x;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a, int64_t blocks)
+{
+    __shared__ float sums[8][256];
+    prepare<T>(a, blockIdx.x, sums);
+    for (int64_t more = (int64_t)blockIdx.x + gridDim.x; more < blocks; more += gridDim.x) {  // (where a launch has no room for all of them)
+        __syncthreads();
+        prepare<T>(a, more, sums);
+    }
 }
 
 // dX's rows: 64 columns from `col` on of what dY W gives, 32 rows from `row0` on
@@ -368,10 +381,10 @@ size_t lay_out(const qb_linear_grads &l, GradArgs &a, Plan &p, uint8_t *base)
     a.t_blocks = (a.T + kRowBlock - 1) / kRowBlock;
     a.n_blocks = (a.N + 255) / 256;
     const bool stage = (l.dX || l.dW) && !readable(l), expand = l.dW && !l.X;
-    a.x_blocks = expand ? (int)((l.T * (l.K / 8) + 256 * kAtOnce - 1) / (256 * kAtOnce)) : 0;
+    a.x_blocks = expand ? (l.T * (l.K / 8) + 256 * kAtOnce - 1) / (256 * kAtOnce) : 0;
     a.db_parts = !l.dbias ? 0 : l.dW ? p.w_parts : a.t_blocks;
     if (!l.dbias || l.dW) a.t_blocks = 0;
-    a.y_blocks = stage ? (int)((l.T * (a.N8 / 8) + 256 * kAtOnce - 1) / (256 * kAtOnce)) : 0;
+    a.y_blocks = stage ? (l.T * (a.N8 / 8) + 256 * kAtOnce - 1) / (256 * kAtOnce) : 0;
     if (expand) a.Xs = reinterpret_cast<uint16_t *>(take((size_t)a.T * a.K * 2));
     if (stage) a.dYs = reinterpret_cast<uint16_t *>(take((size_t)a.T * a.N8 * 2));
     if (l.dbias && !(l.dW && a.db_parts == 1)) a.db = reinterpret_cast<float *>(take((size_t)a.db_parts * a.N * 4));
@@ -383,8 +396,8 @@ size_t lay_out(const qb_linear_grads &l, GradArgs &a, Plan &p, uint8_t *base)
 template <typename T>
 qb_status launch(const GradArgs &a, int size, hipStream_t st)
 {
-    const int64_t first = (int64_t)a.x_blocks + a.y_blocks + (int64_t)a.n_blocks * a.t_blocks;
-    if (first > 0) linear_prepare_kernel<T><<<(int)first, 256, 0, st>>>(a);
+    const int64_t first = a.x_blocks + a.y_blocks + (int64_t)a.n_blocks * a.t_blocks;
+    if (first > 0) linear_prepare_kernel<T><<<(int)std::min(first, kMostBlocks), 256, 0, st>>>(a, first);
     const int groups = a.x_tiles * a.x_parts + a.w_tiles * a.w_parts;
     if (groups > 0) {
         if (size == 3) linear_grads_kernel<T, Large><<<groups, 64 * Large::kWaves, 0, st>>>(a);
