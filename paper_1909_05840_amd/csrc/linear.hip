@@ -243,6 +243,7 @@ typedef Tile<1, 2, 2, 1, 3, 2> Least;  // 64 x 64
 struct Plan {
     int size, parts;  // 0 least .. 4 large; few tokens: -M
 };
+int64_t padded(int64_t N) { return (N + 63) / 64 * 64; }  // a part's rows: whole groups are written and read
 template <typename S>
 int64_t tiles_of(int64_t T, int64_t N) { return ((T + S::BN - 1) / S::BN) * ((N + S::BM - 1) / S::BM); }
 // Few tokens: a launch's ends and the rounds of a wavefront's units, the largest share of a CU, at 45 KB a microsecond (with registers for 64 tokens 32), and what a second
@@ -258,7 +259,7 @@ Plan few_plan(const qb_linear &l, double &least)
             const int64_t groups = (l.N + 16 * m - 1) / (16 * m) * p, units = (l.K / 64 + 8 * p - 1) / (8 * p), at_once = m > 1 || l.T > 32 ? 2 : 4;
             const double share = (double)((groups + 255) / 256) * (double)((16 * m + l.T) * l.K * 2 / p) * 1e-3;
             double cost = (l.T > 32 ? 4.0 + share / 32.0 : 3.0 + share / 45.0) + (double)((units - 1) / at_once);
-            if (p > 1 || l.codes) cost += 2.8 + p * l.T * l.N * 1e-6;
+            if (p > 1 || l.codes) cost += 2.8 + p * l.T * padded(l.N) * 1e-6;
             if (cost < 0.95 * least) {  // (1 x 16384 by 4096, one and two of sixteen neurons: 25.5, 27.6 us)
                 least = cost;
                 best = {-m, p};
@@ -280,7 +281,7 @@ void try_size(Plan &best, double &least, const Cost &c, const qb_linear &l)
         const int64_t length = (steps + p - 1) / p;
         const double share = (double)((tiles * p + 255) / 256 * length) * ((S::BM + S::BN) / 8.0);
         double cost = c.ends * (double)((tiles * p + c.room - 1) / c.room) + std::max(length * c.step, share / c.rate);
-        if (p > 1) cost += 1.5 + p * (double)l.T * l.N * 2.8e-6;
+        if (p > 1) cost += 1.5 + p * (double)l.T * padded(l.N) * 2.8e-6;
         if (cost < least) {
             least = cost;
             best = {c.size, p};
@@ -305,7 +306,7 @@ size_t lay_out(const qb_linear &l, LinearArgs &a, Plan &p)
 {
     p = plan_of(l);
     a.parts = p.parts;
-    a.Np = (int)((l.N + 63) / 64 * 64);
+    a.Np = (int)padded(l.N);
     return p.parts > 1 || (p.size < 0 && l.codes) ? round_up((size_t)p.parts * l.T * a.Np * 4) : 0;
 }
 bool shape_ok(const qb_linear &l) { return l.T >= 0 && l.T <= kMostRows && l.N >= 1 && l.N <= kMostOutputs && k_ok(l.K); }
