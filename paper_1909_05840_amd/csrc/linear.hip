@@ -345,6 +345,15 @@ qb_status launch(const LinearArgs &a, int size, hipStream_t st)
 }
 
 }  // namespace
+
+// host, pure: Plan::size of a call, and into how many parts its contraction is cut
+int linear_fwd_plan(const qb_linear *l, int *parts)
+{
+    const Plan p = plan_of(*l);
+    *parts = p.parts;
+    return p.size;
+}
+
 }  // namespace qb
 
 using namespace qb;

@@ -412,6 +412,16 @@ qb_status launch(const GradArgs &a, int size, hipStream_t st)
 }
 
 }  // namespace
+
+// host, pure: Plan::size of a call, and into how many parts the contractions of dX and dW are cut
+int linear_bwd_plan(const qb_linear_grads *l, int *x_parts, int *w_parts)
+{
+    const Plan p = plan_of(*l);
+    *x_parts = p.x_parts;
+    *w_parts = p.w_parts;
+    return p.size;
+}
+
 }  // namespace qb
 
 using namespace qb;

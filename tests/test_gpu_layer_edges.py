@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import layer_reference as ref
+import test_gpu_layer_norm as layer_norm
 
 pytestmark = pytest.mark.gpu
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
@@ -93,3 +94,10 @@ def test_codes_of_subnormal_scales(qb):
         low, rest = k // n, 2 * (k % n)
         want = (low + ((rest > n) | ((rest == n) & (low % 2 == 1))).int()) * torch.where(torch.arange(64) % 3 == 1, -1, 1)
         assert torch.equal(codes.cpu().int(), want)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("T,W", [(131, 8193), (300, 8256), (131, 10000), (3, 20001), (140, 32768)])
+def test_norm_sums_of_wide_rows_from_8_bits(qb, t, T, W):
+    """rows that are read a second time for the sums over the tokens, in 8 bits"""
+    layer_norm.test_backward_from_8_bits(qb, t, T, W)
