@@ -31,7 +31,7 @@ struct GradArgs {
 
 constexpr int kAtOnce = 2;       // chunks of eight values of X, or of dY, to a thread of the first launch
 constexpr int kRowBlock = 128;   // rows of dY whose sum is one part of dbias
-constexpr int64_t kMostBlocks = (1 << 24) - 1;  // of 256 threads: a launch has less than 2^32 of them
+constexpr int64_t kMostBlocks = (1 << 24) - 1;  // of 256 threads: a launch has less than 2^32 of them, and a second one takes what is left
 
 template <typename T>
 struct TypeOf;
@@ -40,11 +40,11 @@ struct TypeOf<Bf16> { static constexpr int value = QB_TYPE_BF16; };
 template <>
 struct TypeOf<Fp16> { static constexpr int value = QB_TYPE_FP16; };
 
-// block `at_block` of the first launch's work
 template <typename T>
-__device__ __forceinline__ void prepare(const GradArgs &a, int64_t at_block, float (&sums)[8][256])
+__global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a, int64_t first_block)
 {
     typedef Eight<TypeOf<T>::value> E;
+    const int64_t at_block = first_block + blockIdx.x;
     if (at_block < a.x_blocks) {
         const int64_t chunks = (int64_t)a.T * (a.K / 8);
         int64_t at[kAtOnce];
@@ -87,6 +87,7 @@ __device__ __forceinline__ void prepare(const GradArgs &a, int64_t at_block, flo
         for (int u = 0; u < kAtOnce; ++u) e[u].store(a.dYs, at[u] * 8, 8);
         return;
     }
+    __shared__ float sums[8][256];
     const int id = (int)(at_block - a.x_blocks - a.y_blocks), block = id / a.n_blocks, lane = threadIdx.x & 31, team = threadIdx.x >> 5;
     const int n0 = (id - block * a.n_blocks) * 256, col = n0 + lane * 8, row0 = block * kRowBlock, row1 = min(a.T, row0 + kRowBlock);
     float s[8];
@@ -112,17 +113,6 @@ __device__ __forceinline__ void prepare(const GradArgs &a, int64_t at_block, flo
 #pragma unroll
     for (int i = 0; i < 8; ++i) x += sums[i][threadIdx.x];
     a.db[(int64_t)block * a.N + n] = x;
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void linear_prepare_kernel(const GradArgs a, int64_t blocks)
-{
-    __shared__ float sums[8][256];
-    prepare<T>(a, blockIdx.x, sums);
-    for (int64_t more = (int64_t)blockIdx.x + gridDim.x; more < blocks; more += gridDim.x) {  // (where a launch has no room for all of them)
-        __syncthreads();
-        prepare<T>(a, more, sums);
-    }
 }
 
 // dX's rows: 64 columns from `col` on of what dY W gives, 32 rows from `row0` on
@@ -397,7 +387,7 @@ template <typename T>
 qb_status launch(const GradArgs &a, int size, hipStream_t st)
 {
     const int64_t first = a.x_blocks + a.y_blocks + (int64_t)a.n_blocks * a.t_blocks;
-    if (first > 0) linear_prepare_kernel<T><<<(int)std::min(first, kMostBlocks), 256, 0, st>>>(a, first);
+    for (int64_t at = 0; at < first; at += kMostBlocks) linear_prepare_kernel<T><<<(int)std::min(first - at, kMostBlocks), 256, 0, st>>>(a, at);
     const int groups = a.x_tiles * a.x_parts + a.w_tiles * a.w_parts;
     if (groups > 0) {
         if (size == 3) linear_grads_kernel<T, Large><<<groups, 64 * Large::kWaves, 0, st>>>(a);
