@@ -86,7 +86,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_kernel(const LinearA
         for (int u = 0; u < S::kStages; ++u) fetch(u);
         Product<T, S, false, false, false>(lds0, wave, lane).run(z, none, steps, stage, fetch, [&](int s) { wait_step<S>(s, steps); });
     }
-    gather<S>(z, none, lds + S::kStages * S::kStage, wave, lane);
+    gather<S>(z, lds + S::kStages * S::kStage, wave, lane);
     if (wave >= kTeam) return;
     each<S::TM / 2>([&](auto half) {
         constexpr int i = 2 * half;

@@ -147,8 +147,8 @@ __device__ __forceinline__ void copy_step(Feed<N> &f, uint32_t to, int left, int
     f.at += f.step;
 }
 
-// acc += A B^T over one tile's steps, which lie or will lie in the stages from `stage` on.  When the operands of a step's last instructions are in registers its stage is free:
-// `fetch(stage)` starts the copies of the step that comes kStages later, of this tile or of the one that follows.  `arrived(s)` waits for the wavefront's copies of step
+// acc += A B^T over a tile's steps, which lie or will lie in the stages from `stage` on.  When the operands of a step's last instructions are in registers its stage is free:
+// `fetch(stage)` starts the copies of the step that comes kStages later.  `arrived(s)` waits for the wavefront's copies of step
 // s, behind which those of kStages - 1 further steps may be under way for s = 0, else kStages - 2.  With SUMS, sums[j] gets what B's rows add up to over the contraction, a
 // lane's share of its column of block j.
 // Of 256 x 256 tiles more than two stages (5 slots of an operand each, all of LDS) measured the same: 16384 x 1024 by 4096 112.3 us and 113.6, 8192 x 8192 by 8192 867
@@ -223,16 +223,15 @@ __device__ __forceinline__ void wait_step(int s, int steps)
     else if (steps - s >= S::kStages - 1) wait_copies<(S::kStages - 2) * kStep>();
     else wait_copies<0>();
 }
-// The groups' shares of a tile's sums (and of what SUMS adds up) come together in the first group; `room`: S::kSums bytes.
+// The groups' shares of a tile's sums come together in the first group; `room`: S::kSums bytes that nothing else uses.
 template <typename S>
-__device__ __forceinline__ void gather(v16f (&acc)[S::TM][S::TN], float (&sums)[S::TN], uint8_t *room, int wave, int lane)
+__device__ __forceinline__ void gather(v16f (&acc)[S::TM][S::TN], uint8_t *room, int wave, int lane)
 {
     if constexpr (S::KG > 1) {
         constexpr int kTeam = S::WM * S::WN, kValues = S::TM * S::TN * 16;
         const int group = wave / kTeam;
         v4f *const mine = reinterpret_cast<v4f *>(room) + (wave % kTeam * (kValues / 4)) * 64 + lane;
         constexpr int kNext = kTeam * (kValues / 4) * 64;
-        barrier();  // (the last tile's have been read)
         if (group > 0) {
 #pragma unroll
             for (int i = 0; i < S::TM; ++i)

@@ -205,7 +205,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_grads_kernel(const G
             form(Product<T, S, true, true, false>(lds0, wave, lane), Across(), Across(), x, y, left, left);
         }
     }
-    gather<S>(g, db, lds + S::kStages * S::kStage, wave, lane);
+    gather<S>(g, lds + S::kStages * S::kStage, wave, lane);
     if (wave >= S::WM * S::WN) return;
     float *const sums = of_x ? a.dXp : a.dWp;
     const int rows = of_x ? a.T : a.N;
