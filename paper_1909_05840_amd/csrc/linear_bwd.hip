@@ -305,9 +305,9 @@ double done_at(int64_t n1, double t1, int64_t n2, double t2, int64_t places)
     return end;
 }
 // Which tiles, and into how many parts their contractions are cut: the shortest time by that.  Parts cost the launch that adds them up, 3 us, and their bytes, twice, at 3 TB/s
-// (4 where they leave the L2).  Measured (modelled), us: 390 x 768 by 768 least 7.4 (7), small 8.3 (10), middle 10.9; 1000 x 1024 by 1024 12.0 (12), 12.9 (13), 17.2;
-// 390 x 2304 by 768 least 14.9 (13), small with dX in 3 parts 14.5 (18).  Large, dW in 2, 3 and 4 parts: 8190 x 1024 by 4096 148 (154), 166 (171), 159 (159);
-// 16384 x 4096 by 1024 251 (247), 267 (284), 255 (253).
+// (4 where they leave the L2).  Measured over three sets of operands in turn (modelled), us: 390 x 768 by 768 least 8.1 (7.0), small 9.1 (10.3), middle 12.0 (13.2);
+// 1000 x 1024 by 1024 13.3 (12.1), 13.9 (11.9), 18.4 (15.7); 390 x 2304 by 768 least 15.9 (13.0), with dX in 2 parts 16.8 (16.5), small with dX in 3 parts 15.2 (17.7).  Large, dW whole,
+// in 2, 3 and 4 parts: 8190 x 1024 by 4096 232 (229), 162 (154), 154 (171), 155 (160); 16384 x 4096 by 1024 451 (446), 270 (247), 275 (284), 268 (253).
 template <typename S>
 void try_tiles(Plan &best, double &least, const Cost &c, bool dx, bool dw, int64_t T, int64_t N, int64_t K)
 {
