@@ -73,3 +73,29 @@ def test_no_plan_cuts_the_large_tiles_of_the_forward():
             for K in (64, 1024, 32768):
                 size, parts = plan_forward(T, N, K, False)
                 assert size < 3 or parts == 1
+
+
+FORWARD_TILES = {0: (64, 64, 256), 1: (64, 128, 256), 2: (128, 128, 256), 3: (128, 256, 512), 4: (256, 256, 512)}  # outputs, tokens, threads
+BACKWARD_TILES = {0: (64, 64, 256), 1: (64, 128, 256), 2: (128, 128, 256), 3: (256, 256, 512)}                     # inputs, tokens or neurons, threads
+MEMORY = 300e9  # bytes: a result beyond it has nowhere to lie
+
+
+def test_no_launch_has_2_to_32_threads():
+    """more of them are not refused, some just do not run: tiles and joins of every size of call that memory has room for"""
+    for t in range(7, 25):
+        for n in range(21):
+            T, N = 1 << t, 1 << n
+            if T * N * 2 > MEMORY:
+                continue
+            for K in (64, 1024, 32768):
+                size, parts = plan_forward(T, N, K, False)
+                outputs, tokens, threads = FORWARD_TILES[size]
+                assert -(-N // outputs) * -(-T // tokens) * parts * threads < 1 << 32
+                assert parts == 1 or T * -(-N // 64) * 16 < 1 << 32
+                for dX, dW in ((True, True), (True, False), (False, True)):
+                    if T * K * 2 * dX > MEMORY or N * K * 2 * dW > MEMORY:
+                        continue
+                    size, x, w = plan_backward(T, N, K, dX, dW)
+                    inputs, rows, threads = BACKWARD_TILES[size]
+                    assert -(-K // inputs) * (-(-T // rows) * x * dX + -(-N // rows) * w * dW) * threads < 1 << 32
+                    assert (T * (x > 1) + N * (w > 1)) * K // 4 < 1 << 32
